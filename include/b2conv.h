@@ -347,6 +347,113 @@ int b2c_measure_mma_rate(int tile_n, int mmas_per_block, float* device_us, float
  * pairs.  Same allocation, synchronisation and error behaviour as b2c_measure_mma_rate. */
 int b2c_measure_mma_rate_pair(int tile_n, int mmas_per_pair, float* device_us, float* cycles_per_mma, void* cuda_stream);
 
+/* ---- 8-bit float operators (no counterpart in the paper) -------------------------------------------
+ * Linear and expert layers of quantised networks on the same intrinsic: operands in 8-bit floating point
+ * (`tcgen05.mma.kind::f8f6f4`), one fp32 scale for each block of 128, fp32 sums.  All calls are
+ * asynchronous on `cuda_stream`, keep no state between calls, allocate nothing and may be captured in a
+ * graph; two of them may run at once on different streams as long as their outputs and workspaces differ.
+ * Tensors belong to the current device.  Rows are contiguous; `ld*` is the distance between two rows in
+ * elements.  Outputs must not overlap inputs.  Zero rows or tokens are valid and launch nothing. */
+#define B2C_F32 0
+#define B2C_F16 1
+#define B2C_BF16 2
+#define B2C_E4M3 3 /* 1-4-3 bits, largest value 448, no infinity                                    */
+#define B2C_E5M2 4 /* 1-5-2 bits, largest value 57344                                               */
+
+/* Block quantisation of a matrix x [rows][cols] (B2C_F32 / F16 / BF16) to q_type (B2C_E4M3 / E5M2) with one
+ * scale for each block of block_rows x 128 elements; block_rows is 1 (activations) or 128 (weights), the
+ * last blocks may be smaller.  With F the type's largest value and amax the block's largest magnitude,
+ * at least 2^-100:
+ *   scale_dev[row / block_rows][col / 128] = amax / F,   q = the value of q_type nearest to x * F / amax
+ * (ties to even).  A NaN stays NaN in its place and does not enter amax; an infinity makes its block's scale
+ * infinite, its block's finite values 0 and itself NaN, so that the whole block stands for NaN.
+ * ld_scale >= ceil(cols / 128).  Elements between cols and ldq are not written. */
+int b2c_fp8_quantize(const void* x_dev, int x_type, int64_t rows, int32_t cols, int64_t ldx, int block_rows,
+                     int q_type, void* q_dev, int64_t ldq, float* scale_dev, int64_t ld_scale, void* cuda_stream);
+
+/* Product of block-scaled 8-bit matrices: with kb the blocks of 128 along the reduction,
+ *   y[m][n] = sum_kb a_scale[m][kb] * b_scale[n / 128][kb] * sum_{k in kb} a[m][k] * b[n][k]
+ * rounded once to y_type.  a_dev: [rows][K] with one scale for each 1 x 128 block; b_dev: [N][K], dense, with
+ * one scale for each 128 x 128 block, b_scale_dev dense [ceil(N/128)][ceil(K/128)].  K must be a multiple of
+ * 16 and lda too; a_dev and b_dev 16-byte aligned; N any.  The product of two scales is formed in fp32 and
+ * has to be finite and normal there.
+ * groups > 1: b_dev is [groups][N][K] with its scales, and row m belongs to the group g with
+ * offsets_dev[g] <= m < offsets_dev[g + 1] (int32 [groups + 1], device, non-decreasing, within [0, rows];
+ * values outside are taken as the nearest valid ones, one that falls as the largest before it).  Rows of no group are left as they are in y.
+ * offsets_dev may also be given with one group; without it (NULL, groups == 1) all rows are computed. */
+typedef struct {
+  int32_t N, K;                   /* output columns, reduction length (K a multiple of 16)          */
+  int32_t groups;                 /* 1..1024                                                        */
+  int32_t a_type, b_type, y_type; /* a, b: B2C_E4M3 or B2C_E5M2; y: B2C_F32, B2C_F16 or B2C_BF16    */
+} b2c_matmul_desc;
+int b2c_fp8_matmul(const b2c_matmul_desc* desc, int64_t rows, const void* a_dev, int64_t lda, const float* a_scale_dev,
+                   int64_t ld_a_scale, const void* b_dev, const float* b_scale_dev, const int32_t* offsets_dev,
+                   void* y_dev, int64_t ldy, void* cuda_stream);
+
+/* Which experts a token goes to, and with which weights.  For every row of logits_dev [tokens][experts]
+ * (B2C_F32 / F16 / BF16): s = softmax or sigmoid of the row; choice = s + bias_dev[expert] (bias_dev may be
+ * NULL).  With groups > 1 the experts form that many equal runs; a run's score is the largest choice in it
+ * (B2C_GROUP_MAX) or the sum of its two largest (B2C_GROUP_TOP2), and only the topk_groups best runs stay.
+ * The topk experts of largest choice are written in falling order to ids_dev [tokens][topk], and
+ * weights_dev [tokens][topk] gets s (without the bias), divided by the sum over the chosen ones if
+ * `renormalise` is set, times `scale`.  Choices and group scores are compared in 64 bits; equal ones go to
+ * the lowest index.  A logit of -inf or NaN has s = 0; of several +inf in a softmax row each counts as the
+ * largest.  Where the chosen s sum to 0 renormalised weights are 0. */
+#define B2C_SCORE_SOFTMAX 0
+#define B2C_SCORE_SIGMOID 1
+#define B2C_GROUP_MAX 0
+#define B2C_GROUP_TOP2 1
+typedef struct {
+  int32_t experts, topk;       /* experts 1..1024, topk 1..32, topk <= experts / groups * topk_groups */
+  int32_t score;               /* B2C_SCORE_*                                                       */
+  int32_t groups, topk_groups; /* groups 1..32, a divisor of experts; topk_groups 1..groups         */
+  int32_t group_score;         /* B2C_GROUP_*                                                       */
+  int32_t renormalise;         /* 0 or 1                                                            */
+  int32_t logit_type;          /* B2C_F32 / F16 / BF16                                              */
+  float scale;
+} b2c_route_desc;
+int b2c_route(const b2c_route_desc* desc, int64_t tokens, const void* logits_dev, int64_t ld, const float* bias_dev,
+              float* weights_dev, int32_t* ids_dev, void* cuda_stream);
+
+/* Sorts the `pairs` (token, slot) pairs of a route by expert, keeping their order within an expert:
+ * offsets_dev [experts + 1] gets the first sorted position of each expert, rows_dev [pairs] the sorted position of
+ * each pair, order_dev [pairs] (may be NULL) the pair at each position.  An id outside 0..experts-1 (a
+ * token that goes nowhere: padding) has row -1 and no position; positions from offsets[experts] on stay
+ * as they are in order_dev.  workspace_dev: at least b2c_route_sort_workspace_bytes bytes. */
+int b2c_route_sort_workspace_bytes(int64_t pairs, int32_t experts, size_t* bytes);
+int b2c_route_sort(const int32_t* ids_dev, int64_t pairs, int32_t experts, int32_t* offsets_dev, int32_t* rows_dev,
+                   int32_t* order_dev, void* workspace_dev, void* cuda_stream);
+
+/* out[t] = sum_j weights_dev[t][j] * y[rows_dev[t][j]] over the slots with 0 <= rows < y_rows, in slot order, in
+ * fp32, rounded once; zeros for a token without any.  y_type and out_type: B2C_F32 / F16 / BF16. */
+int b2c_route_combine(const void* y_dev, int y_type, int64_t y_rows, int64_t ldy, const int32_t* rows_dev, const float* weights_dev,
+                      int64_t tokens, int32_t topk, int32_t cols, void* out_dev, int out_type, int64_t ldo,
+                      void* cuda_stream);
+
+/* A gated feed-forward layer of routed experts.  For token t and its slots j with expert e = ids_dev[t][j]:
+ *   xq = quantise(x[t]);   h = silu(w1[e][0] . xq) * (w1[e][1] . xq);   hq = quantise(h)
+ *   y[t] = sum_j weights_dev[t][j] * (w2[e] . hq)
+ * with quantise and the products as above (1 x 128 blocks, E4M3; silu(v) = v / (1 + exp(-v)); h is not
+ * rounded before it is quantised).  w1_dev: E4M3 [experts][2][inter][hidden], gate matrix then up matrix,
+ * w1_scale_dev [experts][2][ceil(inter/128)][ceil(hidden/128)]; w2_dev: E4M3 [experts][hidden][inter] with
+ * w2_scale_dev [experts][ceil(hidden/128)][ceil(inter/128)]; all dense, 16-byte aligned.  hidden and inter
+ * are multiples of 16.  The rows of a slot are rounded to `type` before the weighted sum, which is formed in fp32.
+ * ids outside 0..experts-1 add nothing.  workspace_dev: b2c_experts_workspace_bytes bytes for at least this many
+ * tokens, 16-byte aligned; its contents are scratch. */
+typedef struct {
+  int32_t hidden, inter, experts, topk;
+  int32_t type; /* of x and y: B2C_F32, B2C_F16 or B2C_BF16                                          */
+} b2c_experts_desc;
+int b2c_experts_workspace_bytes(const b2c_experts_desc* desc, int64_t tokens, size_t* bytes);
+int b2c_fp8_experts(const b2c_experts_desc* desc, int64_t tokens, const void* x_dev, int64_t ldx, const int32_t* ids_dev,
+                    const float* weights_dev, const void* w1_dev, const float* w1_scale_dev, const void* w2_dev,
+                    const float* w2_scale_dev, void* y_dev, int64_t ldy, void* workspace_dev, void* cuda_stream);
+
+/* Device status of the 8-bit float operators on the current device, as b2c_oneshot_status: *status is B2C_OK, or
+ * B2C_E_TIMEOUT if a kernel gave up on a bounded wait since the last query (the word is then cleared).  Waits
+ * for the device to be idle; not to be called while a stream is being captured. */
+int b2c_fp8_status(int32_t* status);
+
 /* ---- debug build (no counterpart in the paper) ---------------------------------------------------
  * libb2conv_debug.so is the same library compiled with -DB2C_DEBUG_BOUNDS.  In it every address a
  * kernel computes by hand (loads of x, stores and atomics to the outputs and to the scratch; TMA

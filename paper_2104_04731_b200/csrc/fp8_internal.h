@@ -1,0 +1,78 @@
+// Internal declarations of the 8-bit float operators (block quantisation, products with a scale per block of 128,
+// routing, expert layers), shared by their host code and kernel launchers.
+#pragma once
+
+#include <algorithm>
+
+#include "b2c_internal.h"
+
+namespace b2c {
+
+constexpr int kBlock = 128;        // reduction elements (and weight rows) that share one scale
+constexpr int kMaxExperts = 1024;  // groups of a product, experts of a route
+constexpr int kMaxTopk = 32;
+constexpr int kMaxRouteGroups = 32;
+constexpr long long kMaxRows = 0x7FFFFF00LL;  // rows of one call: tile origins stay inside 32 bits
+constexpr float kMinAmax = 0x1p-100f;         // a block's largest magnitude counts as at least this much
+
+#ifdef __CUDACC__
+__host__ __device__
+#endif
+inline long long blocks_of(long long n) { return (n + kBlock - 1) / kBlock; }
+inline int type_bytes(int t) { return t == B2C_F32 ? 4 : (t == B2C_F16 || t == B2C_BF16 ? 2 : 1); }
+
+struct QuantizeArgs {
+  const void* x;
+  long long ldx;
+  uint8_t* q;
+  long long ldq;
+  float* scale;
+  long long lds;
+  long long rows;
+  int cols;
+  int block_rows;  // 1 or 128
+  int x_type, q_type;
+  // Rows of an expert layer: input row t is written to output rows map[t * copies + j] (none where negative).
+  const int32_t* map;
+  int copies;
+};
+
+struct MatmulArgs {
+  const void* a;
+  long long lda;
+  const float* a_scale;
+  long long lds;
+  const void* b;         // [groups][N][K]; gated: [groups][2][N][K], gate rows then up rows
+  const float* b_scale;  // [groups][ceil(N/128)][ceil(K/128)]; gated: [groups][2][...]
+  const int32_t* offsets;  // [groups + 1], or null with one group of all rows
+  void* y;               // gated: 8-bit values
+  long long ldy;
+  float* y_scale;        // gated only
+  long long ldys;
+  int rows, N, K, groups;
+  int a_type, b_type, y_type;
+  int gated;             // y = quantise(silu(a . gate) * (a . up)), blocks of 1 x 128
+};
+
+struct RouteArgs {
+  b2c_route_desc d;
+  long long tokens;
+  const void* logits;
+  long long ld;
+  const float* bias;
+  float* weights;
+  int32_t* ids;
+};
+
+cudaError_t launch_fp8_quantize(const QuantizeArgs& a, cudaStream_t st);
+int launch_fp8_matmul(const MatmulArgs& a, cudaStream_t st);  // B2C_* code
+int fp8_status_read_and_clear(int32_t* status);
+cudaError_t launch_route(const RouteArgs& a, cudaStream_t st);
+size_t route_sort_workspace(long long pairs, int experts);
+cudaError_t launch_route_sort(const int32_t* ids, long long pairs, int experts, int32_t* offsets, int32_t* rows,
+                              int32_t* order, int32_t* workspace, cudaStream_t st);
+cudaError_t launch_route_combine(const void* y, int y_type, long long y_rows, long long ldy, const int32_t* rows, const float* weights,
+                                 long long tokens, int topk, int cols, void* out, int out_type, long long ldo,
+                                 cudaStream_t st);
+
+}  // namespace b2c

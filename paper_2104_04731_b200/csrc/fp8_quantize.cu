@@ -1,0 +1,138 @@
+// Block quantisation to 8-bit floating point, one scale for each 1 x 128 or 128 x 128 block.  Memory-bound: every
+// element is read once and kept in registers between the search for the largest magnitude and the conversion.
+#include "fp8_common.cuh"
+
+namespace b2c {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kLanes = kBlock / 16;  // lanes that share a row of a block, 16 elements each
+
+struct Vec {
+  bool x, q;  // 16-byte loads of x, 16-byte stores of q
+};
+
+template <typename T>
+__device__ __forceinline__ void load_part(const QuantizeArgs& a, bool vec, long long row, int c0, float* v) {
+  const T* p = (const T*)a.x + row * a.ldx + c0;
+  if (vec && c0 + 16 <= a.cols) {
+    load16<T>(p, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = c0 + i < a.cols ? to_float<T>(p[i]) : 0.0f;
+  }
+}
+__device__ __forceinline__ void store_part(const QuantizeArgs& a, bool vec, long long row, int c0, const uint4& w) {
+  uint8_t* p = a.q + row * a.ldq + c0;
+  if (vec && c0 + 16 <= a.cols) {
+    *reinterpret_cast<uint4*>(p) = w;
+  } else {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (c0 + i < a.cols) p[i] = (uint8_t)(u[i >> 2] >> (8 * (i & 3)));
+  }
+}
+__device__ __forceinline__ float amax16(const float* v) {
+  float m = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(v[i]));
+  return m;
+}
+
+// Eight lanes hold the 128 elements of a block, 16 each: 16-byte loads and stores, three shuffles for the maximum.
+template <typename T, int QT>
+__global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const QuantizeArgs a, const Vec vec, const int nb, const long long blocks) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const long long id = (long long)blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;
+  const bool on = id < blocks;
+  const long long row = on ? id / nb : 0;
+  const int blk = on ? (int)(id - row * nb) : 0;
+  const int c0 = blk * kBlock + (threadIdx.x % kLanes) * 16;
+  float v[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+  if (on && c0 < a.cols) load_part<T>(a, vec.x, row, c0, v);
+  float m = amax16(v);
+#pragma unroll
+  for (int d = kLanes / 2; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+  if (!on) return;
+  const BlockScale s = block_scale<QT>(m);
+  const uint4 w = quantize16<QT>(s, v);
+  if (a.map == nullptr) {
+    if (c0 < a.cols) store_part(a, vec.q, row, c0, w);
+    if (threadIdx.x % kLanes == 0) a.scale[row * a.lds + blk] = s.scale;
+  } else {
+    for (int j = 0; j < a.copies; ++j) {
+      const int to = a.map[row * a.copies + j];
+      if (to < 0) continue;
+      if (c0 < a.cols) store_part(a, vec.q, to, c0, w);
+      if (threadIdx.x % kLanes == 0) a.scale[(long long)to * a.lds + blk] = s.scale;
+    }
+  }
+}
+
+// One thread block holds a 128 x 128 block in registers: four rows of 16 elements a thread.
+template <typename T, int QT>
+__global__ void __launch_bounds__(kThreads) quantize_blocks_kernel(const QuantizeArgs a, const Vec vec, const int nb) {
+  __shared__ float part[kThreads / 32];
+  pdl_wait();
+  pdl_launch_dependents();
+  const long long rb = blockIdx.x / nb;
+  const int blk = (int)(blockIdx.x - rb * nb);
+  const int c0 = blk * kBlock + (threadIdx.x % kLanes) * 16;
+  const long long row0 = rb * kBlock + threadIdx.x / kLanes;
+  constexpr int kStep = kThreads / kLanes, kRows = kBlock / kStep;
+  float v[kRows][16];
+  float m = 0.0f;
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[r][i] = 0.0f;
+    if (row0 + r * kStep < a.rows && c0 < a.cols) load_part<T>(a, vec.x, row0 + r * kStep, c0, v[r]);
+  }
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) m = fmaxf(m, amax16(v[r]));
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+  if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = m;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kThreads / 32; ++i) m = fmaxf(m, part[i]);
+  const BlockScale s = block_scale<QT>(m);
+#pragma unroll
+  for (int r = 0; r < kRows; ++r)
+    if (row0 + r * kStep < a.rows && c0 < a.cols) store_part(a, vec.q, row0 + r * kStep, c0, quantize16<QT>(s, v[r]));
+  if (threadIdx.x == 0) a.scale[rb * a.lds + blk] = s.scale;
+}
+
+template <typename T, int QT>
+cudaError_t launch(const QuantizeArgs& a, cudaStream_t st) {
+  const int nb = (int)blocks_of(a.cols);
+  Vec vec;
+  vec.x = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && (a.ldx * sizeof(T)) % 16 == 0;
+  vec.q = (reinterpret_cast<uintptr_t>(a.q) & 15) == 0 && a.ldq % 16 == 0;
+  if (a.block_rows == 1) {
+    const long long blocks = a.rows * nb;
+    const long long grid = (blocks + kThreads / kLanes - 1) / (kThreads / kLanes);
+    if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
+    return launch_pdl(quantize_rows_kernel<T, QT>, dim3((unsigned)grid), dim3(kThreads), 0, st, a, vec, nb, blocks);
+  }
+  const long long grid = blocks_of(a.rows) * nb;
+  if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
+  return launch_pdl(quantize_blocks_kernel<T, QT>, dim3((unsigned)grid), dim3(kThreads), 0, st, a, vec, nb);
+}
+
+}  // namespace
+
+cudaError_t launch_fp8_quantize(const QuantizeArgs& a, cudaStream_t st) {
+#define B2C_BY_TYPE(T) return a.q_type == B2C_E4M3 ? launch<T, B2C_E4M3>(a, st) : launch<T, B2C_E5M2>(a, st)
+  if (a.x_type == B2C_F32) B2C_BY_TYPE(float);
+  if (a.x_type == B2C_F16) B2C_BY_TYPE(__half);
+  B2C_BY_TYPE(__nv_bfloat16);
+#undef B2C_BY_TYPE
+}
+
+}  // namespace b2c
