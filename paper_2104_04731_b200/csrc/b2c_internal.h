@@ -434,6 +434,8 @@ bool stream_plan(const Geom& g, int tile_n, StreamArgs* sa, std::vector<uint64_t
 
 // --- tma.cpp -----------------------------------------------------------------------------------
 // Tensor-map encoders obtained through cudaGetDriverEntryPoint (no link-time libcuda dependency).
+int encode_tiled_3d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint64_t planes, uint64_t row_stride_bytes,
+                    uint64_t plane_stride_bytes, uint32_t box_inner, uint32_t box_rows, int swizzle_bytes);
 int encode_tiled_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer, uint64_t row_stride_bytes,
                     uint32_t box_inner, uint32_t box_outer, int swizzle_bytes);
 int encode_tiled_nhwc_rows(CUtensorMap* map, const void* base, int C_pad, int W, int H, int N, int box_c, int box_w,

@@ -1,162 +1,334 @@
-// Products of block-scaled 8-bit matrices, plain arithmetic: one thread block computes a 64 x 64 tile of one
-// group's rows, the operands are widened to fp32 in shared memory, the sums of a 128-element block are scaled and added.
-#include "fp8_common.cuh"
+// Products of block-scaled 8-bit matrices on the tensor core: the kernel for few rows, and the choice between the two.
+//
+// With few rows the weights are the bytes, and the tensor core's 128 accumulator rows are given to them (the axes
+// are swapped): a thread block owns 128 weight rows and 16 to 128 activation rows, so that an MMA of a few activation rows
+// is no larger than these.  What bounds it is how many bytes are in flight: the reduction is cut over the
+// blocks of a cluster until all SMs have a share, and the partial sums meet in distributed shared memory, in a fixed
+// order, without a second launch or atomics.
+//
+// Roles: warp 0 copies (TMA, 128-byte swizzle), warp 1 issues the MMAs, the others take each block of 128 of the
+// reduction out of tensor memory, scale it and add it up in registers (see fp8_mma.cuh).
+#include "fp8_mma.cuh"
 
 namespace b2c {
 
 namespace {
 
-constexpr int kTile = 64;
-constexpr int kDepth = 32;
+constexpr int kMaxSplit = 8;
+constexpr int kScaleRun = 4;  // blocks of the reduction whose scales are fetched together
 
-__device__ int g_status;
-
-// Row tile `index` over all groups, each group's rows in tiles of `tile` rows: its group, first row and end.
-__device__ bool find_row_tile(const MatmulArgs& a, int index, int tile, int* group, int* row0, int* row_end) {
-  int hi = a.offsets ? max(0, min(a.offsets[0], a.rows)) : 0;
-  for (int g = 0; g < a.groups; ++g) {
-    const int lo = hi;
-    hi = a.offsets ? max(lo, min(a.offsets[g + 1], a.rows)) : a.rows;  // (an offset that falls counts as the one before it)
-    const int tiles = (hi - lo + tile - 1) / tile;
-    if (index < tiles) {
-      *group = g;
-      *row0 = lo + index * tile;
-      *row_end = hi;
-      return true;
-    }
-    index -= tiles;
-  }
-  return false;
-}
-
-__device__ void tile_sums(const MatmulArgs& a, const uint8_t* b, const float* b_scale, int row0, int row_end, int n0,
-                          float (*As)[kTile + 1], float (*Bs)[kTile + 1], float acc[4][4]) {
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  const int kb_all = (int)blocks_of(a.K);
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = 0.0f;
-  for (int kb = 0; kb < kb_all; ++kb) {
-    float part[4][4] = {};
-    for (int k0 = kb * kBlock; k0 < min(a.K, (kb + 1) * kBlock); k0 += kDepth) {
-      for (int i = threadIdx.x; i < kTile * kDepth; i += 256) {
-        const int r = i / kDepth, k = k0 + i % kDepth;
-        As[i % kDepth][r] = row0 + r < row_end && k < a.K ? fp8_to_float(((const uint8_t*)a.a)[(long long)(row0 + r) * a.lda + k], a.a_type) : 0.0f;
-        Bs[i % kDepth][r] = n0 + r < a.N && k < a.K ? fp8_to_float(b[(long long)(n0 + r) * a.K + k], a.b_type) : 0.0f;
-      }
-      __syncthreads();
-      for (int k = 0; k < kDepth; ++k)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) part[i][j] = fmaf(As[k][ty * 4 + i], Bs[k][tx * 4 + j], part[i][j]);
-      __syncthreads();
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int m = row0 + ty * 4 + i, n = n0 + tx * 4 + j;
-        if (m < row_end && n < a.N)
-          acc[i][j] = fmaf(part[i][j], a.a_scale[(long long)m * a.lds + kb] * b_scale[(long long)(n / kBlock) * kb_all + kb], acc[i][j]);
-      }
-  }
-}
+// WT weight tiles of 128 rows (2: gate and up of the same columns) x NT activation rows.
+template <int NT, int WT>
+struct RowsShape {
+  static constexpr int kCols = NT * WT;                   // accumulator columns of one block of the reduction
+  static constexpr int kEpiWarps = kCols >= 64 ? 8 : 4;
+  static constexpr int kThreads = 64 + 32 * kEpiWarps;
+  static constexpr int kWarpCols = kCols / (kEpiWarps / 4);
+  static constexpr int kStageBytes = WT * kTileM * kBlock + NT * kBlock;
+  // two thread blocks share an SM: half of the shared memory (228 KB, 1 KB of it kept for each block; `factor` and the
+  // barriers are static) and of the 512 columns of tensor memory each
+  static constexpr int kFactorBytes = 2 * kScaleRun * kCols * 4;
+  static constexpr int kRing = 113 * 1024 - 1024 - 1024 - kFactorBytes;
+  static constexpr int kStages = kRing / kStageBytes < 8 ? kRing / kStageBytes : 8;
+  static constexpr int kBufs = kCols <= 64 ? 4 : 2;
+  static constexpr int kTmemCols = kCols * kBufs < 32 ? 32 : kCols * kBufs;
+  static constexpr int kPartBytes = kCols * kTileM * 4;   // partial sums, in the place of the stages
+  static constexpr int kSmem = 1024 + (kStages * kStageBytes > kPartBytes ? kStages * kStageBytes : kPartBytes);
+};
 
 template <typename T>
-__global__ void __launch_bounds__(256) matmul_kernel(const MatmulArgs a) {
-  __shared__ float As[kDepth][kTile + 1], Bs[kDepth][kTile + 1];
-  pdl_wait();
-  pdl_launch_dependents();
-  int g, row0, row_end;
-  if (!find_row_tile(a, blockIdx.y, kTile, &g, &row0, &row_end)) return;
-  const int n0 = blockIdx.x * kTile;
-  float acc[4][4];
-  tile_sums(a, (const uint8_t*)a.b + (long long)g * a.N * a.K, a.b_scale + (long long)g * blocks_of(a.N) * blocks_of(a.K), row0, row_end, n0,
-            As, Bs, acc);
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int m = row0 + threadIdx.x / 16 * 4 + i, n = n0 + threadIdx.x % 16 * 4 + j;
-      if (m < row_end && n < a.N) ((T*)a.y)[(long long)m * a.ldy + n] = from_float<T>(acc[i][j]);
-    }
+__device__ __forceinline__ void store4(T* p, const float* v, int n) {
+  if (n >= 4 && (reinterpret_cast<uintptr_t>(p) & (4 * sizeof(T) - 1)) == 0) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]));
+  } else {
+    for (int i = 0; i < min(n, 4); ++i) p[i] = from_float<T>(v[i]);
+  }
+}
+template <>
+__device__ __forceinline__ void store4<float>(float* p, const float* v, int n) {
+  if (n >= 4 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  } else {
+    for (int i = 0; i < min(n, 4); ++i) p[i] = v[i];
+  }
 }
 
-// Gate and up products of 64 rows x 128 columns, then the activation and the quantisation of the 1 x 128 blocks.
-__global__ void __launch_bounds__(256) matmul_gated_kernel(const MatmulArgs a) {
-  extern __shared__ float dyn[];
-  float(*As)[kTile + 1] = (float(*)[kTile + 1])dyn;
-  float(*Bs)[kTile + 1] = As + kDepth;
-  float* H = (float*)(Bs + kDepth);  // [64][128]
-  pdl_wait();
-  pdl_launch_dependents();
-  int g, row0, row_end;
-  if (!find_row_tile(a, blockIdx.y, kTile, &g, &row0, &row_end)) return;
-  for (int half = 0; half < 2; ++half) {
-    const int n0 = blockIdx.x * kBlock + half * kTile;
-    float gate[4][4], up[4][4];
-    const long long mat = (long long)a.N * a.K, sc = blocks_of(a.N) * blocks_of(a.K);
-    tile_sums(a, (const uint8_t*)a.b + 2 * g * mat, a.b_scale + 2 * g * sc, row0, row_end, n0, As, Bs, gate);
-    tile_sums(a, (const uint8_t*)a.b + (2 * g + 1) * mat, a.b_scale + (2 * g + 1) * sc, row0, row_end, n0, As, Bs, up);
-    for (int i = 0; i < 4; ++i)
-      for (int j = 0; j < 4; ++j)
-        H[(threadIdx.x / 16 * 4 + i) * kBlock + half * kTile + threadIdx.x % 16 * 4 + j] = silu(gate[i][j]) * up[i][j];
-  }
-  __syncthreads();
-  for (int r = threadIdx.x / 8; r < kTile; r += 32) {
-    const int m = row0 + r, c0 = blockIdx.x * kBlock + threadIdx.x % 8 * 16;
-    float v[16], mx = 0.0f;
-    for (int i = 0; i < 16; ++i) {
-      v[i] = c0 + i < a.N ? H[r * kBlock + threadIdx.x % 8 * 16 + i] : 0.0f;
-      mx = fmaxf(mx, fabsf(v[i]));
+template <int NT, int WT, typename YT>
+__global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, 2)
+    matmul_rows_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const MatmulArgs a,
+                       const int kb_per_split) {
+  using S = RowsShape<NT, WT>;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ SharedCtl ctl;
+  __shared__ RowTile tile;
+  __shared__ __align__(16) float factor[2][kScaleRun][S::kCols];
+
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
+  const int lane = threadIdx.x & 31;
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const int split = (int)gridDim.z, rank = (int)blockIdx.z;  // (a cluster is the blocks of one z run)
+
+  if (warp == 0) {
+    if (lane < S::kStages) {
+      mbar_init(smem_u32(&ctl.full[lane]), 1);
+      mbar_init(smem_u32(&ctl.empty[lane]), 1);
     }
-    for (int d = 4; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-    const BlockScale s = block_scale<B2C_E4M3>(mx);
-    const uint4 w = quantize16<B2C_E4M3>(s, v);
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-    if (m >= row_end) continue;
-    for (int i = 0; i < 16; ++i)
-      if (c0 + i < a.N) ((uint8_t*)a.y)[(long long)m * a.ldy + c0 + i] = (uint8_t)(u[i >> 2] >> (8 * (i & 3)));
-    if (threadIdx.x % 8 == 0) a.y_scale[(long long)m * a.ldys + blockIdx.x] = s.scale;
+    if (lane < S::kBufs) {
+      mbar_init(smem_u32(&ctl.tmem_full[lane]), 1);
+      mbar_init(smem_u32(&ctl.tmem_empty[lane]), S::kEpiWarps);
+    }
+    if (lane == 0) ctl.abort_flag = 0;
+    if (lane == 9) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_w) : "memory");
+    if (lane == 10) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_x) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl.tmem_base)), "r"(S::kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  pdl_wait();
+  if (warp == 2) {
+    const RowTile t = find_row_tile(a, (int)blockIdx.y, NT);
+    if (lane == 0) tile = t;
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  pdl_launch_dependents();
+  const uint32_t tmem_acc = __shfl_sync(0xffffffffu, ctl.tmem_base, 0);
+  const int group = tile.group, row0 = tile.row0;
+  const int n0 = (int)blockIdx.x * kTileM;
+  const int kb_all = (int)blocks_of(a.K);
+  const int kb0 = rank * kb_per_split, kb1 = min(kb_all, kb0 + kb_per_split);
+
+  if (group < 0) {
+    // (all blocks of the cluster: there is nothing to do)
+  } else if (warp == 0) {
+    // ---------------------------------------------------------------- copies
+    const uint32_t leader = elect_one() ? 1u : 0u;
+    int s = 0;
+    uint32_t ph = 0;
+    for (int kb = kb0; kb < kb1; ++kb) {
+      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.empty[s]), ph ^ 1u, &ctl, &g_fp8_status))) break;
+      const uint32_t full = smem_u32(&ctl.full[s]);
+      const uint32_t dst = smem_base + s * S::kStageBytes;
+      mbar_arrive_expect_tx(full, S::kStageBytes, leader);
+#pragma unroll
+      for (int w = 0; w < WT; ++w) tma_load_3d(dst + w * kTileM * kBlock, &tmap_w, kb * kBlock, n0, group * WT + w, full, leader);
+      tma_load_2d(dst + WT * kTileM * kBlock, &tmap_x, kb * kBlock, row0, full, leader);
+      if (++s == S::kStages) {
+        s = 0;
+        ph ^= 1u;
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    // ---------------------------------------------------------------- MMA issue
+    const uint32_t leader = elect_one() ? 1u : 0u;
+    const uint32_t idesc = make_idesc_f8(kTileM, NT, a.b_type, a.a_type);
+    int s = 0, buf = 0;
+    uint32_t ph = 0, bph = 0;
+    for (int kb = kb0; kb < kb1; ++kb) {
+      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.tmem_empty[buf]), bph ^ 1u, &ctl, &g_fp8_status))) break;
+      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.full[s]), ph, &ctl, &g_fp8_status))) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const int ksteps = min(4, (a.K - kb * kBlock + kMmaK - 1) / kMmaK);
+      const uint32_t base = smem_base + s * S::kStageBytes;
+      const uint64_t xdesc = make_smem_desc(base + WT * kTileM * kBlock, kBlock);
+#pragma unroll
+      for (int w = 0; w < WT; ++w)
+        mma_f8_block<1>(tmem_acc + buf * S::kCols + w * NT, make_smem_desc(base + w * kTileM * kBlock, kBlock), xdesc, idesc, leader, ksteps);
+      mma_commit(smem_u32(&ctl.empty[s]), leader);
+      mma_commit(smem_u32(&ctl.tmem_full[buf]), leader);
+      if (++s == S::kStages) {
+        s = 0;
+        ph ^= 1u;
+      }
+      if (++buf == S::kBufs) {
+        buf = 0;
+        bph ^= 1u;
+      }
+    }
+    __syncwarp();
+  } else {
+    // ---------------------------------------------------------------- scaled sums
+    const int quad = warp & 3;                         // lanes of tensor memory this warp may read
+    const int c0 = ((warp - 2) >> 2) * S::kWarpCols;   // its columns
+    const int et = (int)threadIdx.x - 64;              // thread of this role
+    float2 acc[S::kWarpCols / 2];
+#pragma unroll
+    for (int i = 0; i < S::kWarpCols / 2; ++i) acc[i] = make_float2(0.0f, 0.0f);
+    // thread c fetches the scales of column c (activation row c % NT, weight tile c / NT), a run of blocks ahead
+    const bool fetches = et < S::kCols;
+    const int tok = row0 + et % NT;
+    const float* sx = a.a_scale + (long long)min(tok, a.rows - 1) * a.lds;
+    const float* sw = a.b_scale + ((long long)(group * WT + et / NT) * blocks_of(a.N) + blockIdx.x) * kb_all;
+    float next[kScaleRun];
+    auto fetch = [&](int kb) {
+#pragma unroll
+      for (int i = 0; i < kScaleRun; ++i) next[i] = fetches && kb + i < kb1 ? sx[kb + i] * sw[kb + i] : 0.0f;
+    };
+    fetch(kb0);
+    int buf = 0, run = 0;
+    uint32_t bph = 0;
+    bool ok = true;  // a warp whose wait gave up still meets the others at their barriers
+    for (int kb = kb0; kb < kb1; ++kb) {
+      const int i = (kb - kb0) % kScaleRun;
+      if (i == 0) {
+        // the other half of `factor` may still be read by slower warps; this half was read before the last barrier
+        run ^= 1;
+        if (fetches) {
+#pragma unroll
+          for (int j = 0; j < kScaleRun; ++j) factor[run][j][et] = next[j];
+        }
+        asm volatile("bar.sync 1, %0;" ::"n"(32 * S::kEpiWarps) : "memory");
+        fetch(kb + kScaleRun);
+      }
+      ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.tmem_full[buf]), bph, &ctl, &g_fp8_status));
+      if (!ok) continue;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const uint32_t taddr = tmem_acc + ((uint32_t)(quad * 32) << 16) + (uint32_t)(buf * S::kCols + c0);
+      constexpr int kLd = S::kWarpCols == 32 ? 32 : 16;  // (64 sums a thread leave no room for 32 more values)
+#pragma unroll
+      for (int c = 0; c < S::kWarpCols; c += kLd) {
+        float v[kLd];
+        tmem_ld<kLd>(taddr + c, reinterpret_cast<int32_t*>(v));
+#pragma unroll
+        for (int j = 0; j < kLd; j += 4) {
+          const float4 f = *reinterpret_cast<const float4*>(&factor[run][i][c0 + c + j]);
+          fma2(&acc[(c + j) / 2], make_float2(v[j], v[j + 1]), make_float2(f.x, f.y));
+          fma2(&acc[(c + j) / 2 + 1], make_float2(v[j + 2], v[j + 3]), make_float2(f.z, f.w));
+        }
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&ctl.tmem_empty[buf]));
+      if (++buf == S::kBufs) {
+        buf = 0;
+        bph ^= 1u;
+      }
+    }
+    // every MMA of this block has been waited for, so the stages are free: the sums take their place
+    float* part = reinterpret_cast<float*>(smem_raw + (smem_base - smem_u32(smem_raw)));
+#pragma unroll
+    for (int i = 0; i < S::kWarpCols; ++i)
+      part[(c0 + i) * kTileM + quad * 32 + lane] = (i & 1) ? acc[i / 2].y : acc[i / 2].x;
+  }
+
+  // ---------------------------------------------------------------- sums of the cluster, results
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (ctl.abort_flag) {
+    // copies may still be under way: they land before this block leaves
+    const unsigned long long t0 = global_ns();
+    while (global_ns() - t0 < 50000ull) __nanosleep(1000);
+    __syncthreads();
+  }
+  if (split > 1) cluster_sync();
+  if (group >= 0) {
+    // one warp takes one activation row: each lane four neighbouring columns
+    const int rows = min(NT, tile.row_end - row0);
+    const int n = n0 + 4 * lane;
+    for (int j = rank + split * warp; j < rows; j += split * (S::kThreads / 32)) {
+      float v[WT][4];
+#pragma unroll
+      for (int w = 0; w < WT; ++w) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[w][i] = 0.0f;
+        const uint32_t at = smem_base + (uint32_t)(((w * NT + j) * kTileM + 4 * lane) * 4);
+        for (int z = 0; z < split; ++z) {
+          const float4 p = ld_cluster_f4(split > 1 ? map_to_rank(at, (uint32_t)z) : at);
+          v[w][0] += p.x;
+          v[w][1] += p.y;
+          v[w][2] += p.z;
+          v[w][3] += p.w;
+        }
+      }
+      const long long row = row0 + j;
+      if constexpr (WT == 1) {
+        if (n < a.N) store4<YT>((YT*)a.y + row * a.ldy + n, v[0], a.N - n);
+      } else {
+        float h[4], mx = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          h[i] = silu(v[0][i]) * v[1][i];
+          mx = fmaxf(mx, fabsf(h[i]));
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+        const BlockScale s = block_scale<B2C_E4M3>(mx);
+        const uint32_t q = cvt2<B2C_E4M3>(scaled(s, h[0]), scaled(s, h[1])) | (cvt2<B2C_E4M3>(scaled(s, h[2]), scaled(s, h[3])) << 16);
+        if (n < a.N) *reinterpret_cast<uint32_t*>((uint8_t*)a.y + row * a.ldy + n) = q;  // (N and ldy are multiples of 16)
+        if (lane == 0) a.y_scale[row * a.ldys + blockIdx.x] = s.scale;
+      }
+    }
+  }
+  // no block leaves while another reads its sums
+  if (split > 1) cluster_sync();
+  if (warp == 1) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_acc), "r"(S::kTmemCols) : "memory");
+  }
+}
+
+int fail(cudaError_t e) {
+  set_last_cuda_error((int)e);
+  return B2C_E_CUDA;
+}
+
+template <int NT, int WT, typename YT>
+int launch_rows(const MatmulArgs& a, cudaStream_t st) {
+  using S = RowsShape<NT, WT>;
+  const int n_tiles = (int)blocks_of(a.N), kb_all = (int)blocks_of(a.K);
+  // every group adds at most one tile that is not full
+  const long long row_tiles = a.offsets ? a.rows / NT + std::min(a.groups, a.rows) : (a.rows + NT - 1) / NT;
+  if (row_tiles > 65535) return B2C_E_UNSUPPORTED;
+  const long long busy = (long long)n_tiles * (a.offsets ? (a.rows + NT - 1) / NT : row_tiles);
+  int split = (int)std::min<long long>(kMaxSplit, std::max<long long>(1, 2 * kNumSMs / std::max<long long>(1, busy)));
+  split = std::max(1, std::min(split, kb_all / 2));
+  const int kb_per_split = (kb_all + split - 1) / split;
+  split = (kb_all + kb_per_split - 1) / kb_per_split;
+  CUtensorMap tw, tx;
+  int rc = encode_tiled_3d(&tw, a.b, a.K, a.N, (uint64_t)a.groups * WT, a.K, (uint64_t)a.N * a.K, kBlock, kTileM, kBlock);
+  if (rc == B2C_OK) rc = encode_tiled_2d(&tx, a.a, a.K, a.rows, a.rows > 1 ? a.lda : a.K, kBlock, NT, kBlock);
+  if (rc != B2C_OK) return rc;
+  static std::atomic<unsigned long long> configured{0};
+  cudaError_t e = set_max_dynamic_smem_once(configured, (const void*)matmul_rows_kernel<NT, WT, YT>, S::kSmem);
+  if (e == cudaSuccess)
+    e = launch_pdl_cluster(matmul_rows_kernel<NT, WT, YT>, dim3((unsigned)n_tiles, (unsigned)row_tiles, (unsigned)split), dim3(S::kThreads),
+                           S::kSmem, st, split, tw, tx, a, kb_per_split);
+  return e == cudaSuccess ? B2C_OK : fail(e);
+}
+
+template <int NT>
+int launch_rows_type(const MatmulArgs& a, cudaStream_t st) {
+  if (a.y_type == B2C_F32) return launch_rows<NT, 1, float>(a, st);
+  if (a.y_type == B2C_F16) return launch_rows<NT, 1, __half>(a, st);
+  return launch_rows<NT, 1, __nv_bfloat16>(a, st);
 }
 
 }  // namespace
 
 int launch_fp8_matmul(const MatmulArgs& a, cudaStream_t st) {
-  // every group adds at most one tile that is not full
-  const long long row_tiles = a.rows / kTile + std::min<long long>(a.groups, a.rows);
-  if (row_tiles > 65535) return B2C_E_UNSUPPORTED;
-  cudaError_t e;
+  const int rows = a.offsets ? (a.rows + a.groups - 1) / a.groups : a.rows;  // of a group, on average
   if (a.gated) {
-    const size_t smem = (2 * kDepth * (kTile + 1) + kTile * kBlock) * sizeof(float);
-    static std::atomic<unsigned long long> configured{0};
-    e = set_max_dynamic_smem_once(configured, (const void*)matmul_gated_kernel, (int)smem);
-    if (e == cudaSuccess)
-      e = launch_pdl(matmul_gated_kernel, dim3((unsigned)blocks_of(a.N), (unsigned)row_tiles), dim3(256), smem, st, a);
-  } else {
-    const dim3 grid((unsigned)((a.N + kTile - 1) / kTile), (unsigned)row_tiles);
-    if (a.y_type == B2C_F32) e = launch_pdl(matmul_kernel<float>, grid, dim3(256), 0, st, a);
-    else if (a.y_type == B2C_F16) e = launch_pdl(matmul_kernel<__half>, grid, dim3(256), 0, st, a);
-    else e = launch_pdl(matmul_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, a);
+    if (rows <= 16) return launch_rows<16, 2, uint8_t>(a, st);
+    if (rows <= 32) return launch_rows<32, 2, uint8_t>(a, st);
+    return launch_rows<64, 2, uint8_t>(a, st);
   }
-  if (e != cudaSuccess) {
-    set_last_cuda_error((int)e);
-    return B2C_E_CUDA;
-  }
-  return B2C_OK;
+  if (rows <= 16) return launch_rows_type<16>(a, st);
+  if (rows <= 32) return launch_rows_type<32>(a, st);
+  if (rows <= 64) return launch_rows_type<64>(a, st);
+  return launch_rows_type<128>(a, st);
 }
 
 int fp8_status_read_and_clear(int32_t* status) {
   int s = 0;
   cudaError_t e = cudaDeviceSynchronize();
-  if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&s, g_status, sizeof(s));
+  if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&s, g_fp8_status, sizeof(s));
   const int zero = 0;
-  if (e == cudaSuccess && s != 0) e = cudaMemcpyToSymbol(g_status, &zero, sizeof(zero));
-  if (e != cudaSuccess) {
-    set_last_cuda_error((int)e);
-    return B2C_E_CUDA;
-  }
+  if (e == cudaSuccess && s != 0) e = cudaMemcpyToSymbol(g_fp8_status, &zero, sizeof(zero));
+  if (e != cudaSuccess) return fail(e);
   *status = s;
   return B2C_OK;
 }

@@ -1,0 +1,127 @@
+// Device code shared by the two kernels that form products of block-scaled 8-bit matrices on the tensor core.
+//
+// The intrinsic adds unscaled products, and every block of 128 along the reduction has scales of its own.  So each
+// block is an accumulator of its own in tensor memory (four MMAs of depth 32, the first one overwriting), and the
+// epilogue warps add it, times the product of its two scales, to fp32 sums that they keep in registers.
+#pragma once
+
+#include "conv_mma_cluster.cuh"
+#include "fp8_common.cuh"
+
+namespace b2c {
+
+namespace {
+
+__device__ int g_fp8_status;  // first expired wait of any product kernel on this device
+
+// Instruction descriptor of kind::f8f6f4: D = fp32 (code 1 at bit 4), formats of A and B (E4M3 0, E5M2 1) at bits 7 and
+// 10, both K-major, N/8 at bit 17, M/16 at bit 24.
+__device__ __forceinline__ uint32_t make_idesc_f8(int m, int n, int a_type, int b_type) {
+  return (1u << 4) | ((a_type == B2C_E5M2 ? 1u : 0u) << 7) | ((b_type == B2C_E5M2 ? 1u : 0u) << 10) | ((uint32_t)(n >> 3) << 17) |
+         ((uint32_t)(m >> 4) << 24);
+}
+
+// One block of the reduction: `ksteps` (1..4) MMAs over consecutive 32-byte slices, the first overwrites.
+template <int CTAS>
+__device__ __forceinline__ void mma_f8_block(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t on, int ksteps) {
+#define B2C_F8_BLOCK(GROUP)                                                              \
+  asm volatile(                                                                          \
+      "{\n"                                                                              \
+      ".reg .pred pfalse, ptrue, q0, q1, q2, q3;\n"                                      \
+      ".reg .b64 a1, a2, a3, b1, b2, b3;\n"                                              \
+      "setp.ne.b32 pfalse, 0, 0;\n"                                                      \
+      "setp.eq.b32 ptrue, 0, 0;\n"                                                       \
+      "setp.ne.b32 q0, %4, 0;\n"                                                         \
+      "setp.gt.and.s32 q1, %5, 1, q0;\n"                                                 \
+      "setp.gt.and.s32 q2, %5, 2, q0;\n"                                                 \
+      "setp.gt.and.s32 q3, %5, 3, q0;\n"                                                 \
+      "add.u64 a1, %1, 2;\n"                                                             \
+      "add.u64 b1, %2, 2;\n"                                                             \
+      "add.u64 a2, %1, 4;\n"                                                             \
+      "add.u64 b2, %2, 4;\n"                                                             \
+      "add.u64 a3, %1, 6;\n"                                                             \
+      "add.u64 b3, %2, 6;\n"                                                             \
+      "@q0 tcgen05.mma.cta_group::" GROUP ".kind::f8f6f4 [%0], %1, %2, %3, pfalse;\n"    \
+      "@q1 tcgen05.mma.cta_group::" GROUP ".kind::f8f6f4 [%0], a1, b1, %3, ptrue;\n"     \
+      "@q2 tcgen05.mma.cta_group::" GROUP ".kind::f8f6f4 [%0], a2, b2, %3, ptrue;\n"     \
+      "@q3 tcgen05.mma.cta_group::" GROUP ".kind::f8f6f4 [%0], a3, b3, %3, ptrue;\n"     \
+      "}" ::"r"(d_tmem),                                                                 \
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(on), "r"(ksteps)                           \
+      : "memory")
+  if (CTAS == 1) B2C_F8_BLOCK("1");
+  else B2C_F8_BLOCK("2");
+#undef B2C_F8_BLOCK
+}
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar, uint32_t on) {
+  asm volatile(
+      "{\n.reg .pred q;\nsetp.ne.b32 q, %6, 0;\n"
+      "@q cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n}" ::"r"(dst),
+      "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar), "r"(on)
+      : "memory");
+}
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// acc += v * f for a pair of fp32 values.
+__device__ __forceinline__ void fma2(float2* acc, float2 v, float2 f) {
+  unsigned long long a = *reinterpret_cast<unsigned long long*>(acc);
+  asm("fma.rn.f32x2 %0, %1, %2, %0;"
+      : "+l"(a)
+      : "l"(*reinterpret_cast<unsigned long long*>(&v)), "l"(*reinterpret_cast<unsigned long long*>(&f)));
+  *acc = *reinterpret_cast<float2*>(&a);
+}
+
+// Row tile `index` over all groups, each group's rows cut into tiles of `tile` rows; called by a whole warp.  Offsets are
+// clamped to [0, rows] and never fall, so the groups are disjoint and their tiles at most rows / tile + groups.
+struct RowTile {
+  int group, row0, row_end;  // group < 0: there is no such tile
+};
+__device__ __forceinline__ RowTile find_row_tile(const MatmulArgs& a, int index, int tile) {
+  RowTile r = {-1, 0, 0};
+  if (a.offsets == nullptr) {
+    if ((long long)index * tile < a.rows) r = {0, index * tile, a.rows};
+    return r;
+  }
+  const int lane = threadIdx.x & 31;
+  int run = max(0, min(a.offsets[0], a.rows));
+  for (int g0 = 0; g0 < a.groups; g0 += 32) {
+    int hi = g0 + lane < a.groups ? max(0, min(a.offsets[g0 + lane + 1], a.rows)) : 0;
+    hi = max(hi, run);
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, hi, d);
+      if (lane >= d) hi = max(hi, v);
+    }
+    int lo = __shfl_up_sync(0xffffffffu, hi, 1);
+    if (lane == 0) lo = run;
+    const int tiles = (hi - lo + tile - 1) / tile;
+    int sum = tiles;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, sum, d);
+      if (lane >= d) sum += v;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, index < sum);
+    if (hit) {
+      const int l = __ffs(hit) - 1;
+      r.group = g0 + l;
+      r.row0 = __shfl_sync(0xffffffffu, lo + (index - (sum - tiles)) * tile, l);
+      r.row_end = __shfl_sync(0xffffffffu, hi, l);
+      return r;
+    }
+    index -= __shfl_sync(0xffffffffu, sum, 31);
+    run = __shfl_sync(0xffffffffu, hi, 31);
+  }
+  return r;
+}
+
+}  // namespace
+}  // namespace b2c

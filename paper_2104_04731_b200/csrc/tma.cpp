@@ -82,6 +82,29 @@ int encode_tiled_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t
   return B2C_OK;
 }
 
+// A stack of byte matrices; a box lies in one plane, rows past a plane's end read as zeros.
+int encode_tiled_3d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint64_t planes, uint64_t row_stride_bytes,
+                    uint64_t plane_stride_bytes, uint32_t box_inner, uint32_t box_rows, int swizzle_bytes) {
+  std::call_once(g_once, resolve);
+  if (injected_failure()) return B2C_E_CUDA;
+  if (!g_tiled) {
+    set_last_cuda_error((int)CUDA_ERROR_NOT_FOUND);
+    return B2C_E_CUDA;
+  }
+  cuuint64_t dims[3] = {inner, rows, planes};
+  cuuint64_t strides[2] = {row_stride_bytes, plane_stride_bytes};
+  cuuint32_t box[3] = {box_inner, box_rows, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = g_tiled(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estr,
+                       CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle_of(swizzle_bytes), CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    set_last_cuda_error((int)r);
+    return B2C_E_CUDA;
+  }
+  return B2C_OK;
+}
+
 // NHWC activation tensor with C_pad channels seen as a 4-D tensor {C, W, H, N}.  The bounding box
 // of window origins runs from -pad to (extent - 1) + pad - dil*(kernel - 1) on W and H; the
 // traversal strides are the convolution strides, so that `pixels_per_column` consecutive output
