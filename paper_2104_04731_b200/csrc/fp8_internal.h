@@ -66,6 +66,8 @@ struct RouteArgs {
 
 cudaError_t launch_fp8_quantize(const QuantizeArgs& a, cudaStream_t st);
 int launch_fp8_matmul(const MatmulArgs& a, cudaStream_t st);  // B2C_* code
+int launch_fp8_matmul_pair(const MatmulArgs& a, cudaStream_t st);  // its form for many rows
+cudaError_t fp8_pair_status(int* status);
 int fp8_status_read_and_clear(int32_t* status);
 cudaError_t launch_route(const RouteArgs& a, cudaStream_t st);
 size_t route_sort_workspace(long long pairs, int experts);

@@ -155,9 +155,9 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, 2)
     const int quad = warp & 3;                         // lanes of tensor memory this warp may read
     const int c0 = ((warp - 2) >> 2) * S::kWarpCols;   // its columns
     const int et = (int)threadIdx.x - 64;              // thread of this role
-    float2 acc[S::kWarpCols / 2];
+    f32x2 acc[S::kWarpCols / 2];
 #pragma unroll
-    for (int i = 0; i < S::kWarpCols / 2; ++i) acc[i] = make_float2(0.0f, 0.0f);
+    for (int i = 0; i < S::kWarpCols / 2; ++i) acc[i] = 0;
     // thread c fetches the scales of column c (activation row c % NT, weight tile c / NT), a run of blocks ahead
     const bool fetches = et < S::kCols;
     const int tok = row0 + et % NT;
@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, 2)
         asm volatile("bar.sync 1, %0;" ::"n"(32 * S::kEpiWarps) : "memory");
         fetch(kb + kScaleRun);
       }
-      ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.tmem_full[buf]), bph, &ctl, &g_fp8_status));
+      ok = ok && __all_sync(0xffffffffu, mbar_wait_inline(smem_u32(&ctl.tmem_full[buf]), bph, &ctl, &g_fp8_status));
       if (!ok) continue;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t taddr = tmem_acc + ((uint32_t)(quad * 32) << 16) + (uint32_t)(buf * S::kCols + c0);
@@ -196,8 +196,8 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, 2)
 #pragma unroll
         for (int j = 0; j < kLd; j += 4) {
           const float4 f = *reinterpret_cast<const float4*>(&factor[run][i][c0 + c + j]);
-          fma2(&acc[(c + j) / 2], make_float2(v[j], v[j + 1]), make_float2(f.x, f.y));
-          fma2(&acc[(c + j) / 2 + 1], make_float2(v[j + 2], v[j + 3]), make_float2(f.z, f.w));
+          fma2(&acc[(c + j) / 2], pair_of(v[j], v[j + 1]), pair_of(f.x, f.y));
+          fma2(&acc[(c + j) / 2 + 1], pair_of(v[j + 2], v[j + 3]), pair_of(f.z, f.w));
         }
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -211,8 +211,12 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, 2)
     // every MMA of this block has been waited for, so the stages are free: the sums take their place
     float* part = reinterpret_cast<float*>(smem_raw + (smem_base - smem_u32(smem_raw)));
 #pragma unroll
-    for (int i = 0; i < S::kWarpCols; ++i)
-      part[(c0 + i) * kTileM + quad * 32 + lane] = (i & 1) ? acc[i / 2].y : acc[i / 2].x;
+    for (int i = 0; i < S::kWarpCols; i += 2) {
+      float lo, hi;
+      unpair(acc[i / 2], &lo, &hi);
+      part[(c0 + i) * kTileM + quad * 32 + lane] = lo;
+      part[(c0 + i + 1) * kTileM + quad * 32 + lane] = hi;
+    }
   }
 
   // ---------------------------------------------------------------- sums of the cluster, results
@@ -311,6 +315,7 @@ int launch_rows_type(const MatmulArgs& a, cudaStream_t st) {
 
 int launch_fp8_matmul(const MatmulArgs& a, cudaStream_t st) {
   const int rows = a.offsets ? (a.rows + a.groups - 1) / a.groups : a.rows;  // of a group, on average
+  if (rows > 128) return launch_fp8_matmul_pair(a, st);
   if (a.gated) {
     if (rows <= 16) return launch_rows<16, 2, uint8_t>(a, st);
     if (rows <= 32) return launch_rows<32, 2, uint8_t>(a, st);
@@ -323,13 +328,12 @@ int launch_fp8_matmul(const MatmulArgs& a, cudaStream_t st) {
 }
 
 int fp8_status_read_and_clear(int32_t* status) {
-  int s = 0;
+  int rows = 0, pair = 0;
   cudaError_t e = cudaDeviceSynchronize();
-  if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&s, g_fp8_status, sizeof(s));
-  const int zero = 0;
-  if (e == cudaSuccess && s != 0) e = cudaMemcpyToSymbol(g_fp8_status, &zero, sizeof(zero));
+  if (e == cudaSuccess) e = take_status(&rows);
+  if (e == cudaSuccess) e = fp8_pair_status(&pair);
   if (e != cudaSuccess) return fail(e);
-  *status = s;
+  *status = rows != 0 ? rows : pair;
   return B2C_OK;
 }
 

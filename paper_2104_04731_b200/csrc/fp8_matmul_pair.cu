@@ -1,0 +1,441 @@
+// Products of block-scaled 8-bit matrices for many rows: a pair of thread blocks on neighbouring SMs shares one tile of
+// 256 rows x 256 columns (tcgen05 cta_group::2).  Each block loads its own 128 rows of A and half of the B rows, so
+// that 64 bytes a cycle and SM feed the tensor core at its full rate (512 cycles for a block of 128 of the reduction).
+// What bounds it besides: the 128 x 256 accumulators of every such block go through the registers of eight warps, one
+// FMA each - half of the MMA's time if nothing waits.  Two accumulators in tensor memory (all 512 columns) let the
+// epilogue of one block run under the MMAs of the next.
+//
+// Roles in each block: warp 0 copies, warp 1 of the leader issues the MMAs, warps 2-9 keep the scaled sums: a warp
+// has 32 rows x 128 columns, a thread one row, so its row scale is a register and its column scale the same for the warp.
+// The gated form takes 128 gate rows and the 128 up rows of the same columns as one B tile, ordered so that a thread holds
+// 64 gate sums and the 64 up sums that belong to them; the activation and the quantisation happen in registers.
+#include "fp8_mma.cuh"
+
+namespace b2c {
+
+namespace {
+
+constexpr int kEpiWarps = 8;
+constexpr int kScaleWarps = 2;
+constexpr int kPairThreads = 64 + 32 * (kEpiWarps + kScaleWarps);
+constexpr int kTileN = 256;
+constexpr int kStages = 6;
+constexpr int kABytes = kTileM * kBlock, kBBytes = kTileN / 2 * kBlock;
+constexpr int kPairSmem = 1024 + kStages * (kABytes + kBBytes);
+constexpr int kRun = 4;       // blocks of the reduction whose scales are fetched together
+constexpr int kRunSlots = 3;  // runs of factors in shared memory
+constexpr int kBand = 8;  // row tiles that are walked together, so that their columns' B tiles are read from L2
+
+__device__ __forceinline__ void tma_pair_load_3d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar, uint32_t on) {
+  asm volatile(
+      "{\n.reg .pred q;\nsetp.ne.b32 q, %6, 0;\n"
+      "@q cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], "
+      "[%5];\n}" ::"r"(dst),
+      "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar), "r"(on)
+      : "memory");
+}
+
+// Arrival on a barrier of the leader that hands back accumulator columns.  What it orders are reads of tensor memory, and
+// these have ended (tcgen05.wait::ld): no write of this thread has to be seen by the other side.  With .release, at
+// cluster scope, every arrival waited for the thread's loads of scales under way (2100 of the 2500 cycles of a block).
+__device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
+// Row tiles of all groups; called by a whole warp.
+__device__ __forceinline__ int count_row_tiles(const MatmulArgs& a, int tile) {
+  if (a.offsets == nullptr) return (a.rows + tile - 1) / tile;
+  const int lane = threadIdx.x & 31;
+  int run = max(0, min(a.offsets[0], a.rows)), all = 0;
+  for (int g0 = 0; g0 < a.groups; g0 += 32) {
+    int hi = g0 + lane < a.groups ? max(0, min(a.offsets[g0 + lane + 1], a.rows)) : 0;
+    hi = max(hi, run);
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, hi, d);
+      if (lane >= d) hi = max(hi, v);
+    }
+    int lo = __shfl_up_sync(0xffffffffu, hi, 1);
+    if (lane == 0) lo = run;
+    all += __reduce_add_sync(0xffffffffu, (hi - lo + tile - 1) / tile);
+    run = __shfl_sync(0xffffffffu, hi, 31);
+  }
+  return all;
+}
+
+struct PairTile {
+  int group, row0, row_end, nt;
+};
+// Tile t of the walk: without groups bands of kBand row tiles, column by column; with groups row tile by row tile.
+__device__ __forceinline__ PairTile pair_tile(const MatmulArgs& a, int t, int row_tiles, int n_tiles) {
+  PairTile p;
+  int mt;
+  if (a.offsets == nullptr) {
+    const int band = t / (kBand * n_tiles);
+    const int in = t - band * kBand * n_tiles;
+    const int height = min(kBand, row_tiles - band * kBand);
+    p.nt = in / height;
+    mt = band * kBand + in - p.nt * height;
+  } else {
+    mt = t / n_tiles;
+    p.nt = t - mt * n_tiles;
+  }
+  const RowTile r = find_row_tile(a, mt, 2 * kTileM);
+  p.group = r.group;
+  p.row0 = r.row0;
+  p.row_end = r.row_end;
+  return p;
+}
+
+// 32 values of one row from column n on; `n_end`: columns of the matrix.
+template <typename T>
+__device__ __forceinline__ void store_row32(T* p, const float* v, int n, int n_end) {
+  if (n + 32 <= n_end && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; i += 8)
+        *reinterpret_cast<uint4*>(p + i) = make_uint4(pack2<T>(v[i], v[i + 1]), pack2<T>(v[i + 2], v[i + 3]), pack2<T>(v[i + 4], v[i + 5]),
+                                                      pack2<T>(v[i + 6], v[i + 7]));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (n + i < n_end) p[i] = from_float<T>(v[i]);
+  }
+}
+
+template <bool GATED, typename YT>
+__global__ void __launch_bounds__(kPairThreads, 1)
+    matmul_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b, const MatmulArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ SharedCtl ctl;
+  __shared__ int row_tiles_s;
+  // products of a row's scale and a column block's: [slot][block of the run][column block][row]
+  __shared__ float factor[kRunSlots][kRun][2][kTileM];
+  __shared__ __align__(8) unsigned long long factor_full[kRunSlots], factor_empty[kRunSlots];
+  __shared__ float row_max[2][2][kTileM];  // gated: largest magnitude of a row's halves, by tile parity
+
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
+  const int lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();  // 0: leader (issues the MMAs), 1: peer
+  const int pair_id = (int)(blockIdx.x >> 1), num_pairs = (int)(gridDim.x >> 1);
+  const uint32_t a_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t b_base = a_base + kStages * kABytes;
+
+  if (warp == 0) {
+    if (lane < kStages) {
+      // full[] is used in the leader only: one arrival (its producer) plus the bytes of both blocks
+      mbar_init(smem_u32(&ctl.full[lane]), 1);
+      mbar_init(smem_u32(&ctl.empty[lane]), 1);
+    }
+    if (lane == 8) {
+      for (int b = 0; b < 2; ++b) {
+        mbar_init(smem_u32(&ctl.tmem_full[b]), 1);
+        mbar_init(smem_u32(&ctl.tmem_empty[b]), 2 * kEpiWarps);  // the epilogue warps of both blocks
+      }
+      for (int b = 0; b < kRunSlots; ++b) {
+        mbar_init(smem_u32(&factor_full[b]), kScaleWarps);
+        mbar_init(smem_u32(&factor_empty[b]), kEpiWarps);
+      }
+      ctl.abort_flag = 0;
+    }
+    if (lane == 9) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_a) : "memory");
+    if (lane == 10) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_b) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl.tmem_base)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  pdl_wait();
+  if (warp == 2) {
+    const int n = count_row_tiles(a, 2 * kTileM);
+    if (lane == 0) row_tiles_s = n;
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  // the other block's barriers must be initialised before anything arrives on them
+  cluster_sync();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem_acc = __shfl_sync(0xffffffffu, ctl.tmem_base, 0);
+  const int row_tiles = row_tiles_s;
+  const int cols = GATED ? kBlock : kTileN;  // output columns of a tile
+  const int n_tiles = (a.N + cols - 1) / cols;
+  const int tiles = row_tiles * n_tiles;     // (fits: checked by the host)
+  const int kb_all = (int)blocks_of(a.K);
+
+  if (warp == 0) {
+    // ---------------------------------------------------------------- copies (both blocks)
+    const uint32_t on = elect_one() ? 1u : 0u;
+    int s = 0;
+    uint32_t ph = 0;
+    bool alive = true;
+    for (int t = pair_id; t < tiles && alive; t += num_pairs) {
+      const PairTile p = pair_tile(a, t, row_tiles, n_tiles);
+      const int m = p.row0 + (int)rank * kTileM;
+      for (int kb = 0; kb < kb_all; ++kb) {
+        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.empty[s]), ph ^ 1u, &ctl, &g_fp8_status))) {
+          alive = false;
+          break;
+        }
+        const uint32_t full = map_to_rank(smem_u32(&ctl.full[s]), 0u);
+        if (rank == 0) mbar_arrive_expect_tx(smem_u32(&ctl.full[s]), 2u * (kABytes + kBBytes), on);
+        tma_pair_load_2d(a_base + s * kABytes, &tmap_a, kb * kBlock, m, full, on);
+        const uint32_t dst = b_base + s * kBBytes;
+        if (GATED) {
+          const int n = p.nt * kBlock + (int)rank * 64;
+          tma_pair_load_3d(dst, &tmap_b, kb * kBlock, n, 2 * p.group, full, on);
+          tma_pair_load_3d(dst + 64 * kBlock, &tmap_b, kb * kBlock, n, 2 * p.group + 1, full, on);
+        } else {
+          tma_pair_load_3d(dst, &tmap_b, kb * kBlock, p.nt * kTileN + (int)rank * kTileM, p.group, full, on);
+        }
+        if (++s == kStages) {
+          s = 0;
+          ph ^= 1u;
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    // ---------------------------------------------------------------- MMA issue (leader)
+    if (rank == 0) {
+      const uint32_t on = elect_one() ? 1u : 0u;
+      const uint32_t idesc = make_idesc_f8(2 * kTileM, kTileN, a.a_type, a.b_type);
+      int s = 0, buf = 0;
+      uint32_t ph = 0, bph = 0;
+      bool alive = true;
+      for (int t = pair_id; t < tiles && alive; t += num_pairs) {
+        for (int kb = 0; kb < kb_all; ++kb) {
+          if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.full[s]), ph, &ctl, &g_fp8_status)) ||
+              !__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.tmem_empty[buf]), bph ^ 1u, &ctl, &g_fp8_status))) {
+            alive = false;
+            break;
+          }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const int ksteps = min(4, (a.K - kb * kBlock + kMmaK - 1) / kMmaK);
+          mma_f8_block<2>(tmem_acc + buf * kTileN, make_smem_desc(a_base + s * kABytes, kBlock), make_smem_desc(b_base + s * kBBytes, kBlock), idesc,
+                          on, ksteps);
+          mma_commit_pair(smem_u32(&ctl.empty[s]), on);
+          mma_commit_pair(smem_u32(&ctl.tmem_full[buf]), on);
+          if (++s == kStages) {
+            s = 0;
+            ph ^= 1u;
+          }
+          buf ^= 1;
+          if (buf == 0) bph ^= 1u;
+        }
+      }
+    }
+    pdl_launch_dependents();
+    __syncwarp();
+  } else if (warp >= 2 + kEpiWarps) {
+    // ---------------------------------------------------------------- scales (both blocks)
+    // A thread has two rows.  The loads of a run are under way while the run before it is multiplied and handed over.
+    const int st = (int)threadIdx.x - 32 * (2 + kEpiWarps);
+    const int nb = (int)blocks_of(a.N);
+    int slot = 0;
+    uint32_t sph = 0;
+    bool alive = true;
+    for (int t = pair_id; t < tiles && alive; t += num_pairs) {
+      const PairTile p = pair_tile(a, t, row_tiles, n_tiles);
+      const float* sa[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        sa[h] = a.a_scale + min((long long)p.row0 + (int)rank * kTileM + st + 64 * h, (long long)a.rows - 1) * a.lds;
+      // the two column blocks: gate and up, or the two of the tile (past the end: the last one again)
+      const float* sb[2];
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        sb[c] = a.b_scale + (GATED ? (long long)(2 * p.group + c) * nb + p.nt : (long long)p.group * nb + min(2 * p.nt + c, nb - 1)) * kb_all;
+      float na[2][kRun], ncol[2][kRun];
+      auto fetch = [&](int kb) {
+#pragma unroll
+        for (int i = 0; i < kRun; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            na[h][i] = kb + i < kb_all ? sa[h][kb + i] : 0.0f;
+            ncol[h][i] = kb + i < kb_all ? sb[h][kb + i] : 0.0f;
+          }
+      };
+      fetch(0);
+      for (int kb = 0; kb < kb_all; kb += kRun) {
+        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&factor_empty[slot]), sph ^ 1u, &ctl, &g_fp8_status))) {
+          alive = false;
+          break;
+        }
+#pragma unroll
+        for (int i = 0; i < kRun; ++i)
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) factor[slot][i][c][st + 64 * h] = na[h][i] * ncol[c][i];
+        fetch(kb + kRun);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&factor_full[slot]));
+        if (++slot == kRunSlots) {
+          slot = 0;
+          sph ^= 1u;
+        }
+      }
+    }
+  } else {
+    // ---------------------------------------------------------------- scaled sums and results (both blocks)
+    const int quad = warp & 3;         // lanes of tensor memory this warp may read
+    const int half = (warp - 2) >> 2;  // its 128 columns
+    const uint32_t leader_empty = map_to_rank(smem_u32(&ctl.tmem_empty[0]), 0u);
+    const uint32_t taddr0 = tmem_acc + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * 128);
+    const int in_tile = quad * 32 + lane;
+    int slot = 0;
+    uint32_t sph = 0;
+    int buf = 0, parity = 0;
+    uint32_t bph = 0;
+    bool ok = true;
+    for (int t = pair_id; t < tiles; t += num_pairs, parity ^= 1) {
+      const PairTile p = pair_tile(a, t, row_tiles, n_tiles);
+      const long long m = (long long)p.row0 + (int)rank * kTileM + in_tile;
+      f32x2 acc[64];
+#pragma unroll
+      for (int i = 0; i < 64; ++i) acc[i] = 0;
+#pragma unroll 1
+      for (int kb = 0; kb < kb_all; ++kb) {
+        const int i = kb % kRun;
+        if (i == 0) ok = ok && __all_sync(0xffffffffu, mbar_wait_inline(smem_u32(&factor_full[slot]), sph, &ctl, &g_fp8_status));
+        const float f = factor[slot][i][GATED ? 0 : half][in_tile], fu = GATED ? factor[slot][i][1][in_tile] : 0.0f;
+        if (i == kRun - 1 || kb == kb_all - 1) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&factor_empty[slot]));
+          if (++slot == kRunSlots) {
+            slot = 0;
+            sph ^= 1u;
+          }
+        }
+        const f32x2 ff = pair_of(f, f), ffu = pair_of(fu, fu);
+        ok = ok && __all_sync(0xffffffffu, mbar_wait_inline(smem_u32(&ctl.tmem_full[buf]), bph, &ctl, &g_fp8_status));
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t taddr = taddr0 + (uint32_t)(buf * kTileN);
+#pragma unroll
+        for (int c = 0; c < 128; c += 32) {
+          float v[32];
+          tmem_ld<32>(taddr + c, reinterpret_cast<int32_t*>(v));
+          if (c == 96) {
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster_relaxed(leader_empty + 8 * buf);
+          }
+#pragma unroll
+          for (int j = 0; j < 32; j += 2) fma2(&acc[(c + j) / 2], pair_of(v[j], v[j + 1]), GATED && c >= 64 ? ffu : ff);
+        }
+        buf ^= 1;
+        if (buf == 0) bph ^= 1u;
+      }
+      if constexpr (GATED) {
+        float h[64], u[64], mx = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          unpair(acc[i], &h[2 * i], &h[2 * i + 1]);
+          unpair(acc[32 + i], &u[2 * i], &u[2 * i + 1]);
+        }
+#pragma unroll
+        for (int i = 0; i < 64; ++i) {
+          h[i] = silu(h[i]) * u[i];
+          mx = fmaxf(mx, fabsf(h[i]));
+        }
+        // a block of 128 columns is the two halves of a row: two warps
+        row_max[parity][half][in_tile] = mx;
+        asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");
+        const BlockScale s = block_scale<B2C_E4M3>(fmaxf(mx, row_max[parity][half ^ 1][in_tile]));
+        if (ok && m < p.row_end) {
+          const int n = p.nt * kBlock + half * 64;
+          uint8_t* y = (uint8_t*)a.y + m * a.ldy + n;
+#pragma unroll
+          for (int i = 0; i < 64; i += 16)
+            if (n + i < a.N) *reinterpret_cast<uint4*>(y + i) = quantize16<B2C_E4M3>(s, h + i);  // (N and ldy are multiples of 16)
+          if (half == 0) a.y_scale[m * a.ldys + p.nt] = s.scale;
+        }
+      } else {
+        if (ok && m < p.row_end) {
+          const int n = p.nt * kTileN + half * 128;
+          YT* y = (YT*)a.y + m * a.ldy + n;
+#pragma unroll
+          for (int i = 0; i < 128; i += 32) {
+            float v[32];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) unpair(acc[i / 2 + j], &v[2 * j], &v[2 * j + 1]);
+            if (n + i < a.N) store_row32<YT>(y + i, v, n + i, a.N);
+          }
+        }
+      }
+    }
+  }
+
+  // ---------------------------------------------------------------- teardown
+  // No block of the pair leaves, or frees tensor memory, while the other may still read its shared memory, arrive on
+  // its barriers or write its accumulators.
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (ctl.abort_flag) {
+    const unsigned long long t0 = global_ns();
+    while (global_ns() - t0 < 50000ull) __nanosleep(1000);
+    __syncthreads();
+  }
+  cluster_sync();
+  if (warp == 1) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_acc), "r"(512) : "memory");
+  }
+}
+
+template <bool GATED, typename YT>
+int launch_pair(const MatmulArgs& a, cudaStream_t st) {
+  const long long cols = GATED ? kBlock : kTileN;
+  const long long n_tiles = (a.N + cols - 1) / cols;
+  const long long row_tiles = a.offsets ? a.rows / (2 * kTileM) + std::min(a.groups, a.rows) : (a.rows + 2 * kTileM - 1) / (2 * kTileM);
+  if (row_tiles * n_tiles > 0x7FFFFFFFLL - kNumSMs) return B2C_E_UNSUPPORTED;
+  CUtensorMap ta, tb;
+  int rc = encode_tiled_2d(&ta, a.a, a.K, a.rows, a.rows > 1 ? a.lda : a.K, kBlock, kTileM, kBlock);
+  if (rc == B2C_OK)
+    rc = encode_tiled_3d(&tb, a.b, a.K, a.N, (uint64_t)a.groups * (GATED ? 2 : 1), a.K, (uint64_t)a.N * a.K, kBlock, GATED ? 64 : kTileM, kBlock);
+  if (rc != B2C_OK) return rc;
+  static std::atomic<unsigned long long> configured{0};
+  cudaError_t e = set_max_dynamic_smem_once(configured, (const void*)matmul_pair_kernel<GATED, YT>, kPairSmem);
+  if (e == cudaSuccess) {
+    const int pairs = (int)std::min<long long>(row_tiles * n_tiles, kNumSMs / 2);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(2 * pairs));
+    cfg.blockDim = dim3(kPairThreads);
+    cfg.dynamicSmemBytes = kPairSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    e = cudaLaunchKernelEx(&cfg, matmul_pair_kernel<GATED, YT>, ta, tb, a);
+  }
+  if (e != cudaSuccess) {
+    set_last_cuda_error((int)e);
+    return B2C_E_CUDA;
+  }
+  return B2C_OK;
+}
+
+}  // namespace
+
+int launch_fp8_matmul_pair(const MatmulArgs& a, cudaStream_t st) {
+  if (a.gated) return launch_pair<true, uint8_t>(a, st);
+  if (a.y_type == B2C_F32) return launch_pair<false, float>(a, st);
+  if (a.y_type == B2C_F16) return launch_pair<false, __half>(a, st);
+  return launch_pair<false, __nv_bfloat16>(a, st);
+}
+
+cudaError_t fp8_pair_status(int* status) { return take_status(status); }
+
+}  // namespace b2c

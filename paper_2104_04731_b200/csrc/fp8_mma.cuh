@@ -12,7 +12,15 @@ namespace b2c {
 
 namespace {
 
-__device__ int g_fp8_status;  // first expired wait of any product kernel on this device
+__device__ int g_fp8_status;  // first expired wait of this file's kernels on the device
+
+// Reads and clears it; the device is idle.
+inline cudaError_t take_status(int* status) {
+  const int zero = 0;
+  cudaError_t e = cudaMemcpyFromSymbol(status, g_fp8_status, sizeof(int));
+  if (e == cudaSuccess && *status != 0) e = cudaMemcpyToSymbol(g_fp8_status, &zero, sizeof(zero));
+  return e;
+}
 
 // Instruction descriptor of kind::f8f6f4: D = fp32 (code 1 at bit 4), formats of A and B (E4M3 0, E5M2 1) at bits 7 and
 // 10, both K-major, N/8 at bit 17, M/16 at bit 24.
@@ -70,13 +78,32 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// acc += v * f for a pair of fp32 values.
-__device__ __forceinline__ void fma2(float2* acc, float2 v, float2 f) {
-  unsigned long long a = *reinterpret_cast<unsigned long long*>(acc);
-  asm("fma.rn.f32x2 %0, %1, %2, %0;"
-      : "+l"(a)
-      : "l"(*reinterpret_cast<unsigned long long*>(&v)), "l"(*reinterpret_cast<unsigned long long*>(&f)));
-  *acc = *reinterpret_cast<float2*>(&a);
+// A pair of fp32 values in one 64-bit register pair; acc += v * f in one instruction.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair_of(float lo, float hi) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpair(f32x2 v, float* lo, float* hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*lo), "=f"(*hi) : "l"(v)); }
+__device__ __forceinline__ void fma2(f32x2* acc, f32x2 v, f32x2 f) { asm volatile("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(*acc) : "l"(v), "l"(f)); }
+
+// Bounded wait of the warps that keep sums in registers: as mbar_wait, without a call (which would have to save them).
+__device__ __forceinline__ bool mbar_wait_inline(uint32_t bar, uint32_t parity, SharedCtl* ctl, int* status) {
+  unsigned long long t0 = 0;
+#pragma unroll 1
+  for (int i = 0; !mbar_try_wait(bar, parity); ++i) {
+    if (i < 32) continue;
+    if (ctl->abort_flag) return false;
+    const unsigned long long now = global_ns();
+    if (t0 == 0) t0 = now;
+    if (now - t0 > kWaitLimitNs) {
+      ctl->abort_flag = 1;
+      atomicCAS(status, 0, B2C_E_TIMEOUT);
+      return false;
+    }
+  }
+  return true;
 }
 
 // Row tile `index` over all groups, each group's rows cut into tiles of `tile` rows; called by a whole warp.  Offsets are
