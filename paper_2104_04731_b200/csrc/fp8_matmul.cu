@@ -287,7 +287,8 @@ int launch_rows(const MatmulArgs& a, cudaStream_t st) {
   // every group adds at most one tile that is not full
   const long long row_tiles = a.offsets ? a.rows / NT + std::min(a.groups, a.rows) : (a.rows + NT - 1) / NT;
   if (row_tiles > 65535) return B2C_E_UNSUPPORTED;
-  const long long busy = (long long)n_tiles * (a.offsets ? (a.rows + NT - 1) / NT : row_tiles);
+  // (with groups the number of tiles is known on the device only: as many groups as there are rows may have some)
+  const long long busy = (long long)n_tiles * (a.offsets ? std::max<long long>((a.rows + NT - 1) / NT, std::min(a.groups, a.rows)) : row_tiles);
   int split = (int)std::min<long long>(kMaxSplit, std::max<long long>(1, 2 * kNumSMs / std::max<long long>(1, busy)));
   split = std::max(1, std::min(split, kb_all / 2));
   const int kb_per_split = (kb_all + split - 1) / split;

@@ -115,6 +115,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   __shared__ int row_tiles_s;
   // products of a row's scale and a column block's: [slot][block of the run][column block][row]
   __shared__ float factor[kRunSlots][kRun][2][kTileM];
+  __shared__ PairTile run_tile[kRunSlots];  // the tile that a run belongs to
   __shared__ __align__(8) unsigned long long factor_full[kRunSlots], factor_empty[kRunSlots];
   __shared__ float row_max[2][2][kTileM];  // gated: largest magnitude of a row's halves, by tile parity
 
@@ -233,6 +234,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     __syncwarp();
   } else if (warp >= 2 + kEpiWarps) {
     // ---------------------------------------------------------------- scales (both blocks)
+    // They also find the tiles: the warps of sums, which have no time for that, read them beside the first factors.
     // A thread has two rows.  The loads of a run are under way while the run before it is multiplied and handed over.
     const int st = (int)threadIdx.x - 32 * (2 + kEpiWarps);
     const int nb = (int)blocks_of(a.N);
@@ -272,6 +274,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           for (int c = 0; c < 2; ++c)
 #pragma unroll
             for (int h = 0; h < 2; ++h) factor[slot][i][c][st + 64 * h] = na[h][i] * ncol[c][i];
+        if (st == 0) run_tile[slot] = p;
         fetch(kb + kRun);
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&factor_full[slot]));
@@ -294,8 +297,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     uint32_t bph = 0;
     bool ok = true;
     for (int t = pair_id; t < tiles; t += num_pairs, parity ^= 1) {
-      const PairTile p = pair_tile(a, t, row_tiles, n_tiles);
-      const long long m = (long long)p.row0 + (int)rank * kTileM + in_tile;
+      PairTile p = {0, 0, 0, 0};
       f32x2 acc[64];
 #pragma unroll
       for (int i = 0; i < 64; ++i) acc[i] = 0;
@@ -303,6 +305,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       for (int kb = 0; kb < kb_all; ++kb) {
         const int i = kb % kRun;
         if (i == 0) ok = ok && __all_sync(0xffffffffu, mbar_wait_inline(smem_u32(&factor_full[slot]), sph, &ctl, &g_fp8_status));
+        if (kb == 0) p = run_tile[slot];
         const float f = factor[slot][i][GATED ? 0 : half][in_tile], fu = GATED ? factor[slot][i][1][in_tile] : 0.0f;
         if (i == kRun - 1 || kb == kb_all - 1) {
           __syncwarp();
@@ -332,6 +335,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         buf ^= 1;
         if (buf == 0) bph ^= 1u;
       }
+      const long long m = (long long)p.row0 + (int)rank * kTileM + in_tile;
       if constexpr (GATED) {
         float h[64], u[64], mx = 0.0f;
 #pragma unroll

@@ -17,7 +17,7 @@ template <typename T>
 __device__ __forceinline__ void load_part(const QuantizeArgs& a, bool vec, long long row, int c0, float* v) {
   const T* p = (const T*)a.x + row * a.ldx + c0;
   if (vec && c0 + 16 <= a.cols) {
-    load16<T>(p, v);
+    load16(p, v);
   } else {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = c0 + i < a.cols ? to_float<T>(p[i]) : 0.0f;

@@ -218,29 +218,74 @@ __global__ void __launch_bounds__(kChunk) place_kernel(const int32_t* ids, const
 
 // ---- weighted sum ---------------------------------------------------------------------------------------------------
 
-template <typename T>
-__device__ __forceinline__ float load_type(const void* p, long long i) { return to_float<T>(((const T*)p)[i]); }
-__device__ __forceinline__ float load_any(const void* p, int type, long long i) {
-  return type == B2C_F32 ? load_type<float>(p, i) : (type == B2C_F16 ? load_type<__half>(p, i) : load_type<__nv_bfloat16>(p, i));
+// W neighbouring columns of a row in one load and one store (1 where alignment or width do not allow more).
+template <typename T, int W>
+__device__ __forceinline__ void load_cols(const T* p, float* v) {
+  if constexpr (W == 1) {
+    v[0] = to_float<T>(p[0]);
+  } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < W; i += 4) {
+      const float4 f = *reinterpret_cast<const float4*>(p + i);
+      v[i] = f.x;
+      v[i + 1] = f.y;
+      v[i + 2] = f.z;
+      v[i + 3] = f.w;
+    }
+  } else {
+    static_assert(W == 8, "16 bytes");
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack2<T>(w[i], &v[2 * i], &v[2 * i + 1]);
+  }
+}
+template <typename T, int W>
+__device__ __forceinline__ void store_cols(T* p, const float* v) {
+  if constexpr (W == 1) {
+    p[0] = from_float<T>(v[0]);
+  } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < W; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+  } else {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+  }
 }
 
-__global__ void __launch_bounds__(256) combine_kernel(const void* y, const int y_type, const long long y_rows, const long long ldy, const int32_t* rows,
+// Weighted sum of a token's rows: memory-bound, every row is read once.  A thread has W columns of one token; four slots'
+// loads are under way together.
+template <typename YT, typename OT, int W>
+__global__ void __launch_bounds__(256) combine_kernel(const YT* y, const long long y_rows, const long long ldy, const int32_t* rows,
                                                      const float* weights, const long long tokens, const int topk, const int cols,
-                                                     void* out, const int out_type, const long long ldo) {
+                                                     const int pieces, OT* out, const long long ldo) {
   pdl_wait();
   pdl_launch_dependents();
-  const long long t = blockIdx.x;
-  for (int c = threadIdx.x; c < cols; c += 256) {
-    float sum = 0.0f;
-    for (int j = 0; j < topk; ++j) {
-      const int r = rows[t * topk + j];
-      if (r >= 0 && r < y_rows) sum = fmaf(weights[t * topk + j], load_any(y, y_type, r * ldy + c), sum);
+  const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+  const long long t = id / pieces;
+  const int c = (int)(id - t * pieces) * W;
+  if (t >= tokens) return;
+  const int32_t* r = rows + t * topk;
+  const float* wt = weights + t * topk;
+  float sum[W];
+#pragma unroll
+  for (int i = 0; i < W; ++i) sum[i] = 0.0f;
+  for (int j0 = 0; j0 < topk; j0 += 4) {
+    float v[4][W], w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int row = j0 + j < topk ? r[j0 + j] : -1;
+      const bool on = row >= 0 && row < y_rows;
+      w[j] = on ? wt[j0 + j] : 0.0f;
+#pragma unroll
+      for (int i = 0; i < W; ++i) v[j][i] = 0.0f;
+      if (on) load_cols<YT, W>(y + row * ldy + c, v[j]);
     }
-    const long long o = t * ldo + c;
-    if (out_type == B2C_F32) ((float*)out)[o] = sum;
-    else if (out_type == B2C_F16) ((__half*)out)[o] = from_float<__half>(sum);
-    else ((__nv_bfloat16*)out)[o] = from_float<__nv_bfloat16>(sum);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < W; ++i) sum[i] = fmaf(w[j], v[j][i], sum[i]);
   }
+  store_cols<OT, W>(out + t * ldo + c, sum);
 }
 
 }  // namespace
@@ -281,10 +326,32 @@ cudaError_t launch_route_sort(const int32_t* ids, long long pairs, int experts, 
                     (const int32_t*)(chunks > 1 ? workspace : nullptr), chunks, offsets, rows, order);
 }
 
-cudaError_t launch_route_combine(const void* y, int y_type, long long y_rows, long long ldy, const int32_t* rows, const float* weights, long long tokens,
-                                 int topk, int cols, void* out, int out_type, long long ldo, cudaStream_t st) {
-  return launch_pdl(combine_kernel, dim3((unsigned)tokens), dim3(256), 0, st, y, y_type, y_rows, ldy, rows, weights, tokens, topk, cols, out,
-                    out_type, ldo);
+namespace {
+
+template <typename YT, typename OT>
+cudaError_t combine(const void* y, long long y_rows, long long ldy, const int32_t* rows, const float* weights, long long tokens, int topk,
+                    int cols, void* out, long long ldo, cudaStream_t st) {
+  auto fits = [](const void* p, long long ld, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld * bytes) % 16 == 0; };
+  const bool wide = cols % 8 == 0 && fits(y, ldy, sizeof(YT)) && fits(out, ldo, sizeof(OT));
+  const int pieces = wide ? cols / 8 : cols;
+  const long long grid = (tokens * pieces + 255) / 256;
+  if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
+  return launch_pdl(wide ? combine_kernel<YT, OT, 8> : combine_kernel<YT, OT, 1>, dim3((unsigned)grid), dim3(256), 0, st, (const YT*)y, y_rows,
+                    ldy, rows, weights, tokens, topk, cols, pieces, (OT*)out, ldo);
+}
+
+}  // namespace
+
+cudaError_t launch_route_combine(const void* y, int y_type, long long y_rows, long long ldy, const int32_t* rows, const float* weights,
+                                 long long tokens, int topk, int cols, void* out, int out_type, long long ldo, cudaStream_t st) {
+#define B2C_COMBINE(YT)                                                                                                        \
+  return out_type == B2C_F32   ? combine<YT, float>(y, y_rows, ldy, rows, weights, tokens, topk, cols, out, ldo, st)           \
+         : out_type == B2C_F16 ? combine<YT, __half>(y, y_rows, ldy, rows, weights, tokens, topk, cols, out, ldo, st)          \
+                               : combine<YT, __nv_bfloat16>(y, y_rows, ldy, rows, weights, tokens, topk, cols, out, ldo, st)
+  if (y_type == B2C_F32) B2C_COMBINE(float);
+  if (y_type == B2C_F16) B2C_COMBINE(__half);
+  B2C_COMBINE(__nv_bfloat16);
+#undef B2C_COMBINE
 }
 
 }  // namespace b2c
