@@ -8,121 +8,292 @@ namespace {
 
 constexpr unsigned kAll = 0xffffffffu;
 
-// Doubles as unsigned integers of the same order (NaN below everything else, but above 0, which marks what is out).
+// Floats as unsigned integers of the same order (NaN below everything else, but above 0, which marks what is out).
+__device__ __forceinline__ unsigned order_key(float v) {
+  if (v != v) return 1u;
+  const unsigned b = __float_as_uint(v);
+  return (b >> 31) ? ~b : b | 0x80000000u;
+}
 __device__ __forceinline__ unsigned long long order_key(double v) {
   if (v != v) return 1ull;
-  const long long b = __double_as_longlong(v);
-  return b < 0 ? ~(unsigned long long)b : (unsigned long long)b | 0x8000000000000000ull;
+  const unsigned long long b = (unsigned long long)__double_as_longlong(v);
+  return (b >> 63) ? ~b : b | 0x8000000000000000ull;
 }
-// The larger key, at equal keys the lower index, over the warp.
-__device__ __forceinline__ void warp_best(unsigned long long* key, int* index) {
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) {
-    const unsigned long long k = __shfl_xor_sync(kAll, *key, d);
-    const int i = __shfl_xor_sync(kAll, *index, d);
-    if (k > *key || (k == *key && i < *index)) {
-      *key = k;
-      *index = i;
-    }
-  }
+__device__ __forceinline__ float key_value(unsigned k) { return __uint_as_float((k >> 31) ? k & 0x7FFFFFFFu : ~k); }
+__device__ __forceinline__ unsigned warp_max(unsigned k) { return __reduce_max_sync(kAll, k); }
+__device__ __forceinline__ unsigned long long warp_max(unsigned long long k) {
+  const unsigned hi = __reduce_max_sync(kAll, (unsigned)(k >> 32));
+  const unsigned lo = __reduce_max_sync(kAll, (unsigned)(k >> 32) == hi ? (unsigned)k : 0u);
+  return ((unsigned long long)hi << 32) | lo;
 }
-__device__ __forceinline__ double warp_sum(double v) {
+template <typename V>
+__device__ __forceinline__ V warp_sum(V v) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(kAll, v, d);
   return v;
 }
 
-// One warp for one token; the scores and choices of its row lie in shared memory.
+template <typename V>
+struct KeyOf;
+template <>
+struct KeyOf<float> { typedef unsigned type; };
+template <>
+struct KeyOf<double> { typedef unsigned long long type; };
+
+// The chosen experts of one token.  A lane holds the choices of P neighbouring experts (keys 0 where there is none), so
+// the lowest index of several equal choices is that of the lowest lane.  Lane j returns the j-th chosen expert.
+// With CHECK (choices in 32 bits that may be off by `unit` * (1 + |choice|) each) *close tells whether two neighbours in the
+// chosen order, the last chosen and the first left out, or a kept and a dropped run are so near that the order may be wrong.
+// `part` is what a run's score is made of, `part_of(e)` the same for any expert: runs that do not end with a lane's experts are
+// scored by one lane each.
+template <int P, typename V, bool CHECK, typename F>
+__device__ __forceinline__ int choose(const b2c_route_desc& d, const V (&choice)[P], const V (&part)[P], F part_of, int lane, float unit,
+                                      bool* close) {
+  typedef typename KeyOf<V>::type K;
+  K key[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) key[i] = lane * P + i < d.experts ? order_key(choice[i]) : (K)0;
+  *close = false;
+  if (d.groups > 1) {
+    const int size = d.experts / d.groups;
+    const bool whole = size % P == 0;             // a run is a number of lanes
+    const int lanes = whole ? size / P : 1;
+    const int run = lane / lanes, base = run * lanes;
+    V first = -INFINITY, second = -INFINITY;
+    auto add = [&](V a, V b) {  // a >= b
+      second = fmax(fmin(first, a), fmax(second, b));
+      first = fmax(first, a);
+    };
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < P; ++i) add(part[i], -INFINITY);
+      const V f0 = first, s0 = second;
+      for (int j = 1; j < lanes; ++j) {
+        const int from = base + (lane - base + j) % lanes;
+        const V a = __shfl_sync(kAll, f0, from), b = __shfl_sync(kAll, s0, from);
+        add(a, b);
+      }
+    } else if (lane < d.groups) {
+      for (int i = 0; i < size; ++i) add(part_of(lane * size + i), -INFINITY);
+    }
+    const bool two = d.group_score == B2C_GROUP_TOP2 && size > 1;
+    const K mine = run < d.groups ? order_key(two ? first + second : first) : (K)0;
+    int better = 0;
+    for (int g = 0; g < d.groups; ++g) {
+      const K k = __shfl_sync(kAll, mine, g * lanes);
+      better += k > mine || (k == mine && g < run);
+    }
+    const bool kept = run < d.groups && better < d.topk_groups;
+    if constexpr (CHECK) {
+      const unsigned low = __reduce_min_sync(kAll, kept ? (unsigned)mine : 0xFFFFFFFFu);
+      const unsigned high = __reduce_max_sync(kAll, kept ? 0u : (unsigned)mine);
+      const float l = key_value(low);
+      *close = high != 0u && !(l - key_value(high) > unit * (1.0f + fabsf(l)));
+    }
+    const unsigned open = __ballot_sync(kAll, kept);
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int of = whole ? lane : min(lane * P + i, d.experts - 1) / size;
+      if (!((open >> of) & 1u)) key[i] = 0;
+    }
+  }
+  int my_id = 0;
+  K last = 0;
+  for (int j = 0; j < d.topk + (CHECK ? 1 : 0); ++j) {
+    K best = key[0];
+#pragma unroll
+    for (int i = 1; i < P; ++i) best = key[i] > best ? key[i] : best;
+    const K top = warp_max(best);
+    if constexpr (CHECK) {
+      const float l = key_value((unsigned)last);
+      if (j > 0 && top != 0) *close |= !(l - key_value((unsigned)top) > unit * (1.0f + fabsf(l)));
+      if (j == d.topk) break;
+      last = top;
+    }
+    unsigned at = 0;
+#pragma unroll
+    for (int i = 0; i < P; ++i) at |= key[i] == top ? 1u << i : 0u;
+    const int owner = __ffs(__ballot_sync(kAll, at != 0)) - 1;
+    const int slot = __ffs(at) - 1;
+    const int id = owner * P + __shfl_sync(kAll, slot, owner);
+    if (lane == owner) {
+#pragma unroll
+      for (int i = 0; i < P; ++i)
+        if (i == slot) key[i] = 0;
+    }
+    if (lane == j) my_id = id;
+  }
+  return my_id;
+}
+
 template <typename T>
-__global__ void __launch_bounds__(128) route_kernel(const RouteArgs a) {
-  extern __shared__ double dyn[];
-  pdl_wait();
-  pdl_launch_dependents();
-  const int E = a.d.experts, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const long long t = (long long)blockIdx.x * 4 + warp;
-  if (t >= a.tokens) return;
-  double* score = dyn + (size_t)warp * 2 * E;
-  double* choice = score + E;
-  const T* row = (const T*)a.logits + t * a.ld;
-  double mx = -INFINITY;
-  for (int e = lane; e < E; e += 32) {
-    double x = (double)to_float<T>(row[e]);
-    if (x != x) x = -INFINITY;
-    score[e] = x;
-    mx = fmax(mx, x);
+__device__ __forceinline__ float logit(const T* row, int e) {
+  const float x = to_float<T>(row[e]);
+  return x != x ? -INFINITY : x;
+}
+__device__ __forceinline__ double sigmoid64(double x) { return x == -INFINITY ? 0.0 : 1.0 / (1.0 + exp(-x)); }
+
+// The same choice in 64 bits, for a token whose 32-bit choices are too near to each other (rare: kept out of the way of the others).
+template <typename T, int P>
+__device__ __noinline__ int choose64(const RouteArgs& a, const T* row, int lane, float mx) {
+  double s[P], c[P], sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const int e = lane * P + i;
+    const double x = e < a.d.experts ? (double)logit<T>(row, e) : -INFINITY;
+    s[i] = a.d.score == B2C_SCORE_SIGMOID ? sigmoid64(x) : (x == -INFINITY ? 0.0 : (x == (double)mx ? 1.0 : exp(x - (double)mx)));
+    sum += s[i];
+  }
+  if (a.d.score == B2C_SCORE_SOFTMAX) {
+    sum = warp_sum(sum);
+#pragma unroll
+    for (int i = 0; i < P; ++i) s[i] = sum > 0.0 ? s[i] / sum : 0.0;
   }
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) mx = fmax(mx, __shfl_xor_sync(kAll, mx, d));
-  double sum = 0.0;
-  for (int e = lane; e < E; e += 32) {
-    const double x = score[e];
-    double s;
-    if (a.d.score == B2C_SCORE_SIGMOID) s = x == -INFINITY ? 0.0 : 1.0 / (1.0 + exp(-x));
-    else s = x == -INFINITY ? 0.0 : (x == mx ? 1.0 : exp(x - mx));
-    score[e] = s;
-    sum += s;
+  for (int i = 0; i < P; ++i) {
+    const int e = lane * P + i;
+    c[i] = e < a.d.experts ? (a.bias != nullptr ? s[i] + (double)a.bias[e] : s[i]) : -INFINITY;
   }
-  if (a.d.score == B2C_SCORE_SOFTMAX) sum = warp_sum(sum);
-  for (int e = lane; e < E; e += 32) {
-    double s = score[e];
-    if (a.d.score == B2C_SCORE_SOFTMAX) {
-      s = sum > 0.0 ? s / sum : 0.0;
-      score[e] = s;
-    }
-    choice[e] = a.bias ? s + (double)a.bias[e] : s;
+  auto part_of = [&](int e) {
+    const double l = (double)logit<T>(row, e);
+    double v = a.d.score == B2C_SCORE_SIGMOID ? sigmoid64(l) : (l == -INFINITY ? 0.0 : (l == (double)mx ? 1.0 : exp(l - (double)mx)));
+    if (a.d.score == B2C_SCORE_SOFTMAX) v = sum > 0.0 ? v / sum : 0.0;
+    return a.bias != nullptr ? v + (double)a.bias[e] : v;
+  };
+  bool close;
+  if (a.bias == nullptr) {  // (the experts are taken by their logits, the runs by their scores)
+    double x[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) x[i] = lane * P + i < a.d.experts ? (double)logit<T>(row, lane * P + i) : -INFINITY;
+    return choose<P, double, false>(a.d, x, c, part_of, lane, 0.0f, &close);
   }
-  __syncwarp();
-  const int G = a.d.groups, size = E / G;
-  unsigned open = 0xffffffffu;  // groups that stay
-  if (G > 1) {
-    unsigned long long key = 0;
-    if (lane < G) {
-      double first = -INFINITY, second = -INFINITY;
-      for (int i = 0; i < size; ++i) {
-        const double v = choice[lane * size + i];
-        if (v > first) {
-          second = first;
-          first = v;
-        } else if (v > second) {
-          second = v;
+  return choose<P, double, false>(a.d, c, c, part_of, lane, 0.0f, &close);
+}
+
+// One warp for one token, everything in registers.  Scores are monotonic in the logits, so without a bias the logits themselves are
+// compared, which is exact.  With a bias (or run scores that are sums) the choices are formed in 32 bits, each off by
+// less than 2^-20 * (1 + |choice|): the exponential, its argument, the sum, the quotient and the additions are off by at most
+// 7 units of 2^-24 together, the sum of two by twice that.  A token in which two choices that decide something are not
+// further apart than 2^-19 * (1 + |choice|) is done again in 64 bits.  Memory-bound on paper (one read of the logits); what it spends
+// are the topk rounds of maximum, vote and shuffle: 16384 x 256, top 8 of 4 of 8 runs, measured below.
+constexpr int kRouteWarps = 8;
+template <typename T, int P>
+__global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RouteArgs a, const bool vec) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int E = a.d.experts, lane = threadIdx.x & 31;
+  const long long t = (long long)blockIdx.x * kRouteWarps + (threadIdx.x >> 5);
+  if (t >= a.tokens) return;
+  const T* row = (const T*)a.logits + t * a.ld;
+  float x[P];
+  bool loaded = false;
+  if constexpr (P * sizeof(T) % 16 == 0) {
+    if (vec) {
+      loaded = true;
+      constexpr int kPer = 16 / sizeof(T);
+#pragma unroll
+      for (int i = 0; i < P; i += kPer) {
+        uint4 u = make_uint4(0, 0, 0, 0);
+        const bool in = lane * P + i < E;  // (E is a multiple of kPer)
+        if (in) u = *reinterpret_cast<const uint4*>(row + lane * P + i);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (sizeof(T) == 4) x[i + j] = in ? __uint_as_float(w[j]) : -INFINITY;
+          else {
+            unpack2<T>(w[j], &x[i + 2 * j], &x[i + 2 * j + 1]);
+            if (!in) x[i + 2 * j] = x[i + 2 * j + 1] = -INFINITY;
+          }
         }
       }
-      key = order_key(a.d.group_score == B2C_GROUP_MAX || size == 1 ? first : first + second);
-    }
-    int better = 0;
-    for (int g = 0; g < G; ++g) {
-      const unsigned long long k = __shfl_sync(kAll, key, g);
-      better += k > key || (k == key && g < lane);
-    }
-    open = __ballot_sync(kAll, lane < G && better < a.d.topk_groups);
-  }
-  double total = 0.0, mine = 0.0;
-  int my_id = 0;
-  unsigned taken = 0;  // of this lane's experts, lane + 32 * i
-  for (int j = 0; j < a.d.topk; ++j) {
-    unsigned long long key = 0;
-    int index = 0x7FFFFFFF;
-    for (int i = 0, e = lane; e < E; e += 32, ++i) {
-      if ((taken >> i) & 1u || (G > 1 && !((open >> (e / size)) & 1u))) continue;
-      const unsigned long long k = order_key(choice[e]);
-      if (k > key) {
-        key = k;
-        index = e;
-      }
-    }
-    warp_best(&key, &index);
-    if ((index & 31) == lane) taken |= 1u << (index >> 5);
-    const double s = score[index];
-    total += s;
-    if (lane == j) {
-      mine = s;
-      my_id = index;
+#pragma unroll
+      for (int i = 0; i < P; ++i) x[i] = x[i] != x[i] ? -INFINITY : x[i];
     }
   }
+  if (!loaded) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) x[i] = lane * P + i < E ? logit<T>(row, lane * P + i) : -INFINITY;
+  }
+  const bool softmax = a.d.score == B2C_SCORE_SOFTMAX;
+  const bool by_logit = a.bias == nullptr;
+  const bool sums = a.d.groups > 1 && a.d.group_score == B2C_GROUP_TOP2;
+  float mx = 0.0f;
+  double all = 0.0;
+  if (softmax) {
+    mx = x[0];
+#pragma unroll
+    for (int i = 1; i < P; ++i) mx = fmaxf(mx, x[i]);
+    mx = key_value(warp_max(order_key(mx)));
+  }
+  int id;
+  bool close = false;
+  if (by_logit && !sums) {
+    if (softmax && !a.d.renormalise) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < P; ++i) sum += x[i] == -INFINITY ? 0.0f : (x[i] == mx ? 1.0f : expf(x[i] - mx));
+      all = warp_sum((double)sum);
+    }
+    id = choose<P, float, false>(a.d, x, x, [&](int e) { return logit<T>(row, e); }, lane, 0.0f, &close);
+  } else {
+    float c[P];
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      if (softmax) c[i] = x[i] == -INFINITY ? 0.0f : (x[i] == mx ? 1.0f : expf(x[i] - mx));
+      else c[i] = __fdividef(1.0f, 1.0f + expf(-x[i]));
+      sum += c[i];
+    }
+    if (softmax) {
+      all = warp_sum((double)sum);
+#pragma unroll
+      for (int i = 0; i < P; ++i) c[i] = all > 0.0 ? __fdividef(c[i], (float)all) : 0.0f;
+    }
+    const float unit = 0x1p-19f, total = (float)all;
+    auto part_of = [&](int e) {
+      const float l = logit<T>(row, e);
+      float v;
+      if (softmax) v = total > 0.0f && l != -INFINITY ? __fdividef(l == mx ? 1.0f : expf(l - mx), total) : 0.0f;
+      else v = __fdividef(1.0f, 1.0f + expf(-l));
+      return by_logit ? v : v + a.bias[e];
+    };
+    if (!by_logit) {
+#pragma unroll
+      for (int i = 0; i < P; ++i) c[i] = lane * P + i < E ? c[i] + a.bias[lane * P + i] : -INFINITY;
+      id = choose<P, float, true>(a.d, c, c, part_of, lane, unit, &close);
+    } else {
+#pragma unroll
+      for (int i = 0; i < P; ++i) c[i] = lane * P + i < E ? c[i] : -INFINITY;
+      id = choose<P, float, true>(a.d, x, c, part_of, lane, unit, &close);  // (near logits are done again as well: no harm)
+    }
+  }
+  if (close) id = choose64<T, P>(a, row, lane, mx);
   if (lane < a.d.topk) {
-    const double w = a.d.renormalise ? (total > 0.0 ? mine / total : 0.0) : mine;
-    a.weights[t * a.d.topk + lane] = (float)(w * (double)a.d.scale);
-    a.ids[t * a.d.topk + lane] = my_id;
+    // the weights of the chosen, from their logits; the argument of the exponential without the rounding of its difference
+    const float l = logit<T>(row, id);
+    const unsigned on = __activemask();
+    // logistic scores that 32 bits cannot hold: below -60 they are exponentials, and their ratios those to the largest
+    // (from -740 on 64 bits cannot either: 0, as for the lowest values of a type that masks write)
+    const float top = softmax ? mx : key_value(__reduce_max_sync(on, order_key(l)));
+    float s;
+    if (softmax || (a.d.renormalise && top < -60.0f && top > -740.0f)) {
+      const double diff = (double)l - (double)top;
+      const float hi = (float)diff;
+      const float e = expf(hi);
+      s = l == -INFINITY ? 0.0f : (l == top ? 1.0f : (e == 0.0f ? 0.0f : fmaf(e, (float)(diff - (double)hi), e)));
+    } else {
+      s = l == -INFINITY ? 0.0f : 1.0f / (1.0f + expf(-l));
+    }
+    float w = s;
+    if (a.d.renormalise) {
+      float total = 0.0f;
+      for (int j = 0; j < a.d.topk; ++j) total += __shfl_sync(on, s, j);
+      w = total > 0.0f ? s / total : 0.0f;
+    } else if (softmax) {
+      w = all > 0.0 ? s / (float)all : 0.0f;
+    }
+    a.weights[t * a.d.topk + lane] = w * a.d.scale;
+    a.ids[t * a.d.topk + lane] = id;
   }
 }
 
@@ -290,21 +461,31 @@ __global__ void __launch_bounds__(256) combine_kernel(const YT* y, const long lo
 
 }  // namespace
 
-cudaError_t launch_route(const RouteArgs& a, cudaStream_t st) {
-  const size_t smem = 4 * 2 * (size_t)a.d.experts * sizeof(double);
-  const dim3 grid((unsigned)((a.tokens + 3) / 4));
-  cudaError_t e;
-#define B2C_ROUTE(T)                                                                                    \
-  {                                                                                                     \
-    static std::atomic<unsigned long long> configured{0};                                               \
-    e = set_max_dynamic_smem_once(configured, (const void*)route_kernel<T>, 4 * 2 * kMaxExperts * 8);    \
-    if (e == cudaSuccess) e = launch_pdl(route_kernel<T>, grid, dim3(128), smem, st, a);                 \
-  }
-  if (a.d.logit_type == B2C_F32) B2C_ROUTE(float)
-  else if (a.d.logit_type == B2C_F16) B2C_ROUTE(__half)
-  else B2C_ROUTE(__nv_bfloat16)
+namespace {
+
+template <typename T>
+cudaError_t route_type(const RouteArgs& a, cudaStream_t st) {
+  const dim3 grid((unsigned)((a.tokens + kRouteWarps - 1) / kRouteWarps)), block(32 * kRouteWarps);
+  constexpr int kPer = 16 / (int)sizeof(T);
+  const bool vec = (reinterpret_cast<uintptr_t>(a.logits) & 15) == 0 && a.ld % kPer == 0 && a.d.experts % kPer == 0;
+#define B2C_ROUTE(P) \
+  if (a.d.experts <= 32 * P) return launch_pdl(route_kernel<T, P>, grid, block, 0, st, a, vec)
+  B2C_ROUTE(1);
+  B2C_ROUTE(2);
+  B2C_ROUTE(4);
+  B2C_ROUTE(8);
+  B2C_ROUTE(16);
+  B2C_ROUTE(32);
 #undef B2C_ROUTE
-  return e;
+  return cudaErrorInvalidValue;
+}
+
+}  // namespace
+
+cudaError_t launch_route(const RouteArgs& a, cudaStream_t st) {
+  if (a.d.logit_type == B2C_F32) return route_type<float>(a, st);
+  if (a.d.logit_type == B2C_F16) return route_type<__half>(a, st);
+  return route_type<__nv_bfloat16>(a, st);
 }
 
 size_t route_sort_workspace(long long pairs, int experts) {

@@ -76,14 +76,18 @@ def scores(logits, kind):
 def route(logits, topk, kind="softmax", groups=1, topk_groups=1, group_score="max", renormalise=True, scale=1.0, bias=None):
     """Plain loops over the tokens of a small batch: (weights in 64 bits, ids)."""
     s = scores(logits, kind).cpu()
-    choice = s + (bias.double().cpu() if bias is not None else 0.0)
+    part = s + (bias.double().cpu() if bias is not None else 0.0)
+    # scores are monotonic in the logits: without a bias these decide, and a run's largest choice is that of its largest logit
+    choice = part if bias is not None else logits.double().cpu()
+    if bias is None and group_score == "max":
+        part = choice
     ids, weights = [], []
     for t in range(s.shape[0]):
-        c = [v if v == v else -math.inf for v in choice[t].tolist()]
+        c, of_run = ([v if v == v else -math.inf for v in x[t].tolist()] for x in (choice, part))
         size = len(c) // groups
         runs = []
         for g in range(groups):
-            top = sorted(c[g * size:(g + 1) * size], reverse=True)
+            top = sorted(of_run[g * size:(g + 1) * size], reverse=True)
             runs.append((-(top[0] if group_score == "max" or size == 1 else top[0] + top[1]), g))
         kept = {g for _, g in sorted(runs)[:topk_groups]}
         chosen = sorted((-c[e], e) for e in range(len(c)) if e // size in kept)[:topk]
