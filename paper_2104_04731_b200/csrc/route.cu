@@ -33,44 +33,32 @@ __device__ __forceinline__ V warp_sum(V v) {
   return v;
 }
 
-template <typename V>
-struct KeyOf;
-template <>
-struct KeyOf<float> { typedef unsigned type; };
-template <>
-struct KeyOf<double> { typedef unsigned long long type; };
-
-// The chosen experts of one token.  A lane holds the choices of P neighbouring experts (keys 0 where there is none), so
-// the lowest index of several equal choices is that of the lowest lane.  Lane j returns the j-th chosen expert.
-// With CHECK (choices in 32 bits that may be off by `unit` * (1 + |choice|) each) *close tells whether two neighbours in the
-// chosen order, the last chosen and the first left out, or a kept and a dropped run are so near that the order may be wrong.
-// `part` is what a run's score is made of, `part_of(e)` the same for any expert: runs that do not end with a lane's experts are
-// scored by one lane each.
-template <int P, typename V, bool CHECK, typename F>
-__device__ __forceinline__ int choose(const b2c_route_desc& d, const V (&choice)[P], const V (&part)[P], F part_of, int lane, float unit,
-                                      bool* close) {
-  typedef typename KeyOf<V>::type K;
+// The chosen experts of one token in 64 bits.  A lane holds P neighbouring experts (keys 0 where there is none), so the lowest index
+// of several equal choices is that of the lowest lane.  Lane j returns the j-th chosen expert.  `part` is what a run's score is made
+// of, `part_of(e)` the same for any expert: runs that do not end with a lane's experts are scored by one lane each.
+template <int P, typename F>
+__device__ __forceinline__ int choose_exact(const b2c_route_desc& d, const double (&choice)[P], const double (&part)[P], F part_of, int lane) {
+  typedef unsigned long long K;
   K key[P];
 #pragma unroll
   for (int i = 0; i < P; ++i) key[i] = lane * P + i < d.experts ? order_key(choice[i]) : (K)0;
-  *close = false;
   if (d.groups > 1) {
     const int size = d.experts / d.groups;
     const bool whole = size % P == 0;             // a run is a number of lanes
     const int lanes = whole ? size / P : 1;
     const int run = lane / lanes, base = run * lanes;
-    V first = -INFINITY, second = -INFINITY;
-    auto add = [&](V a, V b) {  // a >= b
+    double first = -INFINITY, second = -INFINITY;
+    auto add = [&](double a, double b) {  // a >= b
       second = fmax(fmin(first, a), fmax(second, b));
       first = fmax(first, a);
     };
     if (whole) {
 #pragma unroll
       for (int i = 0; i < P; ++i) add(part[i], -INFINITY);
-      const V f0 = first, s0 = second;
+      const double f0 = first, s0 = second;
       for (int j = 1; j < lanes; ++j) {
         const int from = base + (lane - base + j) % lanes;
-        const V a = __shfl_sync(kAll, f0, from), b = __shfl_sync(kAll, s0, from);
+        const double a = __shfl_sync(kAll, f0, from), b = __shfl_sync(kAll, s0, from);
         add(a, b);
       }
     } else if (lane < d.groups) {
@@ -84,12 +72,6 @@ __device__ __forceinline__ int choose(const b2c_route_desc& d, const V (&choice)
       better += k > mine || (k == mine && g < run);
     }
     const bool kept = run < d.groups && better < d.topk_groups;
-    if constexpr (CHECK) {
-      const unsigned low = __reduce_min_sync(kAll, kept ? (unsigned)mine : 0xFFFFFFFFu);
-      const unsigned high = __reduce_max_sync(kAll, kept ? 0u : (unsigned)mine);
-      const float l = key_value(low);
-      *close = high != 0u && !(l - key_value(high) > unit * (1.0f + fabsf(l)));
-    }
     const unsigned open = __ballot_sync(kAll, kept);
 #pragma unroll
     for (int i = 0; i < P; ++i) {
@@ -98,18 +80,11 @@ __device__ __forceinline__ int choose(const b2c_route_desc& d, const V (&choice)
     }
   }
   int my_id = 0;
-  K last = 0;
-  for (int j = 0; j < d.topk + (CHECK ? 1 : 0); ++j) {
+  for (int j = 0; j < d.topk; ++j) {
     K best = key[0];
 #pragma unroll
     for (int i = 1; i < P; ++i) best = key[i] > best ? key[i] : best;
     const K top = warp_max(best);
-    if constexpr (CHECK) {
-      const float l = key_value((unsigned)last);
-      if (j > 0 && top != 0) *close |= !(l - key_value((unsigned)top) > unit * (1.0f + fabsf(l)));
-      if (j == d.topk) break;
-      last = top;
-    }
     unsigned at = 0;
 #pragma unroll
     for (int i = 0; i < P; ++i) at |= key[i] == top ? 1u << i : 0u;
@@ -126,11 +101,140 @@ __device__ __forceinline__ int choose(const b2c_route_desc& d, const V (&choice)
   return my_id;
 }
 
+// Keys that carry their place among a lane's experts, so that they can be sorted: either exactly, value in the upper word and
+// place (the lower the larger) in the lower one, or in 32 bits with the place in the lowest bits of the value, which moves it by
+// less than P units of its last place.
+template <int P>
+__device__ __forceinline__ unsigned long long pack_exact(float v, int i) {
+  return ((unsigned long long)order_key(v) << 32) | (unsigned)(P - i);
+}
+__device__ __forceinline__ unsigned value_bits(unsigned long long k) { return (unsigned)(k >> 32); }
+__device__ __forceinline__ unsigned value_bits(unsigned k) { return k; }
+template <int P>
+__device__ __forceinline__ int place_of(unsigned long long k) { return P - (int)(unsigned)k; }
+template <int P>
+__device__ __forceinline__ int place_of(unsigned k) { return P - 1 - (int)(k & (P - 1)); }
+
+// Largest first: Batcher's odd-even merge sort, unrolled.
+template <int P, typename K>
+__device__ __forceinline__ void sort_lane(K (&k)[P]) {
+#pragma unroll
+  for (int p = 1; p < P; p *= 2)
+#pragma unroll
+    for (int q = p; q >= 1; q /= 2)
+#pragma unroll
+      for (int j = q % p; j + q < P; j += 2 * q)
+#pragma unroll
+        for (int i = 0; i < q; ++i)
+          if (i + j + q < P && (i + j) / (2 * p) == (i + j + q) / (2 * p)) {
+            const K a = k[i + j], b = k[i + j + q];
+            k[i + j] = a > b ? a : b;
+            k[i + j + q] = a > b ? b : a;
+          }
+}
+
+// choose() for 32-bit choices: every lane sorts its own once, a round compares the lanes' first ones.
+template <int P, typename K, bool CHECK, typename F>
+__device__ __forceinline__ int choose32(const b2c_route_desc& d, const float (&choice)[P], F part_of, int lane, float unit, bool* close) {
+  constexpr bool kExact = sizeof(K) == 8;
+  K key[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    if constexpr (kExact) key[i] = lane * P + i < d.experts ? pack_exact<P>(choice[i], i) : 0ull;
+    else key[i] = lane * P + i < d.experts ? ((order_key(choice[i]) & ~(unsigned)(P - 1)) | (unsigned)(P - 1 - i)) : 0u;
+  }
+  sort_lane<P, K>(key);
+  *close = false;
+  bool by_expert = false;  // runs that do not end with a lane's experts: keys are dropped one by one
+  unsigned open = kAll;
+  const int size = d.experts / d.groups;
+  if (d.groups > 1) {
+    by_expert = size % P != 0;
+    const int lanes = by_expert ? 1 : size / P;
+    const int run = lane / lanes;
+    float first = -INFINITY, second = -INFINITY;
+    auto add = [&](float a, float b) {  // a >= b
+      second = fmaxf(fminf(first, a), fmaxf(second, b));
+      first = fmaxf(first, a);
+    };
+    if (!by_expert) {
+      const float f0 = key_value(value_bits(key[0])), s0 = P > 1 ? key_value(value_bits(key[P > 1 ? 1 : 0])) : -INFINITY;
+      add(f0, s0);
+      int from = lane;
+      for (int j = 1; j < lanes; ++j) {
+        from = from + 1 == (run + 1) * lanes ? run * lanes : from + 1;
+        const float a = __shfl_sync(kAll, f0, from), b = __shfl_sync(kAll, s0, from);
+        add(a, b);
+      }
+    } else if (lane < d.groups) {
+      for (int i = 0; i < size; ++i) add(part_of(lane * size + i), -INFINITY);
+    }
+    const bool two = d.group_score == B2C_GROUP_TOP2 && size > 1;
+    const unsigned mine = run < d.groups ? order_key(two ? first + second : first) : 0u;
+    int better = 0;
+    for (int g = 0; g < d.groups; ++g) {
+      const unsigned k = __shfl_sync(kAll, mine, g * lanes);
+      better += k > mine || (k == mine && g < run);
+    }
+    const bool kept = run < d.groups && better < d.topk_groups;
+    if constexpr (CHECK) {
+      const float low = key_value(__reduce_min_sync(kAll, kept ? mine : 0xFFFFFFFFu));
+      const unsigned high = __reduce_max_sync(kAll, kept ? 0u : mine);
+      *close = high != 0u && !(low - key_value(high) > 2.0f * unit * (1.0f + fabsf(low)));
+    }
+    open = __ballot_sync(kAll, kept);
+    if (!by_expert && !kept) {
+#pragma unroll
+      for (int i = 0; i < P; ++i) key[i] = 0;
+    }
+  }
+  int my_id = 0;
+  float my_value = 0.0f;
+  for (int j = 0; j < d.topk;) {
+    const unsigned mine = value_bits(key[0]);
+    const unsigned top = __reduce_max_sync(kAll, mine);
+    const int owner = __ffs(__ballot_sync(kAll, mine == top)) - 1;
+    int id;
+    if constexpr (kExact) id = __shfl_sync(kAll, lane * P + place_of<P>(key[0]), owner);
+    else id = owner * P + place_of<P>(top);
+    if (lane == owner) {
+#pragma unroll
+      for (int i = 0; i + 1 < P; ++i) key[i] = key[i + 1];
+      key[P - 1] = 0;
+    }
+    if (by_expert && !((open >> (id / size)) & 1u)) continue;  // of a dropped run
+    if (lane == j) {
+      my_id = id;
+      if constexpr (CHECK) my_value = key_value(top);
+    }
+    ++j;
+  }
+  if constexpr (CHECK) {
+    // each chosen one against the next, the last against the first that was left out
+    float next = __shfl_down_sync(kAll, my_value, 1);
+    unsigned left = 0u;
+    if (!by_expert) {
+      left = __reduce_max_sync(kAll, value_bits(key[0]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < P; ++i)
+        if (value_bits(key[i]) != 0u && ((open >> ((lane * P + place_of<P>(key[i])) / size)) & 1u)) left = max(left, value_bits(key[i]));
+      left = __reduce_max_sync(kAll, left);
+    }
+    const bool ends = lane == d.topk - 1;
+    if (ends) next = left != 0u ? key_value(left) : -INFINITY;
+    const bool near = lane < d.topk && !(ends && left == 0u) && !(my_value - next > unit * (1.0f + fabsf(my_value)));
+    *close |= __any_sync(kAll, near);
+  }
+  return my_id;
+}
+
 template <typename T>
 __device__ __forceinline__ float logit(const T* row, int e) {
   const float x = to_float<T>(row[e]);
   return x != x ? -INFINITY : x;
 }
+
 __device__ __forceinline__ double sigmoid64(double x) { return x == -INFINITY ? 0.0 : 1.0 / (1.0 + exp(-x)); }
 
 // The same choice in 64 bits, for a token whose 32-bit choices are too near to each other (rare: kept out of the way of the others).
@@ -160,25 +264,25 @@ __device__ __noinline__ int choose64(const RouteArgs& a, const T* row, int lane,
     if (a.d.score == B2C_SCORE_SOFTMAX) v = sum > 0.0 ? v / sum : 0.0;
     return a.bias != nullptr ? v + (double)a.bias[e] : v;
   };
-  bool close;
   if (a.bias == nullptr) {  // (the experts are taken by their logits, the runs by their scores)
     double x[P];
 #pragma unroll
     for (int i = 0; i < P; ++i) x[i] = lane * P + i < a.d.experts ? (double)logit<T>(row, lane * P + i) : -INFINITY;
-    return choose<P, double, false>(a.d, x, c, part_of, lane, 0.0f, &close);
+    return choose_exact<P>(a.d, x, c, part_of, lane);
   }
-  return choose<P, double, false>(a.d, c, c, part_of, lane, 0.0f, &close);
+  return choose_exact<P>(a.d, c, c, part_of, lane);
 }
 
 // One warp for one token, everything in registers.  Scores are monotonic in the logits, so without a bias the logits themselves are
-// compared, which is exact.  With a bias (or run scores that are sums) the choices are formed in 32 bits, each off by
-// less than 2^-20 * (1 + |choice|): the exponential, its argument, the sum, the quotient and the additions are off by at most
-// 7 units of 2^-24 together, the sum of two by twice that.  A token in which two choices that decide something are not
-// further apart than 2^-19 * (1 + |choice|) is done again in 64 bits.  Memory-bound on paper (one read of the logits); what it spends
-// are the topk rounds of maximum, vote and shuffle: 16384 x 256, top 8 of 4 of 8 runs, measured below.
+// compared, which is exact.  With a bias (or run scores that are sums) the choices are formed in 32 bits: exponential, sum, quotient
+// and additions put each off by at most 7 units of 2^-24 * (1 + |choice|), its place in the key's lowest bits by P - 1 units of 2^-23,
+// together less than 2^-19 for P <= 8 and 2^-17 beyond, and sums of two by twice that.  A token in which two choices that decide
+// something are not further apart than twice this (about one in fifty at 256 experts) is chosen again with the places beside the
+// values (2^-20), and if it is still undecided (one in two hundred) in 64 bits.
+// Memory-bound on paper (one read of the logits); what it spends are the instructions of exponentials, sort and topk rounds.
 constexpr int kRouteWarps = 8;
 template <typename T, int P>
-__global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RouteArgs a, const bool vec) {
+__global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RouteArgs a, const bool vec, const bool bias_vec) {
   pdl_wait();
   pdl_launch_dependents();
   const int E = a.d.experts, lane = threadIdx.x & 31;
@@ -234,14 +338,14 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RouteArgs
       for (int i = 0; i < P; ++i) sum += x[i] == -INFINITY ? 0.0f : (x[i] == mx ? 1.0f : expf(x[i] - mx));
       all = warp_sum((double)sum);
     }
-    id = choose<P, float, false>(a.d, x, x, [&](int e) { return logit<T>(row, e); }, lane, 0.0f, &close);
+    id = choose32<P, unsigned long long, false>(a.d, x, [&](int e) { return logit<T>(row, e); }, lane, 0.0f, &close);
   } else {
     float c[P];
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       if (softmax) c[i] = x[i] == -INFINITY ? 0.0f : (x[i] == mx ? 1.0f : expf(x[i] - mx));
-      else c[i] = __fdividef(1.0f, 1.0f + expf(-x[i]));
+      else c[i] = __fdividef(1.0f, 1.0f + __expf(-x[i]));
       sum += c[i];
     }
     if (softmax) {
@@ -249,49 +353,58 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RouteArgs
 #pragma unroll
       for (int i = 0; i < P; ++i) c[i] = all > 0.0 ? __fdividef(c[i], (float)all) : 0.0f;
     }
-    const float unit = 0x1p-19f, total = (float)all;
+    const float total = (float)all;
     auto part_of = [&](int e) {
       const float l = logit<T>(row, e);
       float v;
       if (softmax) v = total > 0.0f && l != -INFINITY ? __fdividef(l == mx ? 1.0f : expf(l - mx), total) : 0.0f;
-      else v = __fdividef(1.0f, 1.0f + expf(-l));
+      else v = __fdividef(1.0f, 1.0f + __expf(-l));
       return by_logit ? v : v + a.bias[e];
     };
     if (!by_logit) {
+      if (P >= 4 && bias_vec) {
 #pragma unroll
-      for (int i = 0; i < P; ++i) c[i] = lane * P + i < E ? c[i] + a.bias[lane * P + i] : -INFINITY;
-      id = choose<P, float, true>(a.d, c, c, part_of, lane, unit, &close);
-    } else {
+        for (int i = 0; i + 3 < P; i += 4)
+          if (lane * P + i < E) {
+            const float4 b = *reinterpret_cast<const float4*>(a.bias + lane * P + i);
+            c[i] += b.x;
+            c[i + 1] += b.y;
+            c[i + 2] += b.z;
+            c[i + 3] += b.w;
+          }
+      } else {
 #pragma unroll
-      for (int i = 0; i < P; ++i) c[i] = lane * P + i < E ? c[i] : -INFINITY;
-      id = choose<P, float, true>(a.d, x, c, part_of, lane, unit, &close);  // (near logits are done again as well: no harm)
+        for (int i = 0; i < P; ++i)
+          if (lane * P + i < E) c[i] += a.bias[lane * P + i];
+      }
     }
+    id = choose32<P, unsigned, true>(a.d, c, part_of, lane, P <= 8 ? 0x1p-18f : 0x1p-16f, &close);
+    if (close) id = choose32<P, unsigned long long, true>(a.d, c, part_of, lane, 0x1p-20f, &close);
   }
   if (close) id = choose64<T, P>(a, row, lane, mx);
-  if (lane < a.d.topk) {
-    // the weights of the chosen, from their logits; the argument of the exponential without the rounding of its difference
-    const float l = logit<T>(row, id);
-    const unsigned on = __activemask();
-    // logistic scores that 32 bits cannot hold: below -60 they are exponentials, and their ratios those to the largest
-    // (from -740 on 64 bits cannot either: 0, as for the lowest values of a type that masks write)
-    const float top = softmax ? mx : key_value(__reduce_max_sync(on, order_key(l)));
-    float s;
-    if (softmax || (a.d.renormalise && top < -60.0f && top > -740.0f)) {
-      const double diff = (double)l - (double)top;
-      const float hi = (float)diff;
-      const float e = expf(hi);
-      s = l == -INFINITY ? 0.0f : (l == top ? 1.0f : (e == 0.0f ? 0.0f : fmaf(e, (float)(diff - (double)hi), e)));
-    } else {
-      s = l == -INFINITY ? 0.0f : 1.0f / (1.0f + expf(-l));
-    }
-    float w = s;
-    if (a.d.renormalise) {
-      float total = 0.0f;
-      for (int j = 0; j < a.d.topk; ++j) total += __shfl_sync(on, s, j);
-      w = total > 0.0f ? s / total : 0.0f;
-    } else if (softmax) {
-      w = all > 0.0 ? s / (float)all : 0.0f;
-    }
+  // the weights of the chosen, from their logits; the argument of the exponential without the rounding of its difference
+  const bool on = lane < a.d.topk;
+  const float l = on ? logit<T>(row, id) : -INFINITY;
+  // logistic scores that 32 bits cannot hold: below -60 they are exponentials, and their ratios those to the largest
+  // (from -740 on 64 bits cannot either: 0, as for the lowest values of a type that masks write)
+  const float top = softmax ? mx : key_value(__reduce_max_sync(kAll, order_key(l)));
+  float s;
+  if (softmax || (a.d.renormalise && top < -60.0f && top > -740.0f)) {
+    const double diff = (double)l - (double)top;
+    const float hi = (float)diff;
+    const float e = expf(hi);
+    s = l == -INFINITY ? 0.0f : (l == top ? 1.0f : (e == 0.0f ? 0.0f : fmaf(e, (float)(diff - (double)hi), e)));
+  } else {
+    s = l == -INFINITY ? 0.0f : 1.0f / (1.0f + expf(-l));
+  }
+  float w = s;
+  if (a.d.renormalise) {
+    const float total = warp_sum(s);
+    w = total > 0.0f ? s / total : 0.0f;
+  } else if (softmax) {
+    w = all > 0.0 ? s / (float)all : 0.0f;
+  }
+  if (on) {
     a.weights[t * a.d.topk + lane] = w * a.d.scale;
     a.ids[t * a.d.topk + lane] = id;
   }
@@ -466,10 +579,11 @@ namespace {
 template <typename T>
 cudaError_t route_type(const RouteArgs& a, cudaStream_t st) {
   const dim3 grid((unsigned)((a.tokens + kRouteWarps - 1) / kRouteWarps)), block(32 * kRouteWarps);
+  const bool bias_vec = (reinterpret_cast<uintptr_t>(a.bias) & 15) == 0 && a.d.experts % 4 == 0;
   constexpr int kPer = 16 / (int)sizeof(T);
   const bool vec = (reinterpret_cast<uintptr_t>(a.logits) & 15) == 0 && a.ld % kPer == 0 && a.d.experts % kPer == 0;
 #define B2C_ROUTE(P) \
-  if (a.d.experts <= 32 * P) return launch_pdl(route_kernel<T, P>, grid, block, 0, st, a, vec)
+  if (a.d.experts <= 32 * P) return launch_pdl(route_kernel<T, P>, grid, block, 0, st, a, vec, bias_vec)
   B2C_ROUTE(1);
   B2C_ROUTE(2);
   B2C_ROUTE(4);
