@@ -352,88 +352,47 @@ def measure_mma_rate_pair(tile_n: int = 256, mmas_per_pair: int = 20000, stream=
 
 
 # ---- 8-bit float operators ----------------------------------------------------------------------------------------------
+#
+# Tensors are checked and handed over by a small native module (_binding.so): shapes, types, strides and devices, which the library
+# does not see.  What it refuses is raised as B2CError(E_INVALID_ARG) and the like before anything is launched.
 
-_types = {}  # torch dtype -> element type, once torch is there
-
-
-def _type_of(t, what):
-    if not _types:
-        import torch
-
-        _types.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3, torch.float8_e5m2: E5M2})
-    v = _types.get(t.dtype)
-    _need(v is not None, what)
-    return v
+_native = None
 
 
-def _need(ok, what):
-    """The library sees pointers only: what it cannot see of a tensor (shape, device, strides) is checked here."""
-    if not ok:
-        raise B2CError(E_INVALID_ARG, what)
+def _load_native():
+    global _native
+    if _native is None:
+        lib = load()
+        import torch  # noqa: F401  (its libraries have to be there first)
+
+        from . import _binding
+
+        _binding.bind(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in (
+            "b2c_fp8_quantize", "b2c_fp8_matmul", "b2c_route", "b2c_route_sort_workspace_bytes", "b2c_route_sort", "b2c_route_combine",
+            "b2c_experts_workspace_bytes", "b2c_fp8_experts")))
+        _native = _binding
+    return _native
 
 
-def _on_device(what, *tensors):
-    """Every tensor lies on the current device."""
-    here = tensors[0].get_device()
-    _need(here >= 0 and here == _current_device(), what + ": a tensor is not on the current CUDA device")
-    for t in tensors:
-        _need(t is None or t.get_device() == here, what + ": a tensor is not on the current CUDA device")
-
-
-def _current_device():
-    import torch
-
-    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else torch.cuda.current_device()
-
-
-def _ld(t, what):
-    """Distance between the rows of a matrix with contiguous rows."""
-    rows, cols = t.shape
-    sr, sc = t.stride()
-    _need(sc == 1 or cols == 1, what + ": rows are not contiguous")
-    if rows <= 1:
-        return cols
-    _need(sr >= cols, what + ": rows overlap")
-    return sr
+def _refused(where: str, code: int, what: str):
+    raise B2CError(code, "%s: %s" % (where, what) if what else where)
 
 
 def fp8_quantize(x, q, scale, block_rows: int = 1, stream=None):
     """Quantises x [rows, cols] (float32 / float16 / bfloat16) into q (float8, same shape) with one scale for each block of
     block_rows (1 or 128) x 128 elements: scale float32 [ceil(rows / block_rows), ceil(cols / 128)]."""
-    w = "b2c_fp8_quantize"
-    _need(x.dim() == 2 and q.shape == x.shape and scale.dim() == 2 and block_rows in (1, 128), w + ": shapes")
-    rows, cols = x.shape
-    _need(tuple(scale.shape) == (-(-rows // block_rows), -(-cols // 128)) and _type_of(scale, w) == F32, w + ": scale")
-    _on_device(w, x, q, scale)
-    _check(load().b2c_fp8_quantize(x.data_ptr(), _type_of(x, w), rows, cols, _ld(x, w), block_rows, _type_of(q, w), q.data_ptr(),
-                                   _ld(q, w), scale.data_ptr(), _ld(scale, w), _stream_ptr(stream)), w)
+    r = (_native or _load_native()).quantize(x, q, scale, block_rows, stream and stream.cuda_stream)
+    if r:
+        _refused("b2c_fp8_quantize", *r)
 
 
 def fp8_matmul(a, a_scale, b, b_scale, y, offsets=None, stream=None):
     """y = a . b^T of block-scaled float8 matrices.  a [rows, K] with a_scale [rows, ceil(K / 128)]; b [N, K] with b_scale
     [ceil(N / 128), ceil(K / 128)]; y [rows, N] float32 / float16 / bfloat16.  With b [groups, N, K] (and its scales) row m is
     multiplied with the matrix of the group whose run offsets[g] <= m < offsets[g + 1] (int32 [groups + 1]) it is in."""
-    w = "b2c_fp8_matmul"
-    _need(a.dim() == 2 and y.dim() == 2 and a_scale.dim() == 2 and b.dim() in (2, 3) and b_scale.dim() == b.dim(), w + ": shapes")
-    rows, K = a.shape
-    N = b.shape[-2]
-    groups = b.shape[0] if b.dim() == 3 else 1
-    _need(b.shape[-1] == K and tuple(y.shape) == (rows, N) and tuple(a_scale.shape) == (rows, -(-K // 128)), w + ": shapes")
-    _need(tuple(b_scale.shape[-2:]) == (-(-N // 128), -(-K // 128)) and (b.dim() == 2 or b_scale.shape[0] == groups), w + ": b_scale")
-    _need(b.is_contiguous() and b_scale.is_contiguous() and _type_of(a_scale, w) == F32 and _type_of(b_scale, w) == F32, w + ": b, scales")
-    _need((b.dim() == 2) == (offsets is None), w + ": offsets go with a stack of matrices")
-    if offsets is not None:
-        _need(offsets.dim() == 1 and offsets.numel() == groups + 1 and offsets.is_contiguous() and offsets.dtype == _torch_int32(), w + ": offsets")
-    _on_device(w, a, a_scale, b, b_scale, y, offsets)
-    d = MatmulDesc(N, K, groups, _type_of(a, w), _type_of(b, w), _type_of(y, w))
-    _check(load().b2c_fp8_matmul(ctypes.byref(d), rows, a.data_ptr(), _ld(a, w), a_scale.data_ptr(), _ld(a_scale, w), b.data_ptr(),
-                                 b_scale.data_ptr(), _dptr(offsets), y.data_ptr(), _ld(y, w), _stream_ptr(stream)), w)
-
-
-def _torch_int32():
-    import torch
-
-    return torch.int32
+    r = (_native or _load_native()).matmul(a, a_scale, b, b_scale, y, offsets, stream and stream.cuda_stream)
+    if r:
+        _refused("b2c_fp8_matmul", *r)
 
 
 def make_route_desc(experts, topk, score=SCORE_SOFTMAX, groups=1, topk_groups=1, group_score=GROUP_MAX, renormalise=True,
@@ -444,17 +403,9 @@ def make_route_desc(experts, topk, score=SCORE_SOFTMAX, groups=1, topk_groups=1,
 def route(desc: RouteDesc, logits, weights, ids, bias=None, stream=None):
     """Best experts of every row of logits [tokens, experts]: weights float32 and ids int32 [tokens, topk], both contiguous.
     bias: float32 [experts] or None.  The logits' type is taken from the tensor."""
-    w = "b2c_route"
-    _need(logits.dim() == 2 and logits.shape[1] == desc.experts, w + ": logits")
-    tokens = logits.shape[0]
-    _need(tuple(weights.shape) == tuple(ids.shape) == (tokens, desc.topk) and weights.is_contiguous() and ids.is_contiguous(), w + ": outputs")
-    _need(_type_of(weights, w) == F32 and ids.dtype == _torch_int32(), w + ": output types")
-    _need(bias is None or (tuple(bias.shape) == (desc.experts,) and bias.is_contiguous() and _type_of(bias, w) == F32), w + ": bias")
-    _on_device(w, logits, weights, ids, bias)
-    d = RouteDesc.from_buffer_copy(desc)
-    d.logit_type = _type_of(logits, w)
-    _check(load().b2c_route(ctypes.byref(d), tokens, logits.data_ptr(), _ld(logits, w), _dptr(bias), weights.data_ptr(), ids.data_ptr(),
-                            _stream_ptr(stream)), w)
+    r = (_native or _load_native()).route(desc, logits, weights, ids, bias, stream and stream.cuda_stream)
+    if r:
+        _refused("b2c_route", *r)
 
 
 def route_sort_workspace_bytes(pairs: int, experts: int) -> int:
@@ -466,29 +417,16 @@ def route_sort_workspace_bytes(pairs: int, experts: int) -> int:
 def route_sort(ids, experts: int, offsets, rows, order=None, workspace=None, stream=None):
     """Stable sort of the (token, slot) pairs of ids (int32, any shape, contiguous) by expert: offsets int32 [experts + 1], rows int32
     (sorted position of every pair, -1 for an id that is no expert), order int32 [pairs] (pair at every position)."""
-    w = "b2c_route_sort"
-    i32 = _torch_int32()
-    n = ids.numel()
-    _need(ids.dtype == offsets.dtype == rows.dtype == i32 and ids.is_contiguous() and offsets.is_contiguous() and rows.is_contiguous(), w + ": types")
-    _need(offsets.numel() == experts + 1 and rows.numel() == n, w + ": shapes")
-    _need(order is None or (order.dtype == i32 and order.numel() == n and order.is_contiguous()), w + ": order")
-    need = route_sort_workspace_bytes(n, experts)
-    _need(need == 0 or (workspace is not None and workspace.is_contiguous() and workspace.numel() * workspace.element_size() >= need), w + ": workspace")
-    _on_device(w, ids, offsets, rows, order, workspace)
-    _check(load().b2c_route_sort(ids.data_ptr(), n, experts, offsets.data_ptr(), rows.data_ptr(), _dptr(order), _dptr(workspace),
-                                 _stream_ptr(stream)), w)
+    r = (_native or _load_native()).sort(ids, experts, offsets, rows, order, workspace, stream and stream.cuda_stream)
+    if r:
+        _refused("b2c_route_sort", *r)
 
 
 def route_combine(y, rows, weights, out, stream=None):
     """out[t] = sum_j weights[t, j] * y[rows[t, j]] over the slots whose row is one of y's; rows int32 and weights float32 [tokens, topk]."""
-    w = "b2c_route_combine"
-    _need(y.dim() == 2 and out.dim() == 2 and rows.dim() == 2 and tuple(rows.shape) == tuple(weights.shape), w + ": shapes")
-    tokens, topk = rows.shape
-    _need(tuple(out.shape) == (tokens, y.shape[1]) and rows.dtype == _torch_int32() and _type_of(weights, w) == F32, w + ": shapes")
-    _need(rows.is_contiguous() and weights.is_contiguous(), w + ": rows, weights")
-    _on_device(w, y, rows, weights, out)
-    _check(load().b2c_route_combine(y.data_ptr(), _type_of(y, w), y.shape[0], _ld(y, w), rows.data_ptr(), weights.data_ptr(), tokens, topk, y.shape[1],
-                                    out.data_ptr(), _type_of(out, w), _ld(out, w), _stream_ptr(stream)), w)
+    r = (_native or _load_native()).combine(y, rows, weights, out, stream and stream.cuda_stream)
+    if r:
+        _refused("b2c_route_combine", *r)
 
 
 def experts_workspace_bytes(hidden: int, inter: int, experts: int, topk: int, tokens: int, dtype: int = BF16) -> int:
@@ -502,26 +440,9 @@ def experts_workspace_bytes(hidden: int, inter: int, experts: int, topk: int, to
 def fp8_experts(x, ids, weights, w1, w1_scale, w2, w2_scale, y, workspace, stream=None):
     """Gated feed-forward layer of routed experts: x, y [tokens, hidden]; ids int32 and weights float32 [tokens, topk]; w1 float8_e4m3fn
     [experts, 2, inter, hidden] (gate, up) and w2 [experts, hidden, inter] with their block scales."""
-    w = "b2c_fp8_experts"
-    _need(x.dim() == 2 and y.shape == x.shape and y.dtype == x.dtype and ids.dim() == 2 and w1.dim() == 4 and w2.dim() == 3, w + ": shapes")
-    tokens, hidden = x.shape
-    topk = ids.shape[1]
-    experts, _, inter, _ = w1.shape
-    hb, ib = -(-hidden // 128), -(-inter // 128)
-    _need(tuple(ids.shape) == tuple(weights.shape) == (tokens, topk) and ids.dtype == _torch_int32() and _type_of(weights, w) == F32, w + ": ids, weights")
-    _need(tuple(w1.shape) == (experts, 2, inter, hidden) and tuple(w1_scale.shape) == (experts, 2, ib, hb), w + ": w1")
-    _need(tuple(w2.shape) == (experts, hidden, inter) and tuple(w2_scale.shape) == (experts, hb, ib), w + ": w2")
-    _need(_type_of(w1, w) == _type_of(w2, w) == E4M3 and _type_of(w1_scale, w) == _type_of(w2_scale, w) == F32, w + ": weight types")
-    _need(all(t.is_contiguous() for t in (ids, weights, w1, w1_scale, w2, w2_scale, workspace)), w + ": not contiguous")
-    _on_device(w, x, ids, weights, w1, w1_scale, w2, w2_scale, y, workspace)
-    d = ExpertsDesc(hidden, inter, experts, topk, _type_of(x, w))
-    n = ctypes.c_size_t()
-    _check(load().b2c_experts_workspace_bytes(ctypes.byref(d), tokens, ctypes.byref(n)), w)
-    if workspace.numel() * workspace.element_size() < n.value:
-        raise B2CError(E_WORKSPACE_TOO_SMALL, w)
-    _check(load().b2c_fp8_experts(ctypes.byref(d), tokens, x.data_ptr(), _ld(x, w), ids.data_ptr(), weights.data_ptr(), w1.data_ptr(),
-                                  w1_scale.data_ptr(), w2.data_ptr(), w2_scale.data_ptr(), y.data_ptr(), _ld(y, w), workspace.data_ptr(),
-                                  _stream_ptr(stream)), w)
+    r = (_native or _load_native()).experts(x, ids, weights, w1, w1_scale, w2, w2_scale, y, workspace, stream and stream.cuda_stream)
+    if r:
+        _refused("b2c_fp8_experts", *r)
 
 
 def fp8_status() -> int:

@@ -14,6 +14,9 @@ SOURCES = ["api.cpp", "planner.cpp", "tma.cpp", "layout.cu", "conv_mma.cu", "con
            "fp8_api.cpp", "fp8_quantize.cu", "fp8_matmul.cu", "fp8_matmul_pair.cu", "route.cu"]
 
 
+BINDING = os.path.join(HERE, "_binding.so")  # tensor checks of the 8-bit float operators, against torch's headers
+
+
 def _nvcc() -> str:
     for cand in (os.environ.get("NVCC"), "/usr/local/cuda/bin/nvcc", "nvcc"):
         if cand and (os.path.isabs(cand) and os.path.exists(cand) or not os.path.isabs(cand)):
@@ -29,8 +32,32 @@ def needs_build(so: str = SO) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def binding_command(out: str) -> list:
+    import sysconfig
+
+    import torch
+
+    root = os.path.dirname(torch.__file__)
+    inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+           os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include"), sysconfig.get_paths()["include"], os.path.join(ROOT, "include")]
+    return (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI] +
+            [x for p in inc for x in ("-I", p)] + ["-o", out, os.path.join(CSRC, "binding.cpp"), "-L", os.path.join(root, "lib"),
+                                                   "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
+
+
+def build_binding(force: bool = False) -> str:
+    deps = [os.path.join(CSRC, "binding.cpp"), os.path.join(ROOT, "include", "b2conv.h")]
+    if not force and os.path.exists(BINDING) and all(os.path.getmtime(d) <= os.path.getmtime(BINDING) for d in deps):
+        return BINDING
+    tmp = BINDING + ".tmp.%d" % os.getpid()
+    subprocess.check_call(binding_command(tmp))
+    os.replace(tmp, BINDING)
+    return BINDING
+
+
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
     so = SO_DEBUG if debug else SO
+    build_binding(force and not debug)
     if not force and not needs_build(so):
         return so
     cmd = [

@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, 2)
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
         const BlockScale s = block_scale<B2C_E4M3>(mx);
-        const uint32_t q = cvt2<B2C_E4M3>(scaled(s, h[0]), scaled(s, h[1])) | (cvt2<B2C_E4M3>(scaled(s, h[2]), scaled(s, h[3])) << 16);
+        const uint32_t q = __byte_perm(quantize2<B2C_E4M3>(s, h[0], h[1]), quantize2<B2C_E4M3>(s, h[2], h[3]), 0x5410);
         if (n < a.N) *reinterpret_cast<uint32_t*>((uint8_t*)a.y + row * a.ldy + n) = q;  // (N and ldy are multiples of 16)
         if (lane == 0) a.y_scale[row * a.ldys + blockIdx.x] = s.scale;
       }

@@ -78,16 +78,6 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// A pair of fp32 values in one 64-bit register pair; acc += v * f in one instruction.
-typedef unsigned long long f32x2;
-__device__ __forceinline__ f32x2 pair_of(float lo, float hi) {
-  f32x2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ void unpair(f32x2 v, float* lo, float* hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*lo), "=f"(*hi) : "l"(v)); }
-__device__ __forceinline__ void fma2(f32x2* acc, f32x2 v, f32x2 f) { asm volatile("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(*acc) : "l"(v), "l"(f)); }
-
 // Bounded wait of the warps that keep sums in registers: as mbar_wait, without a call (which would have to save them).
 __device__ __forceinline__ bool mbar_wait_inline(uint32_t bar, uint32_t parity, SharedCtl* ctl, int* status) {
   unsigned long long t0 = 0;

@@ -132,10 +132,10 @@ def test_experts_limits_and_workspace(lib):
     assert lib.b2c_fp8_status(None) == BAD
 
 
-def refused(call, *args, **kw):
+def refused(call, *args, code=BAD, **kw):
     with pytest.raises(b2c.B2CError) as e:
         call(*args, **kw)
-    assert e.value.code == BAD
+    assert e.value.code == code
 
 
 def test_binding_refuses_what_the_library_cannot_see(lib):
@@ -148,6 +148,9 @@ def test_binding_refuses_what_the_library_cannot_see(lib):
     refused(b2c.fp8_quantize, x, q, s, block_rows=2)
     refused(b2c.fp8_quantize, x, q, s.double())
     refused(b2c.fp8_quantize, x, q, s)  # not on the device
+    refused(b2c.fp8_quantize, x, q, None)
+    refused(b2c.fp8_quantize, x.t()[:4, :4], q[:, :4], s[:, :1])
+    refused(b2c.fp8_quantize, x[:1].expand(4, 256), q, s)
     a, sa, b, sb, y = q, s, torch.zeros(100, 256).to(f8), torch.zeros(1, 2), torch.zeros(4, 100)
     for args in [(a[:, :128], sa, b, sb, y), (a, sa[:, :1], b, sb, y), (a, sa, b, sb[:, :1], y), (a, sa, b, sb, y[:, :99]), (a, sa, b.t(), sb, y),
                  (a, sa.double(), b, sb, y), (a, sa, b[None], sb[None], y), (a, sa, b, sb, y)]:
@@ -162,7 +165,8 @@ def test_binding_refuses_what_the_library_cannot_see(lib):
     refused(b2c.route, d, torch.zeros(4, 8), w, i, bias=torch.zeros(7))
     refused(b2c.route_sort, i, 8, torch.zeros(8, dtype=torch.int32), i.clone())
     refused(b2c.route_sort, i.long(), 8, torch.zeros(9, dtype=torch.int32), i.clone())
-    refused(b2c.route_sort, torch.zeros(5000, dtype=torch.int32), 8, torch.zeros(9, dtype=torch.int32), torch.zeros(5000, dtype=torch.int32))
+    refused(b2c.route_sort, torch.zeros(5000, dtype=torch.int32), 8, torch.zeros(9, dtype=torch.int32), torch.zeros(5000, dtype=torch.int32),
+            code=b2c.E_WORKSPACE_TOO_SMALL)
     refused(b2c.route_combine, torch.zeros(8, 16), i, w, torch.zeros(4, 15))
     refused(b2c.route_combine, torch.zeros(8, 16), i, w.t(), torch.zeros(4, 16))
     h = torch.zeros(4, 128)
