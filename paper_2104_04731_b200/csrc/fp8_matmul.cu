@@ -280,6 +280,26 @@ int fail(cudaError_t e) {
   return B2C_E_CUDA;
 }
 
+// How many thread blocks share a tile's reduction.  What counts is the SM with the most blocks of the reduction to fetch: tiles * split
+// thread blocks are spread over 148 SMs.  A cut costs the exchange of the partial sums, about as long as three such blocks, and more
+// the larger the cluster (measured, 37 x 5136 x 4112, 41 tiles of 33 blocks: 13.7 us with one, 10.3 with two, 8.7 with three,
+// 9.8 with four and 13.7 with seven of them; 1 x 8192 x 8192, 64 tiles of 64: 18.4, 14.6, 15.5, 14.9 and with eight 14.9 us).
+int choose_split(long long tiles, int kb_all, bool counted) {
+  if (!counted && tiles >= kNumSMs) return 1;  // (a guess of the tiles says nothing about the last wave)
+  int best = 1;
+  double least = 0;
+  for (int s = 1; s <= kMaxSplit && 2 * s <= std::max(2, kb_all); ++s) {
+    const int per = (kb_all + s - 1) / s;
+    if ((kb_all + per - 1) / per != s) continue;  // (no thread block without work)
+    const double cost = (double)((tiles * s + kNumSMs - 1) / kNumSMs) * per + (s > 1 ? 2.5 + 0.5 * s : 0.0);
+    if (s == 1 || cost < least) {
+      best = s;
+      least = cost;
+    }
+  }
+  return best;
+}
+
 template <int NT, int WT, typename YT>
 int launch_rows(const MatmulArgs& a, cudaStream_t st) {
   using S = RowsShape<NT, WT>;
@@ -289,10 +309,8 @@ int launch_rows(const MatmulArgs& a, cudaStream_t st) {
   if (row_tiles > 65535) return B2C_E_UNSUPPORTED;
   // (with groups the number of tiles is known on the device only: as many groups as there are rows may have some)
   const long long busy = (long long)n_tiles * (a.offsets ? std::max<long long>((a.rows + NT - 1) / NT, std::min(a.groups, a.rows)) : row_tiles);
-  int split = (int)std::min<long long>(kMaxSplit, std::max<long long>(1, 2 * kNumSMs / std::max<long long>(1, busy)));
-  split = std::max(1, std::min(split, kb_all / 2));
+  const int split = choose_split(busy, kb_all, a.offsets == nullptr);
   const int kb_per_split = (kb_all + split - 1) / split;
-  split = (kb_all + kb_per_split - 1) / kb_per_split;
   CUtensorMap tw, tx;
   int rc = encode_tiled_3d(&tw, a.b, a.K, a.N, (uint64_t)a.groups * WT, a.K, (uint64_t)a.N * a.K, kBlock, kTileM, kBlock);
   if (rc == B2C_OK) rc = encode_tiled_2d(&tx, a.a, a.K, a.rows, a.rows > 1 ? a.lda : a.K, kBlock, NT, kBlock);

@@ -17,11 +17,16 @@ namespace {
 
 constexpr int kEpiWarps = 8;
 constexpr int kScaleWarps = 2;
-constexpr int kPairThreads = 64 + 32 * (kEpiWarps + kScaleWarps);
+constexpr int kEpiWarp0 = 2 + kScaleWarps;  // first warp of the sums: a whole warpgroup before it
+constexpr int kPairThreads = 32 * (kEpiWarp0 + kEpiWarps);
+// Registers: 384 threads are launched with 168 each (a quarter of the SM's 65536 holds three warps).  The sums alone are 128 of a
+// thread, and 64 values on their way from tensor memory beside them hide its latency: 128 * 88 + 256 * 208 = 384 * 168.
+constexpr int kRegsSums = 208, kRegsRest = 88;
 constexpr int kTileN = 256;
-constexpr int kStages = 6;
+constexpr int kStages = 5;
 constexpr int kABytes = kTileM * kBlock, kBBytes = kTileN / 2 * kBlock;
-constexpr int kPairSmem = 1024 + kStages * (kABytes + kBBytes);
+constexpr int kBoxBytes = 32 * 128;  // results of a warp on their way out: 32 rows of 128 bytes
+constexpr int kPairSmem = 1024 + kStages * (kABytes + kBBytes) + kEpiWarps * kBoxBytes;
 constexpr int kRun = 4;       // blocks of the reduction whose scales are fetched together
 constexpr int kRunSlots = 3;  // runs of factors in shared memory
 constexpr int kBand = 8;  // row tiles that are walked together, so that their columns' B tiles are read from L2
@@ -109,7 +114,8 @@ __device__ __forceinline__ void store_row32(T* p, const float* v, int n, int n_e
 
 template <bool GATED, typename YT>
 __global__ void __launch_bounds__(kPairThreads, 1)
-    matmul_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b, const MatmulArgs a) {
+    matmul_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
+                       const __grid_constant__ CUtensorMap tmap_y, const MatmulArgs a, const bool y_boxes) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ SharedCtl ctl;
   __shared__ int row_tiles_s;
@@ -125,6 +131,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   const int pair_id = (int)(blockIdx.x >> 1), num_pairs = (int)(gridDim.x >> 1);
   const uint32_t a_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t b_base = a_base + kStages * kABytes;
+  const uint32_t box_base = b_base + kStages * kBBytes;
 
   if (warp == 0) {
     if (lane < kStages) {
@@ -168,6 +175,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   const int tiles = row_tiles * n_tiles;     // (fits: checked by the host)
   const int kb_all = (int)blocks_of(a.K);
 
+  if (warp < kEpiWarp0) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
   if (warp == 0) {
     // ---------------------------------------------------------------- copies (both blocks)
     const uint32_t on = elect_one() ? 1u : 0u;
@@ -232,11 +241,11 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     }
     pdl_launch_dependents();
     __syncwarp();
-  } else if (warp >= 2 + kEpiWarps) {
+  } else {
     // ---------------------------------------------------------------- scales (both blocks)
     // They also find the tiles: the warps of sums, which have no time for that, read them beside the first factors.
     // A thread has two rows.  The loads of a run are under way while the run before it is multiplied and handed over.
-    const int st = (int)threadIdx.x - 32 * (2 + kEpiWarps);
+    const int st = (int)threadIdx.x - 64;
     const int nb = (int)blocks_of(a.N);
     int slot = 0;
     uint32_t sph = 0;
@@ -284,10 +293,12 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         }
       }
     }
+  }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSums));
     // ---------------------------------------------------------------- scaled sums and results (both blocks)
     const int quad = warp & 3;         // lanes of tensor memory this warp may read
-    const int half = (warp - 2) >> 2;  // its 128 columns
+    const int half = (warp - kEpiWarp0) >> 2;  // its 128 columns
     const uint32_t leader_empty = map_to_rank(smem_u32(&ctl.tmem_empty[0]), 0u);
     const uint32_t taddr0 = tmem_acc + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * 128);
     const int in_tile = quad * 32 + lane;
@@ -301,12 +312,14 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       f32x2 acc[64];
 #pragma unroll
       for (int i = 0; i < 64; ++i) acc[i] = 0;
-#pragma unroll 1
-      for (int kb = 0; kb < kb_all; ++kb) {
+      // Factors of block kb; read while the block before it is added, so that neither the barrier's nor the memory's latency is waited for.
+      float f = 0.0f, fu = 0.0f;
+      auto next_factor = [&](int kb) {
         const int i = kb % kRun;
-        if (i == 0) ok = ok && __all_sync(0xffffffffu, mbar_wait_inline(smem_u32(&factor_full[slot]), sph, &ctl, &g_fp8_status));
+        if (i == 0) ok = ok && mbar_wait_inline(smem_u32(&factor_full[slot]), sph, &ctl, &g_fp8_status);
+        f = factor[slot][i][GATED ? 0 : half][in_tile];
+        if (GATED) fu = factor[slot][i][1][in_tile];
         if (kb == 0) p = run_tile[slot];
-        const float f = factor[slot][i][GATED ? 0 : half][in_tile], fu = GATED ? factor[slot][i][1][in_tile] : 0.0f;
         if (i == kRun - 1 || kb == kb_all - 1) {
           __syncwarp();
           if (lane == 0) mbar_arrive(smem_u32(&factor_empty[slot]));
@@ -315,22 +328,27 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             sph ^= 1u;
           }
         }
+      };
+      next_factor(0);
+#pragma unroll 1
+      for (int kb = 0; kb < kb_all; ++kb) {
         const f32x2 ff = pair_of(f, f), ffu = pair_of(fu, fu);
-        ok = ok && __all_sync(0xffffffffu, mbar_wait_inline(smem_u32(&ctl.tmem_full[buf]), bph, &ctl, &g_fp8_status));
-        if (!ok) break;
+        ok = ok && mbar_wait_inline(smem_u32(&ctl.tmem_full[buf]), bph, &ctl, &g_fp8_status);
+        // (a wait that gave up does not leave the loop: the lanes stay together, and no result is stored)
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t taddr = taddr0 + (uint32_t)(buf * kTileN);
 #pragma unroll
-        for (int c = 0; c < 128; c += 32) {
-          float v[32];
-          tmem_ld<32>(taddr + c, reinterpret_cast<int32_t*>(v));
-          if (c == 96) {
+        for (int c = 0; c < 128; c += 64) {
+          float v[64];
+          tmem_ld64(taddr + c, reinterpret_cast<int32_t*>(v));
+          if (c == 0 && kb + 1 < kb_all) next_factor(kb + 1);
+          if (c == 64) {
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster_relaxed(leader_empty + 8 * buf);
           }
 #pragma unroll
-          for (int j = 0; j < 32; j += 2) fma2(&acc[(c + j) / 2], pair_of(v[j], v[j + 1]), GATED && c >= 64 ? ffu : ff);
+          for (int j = 0; j < 64; j += 2) fma2(&acc[(c + j) / 2], pair_of(v[j], v[j + 1]), GATED && c >= 64 ? ffu : ff);
         }
         buf ^= 1;
         if (buf == 0) bph ^= 1u;
@@ -361,8 +379,43 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           if (half == 0) a.y_scale[m * a.ldys + p.nt] = s.scale;
         }
       } else {
-        if (ok && m < p.row_end) {
-          const int n = p.nt * kTileN + half * 128;
+        const int n = p.nt * kTileN + half * 128;
+        if (y_boxes && p.row0 + (int)rank * kTileM + quad * 32 + 32 <= p.row_end) {
+          // All 32 rows of the warp are this group's: 128 bytes of each go to shared memory (16-byte pieces, swizzled as the tensor map
+          // says) and from there in one copy, which clips what lies past the last column and runs beside the next tile.  (Stores from
+          // registers took 3200 cycles of a tile of bf16, as long as five blocks of the reduction.)
+          constexpr int kCols = 128 / (int)sizeof(YT);
+          const uint32_t box = box_base + (uint32_t)((warp - kEpiWarp0) * kBoxBytes);
+#pragma unroll
+          for (int i = 0; i < 128; i += kCols) {
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            __syncwarp();
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+              constexpr int kPer = 16 / (int)sizeof(YT);
+              float v[kPer];
+#pragma unroll
+              for (int j = 0; j < kPer; j += 2) unpair(acc[(i + c * kPer + j) / 2], &v[j], &v[j + 1]);
+              uint32_t w[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                if constexpr (sizeof(YT) == 4) w[j] = __float_as_uint(v[j]);
+                else w[j] = pack2<YT>(v[2 * j], v[2 * j + 1]);
+              }
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + (uint32_t)(lane * 128 + ((c ^ (lane & 7)) * 16))), "r"(w[0]),
+                           "r"(w[1]), "r"(w[2]), "r"(w[3])
+                           : "memory");
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0 && ok && n + i < a.N) {
+              asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(&tmap_y),
+                           "r"((n + i) * (int)sizeof(YT)), "r"(p.row0 + (int)rank * kTileM + quad * 32), "r"(box)
+                           : "memory");
+              asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            }
+          }
+        } else if (ok && m < p.row_end) {
           YT* y = (YT*)a.y + m * a.ldy + n;
 #pragma unroll
           for (int i = 0; i < 128; i += 32) {
@@ -375,6 +428,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       }
     }
   }
+
+  // copies of results read shared memory: they end before the block does
+  if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
 
   // ---------------------------------------------------------------- teardown
   // No block of the pair leaves, or frees tensor memory, while the other may still read its shared memory, arrive on
@@ -399,10 +455,15 @@ int launch_pair(const MatmulArgs& a, cudaStream_t st) {
   const long long n_tiles = (a.N + cols - 1) / cols;
   const long long row_tiles = a.offsets ? a.rows / (2 * kTileM) + std::min(a.groups, a.rows) : (a.rows + 2 * kTileM - 1) / (2 * kTileM);
   if (row_tiles * n_tiles > 0x7FFFFFFFLL - kNumSMs) return B2C_E_UNSUPPORTED;
-  CUtensorMap ta, tb;
+  CUtensorMap ta, tb, ty;
   int rc = encode_tiled_2d(&ta, a.a, a.K, a.rows, a.rows > 1 ? a.lda : a.K, kBlock, kTileM, kBlock);
   if (rc == B2C_OK)
     rc = encode_tiled_3d(&tb, a.b, a.K, a.N, (uint64_t)a.groups * (GATED ? 2 : 1), a.K, (uint64_t)a.N * a.K, kBlock, GATED ? 64 : kTileM, kBlock);
+  if (rc != B2C_OK) return rc;
+  // results by boxes of 128 bytes x 32 rows where the copy engine can address them
+  const bool y_boxes = !GATED && (reinterpret_cast<uintptr_t>(a.y) & 15) == 0 && (a.ldy * sizeof(YT)) % 16 == 0;
+  ty = ta;
+  if (y_boxes) rc = encode_tiled_2d(&ty, a.y, (uint64_t)a.N * sizeof(YT), a.rows, (uint64_t)a.ldy * sizeof(YT), 128, 32, 128);
   if (rc != B2C_OK) return rc;
   static std::atomic<unsigned long long> configured{0};
   cudaError_t e = set_max_dynamic_smem_once(configured, (const void*)matmul_pair_kernel<GATED, YT>, kPairSmem);
@@ -422,7 +483,7 @@ int launch_pair(const MatmulArgs& a, cudaStream_t st) {
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    e = cudaLaunchKernelEx(&cfg, matmul_pair_kernel<GATED, YT>, ta, tb, a);
+    e = cudaLaunchKernelEx(&cfg, matmul_pair_kernel<GATED, YT>, ta, tb, ty, a, y_boxes);
   }
   if (e != cudaSuccess) {
     set_last_cuda_error((int)e);
