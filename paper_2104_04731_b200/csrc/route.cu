@@ -133,9 +133,17 @@ __device__ __forceinline__ void sort_lane(K (&k)[P]) {
           }
 }
 
-// choose() for 32-bit choices: every lane sorts its own once, a round compares the lanes' first ones.
+// What in an order of 32-bit choices may be wrong, because two of them are nearer than their errors.
+struct Near {
+  bool runs;    // a kept and a dropped run
+  bool inside;  // two neighbours among the chosen
+  bool border;  // the last chosen and the first left out
+};
+
+// choose_exact() for 32-bit choices: every lane sorts its own once, a round compares the lanes' first ones.  Lane j < rounds gets the
+// j-th expert.  With CHECK the choices may be off by half of `unit` * (1 + |choice|), and *near tells what that leaves open.
 template <int P, typename K, bool CHECK, typename F>
-__device__ __forceinline__ int choose32(const b2c_route_desc& d, const float (&choice)[P], F part_of, int lane, float unit, bool* close) {
+__device__ __forceinline__ int choose32(const b2c_route_desc& d, int rounds, const float (&choice)[P], F part_of, int lane, float unit, Near* near) {
   constexpr bool kExact = sizeof(K) == 8;
   K key[P];
 #pragma unroll
@@ -144,7 +152,7 @@ __device__ __forceinline__ int choose32(const b2c_route_desc& d, const float (&c
     else key[i] = lane * P + i < d.experts ? ((order_key(choice[i]) & ~(unsigned)(P - 1)) | (unsigned)(P - 1 - i)) : 0u;
   }
   sort_lane<P, K>(key);
-  *close = false;
+  *near = {false, false, false};
   bool by_expert = false;  // runs that do not end with a lane's experts: keys are dropped one by one
   unsigned open = kAll;
   const int size = d.experts / d.groups;
@@ -180,7 +188,7 @@ __device__ __forceinline__ int choose32(const b2c_route_desc& d, const float (&c
     if constexpr (CHECK) {
       const float low = key_value(__reduce_min_sync(kAll, kept ? mine : 0xFFFFFFFFu));
       const unsigned high = __reduce_max_sync(kAll, kept ? 0u : mine);
-      *close = high != 0u && !(low - key_value(high) > 2.0f * unit * (1.0f + fabsf(low)));
+      near->runs = high != 0u && !(low - key_value(high) > 2.0f * unit * (1.0f + fabsf(low)));
     }
     open = __ballot_sync(kAll, kept);
     if (!by_expert && !kept) {
@@ -190,7 +198,7 @@ __device__ __forceinline__ int choose32(const b2c_route_desc& d, const float (&c
   }
   int my_id = 0;
   float my_value = 0.0f;
-  for (int j = 0; j < d.topk;) {
+  for (int j = 0; j < rounds;) {
     const unsigned mine = value_bits(key[0]);
     const unsigned top = __reduce_max_sync(kAll, mine);
     const int owner = __ffs(__ballot_sync(kAll, mine == top)) - 1;
@@ -221,10 +229,12 @@ __device__ __forceinline__ int choose32(const b2c_route_desc& d, const float (&c
         if (value_bits(key[i]) != 0u && ((open >> ((lane * P + place_of<P>(key[i])) / size)) & 1u)) left = max(left, value_bits(key[i]));
       left = __reduce_max_sync(kAll, left);
     }
-    const bool ends = lane == d.topk - 1;
+    const bool ends = lane == rounds - 1;
     if (ends) next = left != 0u ? key_value(left) : -INFINITY;
-    const bool near = lane < d.topk && !(ends && left == 0u) && !(my_value - next > unit * (1.0f + fabsf(my_value)));
-    *close |= __any_sync(kAll, near);
+    const bool open_order = lane < rounds && !(ends && left == 0u) && !(my_value - next > unit * (1.0f + fabsf(my_value)));
+    const unsigned who = __ballot_sync(kAll, open_order);
+    near->border = ((who >> (rounds - 1)) & 1u) != 0u;
+    near->inside = (who & ((1u << (rounds - 1)) - 1u)) != 0u;
   }
   return my_id;
 }
@@ -273,12 +283,32 @@ __device__ __noinline__ int choose64(const RouteArgs& a, const T* row, int lane,
   return choose_exact<P>(a.d, c, c, part_of, lane);
 }
 
+// The experts of lanes 0 .. count - 1 in the order of their choices in 64 bits.
+__device__ __forceinline__ int order64(double choice, int id, int count, int lane) {
+  const unsigned long long key = order_key(choice);
+  int rank = 0;
+#pragma unroll 1
+  for (int j = 0; j < count; ++j) {
+    const unsigned long long k = __shfl_sync(kAll, key, j);
+    const int i = __shfl_sync(kAll, id, j);
+    rank += k > key || (k == key && i < id);
+  }
+  int sorted = id;
+#pragma unroll 1
+  for (int j = 0; j < count; ++j) {
+    const int r = __shfl_sync(kAll, rank, j), i = __shfl_sync(kAll, id, j);
+    if (r == lane) sorted = i;
+  }
+  return sorted;
+}
+
 // One warp for one token, everything in registers.  Scores are monotonic in the logits, so without a bias the logits themselves are
 // compared, which is exact.  With a bias (or run scores that are sums) the choices are formed in 32 bits: exponential, sum, quotient
 // and additions put each off by at most 7 units of 2^-24 * (1 + |choice|), its place in the key's lowest bits by P - 1 units of 2^-23,
 // together less than 2^-19 for P <= 8 and 2^-17 beyond, and sums of two by twice that.  A token in which two choices that decide
 // something are not further apart than twice this (about one in fifty at 256 experts) is chosen again with the places beside the
-// values (2^-20), and if it is still undecided (one in two hundred) in 64 bits.
+// values (2^-20); where that leaves only the order of the topk + 1 first open (one in two hundred) these few are compared in 64 bits,
+// and else, or if the scores hang on all logits, the token is done in 64 bits from the start.
 // Memory-bound on paper (one read of the logits); what it spends are the instructions of exponentials, sort and topk rounds.
 constexpr int kRouteWarps = 8;
 template <typename T, int P>
@@ -330,7 +360,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RouteArgs
     mx = key_value(warp_max(order_key(mx)));
   }
   int id;
-  bool close = false;
+  Near near;
   if (by_logit && !sums) {
     if (softmax && !a.d.renormalise) {
       float sum = 0.0f;
@@ -338,7 +368,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RouteArgs
       for (int i = 0; i < P; ++i) sum += x[i] == -INFINITY ? 0.0f : (x[i] == mx ? 1.0f : expf(x[i] - mx));
       all = warp_sum((double)sum);
     }
-    id = choose32<P, unsigned long long, false>(a.d, x, [&](int e) { return logit<T>(row, e); }, lane, 0.0f, &close);
+    id = choose32<P, unsigned long long, false>(a.d, a.d.topk, x, [&](int e) { return logit<T>(row, e); }, lane, 0.0f, &near);
   } else {
     float c[P];
     float sum = 0.0f;
@@ -378,10 +408,15 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RouteArgs
           if (lane * P + i < E) c[i] += a.bias[lane * P + i];
       }
     }
-    id = choose32<P, unsigned, true>(a.d, c, part_of, lane, P <= 8 ? 0x1p-18f : 0x1p-16f, &close);
-    if (close) id = choose32<P, unsigned long long, true>(a.d, c, part_of, lane, 0x1p-20f, &close);
+    id = choose32<P, unsigned, true>(a.d, a.d.topk, c, part_of, lane, P <= 8 ? 0x1p-18f : 0x1p-16f, &near);
+    if (near.runs || near.inside || near.border) {
+      // a second look, one expert further, so that a border within the errors lies inside
+      const int rounds = min(min(a.d.topk + 1, 32), E / a.d.groups * a.d.topk_groups);
+      id = choose32<P, unsigned long long, true>(a.d, rounds, c, part_of, lane, 0x1p-20f, &near);
+      if (near.runs || near.border || ((softmax || by_logit) && near.inside)) id = choose64<T, P>(a, row, lane, mx);
+      else if (near.inside) id = order64(sigmoid64((double)logit<T>(row, lane < rounds ? id : 0)) + (double)a.bias[lane < rounds ? id : 0], id, rounds, lane);
+    }
   }
-  if (close) id = choose64<T, P>(a, row, lane, mx);
   // the weights of the chosen, from their logits; the argument of the exponential without the rounding of its difference
   const bool on = lane < a.d.topk;
   const float l = on ? logit<T>(row, id) : -INFINITY;
