@@ -1,7 +1,7 @@
 // Products of block-scaled 8-bit matrices on the tensor core: the kernel for few rows, and the choice between the two.
 //
 // With few rows the weights are the bytes, and the tensor core's 128 accumulator rows are given to them (the axes
-// are swapped): a thread block owns 128 weight rows and 16 to 128 activation rows, so that an MMA of a few activation rows
+// are swapped): a thread block owns 128 weight rows and 16 to 64 activation rows, so that an MMA of a few activation rows
 // is no larger than these.  What bounds it is how many bytes are in flight: the reduction is cut over the
 // blocks of a cluster until all SMs have a share, and the partial sums meet in distributed shared memory, in a fixed
 // order, without a second launch or atomics.
@@ -237,16 +237,23 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, 2)
       float v[WT][4];
 #pragma unroll
       for (int w = 0; w < WT; ++w) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[w][i] = 0.0f;
         const uint32_t at = smem_base + (uint32_t)(((w * NT + j) * kTileM + 4 * lane) * 4);
-        for (int z = 0; z < split; ++z) {
-          const float4 p = ld_cluster_f4(split > 1 ? map_to_rank(at, (uint32_t)z) : at);
-          v[w][0] += p.x;
-          v[w][1] += p.y;
-          v[w][2] += p.z;
-          v[w][3] += p.w;
-        }
+        float4 part[kMaxSplit];  // (all loads first, so that their latency is waited for once)
+#pragma unroll
+        for (int z = 0; z < kMaxSplit; ++z)
+          if (z < split) part[z] = ld_cluster_f4(split > 1 ? map_to_rank(at, (uint32_t)z) : at);
+        v[w][0] = part[0].x;
+        v[w][1] = part[0].y;
+        v[w][2] = part[0].z;
+        v[w][3] = part[0].w;
+#pragma unroll
+        for (int z = 1; z < kMaxSplit; ++z)
+          if (z < split) {
+            v[w][0] += part[z].x;
+            v[w][1] += part[z].y;
+            v[w][2] += part[z].z;
+            v[w][3] += part[z].w;
+          }
       }
       const long long row = row0 + j;
       if constexpr (WT == 1) {
@@ -330,11 +337,24 @@ int launch_rows_type(const MatmulArgs& a, cudaStream_t st) {
   return launch_rows<NT, 1, __nv_bfloat16>(a, st);
 }
 
+// Whether one product of 65 rows or more is better formed by tiles of 128 weight rows x 64 rows, one on each of up to 148 SMs, than by
+// the pair kernel's 256 x 256 on 74 pairs.  In cycles: 770 for a block of the reduction and 4600 besides here (as long as every tile has
+// an SM of its own; two on one take two and a half times as long), 850 and 4000 for a wave there.  Measured, us here / there:
+//   4096 x 4096: 128 rows 11.3 / 18.8, 256 rows 15.5 / 18.9, 320 rows 39 / 19.0;   8192 x 2048: 128 rows 10.2 / 12.6, 200 rows 13.7 / 12.7;
+//   2048 x 7168: 256 rows 15.0 / 27.5, 384 rows 24.5 / 27.5, 512 rows 37.6 / 27.6 (the weights are fetched once for every 64 rows).
+bool rows_kernel_is_better(const MatmulArgs& a) {
+  const long long kb_all = blocks_of(a.K), tiles = blocks_of(a.N) * ((a.rows + 63) / 64);
+  const int split = choose_split(tiles, (int)kb_all, true);
+  if (a.rows > 384 || tiles * split > kNumSMs) return false;
+  const long long waves = (((a.N + 255) / 256) * (long long)((a.rows + 255) / 256) + kNumSMs / 2 - 1) / (kNumSMs / 2);
+  return 770 * ((kb_all + split - 1) / split) + 4600 + (split > 1 ? 2000 : 0) < waves * (850 * kb_all + 4000);
+}
+
 }  // namespace
 
 int launch_fp8_matmul(const MatmulArgs& a, cudaStream_t st) {
   const int rows = a.offsets ? (a.rows + a.groups - 1) / a.groups : a.rows;  // of a group, on average
-  if (rows > 128) return launch_fp8_matmul_pair(a, st);
+  if (rows > 64 && !(a.offsets ? rows <= 128 : rows_kernel_is_better(a))) return launch_fp8_matmul_pair(a, st);
   if (a.gated) {
     if (rows <= 16) return launch_rows<16, 2, uint8_t>(a, st);
     if (rows <= 32) return launch_rows<32, 2, uint8_t>(a, st);
@@ -342,8 +362,7 @@ int launch_fp8_matmul(const MatmulArgs& a, cudaStream_t st) {
   }
   if (rows <= 16) return launch_rows_type<16>(a, st);
   if (rows <= 32) return launch_rows_type<32>(a, st);
-  if (rows <= 64) return launch_rows_type<64>(a, st);
-  return launch_rows_type<128>(a, st);
+  return launch_rows_type<64>(a, st);
 }
 
 int fp8_status_read_and_clear(int32_t* status) {
