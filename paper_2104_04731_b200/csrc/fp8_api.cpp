@@ -181,9 +181,6 @@ int b2c_fp8_experts(const b2c_experts_desc* d, int64_t tokens, const void* x, in
   const long long pairs = tokens * d->topk;
   int32_t* offsets = (int32_t*)(ws + l.offsets);
   int32_t* rows = (int32_t*)(ws + l.rows);
-  rc = from_cuda(launch_route_sort(ids, pairs, d->experts, offsets, rows, nullptr, (int32_t*)(ws + l.sort), st));
-  if (rc != B2C_OK) return rc;
-
   QuantizeArgs q = {};
   q.x = x;
   q.ldx = ldx;
@@ -198,7 +195,12 @@ int b2c_fp8_experts(const b2c_experts_desc* d, int64_t tokens, const void* x, in
   q.q_type = B2C_E4M3;
   q.map = rows;
   q.copies = d->topk;
-  rc = from_cuda(launch_fp8_quantize(q, st));
+  if (pairs <= kSmallPairs) {
+    rc = from_cuda(launch_sort_quantize(q, ids, (int)pairs, d->experts, offsets, rows, st));
+  } else {
+    rc = from_cuda(launch_route_sort(ids, pairs, d->experts, offsets, rows, nullptr, (int32_t*)(ws + l.sort), st));
+    if (rc == B2C_OK) rc = from_cuda(launch_fp8_quantize(q, st));
+  }
   if (rc != B2C_OK) return rc;
 
   MatmulArgs m = {};
@@ -236,6 +238,7 @@ int b2c_fp8_experts(const b2c_experts_desc* d, int64_t tokens, const void* x, in
   m.K = d->inter;
   m.y_type = d->type;
   m.gated = 0;
+  m.early = 1;  // (the first product read its offsets after the sort had ended, and lets no later kernel start before that)
   rc = launch_fp8_matmul(m, st);
   if (rc != B2C_OK) return rc;
   return from_cuda(launch_route_combine(m.y, d->type, pairs, m.ldy, rows, weights, tokens, d->topk, d->hidden, y, d->type, ldy, st));

@@ -51,6 +51,7 @@ struct MatmulArgs {
   long long ldys;
   int rows, N, K, groups;
   int a_type, b_type, y_type;
+  int early;             // weights and offsets are older than the kernel before this one (see matmul_rows_kernel)
   int gated;             // y = quantise(silu(a . gate) * (a . up)), blocks of 1 x 128
 };
 
@@ -65,6 +66,10 @@ struct RouteArgs {
 };
 
 cudaError_t launch_fp8_quantize(const QuantizeArgs& a, cudaStream_t st);
+// launch_route_sort and launch_fp8_quantize (E4M3 rows, a.copies slots a token) in one, for at most kSmallPairs pairs.
+constexpr int kSmallPairs = 1024;
+cudaError_t launch_sort_quantize(const QuantizeArgs& a, const int32_t* ids, int pairs, int experts, int32_t* offsets, int32_t* rows,
+                                 cudaStream_t st);
 int launch_fp8_matmul(const MatmulArgs& a, cudaStream_t st);  // B2C_* code
 int launch_fp8_matmul_pair(const MatmulArgs& a, cudaStream_t st);  // its form for many rows
 cudaError_t fp8_pair_status(int* status);

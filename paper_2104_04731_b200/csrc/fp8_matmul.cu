@@ -56,7 +56,7 @@ __device__ __forceinline__ void store4<float>(float* p, const float* v, int n) {
 template <int NT, int WT, typename YT>
 __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, 2)
     matmul_rows_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const MatmulArgs a,
-                       const int kb_per_split) {
+                       const int kb_per_split, const bool early) {
   using S = RowsShape<NT, WT>;
   extern __shared__ uint8_t smem_raw[];
   __shared__ SharedCtl ctl;
@@ -86,7 +86,9 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, 2)
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl.tmem_base)), "r"(S::kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  pdl_wait();
+  // `early`: neither the weights nor the offsets come from the kernel before this one (nor does anything it overlaps with write them),
+  // so tile and weights are fetched while that one drains; rows and their scales are not touched before it has ended.
+  if (!early) pdl_wait();
   if (warp == 2) {
     const RowTile t = find_row_tile(a, (int)blockIdx.y, NT);
     if (lane == 0) tile = t;
@@ -94,7 +96,7 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, 2)
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  pdl_launch_dependents();
+  if (!early) pdl_launch_dependents();
   const uint32_t tmem_acc = __shfl_sync(0xffffffffu, ctl.tmem_base, 0);
   const int group = tile.group, row0 = tile.row0;
   const int n0 = (int)blockIdx.x * kTileM;
@@ -106,16 +108,25 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, 2)
   } else if (warp == 0) {
     // ---------------------------------------------------------------- copies
     const uint32_t leader = elect_one() ? 1u : 0u;
-    int s = 0;
-    uint32_t ph = 0;
-    for (int kb = kb0; kb < kb1; ++kb) {
-      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.empty[s]), ph ^ 1u, &ctl, &g_fp8_status))) break;
-      const uint32_t full = smem_u32(&ctl.full[s]);
-      const uint32_t dst = smem_base + s * S::kStageBytes;
+    auto load_w = [&](int kb, int s) {
+      const uint32_t full = smem_u32(&ctl.full[s]), dst = smem_base + s * S::kStageBytes;
       mbar_arrive_expect_tx(full, S::kStageBytes, leader);
 #pragma unroll
       for (int w = 0; w < WT; ++w) tma_load_3d(dst + w * kTileM * kBlock, &tmap_w, kb * kBlock, n0, group * WT + w, full, leader);
-      tma_load_2d(dst + WT * kTileM * kBlock, &tmap_x, kb * kBlock, row0, full, leader);
+    };
+    auto load_x = [&](int kb, int s) {
+      tma_load_2d(smem_base + s * S::kStageBytes + WT * kTileM * kBlock, &tmap_x, kb * kBlock, row0, smem_u32(&ctl.full[s]), leader);
+    };
+    const int ahead = early ? min(S::kStages, kb1 - kb0) : 0;
+    for (int i = 0; i < ahead; ++i) load_w(kb0 + i, i);
+    if (early) pdl_wait();
+    for (int i = 0; i < ahead; ++i) load_x(kb0 + i, i);
+    int s = ahead % S::kStages;
+    uint32_t ph = ahead == S::kStages ? 1u : 0u;
+    for (int kb = kb0 + ahead; kb < kb1; ++kb) {
+      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.empty[s]), ph ^ 1u, &ctl, &g_fp8_status))) break;
+      load_w(kb, s);
+      load_x(kb, s);
       if (++s == S::kStages) {
         s = 0;
         ph ^= 1u;
@@ -152,6 +163,10 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, 2)
     __syncwarp();
   } else {
     // ---------------------------------------------------------------- scaled sums
+    if (early) {
+      pdl_wait();
+      pdl_launch_dependents();
+    }
     const int quad = warp & 3;                         // lanes of tensor memory this warp may read
     const int c0 = ((warp - 2) >> 2) * S::kWarpCols;   // its columns
     const int et = (int)threadIdx.x - 64;              // thread of this role
@@ -274,7 +289,8 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, 2)
       }
     }
   }
-  // no block leaves while another reads its sums
+  // no block leaves while another reads its sums, and none before the kernel ahead has ended: what comes after this one relies on that
+  if (early) pdl_wait();
   if (split > 1) cluster_sync();
   if (warp == 1) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -326,7 +342,7 @@ int launch_rows(const MatmulArgs& a, cudaStream_t st) {
   cudaError_t e = set_max_dynamic_smem_once(configured, (const void*)matmul_rows_kernel<NT, WT, YT>, S::kSmem);
   if (e == cudaSuccess)
     e = launch_pdl_cluster(matmul_rows_kernel<NT, WT, YT>, dim3((unsigned)n_tiles, (unsigned)row_tiles, (unsigned)split), dim3(S::kThreads),
-                           S::kSmem, st, split, tw, tx, a, kb_per_split);
+                           S::kSmem, st, split, tw, tx, a, kb_per_split, a.early != 0);
   return e == cudaSuccess ? B2C_OK : fail(e);
 }
 

@@ -164,6 +164,101 @@ __global__ void __launch_bounds__(kThreads) quantize_blocks_kernel(const Quantiz
   if (threadIdx.x == 0) a.scale[rb * a.lds + blk] = s.scale;
 }
 
+// Sort and quantisation of a small batch on its way into an expert layer, in one launch: a thread block takes one token and sorts all
+// pairs for itself (at most kSmallPairs, in shared memory), because a launch of its own for the sort costs more than sorting
+// everywhere.  Same order as the sort on its own: by expert, then by pair.
+constexpr int kWarps = kThreads / 32;
+template <typename T>
+__global__ void __launch_bounds__(kThreads) sort_quantize_kernel(const QuantizeArgs a, const Vec vec, const int nb, const int32_t* ids,
+                                                                 const int pairs, const int experts, int32_t* offsets, int32_t* rows) {
+  extern __shared__ int count[];  // [kWarps][experts], then [experts]: first place of every expert
+  __shared__ int place_s[kMaxTopk], warp_sum_s[kWarps];
+  int* base = count + kWarps * experts;
+  const int t = blockIdx.x, topk = a.copies, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int part = (threadIdx.x % kLanes) * 16, group = threadIdx.x / kLanes;
+  for (int i = threadIdx.x; i < kWarps * experts; i += kThreads) count[i] = 0;
+  pdl_wait();
+  pdl_launch_dependents();
+  float v[16];  // the first block travels while the pairs are sorted
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+  if (group < nb && group * kBlock + part < a.cols) load_part<T>(a, vec.x, t, group * kBlock + part, v);
+  __syncthreads();
+  // each warp counts a run of the pairs; a pair's place in it is the count of its expert so far
+  const int steps = (pairs + kThreads - 1) / kThreads;
+  for (int s = 0; s < steps; ++s) {
+    const int p = (warp * steps + s) * 32 + lane;
+    int id = p < pairs ? ids[p] : -1;
+    if (id >= experts) id = -1;
+    const unsigned same = __match_any_sync(0xffffffffu, id);
+    const int before = id >= 0 ? count[warp * experts + id] : 0;
+    const int rank = __popc(same & ((1u << lane) - 1u));
+    __syncwarp();
+    if (id >= 0 && rank == 0) count[warp * experts + id] = before + __popc(same);
+    __syncwarp();
+    if (p < pairs && p / topk == t) place_s[p - t * topk] = before + rank;
+  }
+  __syncthreads();
+  // places of the warps within an expert, and of the experts: each thread a run of neighbouring experts
+  const int per = (experts + kThreads - 1) / kThreads, e0 = threadIdx.x * per, e1 = min(experts, e0 + per);
+  int mine = 0;
+  for (int e = e0; e < e1; ++e) {
+    int run = 0;
+    for (int w = 0; w < kWarps; ++w) {
+      const int n = count[w * experts + e];
+      count[w * experts + e] = run;
+      run += n;
+    }
+    base[e] = run;
+    mine += run;
+  }
+  int scan = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int n = __shfl_up_sync(0xffffffffu, scan, d);
+    if (lane >= d) scan += n;
+  }
+  if (lane == 31) warp_sum_s[warp] = scan;
+  __syncthreads();
+  int at = scan - mine;
+  for (int w = 0; w < warp; ++w) at += warp_sum_s[w];
+  for (int e = e0; e < e1; ++e) {
+    const int n = base[e];
+    base[e] = at;
+    at += n;
+    if (t == 0) {
+      if (e == 0) offsets[0] = 0;
+      offsets[e + 1] = at;
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < topk) {
+    const int p = t * topk + threadIdx.x, id = ids[p];
+    int to = -1;
+    if (id >= 0 && id < experts) to = base[id] + count[p / 32 / steps * experts + id] + place_s[threadIdx.x];
+    place_s[threadIdx.x] = to;
+    rows[p] = to;
+  }
+  __syncthreads();
+  for (int blk = group; blk < (nb + kThreads / kLanes - 1) / (kThreads / kLanes) * (kThreads / kLanes); blk += kThreads / kLanes) {
+    const int c0 = blk * kBlock + part;
+    if (blk != group) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+      if (blk < nb && c0 < a.cols) load_part<T>(a, vec.x, t, c0, v);
+    }
+    const BlockScale s = block_scale<B2C_E4M3>(block_max(amax16(v)));
+    if (blk >= nb) continue;
+    const uint4 w = quantize16<B2C_E4M3>(s, v);
+    for (int j = 0; j < topk; ++j) {
+      const int to = place_s[j];
+      if (to < 0) continue;
+      if (c0 < a.cols) store_part(a, vec.q, to, c0, w);
+      if (part == 0) a.scale[(long long)to * a.lds + blk] = s.scale;
+    }
+  }
+}
+
 template <typename T, int QT>
 cudaError_t launch(const QuantizeArgs& a, cudaStream_t st) {
   const int nb = (int)blocks_of(a.cols);
@@ -183,7 +278,23 @@ cudaError_t launch(const QuantizeArgs& a, cudaStream_t st) {
   return launch_pdl(quantize_blocks_kernel<T, QT>, dim3((unsigned)grid), dim3(kThreads), 0, st, a, vec, nb);
 }
 
+template <typename T>
+cudaError_t launch_sort(const QuantizeArgs& a, const int32_t* ids, int pairs, int experts, int32_t* offsets, int32_t* rows, cudaStream_t st) {
+  Vec vec;
+  vec.x = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && (a.ldx * sizeof(T)) % 16 == 0;
+  vec.q = true;  // (the workspace's rows: multiples of 16 bytes)
+  return launch_pdl(sort_quantize_kernel<T>, dim3((unsigned)a.rows), dim3(kThreads), (size_t)(kWarps + 1) * experts * sizeof(int), st, a, vec,
+                    (int)blocks_of(a.cols), ids, pairs, experts, offsets, rows);
+}
+
 }  // namespace
+
+cudaError_t launch_sort_quantize(const QuantizeArgs& a, const int32_t* ids, int pairs, int experts, int32_t* offsets, int32_t* rows,
+                                 cudaStream_t st) {
+  if (a.x_type == B2C_F32) return launch_sort<float>(a, ids, pairs, experts, offsets, rows, st);
+  if (a.x_type == B2C_F16) return launch_sort<__half>(a, ids, pairs, experts, offsets, rows, st);
+  return launch_sort<__nv_bfloat16>(a, ids, pairs, experts, offsets, rows, st);
+}
 
 cudaError_t launch_fp8_quantize(const QuantizeArgs& a, cudaStream_t st) {
 #define B2C_BY_TYPE(T) return a.q_type == B2C_E4M3 ? launch<T, B2C_E4M3>(a, st) : launch<T, B2C_E5M2>(a, st)
