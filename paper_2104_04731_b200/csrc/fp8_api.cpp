@@ -34,7 +34,7 @@ int experts_layout(const b2c_experts_desc* d, int64_t tokens, ExpertsLayout* l) 
   if (!d || tokens < 0) return B2C_E_INVALID_ARG;
   if (d->hidden < 16 || d->inter < 16 || d->hidden % 16 || d->inter % 16) return B2C_E_INVALID_ARG;
   if (d->experts < 1 || d->topk < 1 || d->topk > d->experts || !wide_type(d->type)) return B2C_E_INVALID_ARG;
-  if (d->experts > kMaxExperts || d->topk > kMaxTopk) return B2C_E_UNSUPPORTED;
+  if (d->experts > kMaxExperts || d->topk > kMaxTopk || (long long)d->hidden * d->inter >= kMaxStride) return B2C_E_UNSUPPORTED;
   if (tokens > kMaxRows / d->topk) return B2C_E_UNSUPPORTED;
   const size_t pairs = (size_t)tokens * d->topk;
   size_t at = 0;
@@ -88,6 +88,8 @@ int b2c_fp8_matmul(const b2c_matmul_desc* d, int64_t rows, const void* a, int64_
   if (lda < d->K || lda % 16 || ld_a_scale < blocks_of(d->K) || ldy < d->N) return B2C_E_INVALID_ARG;
   if (d->groups > 1 && !offsets) return B2C_E_INVALID_ARG;
   if (d->groups > kMaxExperts || rows > kMaxRows || d->N > (1 << 30) || d->K > (1 << 30)) return B2C_E_UNSUPPORTED;
+  // (strides that a tensor map can hold)
+  if (lda >= kMaxStride || (long long)d->N * d->K >= kMaxStride || ldy * type_bytes(d->y_type) >= kMaxStride) return B2C_E_UNSUPPORTED;
   if (rows == 0) return B2C_OK;
   if (!a || !a_scale || !b || !b_scale || !y) return B2C_E_INVALID_ARG;
   if (!aligned(a, 16) || !aligned(b, 16) || !aligned(a_scale, 4) || !aligned(b_scale, 4) || !aligned(offsets, 4) ||

@@ -133,6 +133,10 @@ __device__ __forceinline__ void sort_lane(K (&k)[P]) {
           }
 }
 
+// A choice that a key can carry its place in: infinities become the largest values, NaN the lowest one.  (Choices that only
+// this makes equal are too near to each other, and compared again as they are.)
+__device__ __forceinline__ float finite(float v) { return fminf(fmaxf(v, -3.402823466e38f), 3.402823466e38f); }
+
 // What in an order of 32-bit choices may be wrong, because two of them are nearer than their errors.
 struct Near {
   bool runs;    // a kept and a dropped run
@@ -201,6 +205,7 @@ __device__ __forceinline__ int choose32(const b2c_route_desc& d, int rounds, con
   for (int j = 0; j < rounds;) {
     const unsigned mine = value_bits(key[0]);
     const unsigned top = __reduce_max_sync(kAll, mine);
+    if (top == 0u) break;  // (nothing left: cannot be, topk is at most what the kept runs hold)
     const int owner = __ffs(__ballot_sync(kAll, mine == top)) - 1;
     int id;
     if constexpr (kExact) id = __shfl_sync(kAll, lane * P + place_of<P>(key[0]), owner);
@@ -267,12 +272,14 @@ __device__ __noinline__ int choose64(const RouteArgs& a, const T* row, int lane,
   for (int i = 0; i < P; ++i) {
     const int e = lane * P + i;
     c[i] = e < a.d.experts ? (a.bias != nullptr ? s[i] + (double)a.bias[e] : s[i]) : -INFINITY;
+    c[i] = c[i] != c[i] ? -INFINITY : c[i];
   }
   auto part_of = [&](int e) {
     const double l = (double)logit<T>(row, e);
     double v = a.d.score == B2C_SCORE_SIGMOID ? sigmoid64(l) : (l == -INFINITY ? 0.0 : (l == (double)mx ? 1.0 : exp(l - (double)mx)));
     if (a.d.score == B2C_SCORE_SOFTMAX) v = sum > 0.0 ? v / sum : 0.0;
-    return a.bias != nullptr ? v + (double)a.bias[e] : v;
+    v = a.bias != nullptr ? v + (double)a.bias[e] : v;
+    return v != v ? -INFINITY : v;
   };
   if (a.bias == nullptr) {  // (the experts are taken by their logits, the runs by their scores)
     double x[P];
@@ -285,7 +292,7 @@ __device__ __noinline__ int choose64(const RouteArgs& a, const T* row, int lane,
 
 // The experts of lanes 0 .. count - 1 in the order of their choices in 64 bits.
 __device__ __forceinline__ int order64(double choice, int id, int count, int lane) {
-  const unsigned long long key = order_key(choice);
+  const unsigned long long key = order_key(choice != choice ? -INFINITY : choice);
   int rank = 0;
 #pragma unroll 1
   for (int j = 0; j < count; ++j) {
@@ -312,7 +319,7 @@ __device__ __forceinline__ int order64(double choice, int id, int count, int lan
 // Memory-bound on paper (one read of the logits); what it spends are the instructions of exponentials, sort and topk rounds.
 constexpr int kRouteWarps = 8;
 template <typename T, int P>
-__global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RouteArgs a, const bool vec, const bool bias_vec) {
+__global__ void __launch_bounds__(32 * kRouteWarps, P <= 8 ? 5 : 1) route_kernel(const RouteArgs a, const bool vec, const bool bias_vec) {
   pdl_wait();
   pdl_launch_dependents();
   const int E = a.d.experts, lane = threadIdx.x & 31;
@@ -389,7 +396,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RouteArgs
       float v;
       if (softmax) v = total > 0.0f && l != -INFINITY ? __fdividef(l == mx ? 1.0f : expf(l - mx), total) : 0.0f;
       else v = __fdividef(1.0f, 1.0f + __expf(-l));
-      return by_logit ? v : v + a.bias[e];
+      return finite(by_logit ? v : v + a.bias[e]);
     };
     if (!by_logit) {
       if (P >= 4 && bias_vec) {
@@ -408,6 +415,8 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RouteArgs
           if (lane * P + i < E) c[i] += a.bias[lane * P + i];
       }
     }
+#pragma unroll
+    for (int i = 0; i < P; ++i) c[i] = finite(c[i]);
     id = choose32<P, unsigned, true>(a.d, a.d.topk, c, part_of, lane, P <= 8 ? 0x1p-18f : 0x1p-16f, &near);
     if (near.runs || near.inside || near.border) {
       // a second look, one expert further, so that a border within the errors lies inside
@@ -463,6 +472,33 @@ __global__ void __launch_bounds__(kChunk) count_kernel(const int32_t* ids, const
   for (int e = threadIdx.x; e < experts; e += kChunk) counts[(size_t)blockIdx.x * experts + e] = hist[e];
 }
 
+// Many chunks: the counts of each expert become the counts of the chunks before, and the row behind them its total.  One warp an expert.
+constexpr int kScanFrom = 64;  // chunks; below, every block of place_kernel adds the counts up for itself
+__global__ void __launch_bounds__(256) scan_kernel(int32_t* counts, const int chunks, const int experts) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int e = (int)blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (e >= experts) return;
+  int run = 0;
+  for (int c0 = 0; c0 < chunks; c0 += 128) {
+    int n[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) n[i] = c0 + 32 * i + lane < chunks ? counts[(size_t)(c0 + 32 * i + lane) * experts + e] : 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      int sum = n[i];
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int up = __shfl_up_sync(kAll, sum, d);
+        if (lane >= d) sum += up;
+      }
+      if (c0 + 32 * i + lane < chunks) counts[(size_t)(c0 + 32 * i + lane) * experts + e] = run + sum - n[i];
+      run += __shfl_sync(kAll, sum, 31);
+    }
+  }
+  if (lane == 0) counts[(size_t)chunks * experts + e] = run;
+}
+
 // Places of a chunk's pairs: the experts before, the chunks before, the warps before, the lanes before.
 __global__ void __launch_bounds__(kChunk) place_kernel(const int32_t* ids, const long long pairs, const int experts, const int32_t* counts,
                                                       const int chunks, int32_t* offsets, int32_t* rows, int32_t* order) {
@@ -486,7 +522,10 @@ __global__ void __launch_bounds__(kChunk) place_kernel(const int32_t* ids, const
   const int e = threadIdx.x;
   int all = 0, before = 0;
   if (e < experts) {
-    if (counts != nullptr) {
+    if (counts != nullptr && chunks > kScanFrom) {
+      before = counts[(size_t)blockIdx.x * experts + e];
+      all = counts[(size_t)chunks * experts + e];
+    } else if (counts != nullptr) {
       for (int c = 0; c < chunks; ++c) {
         const int n = counts[(size_t)c * experts + e];
         if (c < (int)blockIdx.x) before += n;
@@ -638,7 +677,7 @@ cudaError_t launch_route(const RouteArgs& a, cudaStream_t st) {
 }
 
 size_t route_sort_workspace(long long pairs, int experts) {
-  return pairs <= kChunk ? 0 : (size_t)((pairs + kChunk - 1) / kChunk) * experts * sizeof(int32_t);
+  return pairs <= kChunk ? 0 : (size_t)((pairs + kChunk - 1) / kChunk + 1) * experts * sizeof(int32_t);
 }
 
 cudaError_t launch_route_sort(const int32_t* ids, long long pairs, int experts, int32_t* offsets, int32_t* rows, int32_t* order,
@@ -650,6 +689,8 @@ cudaError_t launch_route_sort(const int32_t* ids, long long pairs, int experts, 
   if (e != cudaSuccess) return e;
   if (chunks > 1) {
     e = launch_pdl(count_kernel, dim3((unsigned)chunks), dim3(kChunk), experts * sizeof(int), st, ids, pairs, experts, workspace);
+    if (e == cudaSuccess && chunks > kScanFrom)
+      e = launch_pdl(scan_kernel, dim3((unsigned)(experts + 7) / 8), dim3(256), 0, st, workspace, chunks, experts);
     if (e != cudaSuccess) return e;
   }
   return launch_pdl(place_kernel, dim3((unsigned)chunks), dim3(kChunk), smem, st, ids, pairs, experts,

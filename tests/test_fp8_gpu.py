@@ -162,7 +162,7 @@ def test_matmul_types(lib, rows, N, K, at, bt, yt):
 
 
 @pytest.mark.parametrize("yt", WIDE, ids=str)
-@pytest.mark.parametrize("rows,N,K", [(3, 200, 256), (40, 129, 128), (300, 520, 384)])
+@pytest.mark.parametrize("rows,N,K", [(3, 200, 256), (40, 129, 128), (300, 520, 384), (700, 300, 128)])
 def test_matmul_strides(lib, rows, N, K, yt):
     g = gen(rows)
     a, sa = whole_numbers(g, rows, K + 64, E4, 1)
@@ -173,6 +173,11 @@ def test_matmul_strides(lib, rows, N, K, yt):
         lib.fp8_matmul(a, sa, b, sb, y)
         assert torch.equal(y.double(), ref.matmul(a, sa, b, sb).to(yt).double())
         assert bool((whole[:, N:].float() == 7.0).all())
+    for first in (1, 4, 7):  # results that start off the 16-byte grid
+        whole, _ = poison(rows, N + 8, yt)
+        lib.fp8_matmul(a, sa, b, sb, whole[:, first:first + N])
+        assert torch.equal(whole[:, first:first + N].double(), ref.matmul(a, sa, b, sb).to(yt).double())
+        assert bool((whole[:, :first].float() == 7.0).all()) and bool((whole[:, first + N:].float() == 7.0).all())
 
 
 def group_sizes(kind, groups, rows, g):
@@ -271,6 +276,46 @@ def test_matmul_streams_and_graph(lib, rows):
     assert lib.fp8_status() == lib.OK
 
 
+@pytest.mark.parametrize("rows", [63, 64, 65, 127, 129, 191, 193, 256, 257, 319, 384, 385, 512, 513, 769])
+@pytest.mark.parametrize("N,K", [(128, 2048), (1000, 512), (4096, 128)])
+def test_matmul_row_counts(lib, rows, N, K):
+    """Row counts round which the kernel, its tile or the cut of the reduction change."""
+    g = gen(rows)
+    a, sa = whole_numbers(g, rows, K, E4, 1)
+    b, sb = whole_numbers(g, N, K, E4, 128)
+    _, y = poison(rows, N, torch.bfloat16)
+    lib.fp8_matmul(a, sa, b, sb, y)
+    assert torch.equal(y.double(), ref.matmul(a, sa, b, sb).bfloat16().double())
+    assert lib.fp8_status() == lib.OK
+
+
+def test_tensors_of_more_than_32_bits(lib):
+    """Offsets past 2^31 elements: the last rows of a result, of an input and of their scales."""
+    rows, N = 280000, 8192
+    g = gen(10)
+    a, sa = whole_numbers(g, rows, 128, E4, 1)
+    b, sb = whole_numbers(g, N, 128, E4, 128)
+    y = torch.zeros(rows, N, dtype=torch.bfloat16, device="cuda")
+    lib.fp8_matmul(a, sa, b, sb, y)
+    for lo in (0, 262100, rows - 300):
+        want = ref.matmul(a[lo:lo + 300], sa[lo:lo + 300], b, sb).bfloat16()
+        assert torch.equal(y[lo:lo + 300], want)
+    q, s = torch.empty(rows, N, dtype=torch.uint8, device="cuda").view(E4), torch.empty(rows, N // 128, device="cuda")
+    lib.fp8_quantize(y, q, s)
+    for lo in (0, 262100, rows - 300):
+        assert same8(q[lo:lo + 300], ref.quantize(y[lo:lo + 300], E4)[0])
+    # 16 input rows far apart, few results
+    wide = q.view(torch.uint8).view(-1)[: 16 * (1 << 27)].view(E4).view(16, 1 << 27)[:, :256]
+    sw = torch.ones(16, 2, device="cuda")
+    b2, s2 = whole_numbers(g, 100, 256, E4, 128)
+    small = torch.empty(16, 100, device="cuda")
+    lib.fp8_matmul(wide, sw, b2, s2, small)
+    want = ref.matmul(wide, sw, b2, s2)
+    bound = ref.sum_error(256) * ref.size_of_sums(wide, sw, b2, s2)
+    assert bool(((small.double() - want).abs() <= bound + 2.0 ** -24 * want.abs()).all())
+    assert lib.fp8_status() == lib.OK
+
+
 def test_matmul_repeats_bit_for_bit(lib):
     g = gen(9)
     for rows, N, K in [(1, 2048, 8192), (48, 1030, 4112), (600, 700, 2048)]:
@@ -348,6 +393,20 @@ def test_route_special_rows(lib, kind, groups):
         check_route(lib, x, 6, kind=kind, groups=groups, topk_groups=min(groups, 2), bias=b)
 
 
+@pytest.mark.parametrize("experts,groups", [(64, 1), (64, 4), (60, 3), (256, 8)])
+def test_route_special_bias(lib, experts, groups):
+    """Biases that take experts out, put them first or are NaN."""
+    x = torch.randn(40, experts, generator=gen(15), device="cuda")
+    bias = torch.randn(experts, generator=gen(16), device="cuda") * 0.1
+    bias[::3] = -math.inf
+    bias[1::5] = math.nan
+    bias[2] = math.inf
+    for kind in ("softmax", "sigmoid"):
+        check_route(lib, x, 6, kind=kind, groups=groups, topk_groups=min(groups, 2), bias=bias)
+    bias[:] = math.nan
+    check_route(lib, x, 6, kind="sigmoid", groups=groups, topk_groups=min(groups, 2), bias=bias)
+
+
 def test_route_near_scores_are_told_apart(lib):
     """Choices that differ by less than 32 bits can hold: the larger one is taken."""
     x = torch.zeros(64, 32, device="cuda")
@@ -365,7 +424,8 @@ def test_route_strided_logits(lib):
     check_route(lib, whole[::2, 7:71], 4, kind="softmax")
 
 
-@pytest.mark.parametrize("pairs,experts", [((1, 1), 1), ((1, 4), 64), ((37, 3), 7), ((256, 4), 64), ((300, 8), 256), ((5000, 2), 33), ((3000, 8), 1024)])
+@pytest.mark.parametrize("pairs,experts", [((1, 1), 1), ((1, 4), 64), ((37, 3), 7), ((256, 4), 64), ((300, 8), 256), ((5000, 2), 33), ((3000, 8), 1024),
+                                           ((16384, 4), 9), ((70001, 1), 40), ((90000, 3), 130)])
 def test_route_sort(lib, pairs, experts):
     g = gen(experts)
     ids = torch.randint(-2, experts + 2, pairs, generator=g, device="cuda").int()

@@ -57,6 +57,9 @@ def test_matmul_limits(lib):
     assert lib.b2c_fp8_matmul(ctypes.byref(d), *with_(MATMUL, offsets=P)) == NO
     d = b2c.MatmulDesc(*with_(DESC))
     assert lib.b2c_fp8_matmul(ctypes.byref(d), *with_(MATMUL, rows=1 << 31)) == NO
+    assert lib.b2c_fp8_matmul(ctypes.byref(d), *with_(MATMUL, lda=1 << 40)) == NO
+    wide = b2c.MatmulDesc(*with_(DESC, N=1 << 22, K=1 << 20))
+    assert lib.b2c_fp8_matmul(ctypes.byref(wide), *with_(MATMUL, lda=1 << 20, lds=1 << 13, ldy=1 << 22)) == NO
     assert lib.b2c_fp8_matmul(ctypes.byref(d), *with_(MATMUL, rows=0, a=None)) == b2c.OK
     assert lib.b2c_fp8_matmul(None, *with_(MATMUL)) == BAD
 
