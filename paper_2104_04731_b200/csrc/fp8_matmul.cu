@@ -248,44 +248,62 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, 2)
     // one warp takes one activation row: each lane four neighbouring columns
     const int rows = min(NT, tile.row_end - row0);
     const int n = n0 + 4 * lane;
-    for (int j = rank + split * warp; j < rows; j += split * (S::kThreads / 32)) {
-      float v[WT][4];
+    // (kTogether rows at a time: loads, exponentials and shuffles of one hide those of the others)
+    constexpr int kTogether = WT == 2 ? 4 : 2;
+    const int step = split * (S::kThreads / 32);
+    for (int j0 = rank + split * warp; j0 < rows; j0 += kTogether * step) {
+      float v[kTogether][WT][4];
 #pragma unroll
-      for (int w = 0; w < WT; ++w) {
-        const uint32_t at = smem_base + (uint32_t)(((w * NT + j) * kTileM + 4 * lane) * 4);
-        float4 part[kMaxSplit];  // (all loads first, so that their latency is waited for once)
+      for (int r = 0; r < kTogether; ++r)
 #pragma unroll
-        for (int z = 0; z < kMaxSplit; ++z)
-          if (z < split) part[z] = ld_cluster_f4(split > 1 ? map_to_rank(at, (uint32_t)z) : at);
-        v[w][0] = part[0].x;
-        v[w][1] = part[0].y;
-        v[w][2] = part[0].z;
-        v[w][3] = part[0].w;
+        for (int w = 0; w < WT; ++w) {
+          // (a row past the last one is read from the last column of sums and not stored)
+          const uint32_t at = smem_base + (uint32_t)(((w * NT + min(j0 + r * step, NT - 1)) * kTileM + 4 * lane) * 4);
+          float4 part[kMaxSplit];  // all loads first, so that their latency is waited for once
 #pragma unroll
-        for (int z = 1; z < kMaxSplit; ++z)
-          if (z < split) {
-            v[w][0] += part[z].x;
-            v[w][1] += part[z].y;
-            v[w][2] += part[z].z;
-            v[w][3] += part[z].w;
-          }
-      }
-      const long long row = row0 + j;
+          for (int z = 0; z < kMaxSplit; ++z)
+            if (z < split) part[z] = ld_cluster_f4(split > 1 ? map_to_rank(at, (uint32_t)z) : at);
+          v[r][w][0] = part[0].x;
+          v[r][w][1] = part[0].y;
+          v[r][w][2] = part[0].z;
+          v[r][w][3] = part[0].w;
+#pragma unroll
+          for (int z = 1; z < kMaxSplit; ++z)
+            if (z < split) {
+              v[r][w][0] += part[z].x;
+              v[r][w][1] += part[z].y;
+              v[r][w][2] += part[z].z;
+              v[r][w][3] += part[z].w;
+            }
+        }
       if constexpr (WT == 1) {
-        if (n < a.N) store4<YT>((YT*)a.y + row * a.ldy + n, v[0], a.N - n);
-      } else {
-        float h[4], mx = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          h[i] = silu(v[0][i]) * v[1][i];
-          mx = fmaxf(mx, fabsf(h[i]));
+        for (int r = 0; r < kTogether; ++r)
+          if (n < a.N && j0 + r * step < rows) store4<YT>((YT*)a.y + (long long)(row0 + j0 + r * step) * a.ldy + n, v[r][0], a.N - n);
+      } else {
+        float h[kTogether][4], mx[kTogether];
+#pragma unroll
+        for (int r = 0; r < kTogether; ++r) {
+          mx[r] = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            h[r][i] = silu(v[r][0][i]) * v[r][1][i];
+            mx[r] = fmaxf(mx[r], fabsf(h[r][i]));
+          }
         }
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-        const BlockScale s = block_scale<B2C_E4M3>(mx);
-        const uint32_t q = __byte_perm(quantize2<B2C_E4M3>(s, h[0], h[1]), quantize2<B2C_E4M3>(s, h[2], h[3]), 0x5410);
-        if (n < a.N) *reinterpret_cast<uint32_t*>((uint8_t*)a.y + row * a.ldy + n) = q;  // (N and ldy are multiples of 16)
-        if (lane == 0) a.y_scale[row * a.ldys + blockIdx.x] = s.scale;
+        for (int d = 16; d > 0; d >>= 1)
+#pragma unroll
+          for (int r = 0; r < kTogether; ++r) mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], d));
+#pragma unroll
+        for (int r = 0; r < kTogether; ++r) {
+          if (j0 + r * step >= rows) continue;
+          const long long row = row0 + j0 + r * step;
+          const BlockScale s = block_scale<B2C_E4M3>(mx[r]);
+          const uint32_t q = __byte_perm(quantize2<B2C_E4M3>(s, h[r][0], h[r][1]), quantize2<B2C_E4M3>(s, h[r][2], h[r][3]), 0x5410);
+          if (n < a.N) *reinterpret_cast<uint32_t*>((uint8_t*)a.y + row * a.ldy + n) = q;  // (N and ldy are multiples of 16)
+          if (lane == 0) a.y_scale[row * a.ldys + blockIdx.x] = s.scale;
+        }
       }
     }
   }

@@ -106,23 +106,65 @@ __device__ __forceinline__ PairTile pair_tile(const MatmulArgs& a, int t, int ro
   return p;
 }
 
-// 32 values of one row from column n on; `n_end`: columns of the matrix.
+// A box of results in shared memory (32 rows of 128 bytes, swizzled) to rows of any alignment; called by a whole warp.  Rows one after
+// another, neighbouring lanes neighbouring columns; 16-bit results in words where a row starts on an odd one too.
+// (Two-byte stores of a row a lane, 32 lines an instruction, made a product of 762 x 3937 x 608 take 46 us.)
 template <typename T>
-__device__ __forceinline__ void store_row32(T* p, const float* v, int n, int n_end) {
-  if (n + 32 <= n_end && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
-    if constexpr (sizeof(T) == 4) {
+__device__ __forceinline__ void store_box(T* y, long long ldy, uint32_t box, int rows, int cols, bool wide, int lane) {
+  constexpr int kPer = 16 / (int)sizeof(T);
+  if (wide) {  // rows on the 16-byte grid, but not all of them: eight lanes a row
+    const int c = lane & 7;
 #pragma unroll
-      for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-    } else {
+    for (int r0 = 0; r0 < 32; r0 += 4) {
+      const int r = r0 + (lane >> 3);
+      uint4 w;
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
+                   : "r"(box + (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)))
+                   : "memory");
+      T* dst = y + r * ldy + c * kPer;
+      if (r < rows && c * kPer + kPer <= cols) {
+        *reinterpret_cast<uint4*>(dst) = w;
+      } else if (r < rows) {
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-      for (int i = 0; i < 32; i += 8)
-        *reinterpret_cast<uint4*>(p + i) = make_uint4(pack2<T>(v[i], v[i + 1]), pack2<T>(v[i + 2], v[i + 3]), pack2<T>(v[i + 4], v[i + 5]),
-                                                      pack2<T>(v[i + 6], v[i + 7]));
+        for (int i = 0; i < kPer; ++i)
+          if (c * kPer + i < cols) {
+            if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t*>(dst)[i] = u[i];
+            else reinterpret_cast<uint16_t*>(dst)[i] = (uint16_t)(u[i >> 1] >> (16 * (i & 1)));
+          }
+      }
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (n + i < n_end) p[i] = from_float<T>(v[i]);
+    return;
+  }
+  for (int r = 0; r < rows; ++r) {
+    T* dst = y + r * ldy;
+    const uint32_t line = box + (uint32_t)(r * 128);
+    auto at = [&](int byte) { return line + (uint32_t)((((byte >> 4) ^ (r & 7)) << 4) | (byte & 15)); };
+    if constexpr (sizeof(T) == 4) {
+      uint32_t w;
+      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(at(4 * lane)) : "memory");
+      if (lane < cols) reinterpret_cast<uint32_t*>(dst)[lane] = w;
+    } else {
+      auto load = [&](int e) {
+        uint16_t h;
+        asm volatile("ld.shared.b16 %0, [%1];" : "=h"(h) : "r"(at(2 * e)) : "memory");
+        return (uint32_t)h;
+      };
+      auto one = [&](int e, uint32_t h) {
+        if (e >= 0 && e < cols) reinterpret_cast<uint16_t*>(dst)[e] = (uint16_t)h;
+      };
+      const int odd = (int)(reinterpret_cast<uintptr_t>(dst) >> 1) & 1;
+      const int e = 2 * lane - odd;  // this lane's word: elements e and e + 1
+      const uint32_t lo = load(max(e, 0)), hi = load(e + 1);
+      if (e >= 0 && e + 1 < cols) {
+        *reinterpret_cast<uint32_t*>(dst + e) = lo | (hi << 16);
+      } else {
+        one(e, lo);
+        one(e + 1, hi);
+      }
+      if (odd && lane == 31) one(63, load(63));
+    }
   }
 }
 
@@ -414,50 +456,48 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           if (half == 0) a.y_scale[m * a.ldys + p.nt] = s.scale;
         }
       } else {
-        const int n = p.nt * kTileN + half * 128;
-        if (y_boxes && p.row0 + (int)rank * kTileM + quad * 32 + 32 <= p.row_end) {
-          // All 32 rows of the warp are this group's: 128 bytes of each go to shared memory (16-byte pieces, swizzled as the tensor map
-          // says) and from there in one copy, which clips what lies past the last column and runs beside the next tile.  (Stores from
-          // registers took 3200 cycles of a tile of bf16, as long as five blocks of the reduction.)
-          constexpr int kCols = 128 / (int)sizeof(YT);
-          const uint32_t box = box_base + (uint32_t)((warp - kEpiWarp0) * kBoxBytes);
+        const int n = p.nt * kTileN + half * 128, m0 = p.row0 + (int)rank * kTileM + quad * 32;
+        // 128 bytes of each of the warp's 32 rows go to shared memory (16-byte pieces, swizzled as the tensor map says).  From there, if
+        // the copy engine can address the result and all 32 rows are this group's, in one copy, which clips what lies past the last column
+        // and runs beside the next tile (stores from registers took 3200 cycles of a tile of bf16, as long as five blocks of the
+        // reduction); else by the lanes.
+        const bool by_copy = y_boxes && m0 + 32 <= p.row_end;
+        constexpr int kCols = 128 / (int)sizeof(YT);
+        const uint32_t box = box_base + (uint32_t)((warp - kEpiWarp0) * kBoxBytes);
 #pragma unroll
-          for (int i = 0; i < 128; i += kCols) {
-            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-            __syncwarp();
+        for (int i = 0; i < 128; i += kCols) {
+          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+          __syncwarp();
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {
-              constexpr int kPer = 16 / (int)sizeof(YT);
-              float v[kPer];
+          for (int c = 0; c < 8; ++c) {
+            constexpr int kPer = 16 / (int)sizeof(YT);
+            float v[kPer];
 #pragma unroll
-              for (int j = 0; j < kPer; j += 2) unpair(acc[(i + c * kPer + j) / 2], &v[j], &v[j + 1]);
-              uint32_t w[4];
+            for (int j = 0; j < kPer; j += 2) unpair(acc[(i + c * kPer + j) / 2], &v[j], &v[j + 1]);
+            uint32_t w[4];
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                if constexpr (sizeof(YT) == 4) w[j] = __float_as_uint(v[j]);
-                else w[j] = pack2<YT>(v[2 * j], v[2 * j + 1]);
-              }
-              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + (uint32_t)(lane * 128 + ((c ^ (lane & 7)) * 16))), "r"(w[0]),
-                           "r"(w[1]), "r"(w[2]), "r"(w[3])
-                           : "memory");
+            for (int j = 0; j < 4; ++j) {
+              if constexpr (sizeof(YT) == 4) w[j] = __float_as_uint(v[j]);
+              else w[j] = pack2<YT>(v[2 * j], v[2 * j + 1]);
             }
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + (uint32_t)(lane * 128 + ((c ^ (lane & 7)) * 16))), "r"(w[0]),
+                         "r"(w[1]), "r"(w[2]), "r"(w[3])
+                         : "memory");
+          }
+          if (by_copy) {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0 && ok && n + i < a.N) {
               asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(&tmap_y),
-                           "r"((n + i) * (int)sizeof(YT)), "r"(p.row0 + (int)rank * kTileM + quad * 32), "r"(box)
+                           "r"((n + i) * (int)sizeof(YT)), "r"(m0), "r"(box)
                            : "memory");
               asm volatile("cp.async.bulk.commit_group;" ::: "memory");
             }
-          }
-        } else if (ok && m < p.row_end) {
-          YT* y = (YT*)a.y + m * a.ldy + n;
-#pragma unroll
-          for (int i = 0; i < 128; i += 32) {
-            float v[32];
-#pragma unroll
-            for (int j = 0; j < 16; ++j) unpair(acc[i / 2 + j], &v[2 * j], &v[2 * j + 1]);
-            if (n + i < a.N) store_row32<YT>(y + i, v, n + i, a.N);
+          } else {
+            __syncwarp();
+            if (ok && n + i < a.N)
+              store_box<YT>((YT*)a.y + (long long)m0 * a.ldy + n + i, a.ldy, box, min(32, p.row_end - m0), min(kCols, a.N - n - i), y_boxes, lane);
+            __syncwarp();
           }
         }
       }

@@ -9,29 +9,37 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kLanes = kBlock / 16;  // lanes that share a row of a block, 16 elements each
 
-struct Vec {
-  bool x, q;  // 16-byte loads of x, 16-byte stores of q
+// A lane's 16 elements of the 128 of a block: neighbours, moved by 16-byte loads and stores, where x and q lie on that grid; else every
+// eighth one, so that the eight lanes of a block move neighbouring elements (16 neighbours a lane, one by one, made 11353 x 1183 bf16
+// take 57 us).
+template <bool WIDE>
+struct Part {
+  static constexpr bool wide = WIDE;
+  __device__ __forceinline__ int at(int sub, int i) const { return WIDE ? sub * 16 + i : i * kLanes + sub; }
 };
 
-template <typename T>
-__device__ __forceinline__ void load_part(const QuantizeArgs& a, bool vec, long long row, int c0, float* v) {
-  const T* p = (const T*)a.x + row * a.ldx + c0;
-  if (vec && c0 + 16 <= a.cols) {
-    widen16<T>(load_raw16<T>(p), v);
-  } else {
+template <typename T, bool WIDE>
+__device__ __forceinline__ void load_part(const QuantizeArgs& a, Part<WIDE> part, long long row, int blk, int sub, float* v) {
+  const T* p = (const T*)a.x + row * a.ldx + blk * kBlock;
+  const int left = a.cols - blk * kBlock;
+  if (part.wide && sub * 16 + 16 <= left) {
+    widen16<T>(load_raw16<T>(p + sub * 16), v);
+  } else if (!part.wide || sub * 16 < left) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = c0 + i < a.cols ? to_float<T>(p[i]) : 0.0f;
+    for (int i = 0; i < 16; ++i) v[i] = part.at(sub, i) < left ? to_float<T>(p[part.at(sub, i)]) : 0.0f;
   }
 }
-__device__ __forceinline__ void store_part(const QuantizeArgs& a, bool vec, long long row, int c0, const uint4& w) {
-  uint8_t* p = a.q + row * a.ldq + c0;
-  if (vec && c0 + 16 <= a.cols) {
-    *reinterpret_cast<uint4*>(p) = w;
-  } else {
+template <bool WIDE>
+__device__ __forceinline__ void store_part(const QuantizeArgs& a, Part<WIDE> part, long long row, int blk, int sub, const uint4& w) {
+  uint8_t* p = a.q + row * a.ldq + blk * kBlock;
+  const int left = a.cols - blk * kBlock;
+  if (part.wide && sub * 16 + 16 <= left) {
+    *reinterpret_cast<uint4*>(p + sub * 16) = w;
+  } else if (!part.wide || sub * 16 < left) {
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-      if (c0 + i < a.cols) p[i] = (uint8_t)(u[i >> 2] >> (8 * (i & 3)));
+      if (part.at(sub, i) < left) p[part.at(sub, i)] = (uint8_t)(u[i >> 2] >> (8 * (i & 3)));
   }
 }
 __device__ __forceinline__ float amax16(const float* v) {
@@ -41,14 +49,14 @@ __device__ __forceinline__ float amax16(const float* v) {
   return m;
 }
 
-// Where the 128 elements of a block come from and go to; the eight lanes of a block share it.
-__device__ __forceinline__ void store_block(const QuantizeArgs& a, bool vec, long long row, int blk, int part, const BlockScale& s, const uint4& w) {
-  const int c0 = blk * kBlock + part;
+// The 16 values of a lane to the row, or the rows, of its block.
+template <bool WIDE>
+__device__ __forceinline__ void store_block(const QuantizeArgs& a, Part<WIDE> part, long long row, int blk, int sub, const BlockScale& s, const uint4& w) {
   for (int j = 0; j < (a.map == nullptr ? 1 : a.copies); ++j) {
     const long long to = a.map == nullptr ? row : (long long)a.map[row * a.copies + j];
     if (to < 0) continue;
-    if (c0 < a.cols) store_part(a, vec, to, c0, w);
-    if (part == 0) a.scale[to * a.lds + blk] = s.scale;
+    store_part(a, part, to, blk, sub, w);
+    if (sub == 0) a.scale[to * a.lds + blk] = s.scale;
   }
 }
 __device__ __forceinline__ float block_max(float m) {
@@ -57,24 +65,24 @@ __device__ __forceinline__ float block_max(float m) {
   return m;
 }
 
-// Eight lanes hold the 128 elements of a block, 16 each: 16-byte loads and stores, three shuffles for the maximum.
-template <typename T, int QT>
-__global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const QuantizeArgs a, const Vec vec, const int nb, const long long blocks) {
+// Eight lanes hold the 128 elements of a block, three shuffles give the maximum.
+template <typename T, int QT, bool WIDE>
+__global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const QuantizeArgs a, const int nb, const long long blocks) {
+  constexpr Part<WIDE> part;
   pdl_wait();
   pdl_launch_dependents();
   const long long id = (long long)blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;
   const bool on = id < blocks;
   const long long row = on ? id / nb : 0;
-  const int blk = on ? (int)(id - row * nb) : 0;
-  const int part = (threadIdx.x % kLanes) * 16;
+  const int blk = on ? (int)(id - row * nb) : 0, sub = threadIdx.x % kLanes;
   float v[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) v[i] = 0.0f;
-  if (on && blk * kBlock + part < a.cols) load_part<T>(a, vec.x, row, blk * kBlock + part, v);
+  if (on) load_part<T>(a, part, row, blk, sub, v);
   const float m = block_max(amax16(v));
   if (!on) return;
   const BlockScale s = block_scale<QT>(m);
-  store_block(a, vec.q, row, blk, part, s, quantize16<QT>(s, v));
+  store_block(a, part, row, blk, sub, s, quantize16<QT>(s, v));
 }
 
 // The same for many blocks of aligned rows.  What bounds it there are instructions, not bytes (16384 x 8192 bf16 took 82 us with
@@ -131,14 +139,14 @@ __global__ void __launch_bounds__(kThreads) quantize_many_rows_kernel(const Quan
 }
 
 // One thread block holds a 128 x 128 block in registers: four rows of 16 elements a thread.
-template <typename T, int QT>
-__global__ void __launch_bounds__(kThreads) quantize_blocks_kernel(const QuantizeArgs a, const Vec vec, const int nb) {
-  __shared__ float part[kThreads / 32];
+template <typename T, int QT, bool WIDE>
+__global__ void __launch_bounds__(kThreads, 3) quantize_blocks_kernel(const QuantizeArgs a, const int nb) {
+  constexpr Part<WIDE> part;
+  __shared__ float part_max[kThreads / 32];
   pdl_wait();
   pdl_launch_dependents();
   const long long rb = blockIdx.x / nb;
-  const int blk = (int)(blockIdx.x - rb * nb);
-  const int c0 = blk * kBlock + (threadIdx.x % kLanes) * 16;
+  const int blk = (int)(blockIdx.x - rb * nb), sub = threadIdx.x % kLanes;
   const long long row0 = rb * kBlock + threadIdx.x / kLanes;
   constexpr int kStep = kThreads / kLanes, kRows = kBlock / kStep;
   float v[kRows][16];
@@ -147,20 +155,20 @@ __global__ void __launch_bounds__(kThreads) quantize_blocks_kernel(const Quantiz
   for (int r = 0; r < kRows; ++r) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[r][i] = 0.0f;
-    if (row0 + r * kStep < a.rows && c0 < a.cols) load_part<T>(a, vec.x, row0 + r * kStep, c0, v[r]);
+    if (row0 + r * kStep < a.rows) load_part<T>(a, part, row0 + r * kStep, blk, sub, v[r]);
   }
 #pragma unroll
   for (int r = 0; r < kRows; ++r) m = fmaxf(m, amax16(v[r]));
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-  if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = m;
+  if (threadIdx.x % 32 == 0) part_max[threadIdx.x / 32] = m;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kThreads / 32; ++i) m = fmaxf(m, part[i]);
+  for (int i = 0; i < kThreads / 32; ++i) m = fmaxf(m, part_max[i]);
   const BlockScale s = block_scale<QT>(m);
 #pragma unroll
   for (int r = 0; r < kRows; ++r)
-    if (row0 + r * kStep < a.rows && c0 < a.cols) store_part(a, vec.q, row0 + r * kStep, c0, quantize16<QT>(s, v[r]));
+    if (row0 + r * kStep < a.rows) store_part(a, part, row0 + r * kStep, blk, sub, quantize16<QT>(s, v[r]));
   if (threadIdx.x == 0) a.scale[rb * a.lds + blk] = s.scale;
 }
 
@@ -168,21 +176,22 @@ __global__ void __launch_bounds__(kThreads) quantize_blocks_kernel(const Quantiz
 // pairs for itself (at most kSmallPairs, in shared memory), because a launch of its own for the sort costs more than sorting
 // everywhere.  Same order as the sort on its own: by expert, then by pair.
 constexpr int kWarps = kThreads / 32;
-template <typename T>
-__global__ void __launch_bounds__(kThreads) sort_quantize_kernel(const QuantizeArgs a, const Vec vec, const int nb, const int32_t* ids,
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(kThreads) sort_quantize_kernel(const QuantizeArgs a, const int nb, const int32_t* ids,
                                                                  const int pairs, const int experts, int32_t* offsets, int32_t* rows) {
   extern __shared__ int count[];  // [kWarps][experts], then [experts]: first place of every expert
   __shared__ int place_s[kMaxTopk], warp_sum_s[kWarps];
+  constexpr Part<WIDE> part;
   int* base = count + kWarps * experts;
   const int t = blockIdx.x, topk = a.copies, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int part = (threadIdx.x % kLanes) * 16, group = threadIdx.x / kLanes;
+  const int sub = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
   for (int i = threadIdx.x; i < kWarps * experts; i += kThreads) count[i] = 0;
   pdl_wait();
   pdl_launch_dependents();
   float v[16];  // the first block travels while the pairs are sorted
 #pragma unroll
   for (int i = 0; i < 16; ++i) v[i] = 0.0f;
-  if (group < nb && group * kBlock + part < a.cols) load_part<T>(a, vec.x, t, group * kBlock + part, v);
+  if (group < nb) load_part<T>(a, part, t, group, sub, v);
   __syncthreads();
   // each warp counts a run of the pairs; a pair's place in it is the count of its expert so far
   const int steps = (pairs + kThreads - 1) / kThreads;
@@ -241,11 +250,10 @@ __global__ void __launch_bounds__(kThreads) sort_quantize_kernel(const QuantizeA
   }
   __syncthreads();
   for (int blk = group; blk < (nb + kThreads / kLanes - 1) / (kThreads / kLanes) * (kThreads / kLanes); blk += kThreads / kLanes) {
-    const int c0 = blk * kBlock + part;
     if (blk != group) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) v[i] = 0.0f;
-      if (blk < nb && c0 < a.cols) load_part<T>(a, vec.x, t, c0, v);
+      if (blk < nb) load_part<T>(a, part, t, blk, sub, v);
     }
     const BlockScale s = block_scale<B2C_E4M3>(block_max(amax16(v)));
     if (blk >= nb) continue;
@@ -253,38 +261,40 @@ __global__ void __launch_bounds__(kThreads) sort_quantize_kernel(const QuantizeA
     for (int j = 0; j < topk; ++j) {
       const int to = place_s[j];
       if (to < 0) continue;
-      if (c0 < a.cols) store_part(a, vec.q, to, c0, w);
-      if (part == 0) a.scale[(long long)to * a.lds + blk] = s.scale;
+      store_part(a, part, to, blk, sub, w);
+      if (sub == 0) a.scale[(long long)to * a.lds + blk] = s.scale;
     }
   }
+}
+
+// Whether rows of x and of q lie on 16-byte boundaries.
+template <typename T>
+bool is_wide(const QuantizeArgs& a) {
+  return (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && (a.ldx * sizeof(T)) % 16 == 0 && (reinterpret_cast<uintptr_t>(a.q) & 15) == 0 &&
+         a.ldq % 16 == 0;
 }
 
 template <typename T, int QT>
 cudaError_t launch(const QuantizeArgs& a, cudaStream_t st) {
   const int nb = (int)blocks_of(a.cols);
-  Vec vec;
-  vec.x = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && (a.ldx * sizeof(T)) % 16 == 0;
-  vec.q = (reinterpret_cast<uintptr_t>(a.q) & 15) == 0 && a.ldq % 16 == 0;
+  const bool wide = is_wide<T>(a);
   if (a.block_rows == 1) {
     const long long blocks = a.rows * nb;
     const long long grid = (blocks + kThreads / kLanes - 1) / (kThreads / kLanes);
-    if (vec.x && vec.q && a.cols % 16 == 0 && grid >= 8 * kNumSMs && blocks < (1ll << 30))  // (each SM's 2048 threads have work twice)
+    if (wide && a.cols % 16 == 0 && grid >= 8 * kNumSMs && blocks < (1ll << 30))  // (each SM's 2048 threads have work twice)
       return launch_pdl(quantize_many_rows_kernel<T, QT>, dim3(4 * kNumSMs), dim3(kThreads), 0, st, a, make_fastdiv((uint32_t)nb), (unsigned)blocks);
     if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
-    return launch_pdl(quantize_rows_kernel<T, QT>, dim3((unsigned)grid), dim3(kThreads), 0, st, a, vec, nb, blocks);
+    return launch_pdl(wide ? quantize_rows_kernel<T, QT, true> : quantize_rows_kernel<T, QT, false>, dim3((unsigned)grid), dim3(kThreads), 0, st, a, nb, blocks);
   }
   const long long grid = blocks_of(a.rows) * nb;
   if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
-  return launch_pdl(quantize_blocks_kernel<T, QT>, dim3((unsigned)grid), dim3(kThreads), 0, st, a, vec, nb);
+  return launch_pdl(wide ? quantize_blocks_kernel<T, QT, true> : quantize_blocks_kernel<T, QT, false>, dim3((unsigned)grid), dim3(kThreads), 0, st, a, nb);
 }
 
 template <typename T>
 cudaError_t launch_sort(const QuantizeArgs& a, const int32_t* ids, int pairs, int experts, int32_t* offsets, int32_t* rows, cudaStream_t st) {
-  Vec vec;
-  vec.x = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && (a.ldx * sizeof(T)) % 16 == 0;
-  vec.q = true;  // (the workspace's rows: multiples of 16 bytes)
-  return launch_pdl(sort_quantize_kernel<T>, dim3((unsigned)a.rows), dim3(kThreads), (size_t)(kWarps + 1) * experts * sizeof(int), st, a, vec,
-                    (int)blocks_of(a.cols), ids, pairs, experts, offsets, rows);
+  return launch_pdl(is_wide<T>(a) ? sort_quantize_kernel<T, true> : sort_quantize_kernel<T, false>, dim3((unsigned)a.rows), dim3(kThreads),
+                    (size_t)(kWarps + 1) * experts * sizeof(int), st, a, (int)blocks_of(a.cols), ids, pairs, experts, offsets, rows);
 }
 
 }  // namespace

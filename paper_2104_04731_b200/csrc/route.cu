@@ -1,5 +1,7 @@
 // Routing of tokens to experts: scores, groups and the best experts of each token; the stable sort of the
 // (token, slot) pairs by expert; the weighted sum of the experts' results.
+#include <type_traits>
+
 #include "fp8_common.cuh"
 
 namespace b2c {
@@ -145,9 +147,12 @@ struct Near {
 };
 
 // choose_exact() for 32-bit choices: every lane sorts its own once, a round compares the lanes' first ones.  Lane j < rounds gets the
-// j-th expert.  With CHECK the choices may be off by half of `unit` * (1 + |choice|), and *near tells what that leaves open.
-template <int P, typename K, bool CHECK, typename F>
-__device__ __forceinline__ int choose32(const b2c_route_desc& d, int rounds, const float (&choice)[P], F part_of, int lane, float unit, Near* near) {
+// j-th expert.  With CHECK the choices may be off by half of `unit` * (1 + |choice|), and *near tells what that leaves open.  With PARTS
+// the runs are scored by other values than the experts (positive ones, off by less than a quarter of `unit` of themselves).  32-bit
+// keys without CHECK are for values whose lowest bits are zero (16-bit logits): the place fits into them.
+template <int P, typename K, bool CHECK, bool PARTS, typename F>
+__device__ __forceinline__ int choose32(const b2c_route_desc& d, int rounds, const float (&choice)[P], const float (&part)[P], F part_of, int lane,
+                                        float unit, Near* near) {
   constexpr bool kExact = sizeof(K) == 8;
   K key[P];
 #pragma unroll
@@ -170,8 +175,17 @@ __device__ __forceinline__ int choose32(const b2c_route_desc& d, int rounds, con
       first = fmaxf(first, a);
     };
     if (!by_expert) {
-      const float f0 = key_value(value_bits(key[0])), s0 = P > 1 ? key_value(value_bits(key[P > 1 ? 1 : 0])) : -INFINITY;
-      add(f0, s0);
+      float f0, s0;
+      if constexpr (PARTS) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) add(part[i], -INFINITY);
+        f0 = first;
+        s0 = second;
+      } else {
+        f0 = key_value(value_bits(key[0]));
+        s0 = P > 1 ? key_value(value_bits(key[P > 1 ? 1 : 0])) : -INFINITY;
+        add(f0, s0);
+      }
       int from = lane;
       for (int j = 1; j < lanes; ++j) {
         from = from + 1 == (run + 1) * lanes ? run * lanes : from + 1;
@@ -189,10 +203,10 @@ __device__ __forceinline__ int choose32(const b2c_route_desc& d, int rounds, con
       better += k > mine || (k == mine && g < run);
     }
     const bool kept = run < d.groups && better < d.topk_groups;
-    if constexpr (CHECK) {
+    if constexpr (CHECK || PARTS) {
       const float low = key_value(__reduce_min_sync(kAll, kept ? mine : 0xFFFFFFFFu));
       const unsigned high = __reduce_max_sync(kAll, kept ? 0u : mine);
-      near->runs = high != 0u && !(low - key_value(high) > 2.0f * unit * (1.0f + fabsf(low)));
+      near->runs = high != 0u && !(low - key_value(high) > (PARTS ? unit * fabsf(low) : 2.0f * unit * (1.0f + fabsf(low))));
     }
     open = __ballot_sync(kAll, kept);
     if (!by_expert && !kept) {
@@ -203,12 +217,13 @@ __device__ __forceinline__ int choose32(const b2c_route_desc& d, int rounds, con
   int my_id = 0;
   float my_value = 0.0f;
   for (int j = 0; j < rounds;) {
-    const unsigned mine = value_bits(key[0]);
+    // (exact 32-bit keys: the place is not part of the value, or equal values would not go to the lowest lane)
+    const unsigned mine = kExact || CHECK ? value_bits(key[0]) : value_bits(key[0]) & ~(unsigned)(P - 1);
     const unsigned top = __reduce_max_sync(kAll, mine);
     if (top == 0u) break;  // (nothing left: cannot be, topk is at most what the kept runs hold)
     const int owner = __ffs(__ballot_sync(kAll, mine == top)) - 1;
     int id;
-    if constexpr (kExact) id = __shfl_sync(kAll, lane * P + place_of<P>(key[0]), owner);
+    if constexpr (kExact || !CHECK) id = __shfl_sync(kAll, lane * P + place_of<P>(key[0]), owner);
     else id = owner * P + place_of<P>(top);
     if (lane == owner) {
 #pragma unroll
@@ -368,6 +383,8 @@ __global__ void __launch_bounds__(32 * kRouteWarps, P <= 8 ? 5 : 1) route_kernel
   }
   int id;
   Near near;
+  // logits of 16 bits leave the lowest 13 of a float free; lanes of up to 32 experts need five
+  using LogitKey = typename std::conditional<sizeof(T) == 2, unsigned, unsigned long long>::type;
   if (by_logit && !sums) {
     if (softmax && !a.d.renormalise) {
       float sum = 0.0f;
@@ -375,7 +392,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps, P <= 8 ? 5 : 1) route_kernel
       for (int i = 0; i < P; ++i) sum += x[i] == -INFINITY ? 0.0f : (x[i] == mx ? 1.0f : expf(x[i] - mx));
       all = warp_sum((double)sum);
     }
-    id = choose32<P, unsigned long long, false>(a.d, a.d.topk, x, [&](int e) { return logit<T>(row, e); }, lane, 0.0f, &near);
+    id = choose32<P, LogitKey, false, false>(a.d, a.d.topk, x, x, [&](int e) { return logit<T>(row, e); }, lane, 0.0f, &near);
   } else {
     float c[P];
     float sum = 0.0f;
@@ -415,15 +432,24 @@ __global__ void __launch_bounds__(32 * kRouteWarps, P <= 8 ? 5 : 1) route_kernel
           if (lane * P + i < E) c[i] += a.bias[lane * P + i];
       }
     }
+    if (by_logit) {
+      // the runs by sums of scores, the experts by their logits, which is exact
 #pragma unroll
-    for (int i = 0; i < P; ++i) c[i] = finite(c[i]);
-    id = choose32<P, unsigned, true>(a.d, a.d.topk, c, part_of, lane, P <= 8 ? 0x1p-18f : 0x1p-16f, &near);
-    if (near.runs || near.inside || near.border) {
-      // a second look, one expert further, so that a border within the errors lies inside
-      const int rounds = min(min(a.d.topk + 1, 32), E / a.d.groups * a.d.topk_groups);
-      id = choose32<P, unsigned long long, true>(a.d, rounds, c, part_of, lane, 0x1p-20f, &near);
-      if (near.runs || near.border || ((softmax || by_logit) && near.inside)) id = choose64<T, P>(a, row, lane, mx);
-      else if (near.inside) id = order64(sigmoid64((double)logit<T>(row, lane < rounds ? id : 0)) + (double)a.bias[lane < rounds ? id : 0], id, rounds, lane);
+      for (int i = 0; i < P; ++i)
+        if (lane * P + i >= E) c[i] = -INFINITY;
+      id = choose32<P, LogitKey, false, true>(a.d, a.d.topk, x, c, part_of, lane, 0x1p-18f, &near);
+      if (near.runs) id = choose64<T, P>(a, row, lane, mx);
+    } else {
+#pragma unroll
+      for (int i = 0; i < P; ++i) c[i] = finite(c[i]);
+      id = choose32<P, unsigned, true, false>(a.d, a.d.topk, c, c, part_of, lane, P <= 8 ? 0x1p-18f : 0x1p-16f, &near);
+      if (near.runs || near.inside || near.border) {
+        // a second look, one expert further, so that a border within the errors lies inside
+        const int rounds = min(min(a.d.topk + 1, 32), E / a.d.groups * a.d.topk_groups);
+        id = choose32<P, unsigned long long, true, false>(a.d, rounds, c, c, part_of, lane, 0x1p-20f, &near);
+        if (near.runs || near.border || (softmax && near.inside)) id = choose64<T, P>(a, row, lane, mx);
+        else if (near.inside) id = order64(sigmoid64((double)logit<T>(row, lane < rounds ? id : 0)) + (double)a.bias[lane < rounds ? id : 0], id, rounds, lane);
+      }
     }
   }
   // the weights of the chosen, from their logits; the argument of the exponential without the rounding of its difference
