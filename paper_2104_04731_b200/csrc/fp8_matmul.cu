@@ -28,7 +28,11 @@ struct RowsShape {
   // two thread blocks share an SM: half of the shared memory (228 KB, 1 KB of it kept for each block; `factor` and the
   // barriers are static) and of the 512 columns of tensor memory each
   static constexpr int kFactorBytes = 2 * kScaleRun * kCols * 4;
-  static constexpr int kRing = 113 * 1024 - 1024 - 1024 - kFactorBytes;
+  // (where that is fewer than three stages a block has an SM to itself: two of 40 KB cost the latency of a copy, 0.95 us, for a block
+  // of the reduction)
+  static constexpr int kHalf = 113 * 1024 - 1024 - 1024 - kFactorBytes, kWhole = 227 * 1024 - 1024 - 1024 - kFactorBytes;
+  static constexpr int kPerSm = kHalf / kStageBytes >= 3 ? 2 : 1;
+  static constexpr int kRing = kPerSm == 2 ? kHalf : kWhole;
   static constexpr int kStages = kRing / kStageBytes < 8 ? kRing / kStageBytes : 8;
   static constexpr int kBufs = kCols <= 64 ? 4 : 2;
   static constexpr int kTmemCols = kCols * kBufs < 32 ? 32 : kCols * kBufs;
@@ -54,9 +58,10 @@ __device__ __forceinline__ void store4<float>(float* p, const float* v, int n) {
 }
 
 template <int NT, int WT, typename YT>
-__global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, 2)
+__global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, RowsShape<NT, WT>::kPerSm)
     matmul_rows_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const MatmulArgs a,
                        const int kb_per_split, const bool early) {
+  constexpr int stages = RowsShape<NT, WT>::kStages;
   using S = RowsShape<NT, WT>;
   extern __shared__ uint8_t smem_raw[];
   __shared__ SharedCtl ctl;
@@ -69,7 +74,7 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, 2)
   const int split = (int)gridDim.z, rank = (int)blockIdx.z;  // (a cluster is the blocks of one z run)
 
   if (warp == 0) {
-    if (lane < S::kStages) {
+    if (lane < stages) {
       mbar_init(smem_u32(&ctl.full[lane]), 1);
       mbar_init(smem_u32(&ctl.empty[lane]), 1);
     }
@@ -117,17 +122,17 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, 2)
     auto load_x = [&](int kb, int s) {
       tma_load_2d(smem_base + s * S::kStageBytes + WT * kTileM * kBlock, &tmap_x, kb * kBlock, row0, smem_u32(&ctl.full[s]), leader);
     };
-    const int ahead = early ? min(S::kStages, kb1 - kb0) : 0;
+    const int ahead = early ? min(stages, kb1 - kb0) : 0;
     for (int i = 0; i < ahead; ++i) load_w(kb0 + i, i);
     if (early) pdl_wait();
     for (int i = 0; i < ahead; ++i) load_x(kb0 + i, i);
-    int s = ahead % S::kStages;
-    uint32_t ph = ahead == S::kStages ? 1u : 0u;
+    int s = ahead % stages;
+    uint32_t ph = ahead == stages ? 1u : 0u;
     for (int kb = kb0 + ahead; kb < kb1; ++kb) {
       if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.empty[s]), ph ^ 1u, &ctl, &g_fp8_status))) break;
       load_w(kb, s);
       load_x(kb, s);
-      if (++s == S::kStages) {
+      if (++s == stages) {
         s = 0;
         ph ^= 1u;
       }
@@ -151,7 +156,7 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, 2)
         mma_f8_block<1>(tmem_acc + buf * S::kCols + w * NT, make_smem_desc(base + w * kTileM * kBlock, kBlock), xdesc, idesc, leader, ksteps);
       mma_commit(smem_u32(&ctl.empty[s]), leader);
       mma_commit(smem_u32(&ctl.tmem_full[buf]), leader);
-      if (++s == S::kStages) {
+      if (++s == stages) {
         s = 0;
         ph ^= 1u;
       }
@@ -248,62 +253,45 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, 2)
     // one warp takes one activation row: each lane four neighbouring columns
     const int rows = min(NT, tile.row_end - row0);
     const int n = n0 + 4 * lane;
-    // (kTogether rows at a time: loads, exponentials and shuffles of one hide those of the others)
-    constexpr int kTogether = WT == 2 ? 4 : 2;
-    const int step = split * (S::kThreads / 32);
-    for (int j0 = rank + split * warp; j0 < rows; j0 += kTogether * step) {
-      float v[kTogether][WT][4];
+    // (Code that runs once or twice is paid for when it is fetched, not when it runs: with four rows unrolled side by side this part
+    // took 5 us of a launch of 44 rows.)
+#pragma unroll 1
+    for (int j = rank + split * warp; j < rows; j += split * (S::kThreads / 32)) {
+      float4 v[WT];
 #pragma unroll
-      for (int r = 0; r < kTogether; ++r)
-#pragma unroll
-        for (int w = 0; w < WT; ++w) {
-          // (a row past the last one is read from the last column of sums and not stored)
-          const uint32_t at = smem_base + (uint32_t)(((w * NT + min(j0 + r * step, NT - 1)) * kTileM + 4 * lane) * 4);
-          float4 part[kMaxSplit];  // all loads first, so that their latency is waited for once
-#pragma unroll
-          for (int z = 0; z < kMaxSplit; ++z)
-            if (z < split) part[z] = ld_cluster_f4(split > 1 ? map_to_rank(at, (uint32_t)z) : at);
-          v[r][w][0] = part[0].x;
-          v[r][w][1] = part[0].y;
-          v[r][w][2] = part[0].z;
-          v[r][w][3] = part[0].w;
-#pragma unroll
-          for (int z = 1; z < kMaxSplit; ++z)
-            if (z < split) {
-              v[r][w][0] += part[z].x;
-              v[r][w][1] += part[z].y;
-              v[r][w][2] += part[z].z;
-              v[r][w][3] += part[z].w;
-            }
+      for (int w = 0; w < WT; ++w) {
+        const uint32_t at = smem_base + (uint32_t)(((w * NT + j) * kTileM + 4 * lane) * 4);
+        if (split == 1) {
+          v[w] = ld_shared_f4(at);
+          continue;
         }
-      if constexpr (WT == 1) {
+        float4 part[kMaxSplit];  // (all loads first, so that their latency is waited for once)
 #pragma unroll
-        for (int r = 0; r < kTogether; ++r)
-          if (n < a.N && j0 + r * step < rows) store4<YT>((YT*)a.y + (long long)(row0 + j0 + r * step) * a.ldy + n, v[r][0], a.N - n);
-      } else {
-        float h[kTogether][4], mx[kTogether];
+        for (int z = 0; z < kMaxSplit; ++z)
+          if (z < split) part[z] = ld_cluster_f4(map_to_rank(at, (uint32_t)z));
+        v[w] = part[0];
 #pragma unroll
-        for (int r = 0; r < kTogether; ++r) {
-          mx[r] = 0.0f;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            h[r][i] = silu(v[r][0][i]) * v[r][1][i];
-            mx[r] = fmaxf(mx[r], fabsf(h[r][i]));
+        for (int z = 1; z < kMaxSplit; ++z)
+          if (z < split) {
+            v[w].x += part[z].x;
+            v[w].y += part[z].y;
+            v[w].z += part[z].z;
+            v[w].w += part[z].w;
           }
-        }
+      }
+      const long long row = row0 + j;
+      if constexpr (WT == 1) {
+        const float out[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+        if (n < a.N) store4<YT>((YT*)a.y + row * a.ldy + n, out, a.N - n);
+      } else {
+        const float h[4] = {silu(v[0].x) * v[1].x, silu(v[0].y) * v[1].y, silu(v[0].z) * v[1].z, silu(v[0].w) * v[1].w};
+        float mx = fmaxf(fmaxf(fabsf(h[0]), fabsf(h[1])), fmaxf(fabsf(h[2]), fabsf(h[3])));
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1)
-#pragma unroll
-          for (int r = 0; r < kTogether; ++r) mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], d));
-#pragma unroll
-        for (int r = 0; r < kTogether; ++r) {
-          if (j0 + r * step >= rows) continue;
-          const long long row = row0 + j0 + r * step;
-          const BlockScale s = block_scale<B2C_E4M3>(mx[r]);
-          const uint32_t q = __byte_perm(quantize2<B2C_E4M3>(s, h[r][0], h[r][1]), quantize2<B2C_E4M3>(s, h[r][2], h[r][3]), 0x5410);
-          if (n < a.N) *reinterpret_cast<uint32_t*>((uint8_t*)a.y + row * a.ldy + n) = q;  // (N and ldy are multiples of 16)
-          if (lane == 0) a.y_scale[row * a.ldys + blockIdx.x] = s.scale;
-        }
+        for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+        const BlockScale s = block_scale<B2C_E4M3>(mx);
+        const uint32_t q = __byte_perm(quantize2<B2C_E4M3>(s, h[0], h[1]), quantize2<B2C_E4M3>(s, h[2], h[3]), 0x5410);
+        if (n < a.N) *reinterpret_cast<uint32_t*>((uint8_t*)a.y + row * a.ldy + n) = q;  // (N and ldy are multiples of 16)
+        if (lane == 0) a.y_scale[row * a.ldys + blockIdx.x] = s.scale;
       }
     }
   }
