@@ -73,6 +73,7 @@ cudaError_t launch_sort_quantize(const QuantizeArgs& a, const int32_t* ids, int 
                                  cudaStream_t st);
 int launch_fp8_matmul(const MatmulArgs& a, cudaStream_t st);  // B2C_* code
 int launch_fp8_matmul_pair(const MatmulArgs& a, cudaStream_t st);  // its form for many rows
+long long pair_cycles(const MatmulArgs& a);  // what it takes without groups, in SM cycles
 cudaError_t fp8_pair_status(int* status);
 int fp8_status_read_and_clear(int32_t* status);
 cudaError_t launch_route(const RouteArgs& a, cudaStream_t st);

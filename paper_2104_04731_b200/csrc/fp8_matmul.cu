@@ -360,16 +360,16 @@ int launch_rows_type(const MatmulArgs& a, cudaStream_t st) {
 }
 
 // Whether one product of 65 rows or more is better formed by tiles of 128 weight rows x 64 rows, one on each of up to 148 SMs, than by
-// the pair kernel's 256 x 256 on 74 pairs.  In cycles: 770 for a block of the reduction and 4600 besides here (as long as every tile has
-// an SM of its own; two on one take two and a half times as long), 850 and 4000 for a wave there.  Measured, us here / there:
+// the pair kernel's tiles on 74 pairs.  In cycles: 770 for a block of the reduction and 4600 besides here, as long as every tile has
+// an SM of its own (two on one take two and a half times as long); from 385 rows on the weights, fetched once for every 64 rows, are
+// what counts.  Measured, us here / there (tiles of 256 columns):
 //   4096 x 4096: 128 rows 11.3 / 18.8, 256 rows 15.5 / 18.9, 320 rows 39 / 19.0;   8192 x 2048: 128 rows 10.2 / 12.6, 200 rows 13.7 / 12.7;
-//   2048 x 7168: 256 rows 15.0 / 27.5, 384 rows 24.5 / 27.5, 512 rows 37.6 / 27.6 (the weights are fetched once for every 64 rows).
+//   2048 x 7168: 256 rows 15.0 / 27.5, 384 rows 24.5 / 27.5, 512 rows 37.6 / 27.6.
 bool rows_kernel_is_better(const MatmulArgs& a) {
   const long long kb_all = blocks_of(a.K), tiles = blocks_of(a.N) * ((a.rows + 63) / 64);
   const int split = choose_split(tiles, (int)kb_all, true);
   if (a.rows > 384 || tiles * split > kNumSMs) return false;
-  const long long waves = (((a.N + 255) / 256) * (long long)((a.rows + 255) / 256) + kNumSMs / 2 - 1) / (kNumSMs / 2);
-  return 770 * ((kb_all + split - 1) / split) + 4600 + (split > 1 ? 2000 : 0) < waves * (850 * kb_all + 4000);
+  return 770 * ((kb_all + split - 1) / split) + 4600 + (split > 1 ? 2000 : 0) < pair_cycles(a);
 }
 
 }  // namespace

@@ -28,16 +28,19 @@ constexpr int kPairThreads = 32 * (kEpiWarp0 + kEpiWarps);
 // Registers: 384 threads are launched with 168 each (a quarter of the SM's 65536 holds three warps).  The sums alone are 128 of a
 // thread, and 64 values on their way from tensor memory beside them hide its latency: 128 * 88 + 256 * 208 = 384 * 168.
 constexpr int kRegsSums = 208, kRegsRest = 88;
-constexpr int kTileN = 256;
 constexpr int kABytes = kTileM * kBlock;
 constexpr int kBoxBytes = 32 * 128;  // results of a warp on their way out: 32 rows of 128 bytes
-// CTAS thread blocks share a tile of CTAS * 128 rows (see the head of this file).
-template <int CTAS>
+// CTAS thread blocks share a tile of CTAS * 128 rows and TN columns (see the head of this file).
+template <int CTAS, int TN>
 struct TileShape {
   static constexpr int kRows = CTAS * kTileM;
-  static constexpr int kBRows = kTileN / CTAS;  // B rows that a block brings
+  static constexpr int kBRows = TN / CTAS;  // B rows that a block brings, in boxes of
+  static constexpr int kBoxRows = kBRows < kTileM ? kBRows : kTileM;
   static constexpr int kBBytes = kBRows * kBlock;
-  static constexpr int kStages = CTAS == 2 ? 5 : 3;
+  static constexpr int kStages = CTAS == 1 ? 3 : (TN == 256 ? 5 : 7);
+  static constexpr int kBufs = 512 / TN;       // accumulators in tensor memory
+  static constexpr int kWarpCols = TN / 2;     // accumulator columns of a warp of sums
+  static constexpr int kColBlocks = TN / kBlock;
   static constexpr int kSmem = 1024 + kStages * (kABytes + kBBytes) + kEpiWarps * kBoxBytes;
 };
 constexpr int kRun = 4;       // blocks of the reduction whose scales are fetched together
@@ -168,11 +171,12 @@ __device__ __forceinline__ void store_box(T* y, long long ldy, uint32_t box, int
   }
 }
 
-template <int CTAS, bool GATED, typename YT>
+template <int CTAS, int TN, bool GATED, typename YT>
 __global__ void __launch_bounds__(kPairThreads, 1)
     matmul_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
                        const __grid_constant__ CUtensorMap tmap_y, const MatmulArgs a, const bool y_boxes) {
-  using S = TileShape<CTAS>;
+  using S = TileShape<CTAS, TN>;
+  static_assert(!GATED || TN == 256, "a block of 128 columns is gate and up");
   constexpr int kStages = S::kStages, kBBytes = S::kBBytes;
   extern __shared__ uint8_t smem_raw[];
   __shared__ SharedCtl ctl;
@@ -198,7 +202,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       mbar_init(smem_u32(&ctl.empty[lane]), 1);
     }
     if (lane == 8) {
-      for (int b = 0; b < 2; ++b) {
+      for (int b = 0; b < S::kBufs; ++b) {
         mbar_init(smem_u32(&ctl.tmem_full[b]), 1);
         mbar_init(smem_u32(&ctl.tmem_empty[b]), CTAS * kEpiWarps);  // the warps of sums of both blocks
       }
@@ -233,7 +237,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem_acc = __shfl_sync(0xffffffffu, ctl.tmem_base, 0);
   const int row_tiles = row_tiles_s;
-  const int cols = GATED ? kBlock : kTileN;  // output columns of a tile
+  const int cols = GATED ? kBlock : TN;  // output columns of a tile
   const int n_tiles = (a.N + cols - 1) / cols;
   const int tiles = row_tiles * n_tiles;     // (fits: checked by the host)
   const int kb_all = (int)blocks_of(a.K);
@@ -269,7 +273,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           for (int i = 0; i < S::kBRows / 64; ++i) load_b(i * 64 * kBlock, p.nt * kBlock + ((int)rank * S::kBRows / 128 + (i >> 1)) * 64, 2 * p.group + (i & 1));
         } else {
 #pragma unroll
-          for (int i = 0; i < S::kBRows / kTileM; ++i) load_b(i * kTileM * kBlock, p.nt * kTileN + ((int)rank * S::kBRows / kTileM + i) * kTileM, p.group);
+          for (int i = 0; i < S::kBRows / S::kBoxRows; ++i)
+            load_b(i * S::kBoxRows * kBlock, p.nt * TN + (int)rank * S::kBRows + i * S::kBoxRows, p.group);
         }
         if (++s == kStages) {
           s = 0;
@@ -282,7 +287,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     // ---------------------------------------------------------------- MMA issue (leader)
     if (rank == 0) {
       const uint32_t on = elect_one() ? 1u : 0u;
-      const uint32_t idesc = make_idesc_f8(S::kRows, kTileN, a.a_type, a.b_type);
+      const uint32_t idesc = make_idesc_f8(S::kRows, TN, a.a_type, a.b_type);
       int s = 0, buf = 0;
       uint32_t ph = 0, bph = 0;
       bool alive = true;
@@ -295,7 +300,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const int ksteps = min(4, (a.K - kb * kBlock + kMmaK - 1) / kMmaK);
-          mma_f8_block<CTAS>(tmem_acc + buf * kTileN, make_smem_desc(a_base + s * kABytes, kBlock), make_smem_desc(b_base + s * kBBytes, kBlock), idesc,
+          mma_f8_block<CTAS>(tmem_acc + buf * TN, make_smem_desc(a_base + s * kABytes, kBlock), make_smem_desc(b_base + s * kBBytes, kBlock), idesc,
                           on, ksteps);
           if constexpr (CTAS == 2) {
             mma_commit_pair(smem_u32(&ctl.empty[s]), on);
@@ -308,8 +313,10 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             s = 0;
             ph ^= 1u;
           }
-          buf ^= 1;
-          if (buf == 0) bph ^= 1u;
+          if (++buf == S::kBufs) {
+            buf = 0;
+            bph ^= 1u;
+          }
         }
       }
     }
@@ -334,7 +341,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       const float* sb[2];
 #pragma unroll
       for (int c = 0; c < 2; ++c)
-        sb[c] = a.b_scale + (GATED ? (long long)(2 * p.group + c) * nb + p.nt : (long long)p.group * nb + min(2 * p.nt + c, nb - 1)) * kb_all;
+        sb[c] = a.b_scale + (GATED ? (long long)(2 * p.group + c) * nb + p.nt : (long long)p.group * nb + min(p.nt * S::kColBlocks + c % S::kColBlocks, nb - 1)) * kb_all;
       float na[2][kRun], ncol[2][kRun];
       auto fetch = [&](int kb) {
 #pragma unroll
@@ -372,9 +379,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSums));
     // ---------------------------------------------------------------- scaled sums and results (both blocks)
     const int quad = warp & 3;         // lanes of tensor memory this warp may read
-    const int half = (warp - kEpiWarp0) >> 2;  // its 128 columns
+    const int half = (warp - kEpiWarp0) >> 2;  // its columns
     const uint32_t leader_empty = CTAS == 2 ? map_to_rank(smem_u32(&ctl.tmem_empty[0]), 0u) : smem_u32(&ctl.tmem_empty[0]);
-    const uint32_t taddr0 = tmem_acc + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * 128);
+    const uint32_t taddr0 = tmem_acc + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * S::kWarpCols);
     const int in_tile = quad * 32 + lane;
     int slot = 0;
     uint32_t sph = 0;
@@ -383,15 +390,15 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     bool ok = true;
     for (int t = pair_id; t < tiles; t += num_pairs, parity ^= 1) {
       PairTile p = {0, 0, 0, 0};
-      f32x2 acc[64];
+      f32x2 acc[S::kWarpCols / 2];
 #pragma unroll
-      for (int i = 0; i < 64; ++i) acc[i] = 0;
+      for (int i = 0; i < S::kWarpCols / 2; ++i) acc[i] = 0;
       // Factors of block kb; read while the block before it is added, so that neither the barrier's nor the memory's latency is waited for.
       float f = 0.0f, fu = 0.0f;
       auto next_factor = [&](int kb) {
         const int i = kb % kRun;
         if (i == 0) ok = ok && mbar_wait_inline(smem_u32(&factor_full[slot]), sph, &ctl, &g_fp8_status);
-        f = factor[slot][i][GATED ? 0 : half][in_tile];
+        f = factor[slot][i][GATED || S::kColBlocks == 1 ? 0 : half][in_tile];
         if (GATED) fu = factor[slot][i][1][in_tile];
         if (kb == 0) p = run_tile[slot];
         if (i == kRun - 1 || kb == kb_all - 1) {
@@ -410,13 +417,13 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         ok = ok && mbar_wait_inline(smem_u32(&ctl.tmem_full[buf]), bph, &ctl, &g_fp8_status);
         // (a wait that gave up does not leave the loop: the lanes stay together, and no result is stored)
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t taddr = taddr0 + (uint32_t)(buf * kTileN);
+        const uint32_t taddr = taddr0 + (uint32_t)(buf * TN);
 #pragma unroll
-        for (int c = 0; c < 128; c += 64) {
+        for (int c = 0; c < S::kWarpCols; c += 64) {
           float v[64];
           tmem_ld64(taddr + c, reinterpret_cast<int32_t*>(v));
           if (c == 0 && kb + 1 < kb_all) next_factor(kb + 1);
-          if (c == 64) {
+          if (c + 64 == S::kWarpCols) {
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
@@ -427,8 +434,10 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 #pragma unroll
           for (int j = 0; j < 64; j += 2) fma2(&acc[(c + j) / 2], pair_of(v[j], v[j + 1]), GATED && c >= 64 ? ffu : ff);
         }
-        buf ^= 1;
-        if (buf == 0) bph ^= 1u;
+        if (++buf == S::kBufs) {
+          buf = 0;
+          bph ^= 1u;
+        }
       }
       const long long m = (long long)p.row0 + (int)rank * kTileM + in_tile;
       if constexpr (GATED) {
@@ -456,7 +465,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           if (half == 0) a.y_scale[m * a.ldys + p.nt] = s.scale;
         }
       } else {
-        const int n = p.nt * kTileN + half * 128, m0 = p.row0 + (int)rank * kTileM + quad * 32;
+        const int n = p.nt * TN + half * S::kWarpCols, m0 = p.row0 + (int)rank * kTileM + quad * 32;
         // 128 bytes of each of the warp's 32 rows go to shared memory (16-byte pieces, swizzled as the tensor map says).  From there, if
         // the copy engine can address the result and all 32 rows are this group's, in one copy, which clips what lies past the last column
         // and runs beside the next tile (stores from registers took 3200 cycles of a tile of bf16, as long as five blocks of the
@@ -465,7 +474,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         constexpr int kCols = 128 / (int)sizeof(YT);
         const uint32_t box = box_base + (uint32_t)((warp - kEpiWarp0) * kBoxBytes);
 #pragma unroll
-        for (int i = 0; i < 128; i += kCols) {
+        for (int i = 0; i < S::kWarpCols; i += kCols) {
           if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
           __syncwarp();
 #pragma unroll
@@ -525,17 +534,17 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   }
 }
 
-template <int CTAS, bool GATED, typename YT>
+template <int CTAS, int TN, bool GATED, typename YT>
 int launch_pair(const MatmulArgs& a, cudaStream_t st) {
-  using S = TileShape<CTAS>;
-  const long long cols = GATED ? kBlock : kTileN;
+  using S = TileShape<CTAS, TN>;
+  const long long cols = GATED ? kBlock : TN;
   const long long n_tiles = (a.N + cols - 1) / cols;
   const long long row_tiles = a.offsets ? a.rows / S::kRows + std::min(a.groups, a.rows) : (a.rows + S::kRows - 1) / S::kRows;
   if (row_tiles * n_tiles > 0x7FFFFFFFLL - kNumSMs) return B2C_E_UNSUPPORTED;
   CUtensorMap ta, tb, ty;
   int rc = encode_tiled_2d(&ta, a.a, a.K, a.rows, a.rows > 1 ? a.lda : a.K, kBlock, kTileM, kBlock);
   if (rc == B2C_OK)
-    rc = encode_tiled_3d(&tb, a.b, a.K, a.N, (uint64_t)a.groups * (GATED ? 2 : 1), a.K, (uint64_t)a.N * a.K, kBlock, GATED ? 64 : kTileM, kBlock);
+    rc = encode_tiled_3d(&tb, a.b, a.K, a.N, (uint64_t)a.groups * (GATED ? 2 : 1), a.K, (uint64_t)a.N * a.K, kBlock, GATED ? 64 : S::kBoxRows, kBlock);
   if (rc != B2C_OK) return rc;
   // results by boxes of 128 bytes x 32 rows where the copy engine can address them
   const bool y_boxes = !GATED && (reinterpret_cast<uintptr_t>(a.y) & 15) == 0 && (a.ldy * sizeof(YT)) % 16 == 0;
@@ -543,7 +552,7 @@ int launch_pair(const MatmulArgs& a, cudaStream_t st) {
   if (y_boxes) rc = encode_tiled_2d(&ty, a.y, (uint64_t)a.N * sizeof(YT), a.rows, (uint64_t)a.ldy * sizeof(YT), 128, 32, 128);
   if (rc != B2C_OK) return rc;
   static std::atomic<unsigned long long> configured{0};
-  cudaError_t e = set_max_dynamic_smem_once(configured, (const void*)matmul_pair_kernel<CTAS, GATED, YT>, S::kSmem);
+  cudaError_t e = set_max_dynamic_smem_once(configured, (const void*)matmul_pair_kernel<CTAS, TN, GATED, YT>, S::kSmem);
   if (e == cudaSuccess) {
     const int pairs = (int)std::min<long long>(row_tiles * n_tiles, kNumSMs / CTAS);
     cudaLaunchConfig_t cfg = {};
@@ -560,7 +569,7 @@ int launch_pair(const MatmulArgs& a, cudaStream_t st) {
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = CTAS == 2 ? 2 : 1;
-    e = cudaLaunchKernelEx(&cfg, matmul_pair_kernel<CTAS, GATED, YT>, ta, tb, ty, a, y_boxes);
+    e = cudaLaunchKernelEx(&cfg, matmul_pair_kernel<CTAS, TN, GATED, YT>, ta, tb, ty, a, y_boxes);
   }
   if (e != cudaSuccess) {
     set_last_cuda_error((int)e);
@@ -569,26 +578,36 @@ int launch_pair(const MatmulArgs& a, cudaStream_t st) {
   return B2C_OK;
 }
 
+template <int CTAS, int TN>
+int launch_type(const MatmulArgs& a, cudaStream_t st) {
+  if (a.y_type == B2C_F32) return launch_pair<CTAS, TN, false, float>(a, st);
+  if (a.y_type == B2C_F16) return launch_pair<CTAS, TN, false, __half>(a, st);
+  return launch_pair<CTAS, TN, false, __nv_bfloat16>(a, st);
+}
+
 }  // namespace
 
 namespace {
 
-template <int CTAS>
-int launch_type(const MatmulArgs& a, cudaStream_t st) {
-  if (a.gated) return launch_pair<CTAS, true, uint8_t>(a, st);
-  if (a.y_type == B2C_F32) return launch_pair<CTAS, false, float>(a, st);
-  if (a.y_type == B2C_F16) return launch_pair<CTAS, false, __half>(a, st);
-  return launch_pair<CTAS, false, __nv_bfloat16>(a, st);
+// Cycles by tiles of `tn` columns: the tiles of 128 are for products with fewer tiles than pairs.  A block of the reduction takes them 560
+// cycles instead of 850 (4096 x 4096: 512 rows 14.7 and 19.1 us, 768 rows, where they need a second wave, 24.2 and 19.9).
+long long tile_cycles(const MatmulArgs& a, int tn) {
+  const long long tiles = ((a.N + tn - 1) / tn) * (long long)((a.rows + 2 * kTileM - 1) / (2 * kTileM));
+  const long long waves = (tiles + kNumSMs / 2 - 1) / (kNumSMs / 2);
+  return waves * ((tn == 128 ? 560 : 850) * blocks_of(a.K) + 4000);
 }
 
 }  // namespace
+
+long long pair_cycles(const MatmulArgs& a) { return std::min(tile_cycles(a, 128), tile_cycles(a, 256)); }
 
 int launch_fp8_matmul_pair(const MatmulArgs& a, cudaStream_t st) {
   const int rows = a.offsets ? (a.rows + a.groups - 1) / a.groups : a.rows;  // of a group, on average
   // Half a tile of every group is empty: 64 rows of a tile of its own, 128 of a pair's, which is 7 % faster a row.  Even at some
   // 800 rows of a group; without groups the pair always.
-  if (a.offsets && rows <= 768) return launch_type<1>(a, st);
-  return launch_type<2>(a, st);
+  if (a.gated) return rows <= 768 ? launch_pair<1, 256, true, uint8_t>(a, st) : launch_pair<2, 256, true, uint8_t>(a, st);
+  if (a.offsets) return rows <= 768 ? launch_type<1, 256>(a, st) : launch_type<2, 256>(a, st);
+  return tile_cycles(a, 128) < tile_cycles(a, 256) ? launch_type<2, 128>(a, st) : launch_type<2, 256>(a, st);
 }
 
 cudaError_t fp8_pair_status(int* status) { return take_status(status); }
