@@ -182,8 +182,9 @@ __device__ __forceinline__ int choose32(const b2c_route_desc& d, int rounds, con
         f0 = first;
         s0 = second;
       } else {
-        f0 = key_value(value_bits(key[0]));
-        s0 = P > 1 ? key_value(value_bits(key[P > 1 ? 1 : 0])) : -INFINITY;
+        constexpr unsigned kValue = kExact || CHECK ? 0xFFFFFFFFu : ~(unsigned)(P - 1);  // (equal runs: the first, wherever in a lane their best is)
+        f0 = key_value(value_bits(key[0]) & kValue);
+        s0 = P > 1 ? key_value(value_bits(key[P > 1 ? 1 : 0]) & kValue) : -INFINITY;
         add(f0, s0);
       }
       int from = lane;

@@ -419,6 +419,17 @@ def test_route_near_scores_are_told_apart(lib):
     check_route(lib, near, 5, kind="sigmoid", bias=torch.full((64,), 0.5, device="cuda"))
 
 
+def test_route_equal_runs(lib):
+    """Runs whose best logits are equal: the first ones are kept, in whatever place their best ones stand."""
+    x = torch.zeros(40, 256, device="cuda")
+    for g in range(8):
+        x[torch.arange(40), 32 * g + (torch.arange(40, device="cuda") * (7 - g)) % 32] = 5.0
+    for xt in WIDE:
+        for kind in ("softmax", "sigmoid"):
+            for score in ("max", "top2"):
+                check_route(lib, x.to(xt), 4, kind=kind, groups=8, topk_groups=3, group_score=score)
+
+
 def test_route_strided_logits(lib):
     whole = torch.randn(20, 100, generator=gen(14), device="cuda")
     check_route(lib, whole[::2, 7:71], 4, kind="softmax")
