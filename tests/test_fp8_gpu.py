@@ -419,6 +419,45 @@ def test_route_near_scores_are_told_apart(lib):
     check_route(lib, near, 5, kind="sigmoid", bias=torch.full((64,), 0.5, device="cuda"))
 
 
+@pytest.mark.parametrize("xt", WIDE, ids=str)
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("tokens,experts,topk,groups,topk_groups,group_score", [
+    (400, 256, 8, 8, 4, "top2"), (401, 256, 15, 1, 1, "max"), (411, 33, 5, 1, 1, "max"), (397, 64, 6, 16, 5, "top2"), (501, 64, 3, 4, 2, "max"),
+    (397, 240, 8, 5, 2, "top2"), (399, 96, 6, 4, 1, "max"), (300, 512, 16, 8, 4, "max")])
+def test_route_ties_among_others(lib, tokens, experts, topk, groups, topk_groups, group_score, kind, xt):
+    """Every third token has equal and nearly equal logits, so that neighbouring tokens need different looks."""
+    g = gen(tokens + experts)
+    x = torch.randn(tokens, experts, generator=g, device="cuda") * 2
+    x[::3] = torch.round(x[::3]) + torch.arange(experts, device="cuda") % 4 * 2.0 ** -21
+    x = x.to(xt)
+    bias = torch.randn(experts, generator=g, device="cuda") * 0.1
+    bias[::2] = 0.125
+    for b in (None, bias):
+        for renormalise, scale in ((True, 1.0), (False, 2.5)):
+            check_route(lib, x, topk, kind=kind, groups=groups, topk_groups=topk_groups, group_score=group_score, renormalise=renormalise,
+                        scale=scale, bias=b)
+
+
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts,groups", [(64, 1), (64, 4), (256, 8)])
+def test_route_special_rows_among_others(lib, kind, experts, groups):
+    """Emptied rows, infinities, NaN and ties beside ordinary tokens, and biases of the same kinds."""
+    x = torch.randn(143, experts, generator=gen(17), device="cuda")
+    x[0::14] = -math.inf
+    x[1::14, 3:] = -math.inf
+    x[2::14, 17] = math.nan
+    x[4::14, 9::31] = math.inf
+    x[5::14] = torch.finfo(torch.float32).min
+    x[7::14] = 0.0
+    x[8::14] = math.nan
+    x[11::14] = -200.0 - torch.arange(experts, device="cuda") % 3
+    bias = torch.randn(experts, generator=gen(18), device="cuda") * 0.1
+    some = bias.clone()
+    some[::3], some[1::5], some[2] = -math.inf, math.nan, math.inf
+    for b in (None, bias, some):
+        check_route(lib, x, 6, kind=kind, groups=groups, topk_groups=min(groups, 2), bias=b)
+
+
 def test_route_equal_runs(lib):
     """Runs whose best logits are equal: the first ones are kept, in whatever place their best ones stand."""
     x = torch.zeros(40, 256, device="cuda")
