@@ -456,9 +456,11 @@ __global__ void __launch_bounds__(32 * kRouteWarps, P <= 8 ? 5 : 1) route_kernel
   // the weights of the chosen, from their logits; the argument of the exponential without the rounding of its difference
   const bool on = lane < a.d.topk;
   const float l = on ? logit<T>(row, id) : -INFINITY;
-  // logistic scores that 32 bits cannot hold: below -60 they are exponentials, and their ratios those to the largest
-  // (from -740 on 64 bits cannot either: 0, as for the lowest values of a type that masks write)
-  const float top = softmax ? mx : key_value(__reduce_max_sync(kAll, order_key(l)));
+  // Scores that 32 bits cannot hold: renormalised ones are taken relative to the largest chosen one, which may be far below the
+  // largest of the row where a bias or a run decides; logistic ones below -60 are exponentials.  (From -740 on 64 bits cannot
+  // hold them either: 0, as for the lowest values of a type that masks write.)
+  const float best = key_value(__reduce_max_sync(kAll, order_key(l)));
+  const float top = softmax && !(a.d.renormalise && mx - best < 740.0f) ? mx : best;
   float s;
   if (softmax || (a.d.renormalise && top < -60.0f && top > -740.0f)) {
     const double diff = (double)l - (double)top;
@@ -466,7 +468,8 @@ __global__ void __launch_bounds__(32 * kRouteWarps, P <= 8 ? 5 : 1) route_kernel
     const float e = expf(hi);
     s = l == -INFINITY ? 0.0f : (l == top ? 1.0f : (e == 0.0f ? 0.0f : fmaf(e, (float)(diff - (double)hi), e)));
   } else {
-    s = l == -INFINITY ? 0.0f : 1.0f / (1.0f + expf(-l));
+    const float e = expf(l < -60.0f ? l : -l);
+    s = l < -60.0f ? e : 1.0f / (1.0f + e);
   }
   float w = s;
   if (a.d.renormalise) {

@@ -469,6 +469,19 @@ def test_route_equal_runs(lib):
                 check_route(lib, x.to(xt), 4, kind=kind, groups=8, topk_groups=3, group_score=score)
 
 
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+def test_route_weights_of_small_scores(lib, kind):
+    """A bias or a run that takes experts whose scores 32 bits hardly hold or do not hold."""
+    base = torch.tensor([50.0, -60.0, -88.0, -95.0, -100.0, -120.0, -600.0, -1500.0], device="cuda")
+    x = torch.cat([base[:, None] + torch.randn(8, 32, generator=gen(19), device="cuda"), torch.randn(8, 32, generator=gen(20), device="cuda") * 40], 1)
+    x[:, 40] = 60.0
+    bias = torch.zeros(64, device="cuda")
+    bias[:16] = 4.0
+    for renormalise in (True, False):
+        check_route(lib, x, 5, kind=kind, renormalise=renormalise, bias=bias)
+        check_route(lib, x, 5, kind=kind, renormalise=renormalise, groups=2, topk_groups=1, bias=bias)
+
+
 def test_route_strided_logits(lib):
     whole = torch.randn(20, 100, generator=gen(14), device="cuda")
     check_route(lib, whole[::2, 7:71], 4, kind="softmax")
