@@ -397,8 +397,10 @@ int b2c_fp8_matmul(const b2c_matmul_desc* desc, int64_t rows, const void* a_dev,
  * The topk experts of largest choice are written in falling order to ids_dev [tokens][topk], and
  * weights_dev [tokens][topk] gets s (without the bias), divided by the sum over the chosen ones if
  * `renormalise` is set, times `scale`.  Choices and run scores are compared as if formed in 64 bits (without a
- * bias a larger logit is a larger choice, however near the scores are); equal ones go to the lowest index.  A logit of -inf or NaN has s = 0, a choice that is NaN
- * counts as -inf; of several +inf in a softmax row each counts as the largest.  Where the chosen s sum to 0 renormalised weights are 0. */
+ * bias a larger logit is a larger choice, however near the scores are); equal ones go to the lowest index.  A logit of
+ * -inf or NaN has s = 0, a choice that is NaN counts as -inf, and so does a run score of +inf and -inf; of several +inf
+ * in a softmax row each counts as the largest.  Where the chosen s sum to 0 renormalised weights are 0.
+ * Weights are right to a few roundings of 32 bits; below 2^-121 * scale to that amount. */
 #define B2C_SCORE_SOFTMAX 0
 #define B2C_SCORE_SIGMOID 1
 #define B2C_GROUP_MAX 0

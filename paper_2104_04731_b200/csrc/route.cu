@@ -67,7 +67,8 @@ __device__ __forceinline__ int choose_exact(const b2c_route_desc& d, const doubl
       for (int i = 0; i < size; ++i) add(part_of(lane * size + i), -INFINITY);
     }
     const bool two = d.group_score == B2C_GROUP_TOP2 && size > 1;
-    const K mine = run < d.groups ? order_key(two ? first + second : first) : (K)0;
+    const double score = two ? (second == -INFINITY ? second : first + second) : first;  // (+inf and -inf: -inf)
+    const K mine = run < d.groups ? order_key(score) : (K)0;
     int better = 0;
     for (int g = 0; g < d.groups; ++g) {
       const K k = __shfl_sync(kAll, mine, g * lanes);
@@ -197,7 +198,9 @@ __device__ __forceinline__ int choose32(const b2c_route_desc& d, int rounds, con
       for (int i = 0; i < size; ++i) add(part_of(lane * size + i), -INFINITY);
     }
     const bool two = d.group_score == B2C_GROUP_TOP2 && size > 1;
-    const unsigned mine = run < d.groups ? order_key(two ? first + second : first) : 0u;
+    // (infinities are the largest values here: a sum with the lowest one is that, and sums stay between them)
+    const float score = two ? (second <= -3.402823466e38f ? -3.402823466e38f : finite(first + second)) : first;
+    const unsigned mine = run < d.groups ? order_key(score) : 0u;
     int better = 0;
     for (int g = 0; g < d.groups; ++g) {
       const unsigned k = __shfl_sync(kAll, mine, g * lanes);
@@ -263,7 +266,7 @@ __device__ __forceinline__ int choose32(const b2c_route_desc& d, int rounds, con
 template <typename T>
 __device__ __forceinline__ float logit(const T* row, int e) {
   const float x = to_float<T>(row[e]);
-  return x != x ? -INFINITY : x;
+  return x != x ? -INFINITY : x + 0.0f;  // (a zero loses its sign, so that all zeros are equal)
 }
 
 __device__ __forceinline__ double sigmoid64(double x) { return x == -INFINITY ? 0.0 : 1.0 / (1.0 + exp(-x)); }
@@ -364,7 +367,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps, P <= 8 ? 5 : 1) route_kernel
         }
       }
 #pragma unroll
-      for (int i = 0; i < P; ++i) x[i] = x[i] != x[i] ? -INFINITY : x[i];
+      for (int i = 0; i < P; ++i) x[i] = x[i] != x[i] ? -INFINITY : x[i] + 0.0f;
     }
   }
   if (!loaded) {
@@ -457,19 +460,19 @@ __global__ void __launch_bounds__(32 * kRouteWarps, P <= 8 ? 5 : 1) route_kernel
   const bool on = lane < a.d.topk;
   const float l = on ? logit<T>(row, id) : -INFINITY;
   // Scores that 32 bits cannot hold: renormalised ones are taken relative to the largest chosen one, which may be far below the
-  // largest of the row where a bias or a run decides; logistic ones below -60 are exponentials.  (From -740 on 64 bits cannot
+  // largest of the row where a bias or a run decides; logistic ones below -17 are exponentials in 32 bits (1 + e^l rounds to 1).  (From -740 on 64 bits cannot
   // hold them either: 0, as for the lowest values of a type that masks write.)
   const float best = key_value(__reduce_max_sync(kAll, order_key(l)));
   const float top = softmax && !(a.d.renormalise && mx - best < 740.0f) ? mx : best;
   float s;
-  if (softmax || (a.d.renormalise && top < -60.0f && top > -740.0f)) {
+  if (softmax || (a.d.renormalise && top < -17.0f && top > -740.0f)) {
     const double diff = (double)l - (double)top;
     const float hi = (float)diff;
     const float e = expf(hi);
     s = l == -INFINITY ? 0.0f : (l == top ? 1.0f : (e == 0.0f ? 0.0f : fmaf(e, (float)(diff - (double)hi), e)));
   } else {
-    const float e = expf(l < -60.0f ? l : -l);
-    s = l < -60.0f ? e : 1.0f / (1.0f + e);
+    const float e = expf(l < -17.0f ? l : -l);
+    s = l < -17.0f ? e : 1.0f / (1.0f + e);
   }
   float w = s;
   if (a.d.renormalise) {

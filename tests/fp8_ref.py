@@ -88,7 +88,8 @@ def route(logits, topk, kind="softmax", groups=1, topk_groups=1, group_score="ma
         runs = []
         for g in range(groups):
             top = sorted(of_run[g * size:(g + 1) * size], reverse=True)
-            runs.append((-(top[0] if group_score == "max" or size == 1 else top[0] + top[1]), g))
+            score = top[0] if group_score == "max" or size == 1 else top[0] + top[1]
+            runs.append((-score if score == score else math.inf, g))
         kept = {g for _, g in sorted(runs)[:topk_groups]}
         chosen = sorted((-c[e], e) for e in range(len(c)) if e // size in kept)[:topk]
         chosen = [e for _, e in chosen]

@@ -469,10 +469,35 @@ def test_route_equal_runs(lib):
                 check_route(lib, x.to(xt), 4, kind=kind, groups=8, topk_groups=3, group_score=score)
 
 
+def test_route_signed_zeros(lib):
+    """-0 and +0 are equal."""
+    x = torch.tensor([1.0, -1.0], device="cuda")[torch.randint(0, 2, (60, 96), generator=gen(21), device="cuda")] * 0.0
+    x[::2, 70] = 1.0
+    for xt in WIDE:
+        for kind in ("softmax", "sigmoid"):
+            check_route(lib, x.to(xt), 4, kind=kind)
+            check_route(lib, x.to(xt), 4, kind=kind, groups=3, topk_groups=1)
+            check_route(lib, x.to(xt), 4, kind=kind, bias=-x[0])
+
+
+@pytest.mark.parametrize("experts,groups", [(64, 8), (64, 32), (60, 20), (256, 8)])
+def test_route_runs_with_infinite_biases(lib, experts, groups):
+    """Runs that a bias empties or puts first, in part and as a whole: sums of +inf and -inf are the lowest."""
+    x = torch.randn(60, experts, generator=gen(22), device="cuda")
+    size = experts // groups
+    for seed in range(6):
+        pick = torch.randint(0, 3, (experts,), generator=gen(30 + seed), device="cuda")
+        bias = torch.tensor([0.125, math.inf, -math.inf], device="cuda")[pick]
+        if seed % 2:
+            bias[pick == 0] = math.nan
+        for kind in ("softmax", "sigmoid"):
+            check_route(lib, x, min(4, 3 * size), kind=kind, groups=groups, topk_groups=3, group_score="top2", bias=bias)
+
+
 @pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
 def test_route_weights_of_small_scores(lib, kind):
     """A bias or a run that takes experts whose scores 32 bits hardly hold or do not hold."""
-    base = torch.tensor([50.0, -60.0, -88.0, -95.0, -100.0, -120.0, -600.0, -1500.0], device="cuda")
+    base = torch.tensor([50.0, -20.0, -88.0, -95.0, -100.0, -120.0, -600.0, -1500.0], device="cuda")
     x = torch.cat([base[:, None] + torch.randn(8, 32, generator=gen(19), device="cuda"), torch.randn(8, 32, generator=gen(20), device="cuda") * 40], 1)
     x[:, 40] = 60.0
     bias = torch.zeros(64, device="cuda")
