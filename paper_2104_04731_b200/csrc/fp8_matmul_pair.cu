@@ -467,10 +467,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       } else {
         const int n = p.nt * TN + half * S::kWarpCols, m0 = p.row0 + (int)rank * kTileM + quad * 32;
         // 128 bytes of each of the warp's 32 rows go to shared memory (16-byte pieces, swizzled as the tensor map says).  From there, if
-        // the copy engine can address the result and all 32 rows are this group's, in one copy, which clips what lies past the last column
-        // and runs beside the next tile (stores from registers took 3200 cycles of a tile of bf16, as long as five blocks of the
-        // reduction); else by the lanes.
-        const bool by_copy = y_boxes && m0 + 32 <= p.row_end;
+        // the copy engine can address the result and all 32 rows are this group's, in one copy, which runs beside the next tile (stores
+        // from registers took 3200 cycles of a tile of bf16, as long as five blocks of the reduction); else by the lanes.  The copy
+        // clips what lies past the last column in steps of 16 bytes: a box that the result ends in at another place is left to the lanes.
         constexpr int kCols = 128 / (int)sizeof(YT);
         const uint32_t box = box_base + (uint32_t)((warp - kEpiWarp0) * kBoxBytes);
 #pragma unroll
@@ -493,6 +492,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
                          "r"(w[1]), "r"(w[2]), "r"(w[3])
                          : "memory");
           }
+          const bool by_copy = y_boxes && m0 + 32 <= p.row_end && (n + i + kCols <= a.N || a.N * (int)sizeof(YT) % 16 == 0);
           if (by_copy) {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();

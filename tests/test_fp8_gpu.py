@@ -173,6 +173,11 @@ def test_matmul_strides(lib, rows, N, K, yt):
         lib.fp8_matmul(a, sa, b, sb, y)
         assert torch.equal(y.double(), ref.matmul(a, sa, b, sb).to(yt).double())
         assert bool((whole[:, N:].float() == 7.0).all())
+    for n in (N - 1, N - 2, N - 93, N - 101):  # rows on the 16-byte grid that end off it
+        whole, _ = poison(rows, N // 8 * 8 + 16, yt)
+        lib.fp8_matmul(a, sa, b[:n], sb[:ref.nb(n)], whole[:, :n])
+        assert torch.equal(whole[:, :n].double(), ref.matmul(a, sa, b[:n], sb[:ref.nb(n)]).to(yt).double())
+        assert bool((whole[:, n:].float() == 7.0).all())
     for first in (1, 4, 7):  # results that start off the 16-byte grid
         whole, _ = poison(rows, N + 8, yt)
         lib.fp8_matmul(a, sa, b, sb, whole[:, first:first + N])
