@@ -100,6 +100,29 @@ def test_quantize_special_values(lib, block, xt):
     assert bool(((s.double() - scale).abs()[finite] <= 2.0 ** -24 * scale[finite]).all())
 
 
+@pytest.mark.parametrize("xt", WIDE, ids=str)
+@pytest.mark.parametrize("dtype", [E4, E5], ids=["e4m3", "e5m2"])
+@pytest.mark.parametrize("block", [1, 128])
+@pytest.mark.parametrize("rows,cols,first", [(300, 777, 0), (300, 640, 3), (9000, 2000, 0)])
+def test_quantize_special_values_among_others(lib, rows, cols, first, block, dtype, xt):
+    """Rows off the 16-byte grid and very many blocks: NaN, infinities, zeros of both signs, the smallest and the largest values."""
+    x = torch.randn(rows, first + cols, generator=gen(4), device="cuda").bfloat16().to(xt)[:, first:]
+    tiny, large = torch.finfo(xt).tiny, torch.finfo(xt).max
+    spots = torch.rand(rows, cols, generator=gen(5), device="cuda")
+    x[1::128][spots[1::128] < 2e-3] = math.nan
+    x[200::256][spots[200::256] < 2e-3] = math.inf
+    x[201::256][spots[201::256] < 1e-3] = -math.inf
+    x[130::512] = -0.0
+    x[131::512] = tiny / 4
+    x[132::512][spots[132::512] < 0.01] = -large
+    q, s = run_quantize(lib, x, dtype, block)
+    want, scale = ref.quantize(x, dtype, block)
+    finite = scale.isfinite()
+    assert bool((s.isinf() == scale.isinf()).all()) and bool((s.isnan() == scale.isnan()).all())
+    assert bool(((s.double() - scale).abs()[finite] <= 2.0 ** -24 * scale[finite]).all())
+    assert same8(q, want)
+
+
 @pytest.mark.parametrize("block", [1, 128])
 def test_quantize_strides_and_alignment(lib, block):
     base = torch.randn(70, 1024, generator=gen(4), device="cuda").bfloat16()
