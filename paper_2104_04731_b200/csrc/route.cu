@@ -144,6 +144,7 @@ __device__ __forceinline__ float finite(float v) { return fminf(fmaxf(v, -3.4028
 struct Near {
   bool runs;    // a kept and a dropped run
   bool inside;  // two neighbours among the chosen
+  bool last;    // the two last ones among the chosen
   bool border;  // the last chosen and the first left out
 };
 
@@ -162,7 +163,7 @@ __device__ __forceinline__ int choose32(const b2c_route_desc& d, int rounds, con
     else key[i] = lane * P + i < d.experts ? ((order_key(choice[i]) & ~(unsigned)(P - 1)) | (unsigned)(P - 1 - i)) : 0u;
   }
   sort_lane<P, K>(key);
-  *near = {false, false, false};
+  *near = {false, false, false, false};
   bool by_expert = false;  // runs that do not end with a lane's experts: keys are dropped one by one
   unsigned open = kAll;
   const int size = d.experts / d.groups;
@@ -198,8 +199,10 @@ __device__ __forceinline__ int choose32(const b2c_route_desc& d, int rounds, con
       for (int i = 0; i < size; ++i) add(part_of(lane * size + i), -INFINITY);
     }
     const bool two = d.group_score == B2C_GROUP_TOP2 && size > 1;
-    // (infinities are the largest values here: a sum with the lowest one is that, and sums stay between them)
-    const float score = two ? (second <= -3.402823466e38f ? -3.402823466e38f : finite(first + second)) : first;
+    // (infinities are about the largest values here, up to the place in their keys: a sum with the lowest one is that, and sums stay
+    // between them; a sum of both is left to 64 bits)
+    constexpr float kHuge = 3.4028e38f;
+    const float score = two ? (second <= -kHuge ? -3.402823466e38f : finite(first + second)) : first;
     const unsigned mine = run < d.groups ? order_key(score) : 0u;
     int better = 0;
     for (int g = 0; g < d.groups; ++g) {
@@ -211,6 +214,7 @@ __device__ __forceinline__ int choose32(const b2c_route_desc& d, int rounds, con
       const float low = key_value(__reduce_min_sync(kAll, kept ? mine : 0xFFFFFFFFu));
       const unsigned high = __reduce_max_sync(kAll, kept ? 0u : mine);
       near->runs = high != 0u && !(low - key_value(high) > (PARTS ? unit * fabsf(low) : 2.0f * unit * (1.0f + fabsf(low))));
+      if (!PARTS) near->runs |= __any_sync(kAll, two && first >= kHuge && second <= -kHuge);
     }
     open = __ballot_sync(kAll, kept);
     if (!by_expert && !kept) {
@@ -258,6 +262,7 @@ __device__ __forceinline__ int choose32(const b2c_route_desc& d, int rounds, con
     const bool open_order = lane < rounds && !(ends && left == 0u) && !(my_value - next > unit * (1.0f + fabsf(my_value)));
     const unsigned who = __ballot_sync(kAll, open_order);
     near->border = ((who >> (rounds - 1)) & 1u) != 0u;
+    near->last = rounds > 1 && ((who >> (rounds - 2)) & 1u) != 0u;
     near->inside = (who & ((1u << (rounds - 1)) - 1u)) != 0u;
   }
   return my_id;
@@ -332,9 +337,10 @@ __device__ __forceinline__ int order64(double choice, int id, int count, int lan
 // compared, which is exact.  With a bias (or run scores that are sums) the choices are formed in 32 bits: exponential, sum, quotient
 // and additions put each off by at most 7 units of 2^-24 * (1 + |choice|), its place in the key's lowest bits by P - 1 units of 2^-23,
 // together less than 2^-19 for P <= 8 and 2^-17 beyond, and sums of two by twice that.  A token in which two choices that decide
-// something are not further apart than twice this (about one in fifty at 256 experts) is chosen again with the places beside the
-// values (2^-20); where that leaves only the order of the topk + 1 first open (one in two hundred) these few are compared in 64 bits,
-// and else, or if the scores hang on all logits, the token is done in 64 bits from the start.
+// something are not further apart than twice this (about one in fifty at 256 experts) needs a second look: where only the order of the
+// topk + 1 first is open, these few are compared in 64 bits; else all are chosen again with the places beside the values (2^-20), and
+// where that does not settle it, or if the scores hang on all logits, the token is done in 64 bits from the start.  (All such tokens
+// chosen again: 26.2 us for the work below, now 25.7; none looked at twice, which is wrong: 22.)
 // Memory-bound on paper (one read of the logits); what it spends are the instructions of exponentials, sort and topk rounds (16384 tokens
 // of 256 experts, 8 of 4 of 8 runs: 26 us, issue slots 73 % busy, against 2.8 us for the bytes).  Two tokens a warp, 16 lanes each, took
 // 38: the largest of 16 lanes is four exchanges, that of a warp one instruction.
@@ -393,23 +399,23 @@ __global__ void __launch_bounds__(32 * kRouteWarps, P <= 8 ? 5 : 1) route_kernel
   using LogitKey = typename std::conditional<sizeof(T) == 2, unsigned, unsigned long long>::type;
   if (by_logit && !sums) {
     if (softmax && !a.d.renormalise) {
-      float sum = 0.0f;
+      float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // (four: a sum of 32 in a row would be off by up to 31 roundings)
 #pragma unroll
-      for (int i = 0; i < P; ++i) sum += x[i] == -INFINITY ? 0.0f : (x[i] == mx ? 1.0f : expf(x[i] - mx));
-      all = warp_sum((double)sum);
+      for (int i = 0; i < P; ++i) sum[i & 3] += x[i] == -INFINITY ? 0.0f : (x[i] == mx ? 1.0f : expf(x[i] - mx));
+      all = warp_sum((double)((sum[0] + sum[1]) + (sum[2] + sum[3])));
     }
     id = choose32<P, LogitKey, false, false>(a.d, a.d.topk, x, x, [&](int e) { return logit<T>(row, e); }, lane, 0.0f, &near);
   } else {
     float c[P];
-    float sum = 0.0f;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       if (softmax) c[i] = x[i] == -INFINITY ? 0.0f : (x[i] == mx ? 1.0f : expf(x[i] - mx));
       else c[i] = __fdividef(1.0f, 1.0f + __expf(-x[i]));
-      sum += c[i];
+      sum[i & 3] += c[i];
     }
     if (softmax) {
-      all = warp_sum((double)sum);
+      all = warp_sum((double)((sum[0] + sum[1]) + (sum[2] + sum[3])));
 #pragma unroll
       for (int i = 0; i < P; ++i) c[i] = all > 0.0 ? __fdividef(c[i], (float)all) : 0.0f;
     }
@@ -448,13 +454,19 @@ __global__ void __launch_bounds__(32 * kRouteWarps, P <= 8 ? 5 : 1) route_kernel
     } else {
 #pragma unroll
       for (int i = 0; i < P; ++i) c[i] = finite(c[i]);
-      id = choose32<P, unsigned, true, false>(a.d, a.d.topk, c, c, part_of, lane, P <= 8 ? 0x1p-18f : 0x1p-16f, &near);
-      if (near.runs || near.inside || near.border) {
-        // a second look, one expert further, so that a border within the errors lies inside
-        const int rounds = min(min(a.d.topk + 1, 32), E / a.d.groups * a.d.topk_groups);
-        id = choose32<P, unsigned long long, true, false>(a.d, rounds, c, c, part_of, lane, 0x1p-20f, &near);
-        if (near.runs || near.border || (softmax && near.inside)) id = choose64<T, P>(a, row, lane, mx);
-        else if (near.inside) id = order64(sigmoid64((double)logit<T>(row, lane < rounds ? id : 0)) + (double)a.bias[lane < rounds ? id : 0], id, rounds, lane);
+      // one expert further than asked for, so that a border within the errors lies inside
+      const int rounds = min(min(a.d.topk + 1, 32), E / a.d.groups * a.d.topk_groups);
+      const bool further = rounds > a.d.topk;
+      id = choose32<P, unsigned, true, false>(a.d, rounds, c, c, part_of, lane, P <= 8 ? 0x1p-18f : 0x1p-16f, &near);
+      if (near.runs || near.inside || (near.border && !further)) {
+        if (near.runs || (near.border && (near.last || !further)))
+          id = choose32<P, unsigned long long, true, false>(a.d, rounds, c, c, part_of, lane, 0x1p-20f, &near);
+        if (near.runs || (near.border && (near.last || !further)) || (softmax && near.inside)) {
+          id = choose64<T, P>(a, row, lane, mx);
+        } else if (near.inside) {
+          const int e = lane < rounds ? id : 0;
+          id = order64(sigmoid64((double)logit<T>(row, e)) + (double)a.bias[e], id, rounds, lane);
+        }
       }
     }
   }

@@ -486,6 +486,15 @@ def test_route_special_rows_among_others(lib, kind, experts, groups):
         check_route(lib, x, 6, kind=kind, groups=groups, topk_groups=min(groups, 2), bias=b)
 
 
+@pytest.mark.parametrize("experts", [885, 1024])
+def test_route_weights_of_many_experts(lib, experts):
+    """Sums over a whole row of like terms: their roundings stay few."""
+    for seed in range(8):
+        x = torch.rand(400, experts, generator=gen(40 + seed), device="cuda") * 0.5 ** seed
+        check_route(lib, x, 5, kind="softmax", renormalise=False, scale=2.5)
+        check_route(lib, x, 5, kind="softmax", renormalise=False, bias=x[0])
+
+
 def test_route_equal_runs(lib):
     """Runs whose best logits are equal: the first ones are kept, in whatever place their best ones stand."""
     x = torch.zeros(40, 256, device="cuda")
@@ -508,16 +517,18 @@ def test_route_signed_zeros(lib):
             check_route(lib, x.to(xt), 4, kind=kind, bias=-x[0])
 
 
-@pytest.mark.parametrize("experts,groups", [(64, 8), (64, 32), (60, 20), (256, 8)])
+@pytest.mark.parametrize("experts,groups", [(64, 8), (64, 32), (60, 20), (60, 30), (256, 8), (256, 32), (96, 24)])
 def test_route_runs_with_infinite_biases(lib, experts, groups):
     """Runs that a bias empties or puts first, in part and as a whole: sums of +inf and -inf are the lowest."""
     x = torch.randn(60, experts, generator=gen(22), device="cuda")
     size = experts // groups
-    for seed in range(6):
+    for seed in range(8):
         pick = torch.randint(0, 3, (experts,), generator=gen(30 + seed), device="cuda")
         bias = torch.tensor([0.125, math.inf, -math.inf], device="cuda")[pick]
         if seed % 2:
             bias[pick == 0] = math.nan
+        if seed == 4:
+            bias[::5] = torch.finfo(torch.float32).min
         for kind in ("softmax", "sigmoid"):
             check_route(lib, x, min(4, 3 * size), kind=kind, groups=groups, topk_groups=3, group_score="top2", bias=bias)
 
