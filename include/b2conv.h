@@ -439,7 +439,7 @@ int b2c_route_combine(const void* y_dev, int y_type, int64_t y_rows, int64_t ldy
  * rounded before it is quantised).  w1_dev: E4M3 [experts][2][inter][hidden], gate matrix then up matrix,
  * w1_scale_dev [experts][2][ceil(inter/128)][ceil(hidden/128)]; w2_dev: E4M3 [experts][hidden][inter] with
  * w2_scale_dev [experts][ceil(hidden/128)][ceil(inter/128)]; all dense, 16-byte aligned.  hidden and inter
- * are multiples of 16.  The rows of a slot are rounded to `type` before the weighted sum, which is formed in fp32.
+ * are multiples of 16.  The rows of the slots and their weighted sum are formed in fp32 and rounded once, to `type`.
  * ids outside 0..experts-1 add nothing.  workspace_dev: b2c_experts_workspace_bytes bytes for at least this many
  * tokens, 16-byte aligned; its contents are scratch. */
 typedef struct {

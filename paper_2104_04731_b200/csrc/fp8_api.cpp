@@ -50,7 +50,7 @@ int experts_layout(const b2c_experts_desc* d, int64_t tokens, ExpertsLayout* l) 
   l->xs = part(4 * pairs * blocks_of(d->hidden));
   l->hq = part(pairs * d->inter);
   l->hs = part(4 * pairs * blocks_of(d->inter));
-  l->y = part(pairs * d->hidden * type_bytes(d->type));
+  l->y = part(pairs * d->hidden * 4);
   l->total = at;
   return B2C_OK;
 }
@@ -238,12 +238,14 @@ int b2c_fp8_experts(const b2c_experts_desc* d, int64_t tokens, const void* x, in
   m.ldys = 0;
   m.N = d->hidden;
   m.K = d->inter;
-  m.y_type = d->type;
+  // A slot's row is a partial sum: it stays in 32 bits, and y is rounded once.  (In the layer's type, half the traffic, 784 * 257 - 784 * 256
+  // came out as 1024 in bf16 and NaN in f16; 8192 tokens, 4 of 64 experts, 2048 x 1024: 420 us instead of 379.)
+  m.y_type = B2C_F32;
   m.gated = 0;
   m.early = 1;  // (the first product read its offsets after the sort had ended, and lets no later kernel start before that)
   rc = launch_fp8_matmul(m, st);
   if (rc != B2C_OK) return rc;
-  return from_cuda(launch_route_combine(m.y, d->type, pairs, m.ldy, rows, weights, tokens, d->topk, d->hidden, y, d->type, ldy, st));
+  return from_cuda(launch_route_combine(m.y, B2C_F32, pairs, m.ldy, rows, weights, tokens, d->topk, d->hidden, y, d->type, ldy, st));
 }
 
 int b2c_fp8_status(int32_t* status) {
