@@ -397,7 +397,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       float f = 0.0f, fu = 0.0f;
       auto next_factor = [&](int kb) {
         const int i = kb % kRun;
-        if (i == 0) ok = ok && mbar_wait_inline(smem_u32(&factor_full[slot]), sph, &ctl, &g_fp8_status);
+        if (i == 0) ok = ok && __all_sync(0xffffffffu, mbar_wait_inline(smem_u32(&factor_full[slot]), sph, &ctl, &g_fp8_status));
         f = factor[slot][i][GATED || S::kColBlocks == 1 ? 0 : half][in_tile];
         if (GATED) fu = factor[slot][i][1][in_tile];
         if (kb == 0) p = run_tile[slot];
@@ -414,8 +414,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 #pragma unroll 1
       for (int kb = 0; kb < kb_all; ++kb) {
         const f32x2 ff = pair_of(f, f), ffu = pair_of(fu, fu);
-        ok = ok && mbar_wait_inline(smem_u32(&ctl.tmem_full[buf]), bph, &ctl, &g_fp8_status);
-        // (a wait that gave up does not leave the loop: the lanes stay together, and no result is stored)
+        // (voted, so that the lanes are together at the warp-wide loads and agree on whether there is a result; a wait that gave up does not
+        // leave the loop)
+        ok = ok && __all_sync(0xffffffffu, mbar_wait_inline(smem_u32(&ctl.tmem_full[buf]), bph, &ctl, &g_fp8_status));
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t taddr = taddr0 + (uint32_t)(buf * TN);
 #pragma unroll
