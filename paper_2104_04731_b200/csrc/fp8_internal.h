@@ -56,6 +56,13 @@ struct MatmulArgs {
   int gated;             // y = quantise(silu(a . gate) * (a . up)), blocks of 1 x 128
 };
 
+// Whether the copy engine can take a product's results out (boxes of a map of bytes): rows on its 16-byte grid, and the byte a row ends
+// at within the copy's 32-bit coordinates.
+inline bool results_by_copy(const MatmulArgs& a) {
+  const long long bytes = type_bytes(a.y_type);
+  return !a.gated && (reinterpret_cast<uintptr_t>(a.y) & 15) == 0 && a.ldy * bytes % 16 == 0 && a.N * bytes <= 0x7FFFFFFFLL;
+}
+
 struct RouteArgs {
   b2c_route_desc d;
   long long tokens;

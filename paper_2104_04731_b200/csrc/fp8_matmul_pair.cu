@@ -547,8 +547,7 @@ int launch_pair(const MatmulArgs& a, cudaStream_t st) {
   if (rc == B2C_OK)
     rc = encode_tiled_3d(&tb, a.b, a.K, a.N, (uint64_t)a.groups * (GATED ? 2 : 1), a.K, (uint64_t)a.N * a.K, kBlock, GATED ? 64 : S::kBoxRows, kBlock);
   if (rc != B2C_OK) return rc;
-  // results by boxes of 128 bytes x 32 rows where the copy engine can address them
-  const bool y_boxes = !GATED && (reinterpret_cast<uintptr_t>(a.y) & 15) == 0 && (a.ldy * sizeof(YT)) % 16 == 0;
+  const bool y_boxes = results_by_copy(a);  // (of 128 bytes x 32 rows)
   ty = ta;
   if (y_boxes) rc = encode_tiled_2d(&ty, a.y, (uint64_t)a.N * sizeof(YT), a.rows, (uint64_t)a.ldy * sizeof(YT), 128, 32, 128);
   if (rc != B2C_OK) return rc;

@@ -2,6 +2,7 @@
 import glob
 import os
 import re
+import subprocess
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CSRC = os.path.join(ROOT, "paper_2104_04731_b200", "csrc")
@@ -19,3 +20,13 @@ def test_results_of_waits_are_voted():
             waits += 1
             assert line[:call.start()].strip().endswith("__all_sync(0xffffffffu,"), (os.path.basename(path), n + 1, line)
     assert waits >= 10
+
+
+def test_decisions_about_large_sizes(tmp_path):
+    """Sizes that no test can run (results of more than 2 GiB a row): what the host decides about them, as a small program."""
+    exe = str(tmp_path / "fp8_decisions")
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-I", os.path.join(cuda, "include"), "-I", os.path.join(ROOT, "include"), "-I", CSRC,
+                           os.path.join(ROOT, "tests", "fp8_decisions.cpp"), "-o", exe])
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout + r.stderr
