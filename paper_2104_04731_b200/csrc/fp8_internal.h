@@ -56,6 +56,9 @@ struct MatmulArgs {
   int gated;             // y = quantise(silu(a . gate) * (a . up)), blocks of 1 x 128
 };
 
+// Rows of a group, on average (all rows without groups).
+inline int rows_of_a_group(const MatmulArgs& a) { return a.offsets ? (int)(((long long)a.rows + a.groups - 1) / a.groups) : a.rows; }
+
 // Whether the copy engine can take a product's results out (boxes of a map of bytes): rows on its 16-byte grid, and the byte a row ends
 // at within the copy's 32-bit coordinates.
 inline bool results_by_copy(const MatmulArgs& a) {

@@ -375,7 +375,7 @@ bool rows_kernel_is_better(const MatmulArgs& a) {
 }  // namespace
 
 int launch_fp8_matmul(const MatmulArgs& a, cudaStream_t st) {
-  const int rows = a.offsets ? (a.rows + a.groups - 1) / a.groups : a.rows;  // of a group, on average
+  const int rows = rows_of_a_group(a);
   if (rows > 64 && !(a.offsets ? rows <= 128 : rows_kernel_is_better(a))) return launch_fp8_matmul_pair(a, st);
   if (a.gated) {
     if (rows <= 16) return launch_rows<16, 2, uint8_t>(a, st);

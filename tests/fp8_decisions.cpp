@@ -1,4 +1,4 @@
-// Decisions of the host about products whose sizes no test can run: which results the copy engine takes out.
+// Decisions of the host about products whose sizes no test can run: which results the copy engine takes out, rows of a group.
 #include <cstdio>
 
 #include "fp8_internal.h"
@@ -29,5 +29,18 @@ int main() {
         a.y = (void*)(4096 + type_bytes(t));
         check(!results_by_copy(a), "first row off the grid", a.N);
       }
+  // with groups the average chooses the kernel
+  const int32_t offsets[2] = {0, 0};
+  for (long long rows : {1ll, 1000ll, 1ll << 30, kMaxRows - 1000, kMaxRows})
+    for (int groups : {1, 2, 3, 256, 257, 700, kMaxExperts}) {
+      MatmulArgs a = {};
+      a.rows = (int)rows;
+      a.groups = groups;
+      a.offsets = offsets;
+      const long long n = rows_of_a_group(a);
+      check(n * groups >= rows && (n - 1) * groups < rows, "rows of a group", rows);
+      a.offsets = nullptr;
+      check(rows_of_a_group(a) == rows, "rows without groups", rows);
+    }
   return wrong ? 1 : 0;
 }
