@@ -110,6 +110,7 @@ PyObject* quantize(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     c.need(shaped(*s, (rows + block - 1) / block, blocks(cols)) && is_f32(*s), "scale");
     c.need(type_of(*x) >= 0 && type_of(*q) >= 0, "types");
     c.need(ld(*x) >= 0 && ld(*q) >= 0 && ld(*s) >= 0, "rows are not contiguous, or overlap");
+    c.need(cols <= INT32_MAX, "sizes", B2C_E_UNSUPPORTED);
     for (const at::Tensor* t : {x, q, s}) c.on_device(t);
     if (c.code == B2C_OK)
       c.code = p_quantize(x->data_ptr(), type_of(*x), rows, (int32_t)cols, ld(*x), (int)block, type_of(*q), q->data_ptr(), ld(*q),

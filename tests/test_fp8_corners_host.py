@@ -4,6 +4,11 @@ import os
 import re
 import subprocess
 
+import pytest
+import torch
+
+import paper_2104_04731_b200 as b2c
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CSRC = os.path.join(ROOT, "paper_2104_04731_b200", "csrc")
 
@@ -30,3 +35,26 @@ def test_decisions_about_large_sizes(tmp_path):
                            os.path.join(ROOT, "tests", "fp8_decisions.cpp"), "-o", exe])
     r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stdout + r.stderr
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2104_04731_b200 import build
+
+    build.build()
+    return b2c.load()
+
+
+def code_of(call, *args, **kw):
+    with pytest.raises(b2c.B2CError) as e:
+        call(*args, **kw)
+    return e.value.code
+
+
+@pytest.mark.parametrize("cols", [2 ** 31, 2 ** 32 + 64, 2 ** 33])
+@pytest.mark.parametrize("block", [1, 128])
+def test_quantize_refuses_more_columns_than_its_argument_holds(lib, cols, block):
+    """Tensors without memory: the sizes are refused before anything else is asked of them (2^32 + 64 columns were taken as 64)."""
+    x = torch.empty(1, cols, dtype=torch.bfloat16, device="meta")
+    q = torch.empty(1, cols, dtype=torch.float8_e4m3fn, device="meta")
+    assert code_of(b2c.fp8_quantize, x, q, torch.empty(1, -(-cols // 128), device="meta"), block_rows=block) == b2c.E_UNSUPPORTED
