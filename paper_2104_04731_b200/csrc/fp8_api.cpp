@@ -35,6 +35,7 @@ int experts_layout(const b2c_experts_desc* d, int64_t tokens, ExpertsLayout* l) 
   if (d->hidden < 16 || d->inter < 16 || d->hidden % 16 || d->inter % 16) return B2C_E_INVALID_ARG;
   if (d->experts < 1 || d->topk < 1 || d->topk > d->experts || !wide_type(d->type)) return B2C_E_INVALID_ARG;
   if (d->experts > kMaxExperts || d->topk > kMaxTopk || (long long)d->hidden * d->inter >= kMaxStride) return B2C_E_UNSUPPORTED;
+  if (d->hidden > kMaxCols || d->inter > kMaxCols) return B2C_E_UNSUPPORTED;
   if (tokens > kMaxRows / d->topk) return B2C_E_UNSUPPORTED;
   const size_t pairs = (size_t)tokens * d->topk;
   size_t at = 0;
@@ -65,7 +66,7 @@ int b2c_fp8_quantize(const void* x, int x_type, int64_t rows, int32_t cols, int6
   if (rows < 0 || cols < 1 || ldx < cols || ldq < cols || ld_scale < blocks_of(cols)) return B2C_E_INVALID_ARG;
   if (rows == 0) return B2C_OK;
   if (!x || !q || !scale || !aligned(x, type_bytes(x_type)) || !aligned(scale, 4)) return B2C_E_INVALID_ARG;
-  if (rows > kMaxRows || cols > (1 << 30)) return B2C_E_UNSUPPORTED;
+  if (rows > kMaxRows || cols > kMaxCols) return B2C_E_UNSUPPORTED;
   QuantizeArgs a = {};
   a.x = x;
   a.ldx = ldx;
@@ -87,7 +88,7 @@ int b2c_fp8_matmul(const b2c_matmul_desc* d, int64_t rows, const void* a, int64_
   if (!fp8_type(d->a_type) || !fp8_type(d->b_type) || !wide_type(d->y_type)) return B2C_E_INVALID_ARG;
   if (lda < d->K || lda % 16 || ld_a_scale < blocks_of(d->K) || ldy < d->N) return B2C_E_INVALID_ARG;
   if (d->groups > 1 && !offsets) return B2C_E_INVALID_ARG;
-  if (d->groups > kMaxExperts || rows > kMaxRows || d->N > (1 << 30) || d->K > (1 << 30)) return B2C_E_UNSUPPORTED;
+  if (d->groups > kMaxExperts || rows > kMaxRows || d->N > kMaxCols || d->K > kMaxCols) return B2C_E_UNSUPPORTED;
   // (strides that a tensor map can hold)
   if (lda >= kMaxStride || (long long)d->N * d->K >= kMaxStride || ldy * type_bytes(d->y_type) >= kMaxStride) return B2C_E_UNSUPPORTED;
   if (rows == 0) return B2C_OK;
@@ -150,7 +151,7 @@ int b2c_route_combine(const void* y, int y_type, int64_t y_rows, int64_t ldy, co
                       int32_t topk, int32_t cols, void* out, int out_type, int64_t ldo, void* cuda_stream) {
   if (!wide_type(y_type) || !wide_type(out_type) || tokens < 0 || y_rows < 0 || topk < 1 || cols < 1 || ldy < cols || ldo < cols)
     return B2C_E_INVALID_ARG;
-  if (topk > kMaxTopk || tokens > kMaxRows || cols > (1 << 30)) return B2C_E_UNSUPPORTED;
+  if (topk > kMaxTopk || tokens > kMaxRows || cols > kMaxCols) return B2C_E_UNSUPPORTED;
   if (tokens == 0) return B2C_OK;
   if ((!y && y_rows > 0) || !rows || !weights || !out || !aligned(y, type_bytes(y_type)) || !aligned(rows, 4) || !aligned(weights, 4) ||
       !aligned(out, type_bytes(out_type)))

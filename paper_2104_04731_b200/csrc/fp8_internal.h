@@ -13,6 +13,7 @@ constexpr int kMaxExperts = 1024;  // groups of a product, experts of a route
 constexpr int kMaxTopk = 32;
 constexpr int kMaxRouteGroups = 32;
 constexpr long long kMaxRows = 0x7FFFFF00LL;  // rows of one call: tile origins stay inside 32 bits
+constexpr int kMaxCols = 1 << 30;  // columns and reduction lengths: so do the columns that a tile rounds up to
 constexpr long long kMaxStride = 1ll << 40;  // bytes; tensor maps hold no more
 constexpr float kMinAmax = 0x1p-100f;         // a block's largest magnitude counts as at least this much
 

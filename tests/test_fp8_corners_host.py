@@ -1,4 +1,5 @@
 """What of the 8-bit float operators can be checked without a device: sources, decisions of the host, refusals."""
+import ctypes
 import glob
 import os
 import re
@@ -58,3 +59,15 @@ def test_quantize_refuses_more_columns_than_its_argument_holds(lib, cols, block)
     x = torch.empty(1, cols, dtype=torch.bfloat16, device="meta")
     q = torch.empty(1, cols, dtype=torch.float8_e4m3fn, device="meta")
     assert code_of(b2c.fp8_quantize, x, q, torch.empty(1, -(-cols // 128), device="meta"), block_rows=block) == b2c.E_UNSUPPORTED
+
+
+@pytest.mark.parametrize("hidden,inter", [(2 ** 31 - 16, 16), (16, 2 ** 31 - 16), (2 ** 30 + 16, 16), (16, 2 ** 30 + 16)])
+def test_experts_refuse_what_the_products_refuse(lib, hidden, inter):
+    """Columns of a tile past the last one are numbers of 32 bits too; the products take 2^30 columns at most."""
+    n = ctypes.c_size_t()
+    d = b2c.ExpertsDesc(hidden, inter, 4, 2, b2c.BF16)
+    assert lib.b2c_experts_workspace_bytes(ctypes.byref(d), 8, ctypes.byref(n)) == b2c.E_UNSUPPORTED
+    p = 1 << 20
+    assert lib.b2c_fp8_experts(ctypes.byref(d), 8, p, hidden, p, p, p, p, p, p, p, hidden, p, None) == b2c.E_UNSUPPORTED
+    d = b2c.ExpertsDesc(2 ** 30, 16, 4, 2, b2c.BF16)
+    assert lib.b2c_experts_workspace_bytes(ctypes.byref(d), 8, ctypes.byref(n)) == b2c.OK
