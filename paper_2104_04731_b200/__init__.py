@@ -7,6 +7,7 @@ There is no fallback: if the shared library is missing, ``load()`` raises.
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 from typing import List, Optional, Tuple
 
@@ -353,7 +354,7 @@ def measure_mma_rate_pair(tile_n: int = 256, mmas_per_pair: int = 20000, stream=
 
 # ---- 8-bit float operators ----------------------------------------------------------------------------------------------
 #
-# Tensors are checked and handed over by a small native module (_binding.so): shapes, types, strides and devices, which the library
+# Tensors are checked and handed over by a small native module (_binding-*.so): shapes, types, strides and devices, which the library
 # does not see.  What it refuses is raised as B2CError(E_INVALID_ARG) and the like before anything is launched.
 
 _native = None
@@ -365,12 +366,18 @@ def _load_native():
         lib = load()
         import torch  # noqa: F401  (its libraries have to be there first)
 
-        from . import _binding
+        from .build import binding_path
 
-        _binding.bind(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in (
+        path = binding_path()
+        if not os.path.exists(path):
+            raise ImportError("%s is not built (python -m %s.build)" % (os.path.basename(path), __name__))
+        spec = importlib.util.spec_from_file_location(__name__ + "._binding", path)
+        binding = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(binding)
+        binding.bind(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in (
             "b2c_fp8_quantize", "b2c_fp8_matmul", "b2c_route", "b2c_route_sort_workspace_bytes", "b2c_route_sort", "b2c_route_combine",
             "b2c_experts_workspace_bytes", "b2c_fp8_experts")))
-        _native = _binding
+        _native = binding
     return _native
 
 

@@ -1,6 +1,8 @@
 """Builds libb2conv.so in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
 from __future__ import annotations
 
+import importlib.metadata
+import importlib.util
 import os
 import subprocess
 import sys
@@ -14,7 +16,17 @@ SOURCES = ["api.cpp", "planner.cpp", "tma.cpp", "layout.cu", "conv_mma.cu", "con
            "fp8_api.cpp", "fp8_quantize.cu", "fp8_matmul.cu", "fp8_matmul_pair.cu", "route.cu"]
 
 
-BINDING = os.path.join(HERE, "_binding.so")  # tensor checks of the 8-bit float operators, against torch's headers
+def binding_path() -> str:
+    """Module with the tensor checks of the 8-bit float operators.  It is compiled against the headers of torch and the interpreter, and its
+    name says which: after a change of either there is no file to load until it is built again."""
+    try:
+        torch_version = importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:  # (not installed as a package)
+        import torch
+
+        torch_version = torch.__version__
+    tag = "%s-torch-%s" % (sys.implementation.cache_tag, torch_version)
+    return os.path.join(HERE, "_binding-%s.so" % "".join(c if c.isalnum() or c in "-." else "_" for c in tag))
 
 
 def _nvcc() -> str:
@@ -47,17 +59,25 @@ def binding_command(out: str) -> list:
 
 def build_binding(force: bool = False) -> str:
     deps = [os.path.join(CSRC, "binding.cpp"), os.path.join(ROOT, "include", "b2conv.h")]
-    if not force and os.path.exists(BINDING) and all(os.path.getmtime(d) <= os.path.getmtime(BINDING) for d in deps):
-        return BINDING
-    tmp = BINDING + ".tmp.%d" % os.getpid()
+    so = binding_path()
+    if not force and os.path.exists(so) and all(os.path.getmtime(d) <= os.path.getmtime(so) for d in deps):
+        return so
+    tmp = so + ".tmp.%d" % os.getpid()
     subprocess.check_call(binding_command(tmp))
-    os.replace(tmp, BINDING)
-    return BINDING
+    os.replace(tmp, so)
+    return so
 
 
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
+    """The library first: it needs nvcc alone.  Then the binding, where there is a torch to bind to."""
+    so = build_library(force, verbose, debug)
+    if importlib.util.find_spec("torch") is not None:
+        build_binding(force and not debug)
+    return so
+
+
+def build_library(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
     so = SO_DEBUG if debug else SO
-    build_binding(force and not debug)
     if not force and not needs_build(so):
         return so
     cmd = [

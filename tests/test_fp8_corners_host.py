@@ -71,3 +71,34 @@ def test_experts_refuse_what_the_products_refuse(lib, hidden, inter):
     assert lib.b2c_fp8_experts(ctypes.byref(d), 8, p, hidden, p, p, p, p, p, p, p, hidden, p, None) == b2c.E_UNSUPPORTED
     d = b2c.ExpertsDesc(2 ** 30, 16, 4, 2, b2c.BF16)
     assert lib.b2c_experts_workspace_bytes(ctypes.byref(d), 8, ctypes.byref(n)) == b2c.OK
+
+
+def test_binding_goes_with_its_torch_and_interpreter(lib, monkeypatch):
+    """It reads torch's objects, so one that was compiled for another torch or interpreter is neither kept by the build nor loaded."""
+    from paper_2104_04731_b200 import build
+
+    here = build.build_binding()
+    assert os.path.exists(here) and build.build_binding() == here
+    commands = []
+    monkeypatch.setattr(build.subprocess, "check_call", commands.append)
+    monkeypatch.setattr(build.os, "replace", lambda a, b: None)
+    version = build.importlib.metadata.version
+    monkeypatch.setattr(build.importlib.metadata, "version", lambda name: "9.9.9" if name == "torch" else version(name))
+    assert build.build_binding() != here and len(commands) == 1
+    monkeypatch.setattr(b2c, "_native", None)
+    with pytest.raises(ImportError):
+        b2c.fp8_quantize(None, None, None)
+
+
+def test_library_needs_no_torch(monkeypatch):
+    """nvcc's part comes first, and is all there is without a torch."""
+    from paper_2104_04731_b200 import build
+
+    commands, replaced = [], []
+    monkeypatch.setattr(build.subprocess, "check_call", lambda c: commands.append(os.path.basename(c[0])))
+    monkeypatch.setattr(build.os, "replace", lambda a, b: replaced.append(b))
+    assert build.build(force=True) == build.SO
+    assert commands == ["nvcc", "g++"] and replaced[0] == build.SO
+    commands.clear()
+    monkeypatch.setattr(build.importlib.util, "find_spec", lambda name: None)
+    assert build.build(force=True) == build.SO and commands == ["nvcc"]
