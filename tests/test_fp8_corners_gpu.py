@@ -38,3 +38,43 @@ def test_experts_slots_that_cancel(lib, tokens, xt):
     assert lib.fp8_status() == lib.OK
     want = 784.0 * (1.0 + (n % 8).float()) * w[:, :1]
     assert torch.equal(y, want.to(xt))
+
+
+# ---- runs by the sum of their two largest choices ----------------------------------------------------------------------------------
+
+
+def check_choice(lib, x, topk, kind, groups, topk_groups, bias=None):
+    """Experts as in 64 bits, for every token."""
+    w = torch.empty(x.shape[0], topk, device="cuda")
+    ids = torch.full((x.shape[0], topk), -9, dtype=torch.int32, device="cuda")
+    d = lib.make_route_desc(x.shape[1], topk, lib.SCORE_SOFTMAX if kind == "softmax" else lib.SCORE_SIGMOID, groups, topk_groups, lib.GROUP_TOP2)
+    lib.route(d, x, w, ids, bias=bias)
+    _, want = ref.route(x, topk, kind, groups, topk_groups, "top2", bias=bias)
+    wrong = (ids.cpu() != want).any(-1).nonzero().flatten().tolist()
+    assert not wrong, (len(wrong), wrong[0], ids[wrong[0]], want[wrong[0]])
+
+
+RUNS = [(32, 16, 5), (64, 8, 4), (64, 32, 6), (60, 20, 4), (256, 8, 4), (256, 32, 4), (512, 16, 3), (1024, 32, 7)]
+
+
+@pytest.mark.parametrize("xt", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts,groups,topk_groups", RUNS)
+def test_runs_of_small_scores(lib, experts, groups, topk_groups, kind, xt):
+    """No bias, scores from e^-5 to e^-130: what 32 bits hold with few bits or not at all still decides between runs."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(experts + groups)
+    for below in (5.0, 20.0, 60.0, 80.0, 88.0, 95.0, 100.0, 103.0, 130.0):
+        x = torch.randn(120, experts, generator=g, device="cuda") * 1.5 - below
+        if kind == "softmax":
+            x[:, 3] = 0.0
+        check_choice(lib, x.to(xt), 3, kind, groups, topk_groups)
+
+
+@pytest.mark.parametrize("kind,runs", [("sigmoid", [(-87.0, -88.5), (-87.4, -87.4)]), ("softmax", [(-103.9, -103.9), (-102.95, -200.0)])])
+def test_two_runs_of_small_scores(lib, kind, runs):
+    x = torch.full((1, 32), -300.0, device="cuda")
+    x[0, 0] = 0.0 if kind == "softmax" else -300.0
+    for i, pair in enumerate(runs):
+        x[0, 8 * (i + 1):8 * (i + 1) + 2] = torch.tensor(pair)
+    check_choice(lib, x, 2, kind, 4, 2 if kind == "softmax" else 1)
