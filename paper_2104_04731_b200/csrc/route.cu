@@ -215,7 +215,13 @@ __device__ __forceinline__ int choose32(const b2c_route_desc& d, int rounds, con
       const float low = key_value(__reduce_min_sync(kAll, kept ? mine : 0xFFFFFFFFu));
       const unsigned high = __reduce_max_sync(kAll, kept ? 0u : mine);
       if constexpr (PARTS) near->runs = high != 0u && !(low >= 0x1p-100f && low - key_value(high) > unit * low);
-      else near->runs = high != 0u && !(low - key_value(high) > 2.0f * unit * (1.0f + fabsf(low)));
+      else {
+        // (a sum is off by the errors of its addends, which may be far larger than itself; sums that stand for the largest value, or with
+        // the lowest one, are what they are)
+        const bool adds = two && run < d.groups && fabsf(score) < kHuge;
+        const float addend = __uint_as_float(__reduce_max_sync(kAll, adds ? __float_as_uint(fmaxf(fabsf(first), fabsf(second))) : 0u));
+        near->runs = high != 0u && !(low - key_value(high) > 2.0f * unit * (1.0f + fmaxf(fabsf(low), addend)));
+      }
       if (!PARTS) near->runs |= __any_sync(kAll, two && first >= kHuge && second <= -kHuge);
     }
     open = __ballot_sync(kAll, kept);
@@ -336,12 +342,13 @@ __device__ __forceinline__ int order64(double choice, int id, int count, int lan
 }
 
 // One warp for one token, everything in registers.  Scores are monotonic in the logits, so without a bias the logits themselves are
-// compared, which is exact.  With a bias (or run scores that are sums) the choices are formed in 32 bits: exponential, sum, quotient
-// and additions put each off by at most 7 units of 2^-24 * (1 + |choice|), its place in the key's lowest bits by P - 1 units of 2^-23,
-// together less than 2^-19 for P <= 8 and 2^-17 beyond, and sums of two by twice that.  A token in which two choices that decide
+// compared, which is exact.  With a bias (or run scores that are sums) the choices are formed in 32 bits: exponential, quotient and
+// additions put each off by at most 6 units of 2^-24 * (1 + |choice|), with the sum of a softmax by 12 + P / 4, its place in the key's lowest
+// bits by P - 1 units of 2^-23, together less than 2^-19 for P <= 8 and 2^-17 beyond, and sums of two by that of both, however small they
+// are.  A token in which two choices that decide
 // something are not further apart than twice this (about one in fifty at 256 experts) needs a second look: where only the order of the
-// topk + 1 first is open, these few are compared in 64 bits; else all are chosen again with the places beside the values (2^-20), and
-// where that does not settle it, or if the scores hang on all logits, the token is done in 64 bits from the start.  (All such tokens
+// topk + 1 first is open, these few are compared in 64 bits; else all are chosen again with the places beside the values (2^-20, with a softmax
+// 2^-18), and where that does not settle it, or if the scores hang on all logits, the token is done in 64 bits from the start.  (All such tokens
 // chosen again: 26.2 us for the work below, now 25.7; none looked at twice, which is wrong: 22.)
 // Memory-bound on paper (one read of the logits); what it spends are the instructions of exponentials, sort and topk rounds (16384 tokens
 // of 256 experts, 8 of 4 of 8 runs: 26 us, issue slots 73 % busy, against 2.8 us for the bytes).  Two tokens a warp, 16 lanes each, took
@@ -464,7 +471,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps, P <= 8 ? 5 : 1) route_kernel
       id = choose32<P, unsigned, true, false>(a.d, rounds, c, c, part_of, lane, P <= 8 ? 0x1p-18f : 0x1p-16f, &near);
       if (near.runs || near.inside || (near.border && !further)) {
         if (near.runs || (near.border && (near.last || !further)))
-          id = choose32<P, unsigned long long, true, false>(a.d, rounds, c, c, part_of, lane, 0x1p-20f, &near);
+          id = choose32<P, unsigned long long, true, false>(a.d, rounds, c, c, part_of, lane, softmax ? 0x1p-18f : 0x1p-20f, &near);
         if (near.runs || (near.border && (near.last || !further)) || (softmax && near.inside)) {
           id = choose64<T, P>(a, row, lane, mx);
         } else if (near.inside) {

@@ -78,3 +78,20 @@ def test_two_runs_of_small_scores(lib, kind, runs):
     for i, pair in enumerate(runs):
         x[0, 8 * (i + 1):8 * (i + 1) + 2] = torch.tensor(pair)
     check_choice(lib, x, 2, kind, 4, 2 if kind == "softmax" else 1)
+
+
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts,groups,topk_groups", RUNS)
+def test_runs_with_large_biases_of_both_signs(lib, experts, groups, topk_groups, kind):
+    """The two largest choices of a run cancel: their sum is of the size of the scores, its error of the size of the biases."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(experts)
+    x = torch.randn(300, experts, generator=g, device="cuda") * 1.5
+    size = experts // groups
+    for large in (1e2, 1e3, 1e4, 1e6):
+        bias = torch.full((groups, size), -large, device="cuda")
+        bias[:, size // 2] = large
+        check_choice(lib, x, 3, kind, groups, topk_groups, bias.reshape(-1).contiguous())
+        # a few runs of that kind among others; sums of ordinary choices near to them
+        bias[::3] = 0.01 * torch.randn(bias[::3].shape, generator=g, device="cuda")
+        check_choice(lib, x, 3, kind, groups, topk_groups, bias.reshape(-1).contiguous())
