@@ -175,9 +175,13 @@ __device__ __forceinline__ uint4 quantize16(const BlockScale& b, const float* v)
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// (the quotient within two units of rounding instead of a half: five operations instead of some twenty, and 64 of them stand
-// between the last MMA of a tile and the next one's; a denominator beyond 2^126 gives 0, as it should)
-__device__ __forceinline__ float silu(float v) { return __fdividef(v, 1.0f + expf(-v)); }
+// silu(v) = v / (1 + e^-v), for negative v as v e^v / (1 + e^v): the divisor stays between one and two (1 + e^-v leaves the range of the
+// quotient below v = -87, where v e^v has not left that of fp32).  The quotient within two units of rounding instead of a half: seven
+// operations instead of some twenty, and 64 of them stand between the last MMA of a tile and the next one's.
+__device__ __forceinline__ float silu(float v) {
+  const float e = expf(-fabsf(v));
+  return __fdividef(v < 0.0f ? v * e : v, 1.0f + e);
+}
 
 }  // namespace
 }  // namespace b2c

@@ -95,3 +95,33 @@ def test_runs_with_large_biases_of_both_signs(lib, experts, groups, topk_groups,
         # a few runs of that kind among others; sums of ordinary choices near to them
         bias[::3] = 0.01 * torch.randn(bias[::3].shape, generator=g, device="cuda")
         check_choice(lib, x, 3, kind, groups, topk_groups, bias.reshape(-1).contiguous())
+
+
+@pytest.mark.parametrize("tokens", [1, 30, 150])
+def test_experts_gates_far_below_zero(lib, tokens):
+    """silu(v) = v / (1 + e^-v) of gates where 1 + e^-v does not fit into 32 bits or hardly does, with up values that bring h back.
+
+    Gates, ups and the second product are exact, so what is left of the error is the logistic function's: the exponential to two units of its last
+    place (steps of 2^-149 once it is subnormal), sum, quotient (two units) and two products; then amax / 448 and its product with 448."""
+    num = torch.tensor([3 / 16, 25 / 128, 103 / 512, 27 / 128, 115 / 512, -27 / 128], dtype=torch.float64, device="cuda")
+    E, H = num.numel(), 128
+    gate = -448 * num                                        # -84, -87.5, -90.125, -94.5, -100.625, 94.5
+    x = torch.zeros(E * tokens, H, device="cuda")
+    x[:, 0] = 448.0                                          # scale 1
+    w1 = torch.zeros(E, 2, H, H, device="cuda")
+    w1[:, 0, :, 0], w1[:, 1, :, 0] = -1.0, 1.0
+    s1 = torch.ones(E, 2, 1, 1, device="cuda")
+    s1[:, 0, 0, 0] = num.float()
+    s1[:5, 1] = 2.0 ** 90
+    w2 = torch.zeros(E, H, H, device="cuda")
+    w2[:, :, 5] = 1.0
+    ids = (torch.arange(E * tokens, dtype=torch.int32, device="cuda") % E)[:, None].contiguous()
+    w = torch.ones(E * tokens, 1, device="cuda")
+    y = torch.full((E * tokens, H), math.nan, device="cuda")
+    ws = torch.empty(lib.experts_workspace_bytes(H, H, E, 1, E * tokens, dtype=lib.F32), dtype=torch.uint8, device="cuda")
+    lib.fp8_experts(x, ids, w, w1.to(E4), s1, w2.to(E4), torch.ones(E, 1, 1, device="cuda"), y, ws)
+    assert lib.fp8_status() == lib.OK
+    want = gate / (1 + torch.exp(-gate)) * 448 * s1[:, 1, 0, 0].double()
+    error = 2 * torch.where(gate < 0, 2.0 ** -149 / torch.exp(gate), 0.0) + 12 * 2.0 ** -23
+    e = ids[:, 0].long()
+    assert bool(((y.double() - want[e][:, None]).abs() <= (error * want.abs())[e][:, None]).all()), (y[:E, 0], want)
