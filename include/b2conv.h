@@ -456,6 +456,11 @@ int b2c_fp8_experts(const b2c_experts_desc* desc, int64_t tokens, const void* x_
  * for the device to be idle; not to be called while a stream is being captured. */
 int b2c_fp8_status(int32_t* status);
 
+/* Failure-detection self-test, as b2c_selftest_bounded_wait, of the products' kernels (form 0: few rows, 1: many
+ * rows): waits on barriers nothing completes give up after about one second, record B2C_E_TIMEOUT for
+ * b2c_fp8_status, and the kernel returns normally. */
+int b2c_selftest_fp8_wait(int form, void* cuda_stream);
+
 /* ---- debug build (no counterpart in the paper) ---------------------------------------------------
  * libb2conv_debug.so is the same library compiled with -DB2C_DEBUG_BOUNDS.  In it every address a
  * kernel computes by hand (loads of x, stores and atomics to the outputs and to the scratch; TMA

@@ -41,7 +41,7 @@ EXPORTS = [
     "b2c_last_cuda_error", "b2c_oneshot_status", "b2c_oneshot_cache_clear", "b2c_test_fail_nth_encode", "b2c_selftest_pack_wait", "b2c_measure_mma_rate", "b2c_measure_mma_rate_pair", "b2c_debug_build", "b2c_plan_debug_info",
     "b2c_plan_check_canaries", "b2c_test_shrink_checked_ranges", "b2c_test_kernel_of",
     "b2c_fp8_quantize", "b2c_fp8_matmul", "b2c_route", "b2c_route_sort_workspace_bytes", "b2c_route_sort", "b2c_route_combine",
-    "b2c_experts_workspace_bytes", "b2c_fp8_experts", "b2c_fp8_status",
+    "b2c_experts_workspace_bytes", "b2c_fp8_experts", "b2c_fp8_status", "b2c_selftest_fp8_wait",
 ]
 
 
@@ -150,6 +150,7 @@ def load():
     lib.b2c_experts_workspace_bytes.argtypes = [px, i64, pz]
     lib.b2c_fp8_experts.argtypes = [px, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp]
     lib.b2c_fp8_status.argtypes = [pi32]
+    lib.b2c_selftest_fp8_wait.argtypes = [i32, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name not in ("b2c_plan_destroy", "b2c_status_string"):
@@ -457,6 +458,11 @@ def fp8_status() -> int:
     s = ctypes.c_int32()
     _check(load().b2c_fp8_status(ctypes.byref(s)), "b2c_fp8_status")
     return s.value
+
+
+def selftest_fp8_wait(form: int, stream=None):
+    """Enqueues a bounded wait that cannot complete, of the products for few rows (form 0) or many (1); fp8_status then reports E_TIMEOUT."""
+    _check(load().b2c_selftest_fp8_wait(form, _stream_ptr(stream)), "b2c_selftest_fp8_wait")
 
 
 def debug_build() -> bool:

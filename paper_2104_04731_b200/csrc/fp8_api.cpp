@@ -254,4 +254,9 @@ int b2c_fp8_status(int32_t* status) {
   return fp8_status_read_and_clear(status);
 }
 
+int b2c_selftest_fp8_wait(int form, void* cuda_stream) {
+  if (form != 0 && form != 1) return B2C_E_INVALID_ARG;
+  return from_cuda(form == 0 ? fp8_rows_wait_selftest((cudaStream_t)cuda_stream) : fp8_pair_wait_selftest((cudaStream_t)cuda_stream));
+}
+
 }  // extern "C"

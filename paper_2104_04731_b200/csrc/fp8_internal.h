@@ -87,6 +87,8 @@ int launch_fp8_matmul_pair(const MatmulArgs& a, cudaStream_t st);  // its form f
 long long pair_cycles(const MatmulArgs& a);  // what it takes without groups, in SM cycles
 cudaError_t fp8_pair_status(int* status);
 int fp8_status_read_and_clear(int32_t* status);
+cudaError_t fp8_rows_wait_selftest(cudaStream_t st);
+cudaError_t fp8_pair_wait_selftest(cudaStream_t st);
 cudaError_t launch_route(const RouteArgs& a, cudaStream_t st);
 size_t route_sort_workspace(long long pairs, int experts);
 cudaError_t launch_route_sort(const int32_t* ids, long long pairs, int experts, int32_t* offsets, int32_t* rows,

@@ -387,6 +387,8 @@ int launch_fp8_matmul(const MatmulArgs& a, cudaStream_t st) {
   return launch_rows_type<64>(a, st);
 }
 
+cudaError_t fp8_rows_wait_selftest(cudaStream_t st) { return launch_wait_selftest(st); }
+
 int fp8_status_read_and_clear(int32_t* status) {
   int rows = 0, pair = 0;
   cudaError_t e = cudaDeviceSynchronize();

@@ -610,6 +610,8 @@ int launch_fp8_matmul_pair(const MatmulArgs& a, cudaStream_t st) {
   return tile_cycles(a, 128) < tile_cycles(a, 256) ? launch_type<2, 128>(a, st) : launch_type<2, 256>(a, st);
 }
 
+cudaError_t fp8_pair_wait_selftest(cudaStream_t st) { return launch_wait_selftest(st); }
+
 cudaError_t fp8_pair_status(int* status) { return take_status(status); }
 
 }  // namespace b2c

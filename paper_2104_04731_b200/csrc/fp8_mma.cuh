@@ -120,6 +120,22 @@ __device__ __forceinline__ bool mbar_wait_inline(uint32_t bar, uint32_t parity, 
   return true;
 }
 
+// Each form of the wait, in a block of its own, on a barrier that nothing completes.
+__global__ void __launch_bounds__(32) wait_selftest_kernel() {
+  __shared__ SharedCtl ctl;
+  if (threadIdx.x == 0) {
+    mbar_init(smem_u32(&ctl.full[0]), 1);
+    ctl.abort_flag = 0;
+  }
+  __syncthreads();
+  const bool ok = blockIdx.x == 0 ? mbar_wait(smem_u32(&ctl.full[0]), 0, &ctl, &g_fp8_status) : mbar_wait_inline(smem_u32(&ctl.full[0]), 0, &ctl, &g_fp8_status);
+  if (__any_sync(0xffffffffu, ok)) atomicExch(&g_fp8_status, B2C_E_NOT_READY);  // (cannot be)
+}
+inline cudaError_t launch_wait_selftest(cudaStream_t st) {
+  wait_selftest_kernel<<<2, 32, 0, st>>>();
+  return cudaGetLastError();
+}
+
 // Row tile `index` over all groups, each group's rows cut into tiles of `tile` rows; called by a whole warp.  Offsets are
 // clamped to [0, rows] and never fall, so the groups are disjoint and their tiles at most rows / tile + groups.
 struct RowTile {

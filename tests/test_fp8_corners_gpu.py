@@ -125,3 +125,19 @@ def test_experts_gates_far_below_zero(lib, tokens):
     error = 2 * torch.where(gate < 0, 2.0 ** -149 / torch.exp(gate), 0.0) + 12 * 2.0 ** -23
     e = ids[:, 0].long()
     assert bool(((y.double() - want[e][:, None]).abs() <= (error * want.abs())[e][:, None]).all()), (y[:E, 0], want)
+
+
+# ---- failure detection -------------------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("form,rows", [(0, 5), (1, 600)])
+def test_bounded_wait_reports_timeout_and_products_stay_usable(lib, form, rows):
+    """A wait that cannot complete ends by itself, is reported once, and the kernels run on."""
+    lib.selftest_fp8_wait(form)
+    assert lib.fp8_status() == lib.E_TIMEOUT
+    assert lib.fp8_status() == lib.OK
+    a = torch.randint(-3, 4, (rows, 256), device="cuda").float()
+    b = torch.randint(-3, 4, (200, 256), device="cuda").float()
+    y = torch.empty(rows, 200, device="cuda")
+    lib.fp8_matmul(a.to(E4), torch.ones(rows, 2, device="cuda"), b.to(E4), torch.ones(2, 2, device="cuda"), y)
+    assert torch.equal(y, a @ b.t()) and lib.fp8_status() == lib.OK

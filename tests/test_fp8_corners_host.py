@@ -102,3 +102,8 @@ def test_library_needs_no_torch(monkeypatch):
     commands.clear()
     monkeypatch.setattr(build.importlib.util, "find_spec", lambda name: None)
     assert build.build(force=True) == build.SO and commands == ["nvcc"]
+
+
+def test_selftest_refuses_forms_that_are_none(lib):
+    assert lib.b2c_selftest_fp8_wait(2, None) == b2c.E_INVALID_ARG
+    assert lib.b2c_selftest_fp8_wait(-1, None) == b2c.E_INVALID_ARG
