@@ -248,6 +248,12 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, RowsShape<NT, WT>
     while (global_ns() - t0 < 50000ull) __nanosleep(1000);
     __syncthreads();
   }
+  // Tensor memory goes back before the blocks of the cluster wait for each other: one that held it could wait for one that waits for it,
+  // where a pair kernel of another stream has asked for the same columns in between.
+  if (warp == 1) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_acc), "r"(S::kTmemCols) : "memory");
+  }
   if (split > 1) cluster_sync();
   if (group >= 0) {
     // one warp takes one activation row: each lane four neighbouring columns
@@ -298,10 +304,6 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, RowsShape<NT, WT>
   // no block leaves while another reads its sums, and none before the kernel ahead has ended: what comes after this one relies on that
   if (early) pdl_wait();
   if (split > 1) cluster_sync();
-  if (warp == 1) {
-    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_acc), "r"(S::kTmemCols) : "memory");
-  }
 }
 
 int fail(cudaError_t e) {

@@ -28,6 +28,14 @@ def test_results_of_waits_are_voted():
     assert waits >= 10
 
 
+def test_tensor_memory_goes_back_before_a_cluster_meets():
+    """A block of the few-rows kernel that waits for the others of its cluster holds none: with another stream's kernel between them, a
+    circle of blocks that hold some and blocks that wait for some would not end."""
+    source = open(os.path.join(CSRC, "fp8_matmul.cu")).read()
+    kernel = source[source.index("matmul_rows_kernel(const"):]
+    assert 0 < kernel.index("tcgen05.alloc") < kernel.index("tcgen05.dealloc") < kernel.index("cluster_sync()")
+
+
 def test_decisions_about_large_sizes(tmp_path):
     """Sizes that no test can run (results of more than 2 GiB a row): what the host decides about them, as a small program."""
     exe = str(tmp_path / "fp8_decisions")
