@@ -343,7 +343,7 @@ __device__ __forceinline__ int order64(double choice, int id, int count, int lan
 
 // One warp for one token, everything in registers.  Scores are monotonic in the logits, so without a bias the logits themselves are
 // compared, which is exact.  With a bias (or run scores that are sums) the choices are formed in 32 bits: exponential, quotient and
-// additions put each off by at most 6 units of 2^-24 * (1 + |choice|), with the sum of a softmax by 12 + P / 4, its place in the key's lowest
+// additions put each off by at most 6 units of 2^-24 * (1 + |choice|), with the sum of a softmax by 11, its place in the key's lowest
 // bits by P - 1 units of 2^-23, together less than 2^-19 for P <= 8 and 2^-17 beyond, and sums of two by that of both, however small they
 // are.  A token in which two choices that decide
 // something are not further apart than twice this (about one in fifty at 256 experts) needs a second look: where only the order of the
@@ -408,23 +408,23 @@ __global__ void __launch_bounds__(32 * kRouteWarps, P <= 8 ? 5 : 1) route_kernel
   using LogitKey = typename std::conditional<sizeof(T) == 2, unsigned, unsigned long long>::type;
   if (by_logit && !sums) {
     if (softmax && !a.d.renormalise) {
-      float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // (four: a sum of 32 in a row would be off by up to 31 roundings)
+      // (in 64 bits from the start: 1024 scores of one size put 32-bit partial sums off by a rounding each, always the same way)
 #pragma unroll
-      for (int i = 0; i < P; ++i) sum[i & 3] += x[i] == -INFINITY ? 0.0f : (x[i] == mx ? 1.0f : expf(x[i] - mx));
-      all = warp_sum((double)((sum[0] + sum[1]) + (sum[2] + sum[3])));
+      for (int i = 0; i < P; ++i) all += (double)(x[i] == -INFINITY ? 0.0f : (x[i] == mx ? 1.0f : expf(x[i] - mx)));
+      all = warp_sum(all);
     }
     id = choose32<P, LogitKey, false, false>(a.d, a.d.topk, x, x, [&](int e) { return logit<T>(row, e); }, lane, 0.0f, &near);
   } else {
     float c[P];
-    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       if (softmax) c[i] = x[i] == -INFINITY ? 0.0f : (x[i] == mx ? 1.0f : expf(x[i] - mx));
       else c[i] = __fdividef(1.0f, 1.0f + __expf(-x[i]));
-      sum[i & 3] += c[i];
     }
     if (softmax) {
-      all = warp_sum((double)((sum[0] + sum[1]) + (sum[2] + sum[3])));
+#pragma unroll
+      for (int i = 0; i < P; ++i) all += (double)c[i];
+      all = warp_sum(all);
 #pragma unroll
       for (int i = 0; i < P; ++i) c[i] = all > 0.0 ? __fdividef(c[i], (float)all) : 0.0f;
     }

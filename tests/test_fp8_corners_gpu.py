@@ -141,3 +141,25 @@ def test_bounded_wait_reports_timeout_and_products_stay_usable(lib, form, rows):
     y = torch.empty(rows, 200, device="cuda")
     lib.fp8_matmul(a.to(E4), torch.ones(rows, 2, device="cuda"), b.to(E4), torch.ones(2, 2, device="cuda"), y)
     assert torch.equal(y, a @ b.t()) and lib.fp8_status() == lib.OK
+
+
+# ---- weights -----------------------------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("experts", [512, 600, 1000, 1024])
+def test_weights_of_a_flat_softmax(lib, experts):
+    """Very many scores of about the same size: every one of them may add a rounding to the sum that the weights are divided by.  Tolerance: eight
+    units of 2^-24, as for all weights; two each for the exponentials in the sum and the weight's own, one each for the sum's and the quotient's
+    rounding to 32 bits."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(experts)
+    d = lib.make_route_desc(experts, 8, lib.SCORE_SOFTMAX, renormalise=False)
+    for below in torch.linspace(0.0, 16.0, 33).tolist():
+        x = torch.randn(2000, experts, generator=g, device="cuda") * 0.001 - below
+        x[:, 7] = 0.0
+        w = torch.empty(2000, 8, device="cuda")
+        ids = torch.empty(2000, 8, dtype=torch.int32, device="cuda")
+        lib.route(d, x, w, ids)
+        want = torch.softmax(x.double(), -1).gather(1, ids.long())
+        off = (w.double() - want).abs() / want
+        assert float(off.max()) <= 8 * 2.0 ** -24, (below, float(off.max()) * 2 ** 24)
