@@ -151,8 +151,8 @@ struct Near {
 // choose_exact() for 32-bit choices: every lane sorts its own once, a round compares the lanes' first ones.  Lane j < rounds gets the
 // j-th expert.  With CHECK the choices may be off by half of `unit` * (1 + |choice|), and *near tells what that leaves open.  With PARTS
 // the runs are scored by other values than the experts: scores without a bias, off by less than half of `unit` of themselves from 2^-100
-// on; below that 32 bits hold their addends with fewer bits or not at all, and the runs are left open.  32-bit
-// keys without CHECK are for values whose lowest bits are zero (16-bit logits): the place fits into them.
+// on, and never by more than 2^-20; below that 32 bits hold their addends with fewer bits or not at all, and the runs are left open.
+// 32-bit keys without CHECK are for values whose lowest bits are zero (16-bit logits): the place fits into them.
 template <int P, typename K, bool CHECK, bool PARTS, typename F>
 __device__ __forceinline__ int choose32(const b2c_route_desc& d, int rounds, const float (&choice)[P], const float (&part)[P], F part_of, int lane,
                                         float unit, Near* near) {
@@ -214,7 +214,7 @@ __device__ __forceinline__ int choose32(const b2c_route_desc& d, int rounds, con
     if constexpr (CHECK || PARTS) {
       const float low = key_value(__reduce_min_sync(kAll, kept ? mine : 0xFFFFFFFFu));
       const unsigned high = __reduce_max_sync(kAll, kept ? 0u : mine);
-      if constexpr (PARTS) near->runs = high != 0u && !(low >= 0x1p-100f && low - key_value(high) > unit * low);
+      if constexpr (PARTS) near->runs = high != 0u && !(low >= 0x1p-100f && low - key_value(high) > fminf(unit * low, 0x1p-19f));
       else {
         // (a sum is off by the errors of its addends, which may be far larger than itself; sums that stand for the largest value, or with
         // the lowest one, are what they are)
@@ -459,7 +459,9 @@ __global__ void __launch_bounds__(32 * kRouteWarps, P <= 8 ? 5 : 1) route_kernel
       for (int i = 0; i < P; ++i)
         if (lane * P + i >= E) c[i] = -INFINITY;
       // (from 2^-100 on exponents are above -70: __expf, by its documented bound of 2 + 1.173 |x| units of the last place, is off by
-      // 84 of 2^-23, or the difference from the largest logit by 70 of 2^-24; quotient and sum add a few)
+      // 84 of 2^-23, or the difference from the largest logit by 70 of 2^-24; quotient and sum add a few.  A score close to one hardly
+      // feels that, c (1 - c) |x| or c |log c| of it: 6 and 10 units of 2^-24 a choice, sum included.  By the relative bound alone
+      // 16384 x 256 logistic scores take 31.5 us, with both 26.)
       id = choose32<P, LogitKey, false, true>(a.d, a.d.topk, x, c, part_of, lane, 0x1p-15f, &near);
       if (near.runs) id = choose64<T, P>(a, row, lane, mx);
     } else {
