@@ -463,7 +463,7 @@ int b2c_selftest_fp8_wait(int form, void* cuda_stream);
 
 /* ---- debug build (no counterpart in the paper) ---------------------------------------------------
  * libb2conv_debug.so is the same library compiled with -DB2C_DEBUG_BOUNDS.  In it every address a
- * kernel computes by hand (loads of x, stores and atomics to the outputs and to the scratch; TMA
+ * kernel of the convolution computes by hand (loads of x, stores and atomics to the outputs and to the scratch; TMA
  * copies are clipped by their tensor maps and need no check) is tested against the range of its
  * tensor; the first access outside records B2C_E_BOUNDS, a site number and the byte offset from the
  * range start in the plan's device status words and is skipped, later ones are only skipped.  The

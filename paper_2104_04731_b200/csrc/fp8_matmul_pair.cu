@@ -9,7 +9,7 @@
 // with four accumulators (575 us instead of 563), sixteen warps of sums (813), runs of factors held in registers (592).
 //
 // The smaller tile is for groups of rows: half a tile of every group is empty on average.  32 groups of 240 rows, N 2048, K 4096:
-// pair 121 us, alone 112; 64 groups of 512 rows through the expert layer 390 and 375; 8192^3 in one group 541 and 580.
+// pair 121 us, alone 112; 64 groups of 512 rows through the expert layer, results in 16 bits, 390 and 375; 8192^3 in one group 541 and 580.
 //
 // Roles in each block: warp 0 copies, warp 1 of the leader issues the MMAs, warps 2 and 3 multiply the scales ahead, warps 4-11 keep
 // the scaled sums: a warp has 32 rows x 128 columns, a thread one row, so that all its columns have one factor.

@@ -348,10 +348,10 @@ __device__ __forceinline__ int order64(double choice, int id, int count, int lan
 // are.  A token in which two choices that decide
 // something are not further apart than twice this (about one in fifty at 256 experts) needs a second look: where only the order of the
 // topk + 1 first is open, these few are compared in 64 bits; else all are chosen again with the places beside the values (2^-20, with a softmax
-// 2^-18), and where that does not settle it, or if the scores hang on all logits, the token is done in 64 bits from the start.  (All such tokens
-// chosen again: 26.2 us for the work below, now 25.7; none looked at twice, which is wrong: 22.)
+// 2^-18), and where that does not settle it, or if the scores hang on all logits, the token is done in 64 bits from the start.  (On one run:
+// all such tokens chosen again 26.2 us for the work below, this way 25.7, none looked at twice, which is wrong, 22.)
 // Memory-bound on paper (one read of the logits); what it spends are the instructions of exponentials, sort and topk rounds (16384 tokens
-// of 256 experts, 8 of 4 of 8 runs: 26 us, issue slots 73 % busy, against 2.8 us for the bytes).  Two tokens a warp, 16 lanes each, took
+// of 256 experts, 8 of 4 of 8 runs: 25 to 31 us by the run's clock, issue slots 76 % busy, against 2.8 us for the bytes).  Two tokens a warp, 16 lanes each, took
 // 38: the largest of 16 lanes is four exchanges, that of a warp one instruction.
 constexpr int kRouteWarps = 8;
 template <typename T, int P>
