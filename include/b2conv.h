@@ -366,8 +366,9 @@ int b2c_measure_mma_rate_pair(int tile_n, int mmas_per_pair, float* device_us, f
  * at least 2^-100:
  *   scale_dev[row / block_rows][col / 128] = amax / F,   q = the value of q_type nearest to x * F / amax
  * (ties to even; x * F is rounded to fp32 first, which for 16-bit x changes nothing and may put an fp32 x whose
- * quotient is within 2^-23 of itself from the middle of two values to either).  A NaN stays NaN in its place and does not enter amax; an infinity makes its block's scale
- * infinite, its block's finite values 0 and itself NaN, so that the whole block stands for NaN.
+ * quotient is within 2^-23 of itself from the middle of two values to either).  A NaN stays NaN in its place
+ * and does not enter amax; an infinity makes its block's scale infinite, its block's finite values 0 and
+ * itself NaN, so that the whole block stands for NaN.
  * ld_scale >= ceil(cols / 128).  Elements between cols and ldq are not written. */
 int b2c_fp8_quantize(const void* x_dev, int x_type, int64_t rows, int32_t cols, int64_t ldx, int block_rows,
                      int q_type, void* q_dev, int64_t ldq, float* scale_dev, int64_t ld_scale, void* cuda_stream);
