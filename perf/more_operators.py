@@ -129,7 +129,7 @@ def _quantise(x, fmt, factor, precise=True):
     p = x.to(torch.float64 if precise else torch.float32)
     p = torch.nn.functional.pad(p, (0, -cols % b)).reshape(rows, -1, b)
     amax = p.abs().amax(-1)
-    g = factor.to(p.dtype) if factor is not None else 1.0
+    g = (factor if factor is not None else torch.ones(1, device=x.device)).to(p.dtype)  # (a tensor: by a number torch divides as by its reciprocal)
     if fmt == "mx":  # the least power of two that keeps the block within 6
         m, e = torch.frexp(amax)  # amax = m 2^e, m in [0.5, 1)
         e = torch.where(amax > 0, torch.where(m <= 0.75, e - 3, e - 2), -127).clamp(-127, 127)
@@ -374,13 +374,13 @@ def _exact_quantise(x, fmt, factor):
     block = torch.arange(cols, device=x.device) // b
     amax = torch.zeros(x.shape[0], _blocks(cols, fmt), dtype=torch.float64, device=x.device)
     amax.scatter_reduce_(1, block.expand(x.shape[0], -1), x.abs(), "amax")
-    g = 1.0 if factor is None else factor.double()
+    g = torch.ones(1, dtype=torch.float64, device=x.device) if factor is None else factor.double()
     if fmt == "mx":
         powers = torch.ldexp(torch.ones(255, dtype=torch.float64, device=x.device), torch.arange(255, device=x.device) - 127)
         scale = powers[torch.searchsorted(6.0 * powers, amax).clamp_max(254)]
     else:
         table = torch.arange(127, dtype=torch.uint8, device=x.device).view(torch.float8_e4m3fn).double()  # 0 to 448
-        want = amax / g / 6.0 if factor is None else amax / (6.0 * g)
+        want = amax / (6.0 * g)
         hi = torch.searchsorted(table, want).clamp_max(126)
         lo = (hi - 1).clamp_min(0)
         down, up = want - table[lo], table[hi] - want
