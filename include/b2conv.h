@@ -463,6 +463,71 @@ int b2c_fp8_status(int32_t* status);
  * b2c_fp8_status, and the kernel returns normally. */
 int b2c_selftest_fp8_wait(int form, void* cuda_stream);
 
+/* ---- 4-bit float operators (no counterpart in the paper) -------------------------------------------
+ * The same layers with operands in 4-bit floating point (1-2-1 bits: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) and a scale for each
+ * block of a row, on the tensor core's block-scaled products (`tcgen05.mma.kind::mxf4nvf4`, `kind::mxf4`: the scales are applied
+ * there, sums are fp32).  Two formats:
+ *   B2C_MXFP4: blocks of 32, scale a power of two: a byte b stands for 2^(b - 127), 255 for NaN (E8M0);
+ *   B2C_NVFP4: blocks of 16, scale in E4M3 (not negative), and one fp32 factor for the tensor, kept beside it.
+ * Values are packed two to a byte, the even column in the low half; a row of cols values has ceil(cols / 2) bytes and ceil(cols / 32 or
+ * 16) scales.  Distances between rows are in bytes for both.  The rules of the 8-bit float operators on streams, capture, overlap and
+ * devices hold here too. */
+#define B2C_MXFP4 0
+#define B2C_NVFP4 1
+
+/* Quantisation of x [rows][cols] (B2C_F32 / F16 / BF16), any cols and any distances between rows that do not overlap; the last block of a row
+ * may be smaller.  With amax the block's largest magnitude:
+ *   B2C_MXFP4: scale = the least power of two, at least 2^-127, with amax <= 6 * scale;
+ *   B2C_NVFP4: scale = the E4M3 value nearest to amax / (6 * g), at most 448, with g = *global_scale_dev (1 if that is NULL);
+ *   q = the 4-bit value nearest to x / (scale * g), of larger magnitudes +-6; 0 where the scale is 0.
+ * Ties go to the even code, and both quotients are compared as real numbers: results are exact.  A block with a NaN or an infinity gets the
+ * scale NaN and zeros.  g between 2^-100 and 2^100 (others count as the nearest of these); NULL for B2C_MXFP4.  The last byte of a row of odd
+ * length has zero in its upper half; bytes behind the rows are not written. */
+int b2c_fp4_quantize(const void* x_dev, int x_type, int64_t rows, int32_t cols, int64_t ldx, int format,
+                     const float* global_scale_dev, void* q_dev, int64_t ldq_bytes, void* scale_dev, int64_t ld_scale_bytes,
+                     void* cuda_stream);
+
+/* y = q * scale (times *global_scale_dev if that is given), formed in fp32 and rounded once more to y_type (B2C_F32 / F16 / BF16). */
+int b2c_fp4_dequantize(const void* q_dev, int64_t ldq_bytes, const void* scale_dev, int64_t ld_scale_bytes, int64_t rows, int32_t cols,
+                       int format, const float* global_scale_dev, void* y_dev, int y_type, int64_t ldy, void* cuda_stream);
+
+/* y[m][n] = alpha * sum_k (a[m][k] * a_scale[m][k / block]) * (b[n][k] * b_scale[n][k / block]), rounded once to y_type.
+ * a_dev: [rows][K / 2] bytes, b_dev: [N][K / 2] dense; K a multiple of 32; lda_bytes and both distances between rows of scales
+ * multiples of 16, all four 16-byte aligned; scales of a row of b at ld_b_scale_bytes, of the next matrix N rows on.
+ * alpha_dev: [groups], NULL for 1 (the product of the tensors' factors).  groups and offsets_dev as in b2c_fp8_matmul. */
+typedef struct {
+  int32_t N, K;           /* output columns, reduction length (K a multiple of 32)                  */
+  int32_t groups;         /* 1..1024                                                                */
+  int32_t format, y_type; /* B2C_MXFP4 or B2C_NVFP4, of a and b; B2C_F32, B2C_F16 or B2C_BF16       */
+} b2c_fp4_matmul_desc;
+int b2c_fp4_matmul(const b2c_fp4_matmul_desc* desc, int64_t rows, const void* a_dev, int64_t lda_bytes, const void* a_scale_dev,
+                   int64_t ld_a_scale_bytes, const void* b_dev, const void* b_scale_dev, int64_t ld_b_scale_bytes, const float* alpha_dev,
+                   const int32_t* offsets_dev, void* y_dev, int64_t ldy, void* cuda_stream);
+
+/* The gated feed-forward layer of routed experts, as b2c_fp8_experts, in 4 bits.  For token t and its slots j with expert e = ids[t][j]:
+ *   xq = quantise(x[t], x_global);   v = x_global * w1_global[e];   h = silu(v * w1[e][0] . xq) * (v * w1[e][1] . xq)
+ *   hq = quantise(h, h_global);   y[t] = sum_j weights[t][j] * h_global * w2_global[e] * (w2[e] . hq)
+ * w1_dev: [experts][2][inter][hidden / 2] bytes, gate then up, its scales [experts][2][inter] rows ld_w1_scale_bytes apart; w2_dev:
+ * [experts][hidden][inter / 2], scales [experts][hidden] rows ld_w2_scale_bytes apart; matrices dense, all 16-byte aligned, distances multiples of
+ * 16.  hidden and inter are multiples of 32.  The factors are fp32 on the device, one for x and h, [experts] for the weights; each may be
+ * NULL (1), and is for B2C_MXFP4.  h is not rounded before it is quantised; the rows of the slots and their weighted sum are formed in
+ * fp32, in the order of the slots, and rounded once.  ids outside 0..experts-1 add nothing.  workspace_dev: as there, of
+ * b2c_fp4_experts_workspace_bytes bytes. */
+typedef struct {
+  int32_t hidden, inter, experts, topk;
+  int32_t type, format; /* of x and y: B2C_F32, B2C_F16 or B2C_BF16; of the weights                   */
+} b2c_fp4_experts_desc;
+int b2c_fp4_experts_workspace_bytes(const b2c_fp4_experts_desc* desc, int64_t tokens, size_t* bytes);
+int b2c_fp4_experts(const b2c_fp4_experts_desc* desc, int64_t tokens, const void* x_dev, int64_t ldx, const int32_t* ids_dev,
+                    const float* weights_dev, const void* w1_dev, const void* w1_scale_dev, int64_t ld_w1_scale_bytes,
+                    const void* w2_dev, const void* w2_scale_dev, int64_t ld_w2_scale_bytes, const float* x_global_dev,
+                    const float* w1_global_dev, const float* h_global_dev, const float* w2_global_dev, void* y_dev, int64_t ldy,
+                    void* workspace_dev, void* cuda_stream);
+
+/* As b2c_fp8_status and b2c_selftest_fp8_wait, of the 4-bit operators' kernels. */
+int b2c_fp4_status(int32_t* status);
+int b2c_selftest_fp4_wait(int form, void* cuda_stream);
+
 /* ---- debug build (no counterpart in the paper) ---------------------------------------------------
  * libb2conv_debug.so is the same library compiled with -DB2C_DEBUG_BOUNDS.  In it every address a
  * kernel of the convolution computes by hand (loads of x, stores and atomics to the outputs and to the scratch; TMA

@@ -25,6 +25,7 @@ VARIANT_ROW_UNROLL, VARIANT_SPACE_TO_DEPTH, VARIANT_DILATION_PACK = 4, 5, 6
 VARIANT_CP_SHIFT, VARIANT_S2D_SHIFT, VARIANT_ROWPHASE_SHIFT, VARIANT_IM2COL_WINDOW = 7, 8, 9, 10
 POLICY_AUTO_TIMED, POLICY_MIN_OVERHEAD, POLICY_MIN_WORKSPACE, POLICY_AUTO_TIMED_CONCURRENT = -1, -2, -3, -4
 F32, F16, BF16, E4M3, E5M2 = 0, 1, 2, 3, 4
+MXFP4, NVFP4 = 0, 1
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 GROUP_MAX, GROUP_TOP2 = 0, 1
 VARIANT_NAMES = {0: "channel_pack_tma_im2col", 1: "im2col_explicit", 2: "im2col_gather", 3: "im2col_staged_window",
@@ -42,6 +43,8 @@ EXPORTS = [
     "b2c_plan_check_canaries", "b2c_test_shrink_checked_ranges", "b2c_test_kernel_of",
     "b2c_fp8_quantize", "b2c_fp8_matmul", "b2c_route", "b2c_route_sort_workspace_bytes", "b2c_route_sort", "b2c_route_combine",
     "b2c_experts_workspace_bytes", "b2c_fp8_experts", "b2c_fp8_status", "b2c_selftest_fp8_wait",
+    "b2c_fp4_quantize", "b2c_fp4_dequantize", "b2c_fp4_matmul", "b2c_fp4_experts_workspace_bytes", "b2c_fp4_experts", "b2c_fp4_status",
+    "b2c_selftest_fp4_wait",
 ]
 
 
@@ -73,6 +76,14 @@ class RouteDesc(ctypes.Structure):
 
 class ExpertsDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("hidden", "inter", "experts", "topk", "type")]
+
+
+class Fp4MatmulDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("N", "K", "groups", "format", "y_type")]
+
+
+class Fp4ExpertsDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("hidden", "inter", "experts", "topk", "type", "format")]
 
 
 class B2CError(RuntimeError):
@@ -151,6 +162,14 @@ def load():
     lib.b2c_fp8_experts.argtypes = [px, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp]
     lib.b2c_fp8_status.argtypes = [pi32]
     lib.b2c_selftest_fp8_wait.argtypes = [i32, vp]
+    pm4, px4 = ctypes.POINTER(Fp4MatmulDesc), ctypes.POINTER(Fp4ExpertsDesc)
+    lib.b2c_fp4_quantize.argtypes = [vp, i32, i64, ctypes.c_int32, i64, i32, vp, vp, i64, vp, i64, vp]
+    lib.b2c_fp4_dequantize.argtypes = [vp, i64, vp, i64, i64, ctypes.c_int32, i32, vp, vp, i32, i64, vp]
+    lib.b2c_fp4_matmul.argtypes = [pm4, i64, vp, i64, vp, i64, vp, vp, i64, vp, vp, vp, i64, vp]
+    lib.b2c_fp4_experts_workspace_bytes.argtypes = [px4, i64, pz]
+    lib.b2c_fp4_experts.argtypes = [px4, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, i64, vp, vp, vp, vp, vp, i64, vp, vp]
+    lib.b2c_fp4_status.argtypes = [pi32]
+    lib.b2c_selftest_fp4_wait.argtypes = [i32, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name not in ("b2c_plan_destroy", "b2c_status_string"):
@@ -353,7 +372,7 @@ def measure_mma_rate_pair(tile_n: int = 256, mmas_per_pair: int = 20000, stream=
     return us.value, cyc.value
 
 
-# ---- 8-bit float operators ----------------------------------------------------------------------------------------------
+# ---- 8-bit and 4-bit float operators ------------------------------------------------------------------------------------
 #
 # Tensors are checked and handed over by a small native module (_binding-*.so): shapes, types, strides and devices, which the library
 # does not see.  What it refuses is raised as B2CError(E_INVALID_ARG) and the like before anything is launched.
@@ -377,7 +396,8 @@ def _load_native():
         spec.loader.exec_module(binding)
         binding.bind(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in (
             "b2c_fp8_quantize", "b2c_fp8_matmul", "b2c_route", "b2c_route_sort_workspace_bytes", "b2c_route_sort", "b2c_route_combine",
-            "b2c_experts_workspace_bytes", "b2c_fp8_experts")))
+            "b2c_experts_workspace_bytes", "b2c_fp8_experts", "b2c_fp4_quantize", "b2c_fp4_dequantize", "b2c_fp4_matmul",
+            "b2c_fp4_experts_workspace_bytes", "b2c_fp4_experts")))
         _native = binding
     return _native
 
@@ -463,6 +483,81 @@ def fp8_status() -> int:
 def selftest_fp8_wait(form: int, stream=None):
     """Enqueues a bounded wait that cannot complete, of the products for few rows (form 0) or many (1); fp8_status then reports E_TIMEOUT."""
     _check(load().b2c_selftest_fp8_wait(form, _stream_ptr(stream)), "b2c_selftest_fp8_wait")
+
+
+# In 4 bits: q holds two values a byte (torch.float4_e2m1fn_x2 or torch.uint8, the even column in the low half), and the type of the scales says
+# which format it is: torch.float8_e8m0fnu MXFP4 (blocks of 32), torch.float8_e4m3fn NVFP4 (blocks of 16, and a float32 factor for the tensor).
+
+def fp4_scale_pitch(cols: int, fmt: int) -> int:
+    """Bytes from one row of scales to the next that a product can read: their number, rounded up to a multiple of 16."""
+    block = 32 if fmt == MXFP4 else 16
+    return (-(-cols // block) + 15) // 16 * 16
+
+
+def fp4_empty(rows, cols: int, fmt: int, device="cuda"):
+    """(q, scale) for a matrix of rows x cols values, or a stack of them (rows: a tuple), laid out as the products read them: q of
+    ceil(cols / 2) bytes a row, scale a view into rows of fp4_scale_pitch bytes."""
+    import torch
+
+    lead = tuple(rows) if isinstance(rows, (tuple, list)) else (rows,)
+    q = torch.empty(*lead, (cols + 1) // 2, dtype=torch.uint8, device=device)
+    scale = torch.zeros(*lead, fp4_scale_pitch(cols, fmt), dtype=torch.uint8, device=device)
+    scale = scale.view(torch.float8_e8m0fnu if fmt == MXFP4 else torch.float8_e4m3fn)
+    return q, scale[..., :-(-cols // (32 if fmt == MXFP4 else 16))]
+
+
+def fp4_quantize(x, q, scale, global_scale=None, stream=None):
+    """Quantises x [rows, cols] (float32 / float16 / bfloat16) to 4 bits: q [rows, ceil(cols / 2)], scale [rows, ceil(cols / block)].
+    global_scale: one float32 on the device, the tensor's factor (NVFP4 only; 1 if it is None)."""
+    r = (_native or _load_native()).quantize4(x, q, scale, global_scale, stream and stream.cuda_stream)
+    if r:
+        _refused("b2c_fp4_quantize", *r)
+
+
+def fp4_dequantize(q, scale, y, global_scale=None, stream=None):
+    """y [rows, cols] (float32 / float16 / bfloat16) = the numbers that q, scale and global_scale stand for."""
+    r = (_native or _load_native()).dequantize4(q, scale, y, global_scale, stream and stream.cuda_stream)
+    if r:
+        _refused("b2c_fp4_dequantize", *r)
+
+
+def fp4_matmul(a, a_scale, b, b_scale, y, alpha=None, offsets=None, stream=None):
+    """y = alpha * a . b^T of block-scaled 4-bit matrices of one format.  a [rows, K / 2], b [N, K / 2] with their scales [.., K / block] in rows that start
+    on multiples of 16 bytes (fp4_empty); y [rows, N] float32 / float16 / bfloat16; alpha float32 [1] or None.  With b [groups, N, K / 2] (its
+    scales, alpha [groups]) and offsets as in fp8_matmul each row is multiplied with its group's matrix."""
+    r = (_native or _load_native()).matmul4(a, a_scale, b, b_scale, y, alpha, offsets, stream and stream.cuda_stream)
+    if r:
+        _refused("b2c_fp4_matmul", *r)
+
+
+def fp4_experts_workspace_bytes(hidden: int, inter: int, experts: int, topk: int, tokens: int, fmt: int, dtype: int = BF16) -> int:
+    """Scratch bytes of fp4_experts for up to this many tokens; fmt: of the weights, dtype: type of x and y."""
+    n = ctypes.c_size_t()
+    d = Fp4ExpertsDesc(hidden, inter, experts, topk, dtype, fmt)
+    _check(load().b2c_fp4_experts_workspace_bytes(ctypes.byref(d), tokens, ctypes.byref(n)), "b2c_fp4_experts_workspace_bytes")
+    return n.value
+
+
+def fp4_experts(x, ids, weights, w1, w1_scale, w2, w2_scale, y, workspace, x_global=None, w1_global=None, h_global=None, w2_global=None, stream=None):
+    """Gated feed-forward layer of routed experts with 4-bit weights: x, y [tokens, hidden]; ids int32 and weights float32 [tokens, topk]; w1
+    [experts, 2, inter, hidden / 2] (gate, up) and w2 [experts, hidden, inter / 2] with their scales; the factors of x, w1 [experts], the hidden
+    rows and w2 [experts], each float32 or None."""
+    r = (_native or _load_native()).experts4(x, ids, weights, w1, w1_scale, w2, w2_scale, y, workspace, x_global, w1_global, h_global, w2_global,
+                                             stream and stream.cuda_stream)
+    if r:
+        _refused("b2c_fp4_experts", *r)
+
+
+def fp4_status() -> int:
+    """Waits for the device; OK, or E_TIMEOUT if a kernel of the 4-bit float operators gave up on a bounded wait since the last query."""
+    s = ctypes.c_int32()
+    _check(load().b2c_fp4_status(ctypes.byref(s)), "b2c_fp4_status")
+    return s.value
+
+
+def selftest_fp4_wait(form: int, stream=None):
+    """As selftest_fp8_wait, of the 4-bit products' kernels; fp4_status then reports E_TIMEOUT."""
+    _check(load().b2c_selftest_fp4_wait(form, _stream_ptr(stream)), "b2c_selftest_fp4_wait")
 
 
 def debug_build() -> bool:

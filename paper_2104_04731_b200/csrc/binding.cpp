@@ -1,4 +1,4 @@
-// Python side of the 8-bit float operators: checks of torch tensors and the calls into the library.
+// Python side of the 8-bit and 4-bit float operators: checks of torch tensors and the calls into the library.
 //
 // The calls of single tokens take a few microseconds on the device, and marshalling five tensors in Python cost as much again
 // (quantise 5.0 us, product 7.5 us, expert layer 10.9 us of checks and ctypes conversions; here 0.4 to 0.8 us).  The library
@@ -24,6 +24,11 @@ decltype(&b2c_route_sort) p_sort;
 decltype(&b2c_route_combine) p_combine;
 decltype(&b2c_experts_workspace_bytes) p_experts_bytes;
 decltype(&b2c_fp8_experts) p_experts;
+decltype(&b2c_fp4_quantize) p_quantize4;
+decltype(&b2c_fp4_dequantize) p_dequantize4;
+decltype(&b2c_fp4_matmul) p_matmul4;
+decltype(&b2c_fp4_experts_workspace_bytes) p_experts4_bytes;
+decltype(&b2c_fp4_experts) p_experts4;
 
 // What a call found wrong first.
 struct Call {
@@ -253,11 +258,157 @@ PyObject* experts(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   return c.done();
 }
 
+// ---- 4-bit float operators ----
+// Packed values: torch's packed type, or plain bytes.
+bool is_packed(const at::Tensor& t) { return t.scalar_type() == at::kByte || t.scalar_type() == at::ScalarType::Float4_e2m1fn_x2; }
+// The format by the type of the scales; -1 for any other.
+int format_of(const at::Tensor& scale) {
+  if (scale.scalar_type() == at::ScalarType::Float8_e8m0fnu) return B2C_MXFP4;
+  return scale.scalar_type() == at::kFloat8_e4m3fn ? B2C_NVFP4 : -1;
+}
+int64_t scales4(int64_t cols, int format) { return format == B2C_MXFP4 ? (cols + 31) / 32 : (cols + 15) / 16; }
+int64_t round16(int64_t n) { return (n + 15) / 16 * 16; }
+bool is_one_float(const at::Tensor* t) { return t == nullptr || (t->numel() == 1 && is_f32(*t)); }
+const float* floats(const at::Tensor* t) { return t ? (const float*)t->data_ptr() : nullptr; }
+// Distance between the rows of one matrix, or of matrices that follow each other without a gap, in bytes; -1 if there is none such.  A single
+// row has the distance that its length rounds up to.
+int64_t ld_of_stack(const at::Tensor& t) {
+  const int d = (int)t.dim();
+  const int64_t cols = t.size(d - 1);
+  if (cols > 1 && t.stride(d - 1) != 1) return -1;
+  int64_t step = -1, rows = 1;  // of the rows counted so far
+  for (int i = d - 2; i >= 0; --i) {
+    if (t.size(i) > 1) {
+      if (step < 0) {
+        if (t.stride(i) % rows != 0) return -1;
+        step = t.stride(i) / rows;
+      } else if (t.stride(i) != step * rows) {
+        return -1;
+      }
+    }
+    rows *= t.size(i);
+  }
+  if (step < 0) return round16(cols);
+  return step >= cols ? step : -1;
+}
+
+// quantize4(x, q, scale, global_scale, stream)
+PyObject* quantize4(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  B2C_ARGS(5)
+  Call c{"b2c_fp4_quantize"};
+  const at::Tensor *x = c.tensor(args[0]), *q = c.tensor(args[1]), *s = c.tensor(args[2]), *g = c.tensor(args[3], true);
+  if (c.code != B2C_OK) return c.done();
+  if (c.need(x->dim() == 2 && q->dim() == 2 && s->dim() == 2, "shapes") && c.need(format_of(*s) >= 0 && is_packed(*q) && type_of(*x) >= 0, "types")) {
+    const int64_t rows = x->size(0), cols = x->size(1);
+    const int format = format_of(*s);
+    c.need(shaped(*q, rows, (cols + 1) / 2), "q");
+    c.need(shaped(*s, rows, scales4(cols, format)), "scale");
+    c.need(is_one_float(g), "global_scale");
+    c.need(ld(*x) >= 0 && ld(*q) >= 0 && ld(*s) >= 0, "rows are not contiguous, or overlap");
+    c.need(cols <= INT32_MAX, "sizes", B2C_E_UNSUPPORTED);
+    for (const at::Tensor* t : {x, q, s, g}) c.on_device(t);
+    if (c.code == B2C_OK)
+      c.code = p_quantize4(x->data_ptr(), type_of(*x), rows, (int32_t)cols, ld(*x), format, floats(g), q->data_ptr(), ld(*q), s->data_ptr(), ld(*s),
+                           c.stream(args[4]));
+  }
+  return c.done();
+}
+
+// dequantize4(q, scale, y, global_scale, stream)
+PyObject* dequantize4(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  B2C_ARGS(5)
+  Call c{"b2c_fp4_dequantize"};
+  const at::Tensor *q = c.tensor(args[0]), *s = c.tensor(args[1]), *y = c.tensor(args[2]), *g = c.tensor(args[3], true);
+  if (c.code != B2C_OK) return c.done();
+  if (c.need(y->dim() == 2 && q->dim() == 2 && s->dim() == 2, "shapes") && c.need(format_of(*s) >= 0 && is_packed(*q) && type_of(*y) >= 0, "types")) {
+    const int64_t rows = y->size(0), cols = y->size(1);
+    const int format = format_of(*s);
+    c.need(shaped(*q, rows, (cols + 1) / 2), "q");
+    c.need(shaped(*s, rows, scales4(cols, format)), "scale");
+    c.need(is_one_float(g), "global_scale");
+    c.need(ld(*y) >= 0 && ld(*q) >= 0 && ld(*s) >= 0, "rows are not contiguous, or overlap");
+    c.need(cols <= INT32_MAX, "sizes", B2C_E_UNSUPPORTED);
+    for (const at::Tensor* t : {q, s, y, g}) c.on_device(t);
+    if (c.code == B2C_OK)
+      c.code = p_dequantize4(q->data_ptr(), ld(*q), s->data_ptr(), ld(*s), rows, (int32_t)cols, format, floats(g), y->data_ptr(), type_of(*y), ld(*y),
+                             c.stream(args[4]));
+  }
+  return c.done();
+}
+
+// matmul4(a, a_scale, b, b_scale, y, alpha, offsets, stream)
+PyObject* matmul4(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  B2C_ARGS(8)
+  Call c{"b2c_fp4_matmul"};
+  const at::Tensor *a = c.tensor(args[0]), *sa = c.tensor(args[1]), *b = c.tensor(args[2]), *sb = c.tensor(args[3]), *y = c.tensor(args[4]),
+                   *alpha = c.tensor(args[5], true), *off = c.tensor(args[6], true);
+  if (c.code != B2C_OK) return c.done();
+  if (c.need(a->dim() == 2 && sa->dim() == 2 && y->dim() == 2 && (b->dim() == 2 || b->dim() == 3) && sb->dim() == b->dim(), "shapes") &&
+      c.need((b->dim() == 2) == (off == nullptr), "offsets go with a stack of matrices") &&
+      c.need(format_of(*sa) >= 0 && format_of(*sb) == format_of(*sa) && is_packed(*a) && is_packed(*b) && type_of(*y) >= 0, "types")) {
+    const bool stack = b->dim() == 3;
+    const int format = format_of(*sa);
+    const int64_t rows = a->size(0), bytes = a->size(1), K = 2 * bytes, N = b->size(-2), groups = stack ? b->size(0) : 1;
+    c.need(b->size(-1) == bytes && shaped(*y, rows, N), "shapes");
+    c.need(shaped(*sa, rows, scales4(K, format)), "a_scale");
+    c.need(stack ? shaped(*sb, groups, N, scales4(K, format)) : shaped(*sb, N, scales4(K, format)), "b_scale");
+    c.need(b->is_contiguous(), "b has to be contiguous");
+    c.need(alpha == nullptr || (alpha->numel() == groups && alpha->is_contiguous() && is_f32(*alpha)), "alpha");
+    c.need(off == nullptr || (shaped(*off, groups + 1) && off->is_contiguous() && is_i32(*off)), "offsets");
+    c.need(ld(*a) >= 0 && ld(*sa) >= 0 && ld(*y) >= 0 && ld_of_stack(*sb) >= 0, "rows are not contiguous, or overlap");
+    c.need(N <= INT32_MAX && bytes <= INT32_MAX / 2 && groups <= INT32_MAX, "sizes", B2C_E_UNSUPPORTED);
+    for (const at::Tensor* t : {a, sa, b, sb, y, alpha, off}) c.on_device(t);
+    if (c.code == B2C_OK) {
+      const b2c_fp4_matmul_desc d = {(int32_t)N, (int32_t)K, (int32_t)groups, format, type_of(*y)};
+      c.code = p_matmul4(&d, rows, a->data_ptr(), rows > 1 ? ld(*a) : round16(bytes), sa->data_ptr(), rows > 1 ? ld(*sa) : round16(sa->size(1)), b->data_ptr(),
+                         sb->data_ptr(), ld_of_stack(*sb), floats(alpha), off ? (const int32_t*)off->data_ptr() : nullptr, y->data_ptr(), ld(*y),
+                         c.stream(args[7]));
+    }
+  }
+  return c.done();
+}
+
+// experts4(x, ids, weights, w1, w1_scale, w2, w2_scale, y, workspace, x_global, w1_global, h_global, w2_global, stream)
+PyObject* experts4(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  B2C_ARGS(14)
+  Call c{"b2c_fp4_experts"};
+  const at::Tensor* t[13];
+  for (int i = 0; i < 13; ++i) t[i] = c.tensor(args[i], i >= 9);
+  if (c.code != B2C_OK) return c.done();
+  const at::Tensor &x = *t[0], &ids = *t[1], &w = *t[2], &w1 = *t[3], &s1 = *t[4], &w2 = *t[5], &s2 = *t[6], &y = *t[7], &ws = *t[8];
+  if (c.need(x.dim() == 2 && ids.dim() == 2 && w1.dim() == 4 && w2.dim() == 3 && s1.dim() == 4 && s2.dim() == 3, "shapes") &&
+      c.need(format_of(s1) >= 0 && format_of(s2) == format_of(s1) && is_packed(w1) && is_packed(w2) && type_of(x) >= 0, "types")) {
+    const int format = format_of(s1);
+    const int64_t tokens = x.size(0), hidden = x.size(1), topk = ids.size(1), n = w1.size(0), inter = w1.size(2);
+    c.need(hidden % 2 == 0 && inter % 2 == 0, "shapes");
+    c.need(shaped(y, tokens, hidden) && y.scalar_type() == x.scalar_type(), "y");
+    c.need(shaped(ids, tokens, topk) && shaped(w, tokens, topk) && is_i32(ids) && is_f32(w), "ids, weights");
+    c.need(shaped(w1, n, 2, inter, hidden / 2) && shaped(s1, n, 2, inter, scales4(hidden, format)), "w1");
+    c.need(shaped(w2, n, hidden, inter / 2) && shaped(s2, n, hidden, scales4(inter, format)), "w2");
+    for (int i : {1, 2, 3, 5}) c.need(t[i]->is_contiguous(), "ids, weights and matrices have to be contiguous");
+    c.need(ws.is_contiguous(), "workspace");
+    c.need(is_one_float(t[9]) && is_one_float(t[11]), "x_global, h_global");
+    for (int i : {10, 12}) c.need(t[i] == nullptr || (t[i]->numel() == n && t[i]->is_contiguous() && is_f32(*t[i])), "w1_global, w2_global");
+    c.need(ld(x) >= 0 && ld(y) >= 0 && ld_of_stack(s1) >= 0 && ld_of_stack(s2) >= 0, "rows are not contiguous, or overlap");
+    c.need(hidden <= INT32_MAX && inter <= INT32_MAX && n <= INT32_MAX && topk <= INT32_MAX, "sizes", B2C_E_UNSUPPORTED);
+    for (const at::Tensor* v : t) c.on_device(v);
+    const b2c_fp4_experts_desc d = {(int32_t)hidden, (int32_t)inter, (int32_t)n, (int32_t)topk, type_of(x), format};
+    size_t need = 0;
+    if (c.code == B2C_OK) c.code = p_experts4_bytes(&d, tokens, &need);
+    c.need(bytes_of(ws) >= need, "workspace", B2C_E_WORKSPACE_TOO_SMALL);
+    if (c.code == B2C_OK)
+      c.code = p_experts4(&d, tokens, x.data_ptr(), ld(x), (const int32_t*)ids.data_ptr(), (const float*)w.data_ptr(), w1.data_ptr(), s1.data_ptr(),
+                          ld_of_stack(s1), w2.data_ptr(), s2.data_ptr(), ld_of_stack(s2), floats(t[9]), floats(t[10]), floats(t[11]), floats(t[12]), y.data_ptr(),
+                          ld(y), ws.data_ptr(), c.stream(args[13]));
+  }
+  return c.done();
+}
+
 // bind(addresses of the library's entry points, in the order below)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-  B2C_ARGS(8)
-  void* p[8];
-  for (int i = 0; i < 8; ++i) p[i] = PyLong_AsVoidPtr(args[i]);
+  B2C_ARGS(13)
+  void* p[13];
+  for (int i = 0; i < 13; ++i) p[i] = PyLong_AsVoidPtr(args[i]);
   if (PyErr_Occurred()) return nullptr;
   p_quantize = (decltype(p_quantize))p[0];
   p_matmul = (decltype(p_matmul))p[1];
@@ -267,6 +418,11 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   p_combine = (decltype(p_combine))p[5];
   p_experts_bytes = (decltype(p_experts_bytes))p[6];
   p_experts = (decltype(p_experts))p[7];
+  p_quantize4 = (decltype(p_quantize4))p[8];
+  p_dequantize4 = (decltype(p_dequantize4))p[9];
+  p_matmul4 = (decltype(p_matmul4))p[10];
+  p_experts4_bytes = (decltype(p_experts4_bytes))p[11];
+  p_experts4 = (decltype(p_experts4))p[12];
   Py_RETURN_NONE;
 }
 
@@ -283,7 +439,8 @@ PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
 
 #define B2C_METHOD(f) {#f, (PyCFunction)(void*)guarded<f>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {B2C_METHOD(quantize), B2C_METHOD(matmul),  B2C_METHOD(route), B2C_METHOD(sort),
-                         B2C_METHOD(combine),  B2C_METHOD(experts), B2C_METHOD(bind),  {nullptr, nullptr, 0, nullptr}};
+                         B2C_METHOD(combine),  B2C_METHOD(experts), B2C_METHOD(quantize4), B2C_METHOD(dequantize4), B2C_METHOD(matmul4),
+                         B2C_METHOD(experts4), B2C_METHOD(bind),  {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,180 @@
+// Device code shared by the kernels of the 4-bit float operators: scales of blocks, conversion to 4 bits and back.  Included by each kernel
+// translation unit; unnamed namespace.
+#pragma once
+
+#include "fp4_internal.h"
+#include "fp8_common.cuh"
+
+namespace b2c {
+
+namespace {
+
+constexpr uint32_t kInfBits = 0x7F800000u;
+
+// The tensor's factor, and what is formed of it once a thread.
+struct Factor4 {
+  float g;
+  bool few_bits;  // 17 at most: scale * g is exact in fp32, and so are its products with the borders between 4-bit values
+  double inv_6g;
+};
+__device__ __forceinline__ Factor4 load_factor4(const float* p, int format) {
+  Factor4 f = {1.0f, true, 1.0 / 6.0};
+  if (p != nullptr && format == B2C_NVFP4) {
+    f.g = fminf(fmaxf(*p, 0x1p-100f), 0x1p100f);
+    f.few_bits = (__float_as_uint(f.g) & 0x7Fu) == 0;
+    f.inv_6g = 1.0 / (6.0 * (double)f.g);
+  }
+  return f;
+}
+
+// Scale of a block.  amax: bits of its largest magnitude (as whole numbers these are ordered as the magnitudes, and NaN is the largest).
+struct Scale4 {
+  uint32_t code;  // as stored
+  float r;        // reciprocal of the step, 0 where the values are zeros
+  float step;     // E4M3 and few_bits: the step itself
+};
+// MX: with amax = m * 2^k, 1 <= m < 2, the least power of two s with amax <= 6 s = 1.5 * 2^2 s is 2^(k - 2), or twice that for m > 1.5.
+__device__ __forceinline__ Scale4 scale_mx(uint32_t amax) {
+  Scale4 s;
+  const int e = (int)((amax + 0x3FFFFFu) >> 23) - 2;  // biased; the addend carries from m > 1.5 on
+  const uint32_t code = (uint32_t)max(e, 0);
+  const bool fine = amax < kInfBits;
+  s.code = fine ? code : 255u;
+  s.r = fine ? __uint_as_float((254u - code) << 23) : 0.0f;  // 2^(127 - code), a power of two: products with it are exact
+  s.step = 0.0f;
+  return s;
+}
+// NV: the E4M3 value nearest to the real quotient amax / (6 g).  p is that quotient within 2^-52 of itself.  A border t between two E4M3
+// values has 5 bits, so t * 6 g has 31 at most, and amax, of 24, is that product or differs from it by 2^-31 or more of itself: rounded to 41
+// bits (the sum that does it is Veltkamp's: T. J. Dekker, A floating-point technique for extending the available precision, Numer. Math. 18,
+// 1971) p is on a border where the quotient is, and on its side of it elsewhere.  To fp32 it goes with its last bit set if anything was cut
+// off, which the rounding to four bits then sees.
+__device__ __forceinline__ Scale4 scale_nv(uint32_t amax, const Factor4& f) {
+  Scale4 s;
+  const double p = __dmul_rn((double)__uint_as_float(amax), f.inv_6g);
+  const double c = __dmul_rn(p, 4097.0);
+  const double hi = __dsub_rn(c, __dsub_rn(c, p));
+  float v = __double2float_rz(hi);
+  if ((double)v != hi) v = __uint_as_float(__float_as_uint(v) | 1u);
+  const bool fine = amax < kInfBits;
+  s.code = fine ? (uint32_t)__nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3) : 0x7Fu;
+  s.step = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)s.code, __NV_E4M3))) * f.g;
+  s.r = fine && s.code != 0 ? __frcp_rn(s.step) : 0.0f;
+  return s;
+}
+__device__ __forceinline__ float scale_value(uint32_t code, int format) {
+  if (format == B2C_MXFP4) return code == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float(code == 0 ? 0x400000u : code << 23);
+  return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3)));
+}
+
+// Eight values to 4 bits each, to nearest even, saturating.
+__device__ __forceinline__ uint32_t cvt_e2m1x8(const float* v) {
+  uint32_t r;
+  asm("{\n.reg .b8 b0, b1, b2, b3;\n"
+      "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n"
+      "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n"
+      "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n"
+      "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n"
+      "mov.b32 %0, {b0, b1, b2, b3};\n}"
+      : "=r"(r)
+      : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+  return r;
+}
+// Four values, in the lower half.
+__device__ __forceinline__ uint32_t cvt_e2m1x4(const float* v) {
+  uint32_t r;
+  asm("{\n.reg .b8 b0, b1;\n"
+      "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n"
+      "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n"
+      "mov.b32 %0, {b0, b1, b0, b1};\n}"
+      : "=r"(r)
+      : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]));
+  return r & 0xFFFFu;
+}
+// Eight 4-bit values in halves, exact.
+__device__ __forceinline__ void cvt_f16x8(uint32_t q, uint32_t* h) {
+  asm("{\n.reg .b8 b0, b1, b2, b3;\n"
+      "mov.b32 {b0, b1, b2, b3}, %4;\n"
+      "cvt.rn.f16x2.e2m1x2 %0, b0;\n"
+      "cvt.rn.f16x2.e2m1x2 %1, b1;\n"
+      "cvt.rn.f16x2.e2m1x2 %2, b2;\n"
+      "cvt.rn.f16x2.e2m1x2 %3, b3;\n}"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+      : "r"(q));
+}
+
+// The code of x by its block's borders, each product exact in 64 bits.
+__device__ __noinline__ uint32_t code4_exact(float x, double step) {
+  const double a = fabs((double)x);
+  uint32_t c = 0;
+  c += a > 0.25 * step;
+  c += a >= 0.75 * step;
+  c += a > 1.25 * step;
+  c += a >= 1.75 * step;
+  c += a > 2.5 * step;
+  c += a >= 3.5 * step;
+  c += a > 5.0 * step;
+  return c | (__float_as_uint(x) >> 31 << 3);
+}
+
+// N (4, 8 or 16) values of one block to 4 bits each, as if x / (scale * g) had been rounded as a real number.
+//   MX: multiplication by a power of two.
+//   NV, few_bits: the correctly rounded quotient by Markstein's residual step (see quantize2).  Every product of the step with a border t has 24
+// bits at most, so x is either that product, and the quotient t itself, or differs from it by a unit of x's last place, more than half a
+// unit of t's: the rounded quotient is on the same side.
+//   NV else: x times the rounded reciprocal is within 3 units of the last place (step, reciprocal and product are rounded).  The borders have three
+// bits, so what is nearer to one than 4 units has 20 bits that are nearly all zeros or all ones: rare (8 of 2^20), and decided in 64 bits.
+// A block whose scale is the largest one may be beyond it by any factor, and is decided there too.
+template <int N>
+__device__ __forceinline__ void quantise4(const Scale4& s, const Factor4& f, int format, const float* x, uint32_t* q) {
+  float v[N];
+  bool look = false;
+  if (format == B2C_MXFP4) {
+    const f32x2 r = pair_of(s.r, s.r);
+#pragma unroll
+    for (int i = 0; i < N; i += 2) unpair(mul2(pair_of(x[i], x[i + 1]), r), &v[i], &v[i + 1]);
+  } else if (f.few_bits) {
+    const f32x2 r = pair_of(s.r, s.r), neg = pair_of(-s.step, -s.step);
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const f32x2 u = pair_of(x[i], x[i + 1]), q0 = mul2(u, r);
+      unpair(fma2_of(fma2_of(q0, neg, u), r, q0), &v[i], &v[i + 1]);
+    }
+    look = s.code == 0x7Eu;
+  } else {
+    const f32x2 r = pair_of(s.r, s.r);
+    uint32_t near = 0xFFFFFu;
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      unpair(mul2(pair_of(x[i], x[i + 1]), r), &v[i], &v[i + 1]);
+      // (0.2 is far from every border: zeros, and what is as small, need no look)
+      near = min(near, min((__float_as_uint(fmaxf(fabsf(v[i]), 0.2f)) + 4u) & 0xFFFFFu, (__float_as_uint(fmaxf(fabsf(v[i + 1]), 0.2f)) + 4u) & 0xFFFFFu));
+    }
+    look = (near <= 8u || s.code == 0x7Eu) && s.r != 0.0f;
+  }
+#pragma unroll
+  for (int i = 0; i < N / 8; ++i) q[i] = cvt_e2m1x8(v + 8 * i);
+  if constexpr (N == 4) q[0] = cvt_e2m1x4(v);
+  if (look) {
+    const double step = (double)scale_value(s.code, B2C_NVFP4) * (double)f.g;
+#pragma unroll
+    for (int i = 0; i < (N + 7) / 8; ++i) {
+      uint32_t w = 0;
+#pragma unroll
+      for (int j = 0; j < (N < 8 ? N : 8); ++j) w |= code4_exact(x[8 * i + j], step) << (4 * j);
+      q[i] = w;
+    }
+  }
+  if (s.r == 0.0f) {
+#pragma unroll
+    for (int i = 0; i < (N + 7) / 8; ++i) q[i] = 0;
+  }
+}
+__device__ __forceinline__ Scale4 scale_of(uint32_t amax, const Factor4& f, int format) {
+  return format == B2C_MXFP4 ? scale_mx(amax) : scale_nv(amax, f);
+}
+
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+}  // namespace
+}  // namespace b2c

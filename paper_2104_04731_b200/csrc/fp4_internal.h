@@ -1,0 +1,81 @@
+// Internal declarations of the 4-bit float operators (quantisation with microscales, block-scaled products, expert layers), shared by
+// their host code and kernel launchers.
+#pragma once
+
+#include "fp8_internal.h"
+
+namespace b2c {
+
+constexpr int kFp4Stage = 256;  // reduction elements of a stage: 128 bytes of a row, the width of a swizzled tile
+
+#ifdef __CUDACC__
+__host__ __device__
+#endif
+inline int fp4_block(int format) { return format == B2C_MXFP4 ? 32 : 16; }
+#ifdef __CUDACC__
+__host__ __device__
+#endif
+inline long long fp4_scales(long long cols, int format) { return (cols + fp4_block(format) - 1) / fp4_block(format); }
+inline long long fp4_scale_pitch(long long cols, int format) { return (fp4_scales(cols, format) + 15) / 16 * 16; }
+
+struct Quantize4Args {
+  const void* x;
+  long long ldx;
+  uint8_t* q;
+  long long ldq;
+  uint8_t* scale;
+  long long lds;
+  const float* global;
+  long long rows;
+  int cols;
+  int x_type, format;
+  // Rows of an expert layer: input row t is written to output rows map[t * copies + j] (none where negative).
+  const int32_t* map;
+  int copies;
+};
+
+struct Dequantize4Args {
+  const uint8_t* q;
+  long long ldq;
+  const uint8_t* scale;
+  long long lds;
+  const float* global;
+  long long rows;
+  int cols;
+  int y_type, format;
+  void* y;
+  long long ldy;
+};
+
+struct Matmul4Args {
+  const uint8_t* a;  // [rows][K / 2]
+  long long lda;
+  const uint8_t* a_scale;
+  long long lds;
+  const uint8_t* b;  // [groups][N][K / 2]; gated: [groups][2][N][K / 2], gate rows then up rows
+  const uint8_t* b_scale;
+  long long ldbs;
+  const float* alpha;   // [groups] or null
+  const float* alpha2;  // one more factor of all groups, or null
+  const int32_t* offsets;
+  void* y;              // gated: packed values
+  long long ldy;        // (gated: bytes)
+  uint8_t* y_scale;     // gated only
+  long long ldys;
+  const float* y_global;  // gated only: factor that the results are quantised with
+  int rows, N, K, groups;
+  int format, y_type;
+  int early;  // weights and offsets are older than the kernel before this one (see matmul4_rows_kernel)
+  int gated;  // y = quantise(silu(a . gate) * (a . up))
+};
+
+cudaError_t launch_fp4_quantize(const Quantize4Args& a, cudaStream_t st);
+cudaError_t launch_fp4_dequantize(const Dequantize4Args& a, cudaStream_t st);
+int launch_fp4_matmul(const Matmul4Args& a, cudaStream_t st);  // B2C_* code
+int launch_fp4_matmul_pair(const Matmul4Args& a, cudaStream_t st);  // its form for many rows
+cudaError_t fp4_pair_status(int* status);
+int fp4_status_read_and_clear(int32_t* status);
+cudaError_t fp4_rows_wait_selftest(cudaStream_t st);
+cudaError_t fp4_pair_wait_selftest(cudaStream_t st);
+
+}  // namespace b2c

@@ -1,0 +1,432 @@
+// Products of 4-bit matrices for many rows: tiles of 256 columns x 256 rows, shared by a pair of thread blocks on neighbouring SMs (tcgen05
+// cta_group::2), or x 128 rows of one block.
+//
+// The tensor core applies the scales and keeps the sums of the whole reduction, so a tile's accumulators are read once, at its end: eight warps
+// take them into registers, hand the columns back and turn them into results while the next tile's MMAs run.
+//
+// Roles in each block: warp 0 copies, warp 1 of the leader carries scales to tensor memory (in both blocks) and issues the MMAs, warp 2 turns
+// the scales of the A rows round, warp 3 those of the B rows, which both blocks need for all columns; warps 4-11 take results out, 32 rows x
+// half of the columns each.  The gated form takes 128 gate rows and the 128 up rows of the same columns as one B tile: a thread reads
+// both parts of its columns, so activation and quantisation happen in registers.
+#include "fp4_mma.cuh"
+
+namespace b2c {
+
+namespace {
+
+constexpr int kEpiWarps = 8;
+constexpr int kEpiWarp0 = 4;
+constexpr int kPairThreads = 32 * (kEpiWarp0 + kEpiWarps);
+// 384 threads are launched with 168 registers each; a thread of the results holds 128 sums: 128 * 88 + 256 * 208 = 384 * 168.
+constexpr int kRegsSums = 208, kRegsRest = 88;
+constexpr int kABytes = kTileM * kStageRow;
+constexpr int kBoxBytes = 32 * 128;  // results of a warp on their way out: 32 rows of 128 bytes
+// CTAS thread blocks share a tile of CTAS * 128 rows and TN columns.
+template <int CTAS, int TN>
+struct TileShape4 {
+  static constexpr int kRows = CTAS * kTileM;
+  static constexpr int kBRows = TN / CTAS;  // B rows that a block brings, in boxes of
+  static constexpr int kBoxRows = kBRows < kTileM ? kBRows : kTileM;
+  static constexpr int kBBytes = kBRows * kStageRow;
+  static constexpr int kColTiles = TN / kTileM;                      // of 128 columns
+  static constexpr int kScaleBytes = (1 + kColTiles) * kScaleTile;   // the block's A rows, all B rows
+  static constexpr int kStageBytes = kABytes + kBBytes + kScaleBytes;
+  static constexpr int kStages = CTAS == 1 ? 3 : (TN == 256 ? 5 : 6);
+  static constexpr int kBufs = TN == 256 ? 1 : 2;  // accumulators in tensor memory, beside the scales of two stages
+  static constexpr int kScaleCols = 16 * (1 + kColTiles);
+  static constexpr int kWarpCols = TN / 2;  // accumulator columns of a warp of results
+  static constexpr int kSmem = 1024 + kStages * kStageBytes + kEpiWarps * kBoxBytes;
+  static_assert(kBufs * TN + 2 * kScaleCols <= 512, "tensor memory");
+};
+
+template <int CTAS, int TN, bool GATED, typename YT>
+__global__ void __launch_bounds__(kPairThreads, 1)
+    matmul4_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_as, const __grid_constant__ CUtensorMap tmap_b,
+                        const __grid_constant__ CUtensorMap tmap_bs, const __grid_constant__ CUtensorMap tmap_y, const Matmul4Args a, const bool y_boxes) {
+  using S = TileShape4<CTAS, TN>;
+  static_assert(!GATED || TN == 256, "a block of 128 columns is gate and up");
+  constexpr int kStages = S::kStages, kBBytes = S::kBBytes;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ SharedCtl ctl;
+  __shared__ __align__(8) unsigned long long scales_full[8];  // a stage's scales have come (each block its own)
+  __shared__ __align__(8) unsigned long long turned[8];       // and are in place in all blocks (the leader's)
+  __shared__ int row_tiles_s;
+
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
+  const int lane = threadIdx.x & 31;
+  const uint32_t rank = CTAS == 2 ? cluster_ctarank() : 0u;  // 0: leader (issues the MMAs), 1: peer
+  const int pair_id = (int)blockIdx.x / CTAS, num_pairs = (int)gridDim.x / CTAS;
+  const uint32_t a_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t b_base = a_base + kStages * kABytes;
+  const uint32_t s_base = b_base + kStages * kBBytes;
+  const uint32_t box_base = s_base + kStages * S::kScaleBytes;
+
+  if (warp == 0) {
+    if (lane < kStages) {
+      // full[] is used in the leader only: one arrival (its producer) plus the bytes of both blocks
+      mbar_init(smem_u32(&ctl.full[lane]), 1);
+      mbar_init(smem_u32(&ctl.empty[lane]), 1);
+      mbar_init(smem_u32(&scales_full[lane]), 1);
+      mbar_init(smem_u32(&turned[lane]), 2 * CTAS);
+    }
+    if (lane == 8) {
+      for (int b = 0; b < S::kBufs; ++b) {
+        mbar_init(smem_u32(&ctl.tmem_full[b]), 1);
+        mbar_init(smem_u32(&ctl.tmem_empty[b]), CTAS * kEpiWarps);
+      }
+      ctl.abort_flag = 0;
+    }
+    if (lane == 9) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_a) : "memory");
+    if (lane == 10) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_b) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    if constexpr (CTAS == 2) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl.tmem_base)), "r"(512) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl.tmem_base)), "r"(512) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+  }
+  pdl_wait();
+  if (warp == 2) {
+    const int n = count_row_tiles(a, S::kRows);
+    if (lane == 0) row_tiles_s = n;
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  // the other block's barriers must be initialised before anything arrives on them
+  if (CTAS == 2) cluster_sync();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem_acc = __shfl_sync(0xffffffffu, ctl.tmem_base, 0);
+  const uint32_t tmem_scales = tmem_acc + S::kBufs * TN;
+  const int row_tiles = row_tiles_s;
+  const int cols = GATED ? kTileM : TN;  // output columns of a tile
+  const int n_tiles = (a.N + cols - 1) / cols;
+  const int tiles = row_tiles * n_tiles;  // (fits: checked by the host)
+  const int kb_all = (a.K + kFp4Stage - 1) / kFp4Stage;
+
+  if (warp < kEpiWarp0) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
+    if (warp == 0) {
+      // ---------------------------------------------------------------- copies (both blocks)
+      const uint32_t on = elect_one() ? 1u : 0u;
+      int s = 0;
+      uint32_t ph = 0;
+      bool alive = true;
+      for (int t = pair_id; t < tiles && alive; t += num_pairs) {
+        const PairTile p = pair_tile<CTAS>(a, t, row_tiles, n_tiles);
+        const int m = p.row0 + (int)rank * kTileM;
+        // the tile's columns, 128 at a time: row of the B matrix, and which matrix
+        auto b_row = [&](int i) { return GATED ? p.nt * kTileM : p.nt * TN + i * kTileM; };
+        auto b_plane = [&](int i) { return GATED ? 2 * p.group + i : p.group; };
+        for (int kb = 0; kb < kb_all; ++kb) {
+          if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.empty[s]), ph ^ 1u, &ctl, &g_wait_status))) {
+            alive = false;
+            break;
+          }
+          const uint32_t sfull = smem_u32(&scales_full[s]), sdst = s_base + s * S::kScaleBytes;
+          mbar_arrive_expect_tx(sfull, S::kScaleBytes, on);
+          const int sx = scale_byte(kb, a.format);
+          tma_load_2d(sdst, &tmap_as, sx, m, sfull, on);
+#pragma unroll
+          for (int i = 0; i < S::kColTiles; ++i) tma_load_3d(sdst + (1 + i) * kScaleTile, &tmap_bs, sx, b_row(i), b_plane(i), sfull, on);
+          const uint32_t full = CTAS == 2 ? map_to_rank(smem_u32(&ctl.full[s]), 0u) : smem_u32(&ctl.full[s]);
+          if (rank == 0) mbar_arrive_expect_tx(smem_u32(&ctl.full[s]), (uint32_t)CTAS * (kABytes + kBBytes), on);
+          const uint32_t dst = b_base + s * kBBytes;
+          if constexpr (CTAS == 2) {
+            tma_pair_load_2d(a_base + s * kABytes, &tmap_a, kb * kStageRow, m, full, on);
+            if constexpr (S::kColTiles == 2) tma_pair_load_3d(dst, &tmap_b, kb * kStageRow, b_row((int)rank), b_plane((int)rank), full, on);
+            else tma_pair_load_3d(dst, &tmap_b, kb * kStageRow, p.nt * TN + (int)rank * S::kBRows, p.group, full, on);
+          } else {
+            tma_load_2d(a_base + s * kABytes, &tmap_a, kb * kStageRow, m, full, on);
+#pragma unroll
+            for (int i = 0; i < S::kColTiles; ++i) tma_load_3d(dst + i * kTileM * kStageRow, &tmap_b, kb * kStageRow, b_row(i), b_plane(i), full, on);
+          }
+          if (++s == kStages) {
+            s = 0;
+            ph ^= 1u;
+          }
+        }
+      }
+      __syncwarp();
+    } else if (warp == 1) {
+      // ---------------------------------------------------------------- scales to tensor memory, MMA issue (leader)
+      if (rank == 0) {
+        const uint32_t on = elect_one() ? 1u : 0u;
+        const uint32_t idesc = make_idesc_f4(S::kRows, TN, a.format);
+        const int groups4 = scale_groups(a.format);
+        int s = 0, buf = 0;
+        uint32_t ph = 0, bph = 0, ts_at = 0;
+        bool alive = true;
+        for (int t = pair_id; t < tiles && alive; t += num_pairs) {
+          if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.tmem_empty[buf]), bph ^ 1u, &ctl, &g_wait_status))) break;
+          for (int kb = 0; kb < kb_all; ++kb) {
+            if (!__all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&turned[s]), ph, &ctl, &g_wait_status)) ||
+                !__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.full[s]), ph, &ctl, &g_wait_status))) {
+              alive = false;
+              break;
+            }
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const int ksteps = min(4, (a.K - kb * kFp4Stage + 63) / 64);
+            // (copies and MMAs run in the order in which they are issued)
+            const uint32_t ts = tmem_scales + ts_at, scales = s_base + s * S::kScaleBytes;
+            ts_at = S::kScaleCols - ts_at;
+            for (int j = 0; j < groups4; ++j) {
+              copy_scales<CTAS>(ts + 4 * j, scales + 512 * j, on);
+#pragma unroll
+              for (int i = 0; i < S::kColTiles; ++i)
+                copy_scales<CTAS>(ts + 16 + 4 * (j * S::kColTiles + i), scales + (1 + i) * kScaleTile + 512 * j, on);
+            }
+            mma_f4_stage<CTAS>(tmem_acc + buf * TN, make_smem_desc(a_base + s * kABytes, kStageRow), make_smem_desc(b_base + s * kBBytes, kStageRow), idesc,
+                               ts, ts + 16, 4 * S::kColTiles, a.format, kb > 0, on, ksteps);
+            if constexpr (CTAS == 2) mma_commit_pair(smem_u32(&ctl.empty[s]), on);
+            else mma_commit(smem_u32(&ctl.empty[s]), on);
+            if (++s == kStages) {
+              s = 0;
+              ph ^= 1u;
+            }
+          }
+          if constexpr (CTAS == 2) mma_commit_pair(smem_u32(&ctl.tmem_full[buf]), on);
+          else mma_commit(smem_u32(&ctl.tmem_full[buf]), on);
+          if (++buf == S::kBufs) {
+            buf = 0;
+            bph ^= 1u;
+          }
+        }
+      }
+      pdl_launch_dependents();
+      __syncwarp();
+    } else {
+      // ---------------------------------------------------------------- scales turned round (both blocks)
+      int s = 0;
+      uint32_t ph = 0;
+      bool alive = true;
+      for (int t = pair_id; t < tiles && alive; t += num_pairs) {
+        for (int kb = 0; kb < kb_all; ++kb) {
+          if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&scales_full[s]), ph, &ctl, &g_wait_status))) {
+            alive = false;
+            break;
+          }
+          const uint32_t scales = s_base + s * S::kScaleBytes;
+          if (warp == 2) {
+            turn_scales(scales, kTileM, a.format, kb, lane);
+          } else {
+#pragma unroll
+            for (int i = 0; i < S::kColTiles; ++i) turn_scales(scales + (1 + i) * kScaleTile, kTileM, a.format, kb, lane);
+          }
+          __syncwarp();
+          if (lane == 0) {
+            if constexpr (CTAS == 2) mbar_arrive_cluster(map_to_rank(smem_u32(&turned[s]), 0u));
+            else mbar_arrive(smem_u32(&turned[s]));
+          }
+          if (++s == kStages) {
+            s = 0;
+            ph ^= 1u;
+          }
+        }
+      }
+      __syncwarp();
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSums));
+    // ---------------------------------------------------------------- results (both blocks)
+    const int quad = warp & 3;                 // lanes of tensor memory this warp may read
+    const int half = (warp - kEpiWarp0) >> 2;  // its columns
+    const uint32_t leader_empty = CTAS == 2 ? map_to_rank(smem_u32(&ctl.tmem_empty[0]), 0u) : smem_u32(&ctl.tmem_empty[0]);
+    const uint32_t taddr0 = tmem_acc + ((uint32_t)(quad * 32) << 16);
+    const int in_tile = quad * 32 + lane;
+    Factor4 f;
+    if constexpr (GATED) f = load_factor4(a.y_global, a.format);
+    int buf = 0;
+    uint32_t bph = 0;
+    bool ok = true;
+    for (int t = pair_id; t < tiles; t += num_pairs) {
+      const PairTile p = pair_tile<CTAS>(a, t, row_tiles, n_tiles);
+      const float alpha = alpha_of(a, p.group);
+      // (voted, so that the lanes are together at the warp-wide loads; a wait that gave up does not leave the loop)
+      ok = ok && __all_sync(0xffffffffu, mbar_wait_inline(smem_u32(&ctl.tmem_full[buf]), bph, &ctl, &g_wait_status));
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      float v[S::kWarpCols];
+      // gated: 64 gate columns, then the up columns of the same 64
+#pragma unroll
+      for (int c = 0; c < S::kWarpCols; c += 64)
+        tmem_ld64(taddr0 + (uint32_t)(buf * TN + (GATED ? half * 64 + c * 2 : half * S::kWarpCols + c)), reinterpret_cast<int32_t*>(v + c));
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) {
+        if constexpr (CTAS == 2) mbar_arrive_cluster_relaxed(leader_empty + 8 * buf);
+        else mbar_arrive(leader_empty + 8 * buf);
+      }
+      if (++buf == S::kBufs) {
+        buf = 0;
+        bph ^= 1u;
+      }
+      const long long m = (long long)p.row0 + (int)rank * kTileM + in_tile;
+      if constexpr (GATED) {
+        const int n = p.nt * kTileM + half * 64;
+#pragma unroll
+        for (int i = 0; i < 64; ++i) v[i] = silu(v[i] * alpha) * (v[64 + i] * alpha);
+        uint8_t* y = (uint8_t*)a.y + m * a.ldy + n / 2;
+        const bool on = ok && m < p.row_end;
+#pragma unroll
+        for (int c = 0; c < 64; c += 32) {
+          uint32_t mx[2] = {0, 0}, q[4];
+#pragma unroll
+          for (int i = 0; i < 32; ++i) mx[i >> 4] = max(mx[i >> 4], abs_bits(v[c + i]));
+          if (a.format == B2C_MXFP4) mx[0] = mx[1] = max(mx[0], mx[1]);
+          Scale4 s[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            s[i] = scale_of(mx[i], f, a.format);
+            quantise4<16>(s[i], f, a.format, v + c + 16 * i, q + 2 * i);
+          }
+          if (on && n + c < a.N) {  // (N is a multiple of 32, ldy of 16)
+            *reinterpret_cast<uint4*>(y + c / 2) = make_uint4(q[0], q[1], q[2], q[3]);
+            uint8_t* ys = a.y_scale + m * a.ldys + (n + c) / fp4_block(a.format);
+            if (a.format == B2C_MXFP4) ys[0] = (uint8_t)s[0].code;
+            else *reinterpret_cast<uint16_t*>(ys) = (uint16_t)(s[0].code | (s[1].code << 8));  // (ldys is a multiple of 16)
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < S::kWarpCols; ++i) v[i] *= alpha;
+        const int n = p.nt * TN + half * S::kWarpCols, m0 = p.row0 + (int)rank * kTileM + quad * 32;
+        // 128 bytes of each of the warp's 32 rows go to shared memory (16-byte pieces, swizzled as the tensor map says).  From there, if
+        // the copy engine can address the result and all 32 rows are this group's, in one copy, which runs beside the next tile; else by the
+        // lanes.  The copy clips what lies past the last column in steps of 16 bytes: a box that the result ends in at another place is
+        // left to the lanes.
+        constexpr int kCols = 128 / (int)sizeof(YT);
+        const uint32_t box = box_base + (uint32_t)((warp - kEpiWarp0) * kBoxBytes);
+#pragma unroll
+        for (int i = 0; i < S::kWarpCols; i += kCols) {
+          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+          __syncwarp();
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            constexpr int kPer = 16 / (int)sizeof(YT);
+            const float* u = v + i + c * kPer;
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if constexpr (sizeof(YT) == 4) w[j] = __float_as_uint(u[j]);
+              else w[j] = pack2<YT>(u[2 * j], u[2 * j + 1]);
+            }
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + (uint32_t)(lane * 128 + ((c ^ (lane & 7)) * 16))), "r"(w[0]),
+                         "r"(w[1]), "r"(w[2]), "r"(w[3])
+                         : "memory");
+          }
+          const bool by_copy = y_boxes && m0 + 32 <= p.row_end && (n + i + kCols <= a.N || a.N * (int)sizeof(YT) % 16 == 0);
+          if (by_copy) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0 && ok && n + i < a.N) {
+              asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(&tmap_y),
+                           "r"((n + i) * (int)sizeof(YT)), "r"(m0), "r"(box)
+                           : "memory");
+              asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            }
+          } else {
+            __syncwarp();
+            if (ok && n + i < a.N)
+              store_box<YT>((YT*)a.y + (long long)m0 * a.ldy + n + i, a.ldy, box, min(32, p.row_end - m0), min(kCols, a.N - n - i), y_boxes, lane);
+            __syncwarp();
+          }
+        }
+      }
+    }
+  }
+
+  // copies of results read shared memory: they end before the block does
+  if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+
+  // ---------------------------------------------------------------- teardown
+  // No block of the pair leaves, or frees tensor memory, while the other may still read its shared memory, arrive on
+  // its barriers or write its accumulators.
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (ctl.abort_flag) {
+    const unsigned long long t0 = global_ns();
+    while (global_ns() - t0 < 50000ull) __nanosleep(1000);
+    __syncthreads();
+  }
+  if (CTAS == 2) cluster_sync();
+  if (warp == 1) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if constexpr (CTAS == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_acc), "r"(512) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_acc), "r"(512) : "memory");
+  }
+}
+
+// Whether the copy engine can take a product's results out (see results_by_copy).
+bool boxes_of(const Matmul4Args& a, int bytes) {
+  return !a.gated && (reinterpret_cast<uintptr_t>(a.y) & 15) == 0 && a.ldy * bytes % 16 == 0 && (long long)a.N * bytes <= 0x7FFFFFFFLL;
+}
+
+template <int CTAS, int TN, bool GATED, typename YT>
+int launch_pair(const Matmul4Args& a, cudaStream_t st) {
+  using S = TileShape4<CTAS, TN>;
+  const long long cols = GATED ? kTileM : TN;
+  const long long n_tiles = (a.N + cols - 1) / cols;
+  const long long row_tiles = a.offsets ? a.rows / S::kRows + std::min(a.groups, a.rows) : (a.rows + S::kRows - 1) / S::kRows;
+  if (row_tiles * n_tiles > 0x7FFFFFFFLL - kNumSMs) return B2C_E_UNSUPPORTED;
+  const uint64_t bytes = a.K / 2, scales = fp4_scales(a.K, a.format), planes = (uint64_t)a.groups * (GATED ? 2 : 1);
+  CUtensorMap ta, tas, tb, tbs, ty;
+  int rc = encode_tiled_2d(&ta, a.a, bytes, a.rows, a.rows > 1 ? a.lda : bytes, kStageRow, kTileM, 128);
+  if (rc == B2C_OK) rc = encode_tiled_2d(&tas, a.a_scale, scales, a.rows, a.rows > 1 ? a.lds : fp4_scale_pitch(a.K, a.format), kScaleRow, kTileM, 0);
+  if (rc == B2C_OK) rc = encode_tiled_3d(&tb, a.b, bytes, a.N, planes, bytes, (uint64_t)a.N * bytes, kStageRow, S::kBoxRows, 128);
+  if (rc == B2C_OK) rc = encode_tiled_3d(&tbs, a.b_scale, scales, a.N, planes, a.ldbs, (uint64_t)a.N * a.ldbs, kScaleRow, kTileM, 0);
+  if (rc != B2C_OK) return rc;
+  const bool y_boxes = boxes_of(a, (int)sizeof(YT));  // (of 128 bytes x 32 rows)
+  ty = ta;
+  if (y_boxes) rc = encode_tiled_2d(&ty, a.y, (uint64_t)a.N * sizeof(YT), a.rows, a.rows > 1 ? (uint64_t)a.ldy * sizeof(YT) : ((uint64_t)a.N * sizeof(YT) + 15) / 16 * 16, 128, 32, 128);
+  if (rc != B2C_OK) return rc;
+  static std::atomic<unsigned long long> configured{0};
+  cudaError_t e = set_max_dynamic_smem_once(configured, (const void*)matmul4_pair_kernel<CTAS, TN, GATED, YT>, S::kSmem);
+  if (e == cudaSuccess) {
+    const int pairs = (int)std::min<long long>(row_tiles * n_tiles, kNumSMs / CTAS);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(CTAS * pairs));
+    cfg.blockDim = dim3(kPairThreads);
+    cfg.dynamicSmemBytes = S::kSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = CTAS;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = CTAS == 2 ? 2 : 1;
+    e = cudaLaunchKernelEx(&cfg, matmul4_pair_kernel<CTAS, TN, GATED, YT>, ta, tas, tb, tbs, ty, a, y_boxes);
+  }
+  if (e != cudaSuccess) {
+    set_last_cuda_error((int)e);
+    return B2C_E_CUDA;
+  }
+  return B2C_OK;
+}
+
+template <int CTAS, int TN>
+int launch_type(const Matmul4Args& a, cudaStream_t st) {
+  if (a.y_type == B2C_F32) return launch_pair<CTAS, TN, false, float>(a, st);
+  if (a.y_type == B2C_F16) return launch_pair<CTAS, TN, false, __half>(a, st);
+  return launch_pair<CTAS, TN, false, __nv_bfloat16>(a, st);
+}
+
+}  // namespace
+
+int launch_fp4_matmul_pair(const Matmul4Args& a, cudaStream_t st) {
+  const int rows = a.offsets ? (int)(((long long)a.rows + a.groups - 1) / a.groups) : a.rows;
+  if (a.gated) return rows <= 768 ? launch_pair<1, 256, true, uint8_t>(a, st) : launch_pair<2, 256, true, uint8_t>(a, st);
+  if (a.offsets) return rows <= 768 ? launch_type<1, 256>(a, st) : launch_type<2, 256>(a, st);
+  return launch_type<2, 256>(a, st);
+}
+
+cudaError_t fp4_pair_wait_selftest(cudaStream_t st) { return launch_wait_selftest(st); }
+
+cudaError_t fp4_pair_status(int* status) { return take_status(status); }
+
+}  // namespace b2c

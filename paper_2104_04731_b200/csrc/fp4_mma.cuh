@@ -1,0 +1,124 @@
+// Device code shared by the kernels that form products of 4-bit matrices on the tensor core (tcgen05.mma, block_scale).
+//
+// A stage is 256 elements of the reduction: 128 bytes of every row, four MMAs of depth 64.  The tensor core takes the scales from tensor
+// memory: lane r, column c of a group of four columns holds four consecutive scales of row 32 c + r, for all four quarters of the lanes alike.
+// In memory a row's scales follow each other, so 128 rows come as 128 pieces of 16 bytes; a warp turns them round in place (a lane has the pieces
+// of four rows, 32 apart, and every group of columns takes a word of each) and tcgen05.cp carries 512 bytes to four columns.
+#pragma once
+
+#include "fp4_common.cuh"
+#include "fp8_mma.cuh"
+
+namespace b2c {
+
+namespace {
+
+constexpr int kStageRow = kFp4Stage / 2;  // bytes
+constexpr int kScaleRow = 16;             // bytes of a row's scales that are copied for a stage (MX: of two)
+constexpr int kScaleTile = 128 * kScaleRow;
+
+// Instruction descriptor of kind::mxf4 and kind::mxf4nvf4: both operands E2M1 (code 1 at bits 7 and 10), N/8 at bit 17, kind of the scales (0 E4M3,
+// 1 E8M0) at bit 23, M/16 at bit 24; the half of a scale word that an MMA uses at bits 29 and 4.
+__device__ __forceinline__ uint32_t make_idesc_f4(int m, int n, int format) {
+  return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((format == B2C_MXFP4 ? 1u : 0u) << 23) | ((uint32_t)(m >> 4) << 24);
+}
+constexpr uint32_t kUpperScales = (2u << 29) | (2u << 4);
+
+// Descriptor of 32 lanes x 16 bytes in shared memory, rows of 8 x 16 bytes 128 apart.
+__device__ __forceinline__ uint64_t make_scale_desc(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFF) >> 4) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);
+}
+// 512 bytes at `addr` to four columns of tensor memory; with CTAS == 2 in both blocks of the pair, each from its own shared memory.
+template <int CTAS>
+__device__ __forceinline__ void copy_scales(uint32_t taddr, uint32_t addr, uint32_t on) {
+  const uint64_t desc = make_scale_desc(addr);
+  if constexpr (CTAS == 1)
+    asm volatile("{\n.reg .pred q;\nsetp.ne.b32 q, %2, 0;\n@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n}" ::"r"(taddr), "l"(desc), "r"(on) : "memory");
+  else
+    asm volatile("{\n.reg .pred q;\nsetp.ne.b32 q, %2, 0;\n@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n}" ::"r"(taddr), "l"(desc), "r"(on) : "memory");
+}
+inline __host__ __device__ int scale_groups(int format) { return format == B2C_MXFP4 ? 2 : 4; }  // of four columns, a stage and 128 rows
+
+// One stage: `ksteps` (1..4) MMAs over consecutive 32-byte slices; the first overwrites unless `accumulate`.  Scales of the A rows at
+// sa, a group of four columns for one MMA (NV) or two (MX); of the B rows at sb, groups b_cols columns apart.
+template <int CTAS>
+__device__ __forceinline__ void mma_f4_stage(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t b_cols,
+                                             int format, uint32_t accumulate, uint32_t on, int ksteps) {
+#define B2C_F4_STAGE(GROUP, KIND, SA1, SA2, SA3, SB1, SB2, SB3, ID1)                                              \
+  asm volatile(                                                                                                   \
+      "{\n"                                                                                                       \
+      ".reg .pred pacc, ptrue, q0, q1, q2, q3;\n"                                                                 \
+      ".reg .b64 a1, a2, a3, b1, b2, b3;\n"                                                                       \
+      "setp.ne.b32 pacc, %4, 0;\n"                                                                                \
+      "setp.eq.b32 ptrue, 0, 0;\n"                                                                                \
+      "setp.ne.b32 q0, %5, 0;\n"                                                                                  \
+      "setp.gt.and.s32 q1, %6, 1, q0;\n"                                                                          \
+      "setp.gt.and.s32 q2, %6, 2, q0;\n"                                                                          \
+      "setp.gt.and.s32 q3, %6, 3, q0;\n"                                                                          \
+      "add.u64 a1, %1, 2;\n"                                                                                      \
+      "add.u64 b1, %2, 2;\n"                                                                                      \
+      "add.u64 a2, %1, 4;\n"                                                                                      \
+      "add.u64 b2, %2, 4;\n"                                                                                      \
+      "add.u64 a3, %1, 6;\n"                                                                                      \
+      "add.u64 b3, %2, 6;\n"                                                                                      \
+      "@q0 tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], %1, %2, %3, [%7], [%8], pacc;\n"                 \
+      "@q1 tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], a1, b1, %9, [%10], [%11], ptrue;\n"              \
+      "@q2 tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], a2, b2, %3, [%12], [%13], ptrue;\n"              \
+      "@q3 tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], a3, b3, %9, [%14], [%15], ptrue;\n"              \
+      "}" ::"r"(d_tmem),                                                                                          \
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(on), "r"(ksteps), "r"(sa), "r"(sb), "r"(ID1),      \
+      "r"(SA1), "r"(SB1), "r"(SA2), "r"(SB2), "r"(SA3), "r"(SB3)                                                  \
+      : "memory")
+  if (format == B2C_MXFP4) {
+    if (CTAS == 1) B2C_F4_STAGE("1", "mxf4.block_scale.scale_vec::2X", sa, sa + 4, sa + 4, sb, sb + b_cols, sb + b_cols, idesc | kUpperScales);
+    else B2C_F4_STAGE("2", "mxf4.block_scale.scale_vec::2X", sa, sa + 4, sa + 4, sb, sb + b_cols, sb + b_cols, idesc | kUpperScales);
+  } else {
+    if (CTAS == 1) B2C_F4_STAGE("1", "mxf4nvf4.block_scale.scale_vec::4X", sa + 4, sa + 8, sa + 12, sb + b_cols, sb + 2 * b_cols, sb + 3 * b_cols, idesc);
+    else B2C_F4_STAGE("2", "mxf4nvf4.block_scale.scale_vec::4X", sa + 4, sa + 8, sa + 12, sb + b_cols, sb + 2 * b_cols, sb + 3 * b_cols, idesc);
+  }
+#undef B2C_F4_STAGE
+}
+
+// Byte of a row of scales that the copy for stage kb starts at: on the copy engine's 16-byte grid.
+__device__ __forceinline__ int scale_byte(int kb, int format) { return format == B2C_MXFP4 ? (kb >> 1) * kScaleRow : kb * kScaleRow; }
+
+// The copied scales of up to 128 rows, turned round in place; called by a whole warp.  What follows in the asynchronous proxy sees it
+// after the caller's barrier.
+__device__ __forceinline__ void turn_scales(uint32_t base, int rows, int format, int kb, int lane) {
+  if (format == B2C_MXFP4) {
+    uint32_t lo[4], hi[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      lo[g] = hi[g] = 0;
+      if (32 * g < rows)
+        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(lo[g]), "=r"(hi[g]) : "r"(base + (uint32_t)((32 * g + lane) * kScaleRow + (kb & 1) * 8)) : "memory");
+    }
+    __syncwarp();
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + (uint32_t)(lane * 16)), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + (uint32_t)(512 + lane * 16)), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
+  } else {
+    uint32_t w[4][4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[g][j] = 0;
+      if (32 * g < rows)
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(w[g][0]), "=r"(w[g][1]), "=r"(w[g][2]), "=r"(w[g][3])
+                     : "r"(base + (uint32_t)((32 * g + lane) * kScaleRow))
+                     : "memory");
+    }
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + (uint32_t)(512 * j + lane * 16)), "r"(w[0][j]), "r"(w[1][j]), "r"(w[2][j]), "r"(w[3][j]) : "memory");
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
+
+__device__ __forceinline__ float alpha_of(const Matmul4Args& a, int group) {
+  return (a.alpha != nullptr ? a.alpha[group] : 1.0f) * (a.alpha2 != nullptr ? *a.alpha2 : 1.0f);
+}
+
+}  // namespace
+}  // namespace b2c

@@ -1,0 +1,252 @@
+// Quantisation to 4-bit floating point with microscales, and back.  Memory-bound: every element is read once and kept in registers
+// between the search for its block's largest magnitude and the conversion.
+#include "fp4_common.cuh"
+
+namespace b2c {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kRun = 16;  // elements of a lane: a block of NV, half a block of MX
+
+// Largest magnitude, as bits of fp32, of 16 elements as they lie in memory (of 16-bit types as whole numbers, two at a time).
+__device__ __forceinline__ uint32_t raw_amax(const Raw16<float>& r) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    m = max(m, max(max(r.u[i].x & 0x7FFFFFFFu, r.u[i].y & 0x7FFFFFFFu), max(r.u[i].z & 0x7FFFFFFFu, r.u[i].w & 0x7FFFFFFFu)));
+  return m;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t raw_amax(const Raw16<T>& r) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    m = __vmaxu2(m, r.u[i].x & 0x7FFF7FFFu);
+    m = __vmaxu2(m, r.u[i].y & 0x7FFF7FFFu);
+    m = __vmaxu2(m, r.u[i].z & 0x7FFF7FFFu);
+    m = __vmaxu2(m, r.u[i].w & 0x7FFF7FFFu);
+  }
+  float lo, hi;
+  unpack2<T>(max(m >> 16, m & 0xFFFFu), &lo, &hi);
+  return __float_as_uint(lo) & 0x7FFFFFFFu;
+}
+
+// Elements of a lane to the row, or the rows, of its block.
+__device__ __forceinline__ void store_run(const Quantize4Args& a, long long row, int run, const Scale4& s, const uint32_t* q) {
+  const bool first = a.format == B2C_NVFP4 || (run & 1) == 0;
+  const int at = a.format == B2C_NVFP4 ? run : run >> 1;
+  for (int j = 0; j < (a.map == nullptr ? 1 : a.copies); ++j) {
+    const long long to = a.map == nullptr ? row : (long long)a.map[row * a.copies + j];
+    if (to < 0) continue;
+    *reinterpret_cast<uint2*>(a.q + to * a.ldq + run * (kRun / 2)) = make_uint2(q[0], q[1]);
+    if (first) a.scale[to * a.lds + at] = (uint8_t)s.code;
+  }
+}
+
+// Rows on the grid of 16-byte loads and 8-byte stores, whole blocks of 32: a lane has 16 elements, and those of the next turn are under
+// way while these are converted.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) quantize4_kernel(const Quantize4Args a, const FastDiv per_row, const unsigned runs) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const Factor4 f = load_factor4(a.global, a.format);
+  const unsigned step = gridDim.x * kThreads;
+  unsigned id = blockIdx.x * kThreads + threadIdx.x;
+  Raw16<T> next = {};
+  auto fetch = [&](unsigned i) {
+    if (i >= runs) return;
+    const unsigned row = per_row.div(i);
+    next = load_raw16<T>((const T*)a.x + (long long)row * a.ldx + (i - row * per_row.d) * kRun);
+  };
+  fetch(id);
+  for (unsigned first = blockIdx.x * kThreads; first < runs; first += step, id += step) {  // (the same for all lanes of a warp)
+    const Raw16<T> raw = next;
+    fetch(id + step);
+    uint32_t m = raw_amax(raw);
+    if (a.format == B2C_MXFP4) m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));  // (runs are a multiple of two: a block's lanes both have some)
+    if (id >= runs) continue;
+    const Scale4 s = scale_of(m, f, a.format);
+    float v[kRun];
+    widen16<T>(raw, v);
+    uint32_t q[2];
+    quantise4<kRun>(s, f, a.format, v, q);
+    const unsigned row = per_row.div(id);
+    store_run(a, row, (int)(id - row * per_row.d), s, q);
+  }
+}
+
+// Any rows: the 16 elements of each lane are brought by 16 neighbouring lanes and change hands in shared memory; packed bytes leave the same way.
+constexpr int kPitch = kRun + 1;
+template <typename T>
+__global__ void __launch_bounds__(kThreads) quantize4_any_kernel(const Quantize4Args a, const FastDiv per_row, const long long runs) {
+  __shared__ float stage[kThreads / 32][32 * kPitch];
+  pdl_wait();
+  pdl_launch_dependents();
+  const Factor4 f = load_factor4(a.global, a.format);
+  const int lane = threadIdx.x & 31;
+  float* mine = stage[threadIdx.x >> 5];
+  uint8_t* bytes = reinterpret_cast<uint8_t*>(mine);
+  for (long long first = (long long)blockIdx.x * kThreads + (threadIdx.x & ~31u); first < runs; first += (long long)gridDim.x * kThreads) {
+    const long long id = min(first + lane, runs - 1);
+    // (rows * runs of a row may pass 32 bits: the quotient of the part above 2^31 goes the long way)
+    const long long row = id < (1ll << 31) ? (long long)per_row.div((uint32_t)id) : id / per_row.d;
+    const int run = (int)(id - row * per_row.d);
+    const int left = first + lane < runs ? max(0, min(kRun, a.cols - run * kRun)) : 0;
+    const T* p = (const T*)a.x + row * a.ldx + run * kRun;
+    float v[kRun];
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) {
+      const int from = 2 * i + (lane >> 4);
+      const T* src = (const T*)__shfl_sync(0xffffffffu, (unsigned long long)p, from);
+      const int n = __shfl_sync(0xffffffffu, left, from);
+      v[i] = (lane & 15) < n ? to_float<T>(src[lane & 15]) : 0.0f;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) mine[(2 * i + (lane >> 4)) * kPitch + (lane & 15)] = v[i];
+    __syncwarp();
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) {
+      v[i] = mine[lane * kPitch + i];
+      m = max(m, abs_bits(v[i]));
+    }
+    if (a.format == B2C_MXFP4) m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    const Scale4 s = scale_of(m, f, a.format);
+    uint32_t q[2];
+    quantise4<kRun>(s, f, a.format, v, q);
+    __syncwarp();
+    *reinterpret_cast<uint2*>(bytes + 8 * lane) = make_uint2(q[0], q[1]);
+    __syncwarp();
+    const bool scales = left > 0 && (a.format == B2C_NVFP4 || (run & 1) == 0);
+    for (int j = 0; j < (a.map == nullptr ? 1 : a.copies); ++j) {
+      const long long to = a.map == nullptr ? row : (long long)a.map[row * a.copies + j];
+      const int n = to < 0 ? 0 : (left + 1) / 2;
+      uint8_t* dst = a.q + to * a.ldq + run * (kRun / 2);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int from = 4 * i + (lane >> 3);
+        uint8_t* d = (uint8_t*)__shfl_sync(0xffffffffu, (unsigned long long)dst, from);
+        if ((lane & 7) < __shfl_sync(0xffffffffu, n, from)) d[lane & 7] = bytes[8 * from + (lane & 7)];
+      }
+      if (scales && to >= 0) a.scale[to * a.lds + (a.format == B2C_NVFP4 ? run : run >> 1)] = (uint8_t)s.code;
+    }
+    __syncwarp();
+  }
+}
+
+// Eight values a lane, a 16-byte store of a 16-bit type.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) dequantize4_kernel(const Dequantize4Args a, const FastDiv per_row, const unsigned runs) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const float g = a.global != nullptr ? *a.global : 1.0f;
+  const int shift = a.format == B2C_MXFP4 ? 2 : 1;  // runs of eight in a block
+  constexpr int kAhead = 4;
+  const unsigned step = gridDim.x * kThreads;
+  for (unsigned id0 = blockIdx.x * kThreads + threadIdx.x; id0 < runs; id0 += kAhead * step) {
+    uint32_t q[kAhead], code[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const unsigned id = id0 + i * step;
+      q[i] = code[i] = 0;
+      if (id < runs && id >= id0) {
+        const unsigned row = per_row.div(id), run = id - row * per_row.d;
+        q[i] = *reinterpret_cast<const uint32_t*>(a.q + (long long)row * a.ldq + 4 * run);
+        code[i] = a.scale[(long long)row * a.lds + (run >> shift)];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const unsigned id = id0 + i * step;
+      if (id >= runs || id < id0) continue;
+      const unsigned row = per_row.div(id), run = id - row * per_row.d;
+      const float s = scale_value(code[i], a.format);
+      uint32_t h[4];
+      cvt_f16x8(q[i], h);
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        unpack2<__half>(h[j], &v[2 * j], &v[2 * j + 1]);
+        v[2 * j] = v[2 * j] * s * g;
+        v[2 * j + 1] = v[2 * j + 1] * s * g;
+      }
+      T* dst = (T*)a.y + (long long)row * a.ldy + 8 * run;
+      if constexpr (sizeof(T) == 4) {
+        reinterpret_cast<float4*>(dst)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(dst)[1] = make_float4(v[4], v[5], v[6], v[7]);
+      } else {
+        *reinterpret_cast<uint4*>(dst) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+      }
+    }
+  }
+}
+
+// Any rows: a byte, two values, a lane.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) dequantize4_any_kernel(const Dequantize4Args a, const FastDiv per_row, const long long all) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const float g = a.global != nullptr ? *a.global : 1.0f;
+  const int shift = a.format == B2C_MXFP4 ? 4 : 3;  // bytes in a block
+  for (long long id = (long long)blockIdx.x * kThreads + threadIdx.x; id < all; id += (long long)gridDim.x * kThreads) {
+    const long long row = id < (1ll << 31) ? (long long)per_row.div((uint32_t)id) : id / per_row.d;
+    const int at = (int)(id - row * per_row.d);
+    const uint32_t q = a.q[row * a.ldq + at];
+    const float s = scale_value(a.scale[row * a.lds + (at >> shift)], a.format);
+    uint32_t h[4];
+    cvt_f16x8(q * 0x01010101u, h);  // (of a word that the compiler sees to be a single byte, nvcc 12.9 made zeros)
+    float lo, hi;
+    unpack2<__half>(h[0], &lo, &hi);
+    T* dst = (T*)a.y + row * a.ldy + 2 * at;
+    dst[0] = from_float<T>(lo * s * g);
+    if (2 * at + 1 < a.cols) dst[1] = from_float<T>(hi * s * g);
+  }
+}
+
+bool on_grid(const void* p, long long ld_bytes, long long rows, int grid) {
+  return reinterpret_cast<uintptr_t>(p) % grid == 0 && (rows <= 1 || ld_bytes % grid == 0);
+}
+
+template <typename T>
+cudaError_t launch_quantize(const Quantize4Args& a, cudaStream_t st) {
+  // (an MX row has an even number of runs, so that the two halves of a block are neighbours in a warp)
+  const long long per_row = a.format == B2C_MXFP4 ? (a.cols + 31ll) / 32 * 2 : (a.cols + 15ll) / 16, runs = a.rows * per_row;
+  const bool wide = on_grid(a.x, a.ldx * (long long)sizeof(T), a.rows, 16) && on_grid(a.q, a.ldq, a.map != nullptr ? 2 : a.rows, 8);
+  const long long blocks = (runs + kThreads - 1) / kThreads;
+  const FastDiv div = make_fastdiv((uint32_t)per_row);
+  // resident at once: 8 blocks of 256 threads an SM; all of them load one run ahead
+  if (wide && a.cols % 32 == 0 && runs < (1ll << 30))
+    return launch_pdl(quantize4_kernel<T>, dim3((unsigned)std::min<long long>(blocks, 8 * kNumSMs)), dim3(kThreads), 0, st, a, div, (unsigned)runs);
+  return launch_pdl(quantize4_any_kernel<T>, dim3((unsigned)std::min<long long>(blocks, 64 * kNumSMs)), dim3(kThreads), 0, st, a, div, runs);
+}
+
+template <typename T>
+cudaError_t launch_dequantize(const Dequantize4Args& a, cudaStream_t st) {
+  const bool wide = on_grid(a.y, a.ldy * (long long)sizeof(T), a.rows, 16) && on_grid(a.q, a.ldq, a.rows, 4);
+  if (wide && a.cols % 8 == 0 && a.rows * (a.cols / 8) < (1ll << 30)) {
+    const long long runs = a.rows * (a.cols / 8), blocks = (runs + kThreads - 1) / kThreads;
+    return launch_pdl(dequantize4_kernel<T>, dim3((unsigned)std::min<long long>(blocks, 8 * kNumSMs)), dim3(kThreads), 0, st, a,
+                      make_fastdiv((uint32_t)(a.cols / 8)), (unsigned)runs);
+  }
+  const long long per_row = (a.cols + 1) / 2, all = a.rows * per_row, blocks = (all + kThreads - 1) / kThreads;
+  return launch_pdl(dequantize4_any_kernel<T>, dim3((unsigned)std::min<long long>(blocks, 64 * kNumSMs)), dim3(kThreads), 0, st, a,
+                    make_fastdiv((uint32_t)per_row), all);
+}
+
+}  // namespace
+
+cudaError_t launch_fp4_quantize(const Quantize4Args& a, cudaStream_t st) {
+  if (a.x_type == B2C_F32) return launch_quantize<float>(a, st);
+  if (a.x_type == B2C_F16) return launch_quantize<__half>(a, st);
+  return launch_quantize<__nv_bfloat16>(a, st);
+}
+
+cudaError_t launch_fp4_dequantize(const Dequantize4Args& a, cudaStream_t st) {
+  if (a.y_type == B2C_F32) return launch_dequantize<float>(a, st);
+  if (a.y_type == B2C_F16) return launch_dequantize<__half>(a, st);
+  return launch_dequantize<__nv_bfloat16>(a, st);
+}
+
+}  // namespace b2c

@@ -58,6 +58,24 @@ __device__ __forceinline__ void unpack2<__nv_bfloat16>(uint32_t w, float* lo, fl
   *hi = __uint_as_float(w & 0xFFFF0000u);
 }
 
+// Up to n of four neighbouring results.
+template <typename T>
+__device__ __forceinline__ void store4(T* p, const float* v, int n) {
+  if (n >= 4 && (reinterpret_cast<uintptr_t>(p) & (4 * sizeof(T) - 1)) == 0) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]));
+  } else {
+    for (int i = 0; i < min(n, 4); ++i) p[i] = from_float<T>(v[i]);
+  }
+}
+template <>
+__device__ __forceinline__ void store4<float>(float* p, const float* v, int n) {
+  if (n >= 4 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  } else {
+    for (int i = 0; i < min(n, 4); ++i) p[i] = v[i];
+  }
+}
+
 // A pair of fp32 values in one 64-bit register pair; two multiplications or FMAs are one instruction.
 typedef unsigned long long f32x2;
 __device__ __forceinline__ f32x2 pair_of(float lo, float hi) {

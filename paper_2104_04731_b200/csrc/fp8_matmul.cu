@@ -40,23 +40,6 @@ struct RowsShape {
   static constexpr int kSmem = 1024 + (kStages * kStageBytes > kPartBytes ? kStages * kStageBytes : kPartBytes);
 };
 
-template <typename T>
-__device__ __forceinline__ void store4(T* p, const float* v, int n) {
-  if (n >= 4 && (reinterpret_cast<uintptr_t>(p) & (4 * sizeof(T) - 1)) == 0) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]));
-  } else {
-    for (int i = 0; i < min(n, 4); ++i) p[i] = from_float<T>(v[i]);
-  }
-}
-template <>
-__device__ __forceinline__ void store4<float>(float* p, const float* v, int n) {
-  if (n >= 4 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-  } else {
-    for (int i = 0; i < min(n, 4); ++i) p[i] = v[i];
-  }
-}
-
 template <int NT, int WT, typename YT>
 __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, RowsShape<NT, WT>::kPerSm)
     matmul_rows_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const MatmulArgs a,
@@ -129,7 +112,7 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, RowsShape<NT, WT>
     int s = ahead % stages;
     uint32_t ph = ahead == stages ? 1u : 0u;
     for (int kb = kb0 + ahead; kb < kb1; ++kb) {
-      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.empty[s]), ph ^ 1u, &ctl, &g_fp8_status))) break;
+      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.empty[s]), ph ^ 1u, &ctl, &g_wait_status))) break;
       load_w(kb, s);
       load_x(kb, s);
       if (++s == stages) {
@@ -145,8 +128,8 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, RowsShape<NT, WT>
     int s = 0, buf = 0;
     uint32_t ph = 0, bph = 0;
     for (int kb = kb0; kb < kb1; ++kb) {
-      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.tmem_empty[buf]), bph ^ 1u, &ctl, &g_fp8_status))) break;
-      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.full[s]), ph, &ctl, &g_fp8_status))) break;
+      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.tmem_empty[buf]), bph ^ 1u, &ctl, &g_wait_status))) break;
+      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.full[s]), ph, &ctl, &g_wait_status))) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const int ksteps = min(4, (a.K - kb * kBlock + kMmaK - 1) / kMmaK);
       const uint32_t base = smem_base + s * S::kStageBytes;
@@ -204,7 +187,7 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, RowsShape<NT, WT>
         asm volatile("bar.sync 1, %0;" ::"n"(32 * S::kEpiWarps) : "memory");
         fetch(kb + kScaleRun);
       }
-      ok = ok && __all_sync(0xffffffffu, mbar_wait_inline(smem_u32(&ctl.tmem_full[buf]), bph, &ctl, &g_fp8_status));
+      ok = ok && __all_sync(0xffffffffu, mbar_wait_inline(smem_u32(&ctl.tmem_full[buf]), bph, &ctl, &g_wait_status));
       if (!ok) continue;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t taddr = tmem_acc + ((uint32_t)(quad * 32) << 16) + (uint32_t)(buf * S::kCols + c0);

@@ -12,13 +12,13 @@ namespace b2c {
 
 namespace {
 
-__device__ int g_fp8_status;  // first expired wait of this file's kernels on the device
+__device__ int g_wait_status;  // first expired wait of this file's kernels on the device
 
 // Reads and clears it; the device is idle.
 inline cudaError_t take_status(int* status) {
   const int zero = 0;
-  cudaError_t e = cudaMemcpyFromSymbol(status, g_fp8_status, sizeof(int));
-  if (e == cudaSuccess && *status != 0) e = cudaMemcpyToSymbol(g_fp8_status, &zero, sizeof(zero));
+  cudaError_t e = cudaMemcpyFromSymbol(status, g_wait_status, sizeof(int));
+  if (e == cudaSuccess && *status != 0) e = cudaMemcpyToSymbol(g_wait_status, &zero, sizeof(zero));
   return e;
 }
 
@@ -128,8 +128,8 @@ __global__ void __launch_bounds__(32) wait_selftest_kernel() {
     ctl.abort_flag = 0;
   }
   __syncthreads();
-  const bool ok = blockIdx.x == 0 ? mbar_wait(smem_u32(&ctl.full[0]), 0, &ctl, &g_fp8_status) : mbar_wait_inline(smem_u32(&ctl.full[0]), 0, &ctl, &g_fp8_status);
-  if (__any_sync(0xffffffffu, ok)) atomicExch(&g_fp8_status, B2C_E_NOT_READY);  // (cannot be)
+  const bool ok = blockIdx.x == 0 ? mbar_wait(smem_u32(&ctl.full[0]), 0, &ctl, &g_wait_status) : mbar_wait_inline(smem_u32(&ctl.full[0]), 0, &ctl, &g_wait_status);
+  if (__any_sync(0xffffffffu, ok)) atomicExch(&g_wait_status, B2C_E_NOT_READY);  // (cannot be)
 }
 inline cudaError_t launch_wait_selftest(cudaStream_t st) {
   wait_selftest_kernel<<<2, 32, 0, st>>>();
@@ -141,7 +141,8 @@ inline cudaError_t launch_wait_selftest(cudaStream_t st) {
 struct RowTile {
   int group, row0, row_end;  // group < 0: there is no such tile
 };
-__device__ __forceinline__ RowTile find_row_tile(const MatmulArgs& a, int index, int tile) {
+template <typename Args>
+__device__ __forceinline__ RowTile find_row_tile(const Args& a, int index, int tile) {
   RowTile r = {-1, 0, 0};
   if (a.offsets == nullptr) {
     if ((long long)index * tile < a.rows) r = {0, index * tile, a.rows};
@@ -178,6 +179,133 @@ __device__ __forceinline__ RowTile find_row_tile(const MatmulArgs& a, int index,
     run = __shfl_sync(0xffffffffu, hi, 31);
   }
   return r;
+}
+
+constexpr int kBand = 8;  // row tiles that are walked together, so that their columns' B tiles are read from L2
+
+__device__ __forceinline__ void tma_pair_load_3d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar, uint32_t on) {
+  asm volatile(
+      "{\n.reg .pred q;\nsetp.ne.b32 q, %6, 0;\n"
+      "@q cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], "
+      "[%5];\n}" ::"r"(dst),
+      "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar), "r"(on)
+      : "memory");
+}
+
+// Arrival on a barrier of the leader that hands back accumulator columns.  What it orders are reads of tensor memory, and
+// these have ended (tcgen05.wait::ld): no write of this thread has to be seen by the other side.  With .release, at
+// cluster scope, every arrival waited for the thread's loads of scales under way (2100 of the 2500 cycles of a block).
+__device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
+// Row tiles of all groups; called by a whole warp.
+template <typename Args>
+__device__ __forceinline__ int count_row_tiles(const Args& a, int tile) {
+  if (a.offsets == nullptr) return (a.rows + tile - 1) / tile;
+  const int lane = threadIdx.x & 31;
+  int run = max(0, min(a.offsets[0], a.rows)), all = 0;
+  for (int g0 = 0; g0 < a.groups; g0 += 32) {
+    int hi = g0 + lane < a.groups ? max(0, min(a.offsets[g0 + lane + 1], a.rows)) : 0;
+    hi = max(hi, run);
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, hi, d);
+      if (lane >= d) hi = max(hi, v);
+    }
+    int lo = __shfl_up_sync(0xffffffffu, hi, 1);
+    if (lane == 0) lo = run;
+    all += __reduce_add_sync(0xffffffffu, (hi - lo + tile - 1) / tile);
+    run = __shfl_sync(0xffffffffu, hi, 31);
+  }
+  return all;
+}
+
+struct PairTile {
+  int group, row0, row_end, nt;
+};
+// Tile t of the walk: without groups bands of kBand row tiles, column by column; with groups row tile by row tile.
+template <int CTAS, typename Args>
+__device__ __forceinline__ PairTile pair_tile(const Args& a, int t, int row_tiles, int n_tiles) {
+  PairTile p;
+  int mt;
+  if (a.offsets == nullptr) {
+    const int band = t / (kBand * n_tiles);
+    const int in = t - band * kBand * n_tiles;
+    const int height = min(kBand, row_tiles - band * kBand);
+    p.nt = in / height;
+    mt = band * kBand + in - p.nt * height;
+  } else {
+    mt = t / n_tiles;
+    p.nt = t - mt * n_tiles;
+  }
+  const RowTile r = find_row_tile(a, mt, CTAS * kTileM);
+  p.group = r.group;
+  p.row0 = r.row0;
+  p.row_end = r.row_end;
+  return p;
+}
+
+// A box of results in shared memory (32 rows of 128 bytes, swizzled) to rows of any alignment; called by a whole warp.  Rows one after
+// another, neighbouring lanes neighbouring columns; 16-bit results in words where a row starts on an odd one too.
+// (Two-byte stores of a row a lane, 32 lines an instruction, made a product of 762 x 3937 x 608 take 46 us.)
+template <typename T>
+__device__ __forceinline__ void store_box(T* y, long long ldy, uint32_t box, int rows, int cols, bool wide, int lane) {
+  constexpr int kPer = 16 / (int)sizeof(T);
+  if (wide) {  // rows on the 16-byte grid, but not all of them: eight lanes a row
+    const int c = lane & 7;
+#pragma unroll
+    for (int r0 = 0; r0 < 32; r0 += 4) {
+      const int r = r0 + (lane >> 3);
+      uint4 w;
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
+                   : "r"(box + (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)))
+                   : "memory");
+      T* dst = y + r * ldy + c * kPer;
+      if (r < rows && c * kPer + kPer <= cols) {
+        *reinterpret_cast<uint4*>(dst) = w;
+      } else if (r < rows) {
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+          if (c * kPer + i < cols) {
+            if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t*>(dst)[i] = u[i];
+            else reinterpret_cast<uint16_t*>(dst)[i] = (uint16_t)(u[i >> 1] >> (16 * (i & 1)));
+          }
+      }
+    }
+    return;
+  }
+  for (int r = 0; r < rows; ++r) {
+    T* dst = y + r * ldy;
+    const uint32_t line = box + (uint32_t)(r * 128);
+    auto at = [&](int byte) { return line + (uint32_t)((((byte >> 4) ^ (r & 7)) << 4) | (byte & 15)); };
+    if constexpr (sizeof(T) == 4) {
+      uint32_t w;
+      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(at(4 * lane)) : "memory");
+      if (lane < cols) reinterpret_cast<uint32_t*>(dst)[lane] = w;
+    } else {
+      auto load = [&](int e) {
+        uint16_t h;
+        asm volatile("ld.shared.b16 %0, [%1];" : "=h"(h) : "r"(at(2 * e)) : "memory");
+        return (uint32_t)h;
+      };
+      auto one = [&](int e, uint32_t h) {
+        if (e >= 0 && e < cols) reinterpret_cast<uint16_t*>(dst)[e] = (uint16_t)h;
+      };
+      const int odd = (int)(reinterpret_cast<uintptr_t>(dst) >> 1) & 1;
+      const int e = 2 * lane - odd;  // this lane's word: elements e and e + 1
+      const uint32_t lo = load(max(e, 0)), hi = load(e + 1);
+      if (e >= 0 && e + 1 < cols) {
+        *reinterpret_cast<uint32_t*>(dst + e) = lo | (hi << 16);
+      } else {
+        one(e, lo);
+        one(e + 1, hi);
+      }
+      if (odd && lane == 31) one(63, load(63));
+    }
+  }
 }
 
 }  // namespace
