@@ -29,9 +29,9 @@ __device__ __forceinline__ Factor4 load_factor4(const float* p, int format) {
 
 // Scale of a block.  amax: bits of its largest magnitude (as whole numbers these are ordered as the magnitudes, and NaN is the largest).
 struct Scale4 {
-  uint32_t code;  // as stored
-  float r;        // reciprocal of the step, 0 where the values are zeros
-  float step;     // E4M3 and few_bits: the step itself
+  uint32_t code;   // as stored
+  float r;         // reciprocal of the step, 0 where the values are zeros
+  float step, lo;  // NV: the step is their sum, lo is 0 under a factor of few bits
 };
 // MX: with amax = m * 2^k, 1 <= m < 2, the least power of two s with amax <= 6 s = 1.5 * 2^2 s is 2^(k - 2), or twice that for m > 1.5.
 __device__ __forceinline__ Scale4 scale_mx(uint32_t amax) {
@@ -41,7 +41,7 @@ __device__ __forceinline__ Scale4 scale_mx(uint32_t amax) {
   const bool fine = amax < kInfBits;
   s.code = fine ? code : 255u;
   s.r = fine ? __uint_as_float((254u - code) << 23) : 0.0f;  // 2^(127 - code), a power of two: products with it are exact
-  s.step = 0.0f;
+  s.step = s.lo = 0.0f;
   return s;
 }
 // NV: the E4M3 value nearest to the real quotient amax / (6 g).  p is that quotient within 2^-52 of itself.  A border t between two E4M3
@@ -58,7 +58,9 @@ __device__ __forceinline__ Scale4 scale_nv(uint32_t amax, const Factor4& f) {
   if ((double)v != hi) v = __uint_as_float(__float_as_uint(v) | 1u);
   const bool fine = amax < kInfBits;
   s.code = fine ? (uint32_t)__nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3) : 0x7Fu;
-  s.step = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)s.code, __NV_E4M3))) * f.g;
+  const float t = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)s.code, __NV_E4M3)));
+  s.step = t * f.g;
+  s.lo = fmaf(t, f.g, -s.step);  // (28 bits in all: exact)
   s.r = fine && s.code != 0 ? __frcp_rn(s.step) : 0.0f;
   return s;
 }
@@ -103,68 +105,56 @@ __device__ __forceinline__ void cvt_f16x8(uint32_t q, uint32_t* h) {
       : "r"(q));
 }
 
-// The code of x by its block's borders, each product exact in 64 bits.
-__device__ __noinline__ uint32_t code4_exact(float x, double step) {
-  const double a = fabs((double)x);
-  uint32_t c = 0;
-  c += a > 0.25 * step;
-  c += a >= 0.75 * step;
-  c += a > 1.25 * step;
-  c += a >= 1.75 * step;
-  c += a > 2.5 * step;
-  c += a >= 3.5 * step;
-  c += a > 5.0 * step;
-  return c | (__float_as_uint(x) >> 31 << 3);
-}
-
 // N (4, 8 or 16) values of one block to 4 bits each, as if x / (scale * g) had been rounded as a real number.
 //   MX: multiplication by a power of two.
 //   NV, few_bits: the correctly rounded quotient by Markstein's residual step (see quantize2).  Every product of the step with a border t has 24
 // bits at most, so x is either that product, and the quotient t itself, or differs from it by a unit of x's last place, more than half a
 // unit of t's: the rounded quotient is on the same side.
-//   NV else: x times the rounded reciprocal is within 3 units of the last place (step, reciprocal and product are rounded).  The borders have three
-// bits, so what is nearer to one than 4 units has 20 bits that are nearly all zeros or all ones: rare (8 of 2^20), and decided in 64 bits.
-// A block whose scale is the largest one may be beyond it by any factor, and is decided there too.
+//   NV else: x times the rounded reciprocal says which number t of four bits the quotient is next to; all borders are such numbers.  On which side
+// of t it is says the sign of x - t * step: the step is hi + lo, x - t * hi is exact where it is small, and the rounding of the last
+// sum keeps its sign.  What is converted is t, moved to that side.  (Factors that come from a largest value of few bits put one number
+// in 200 within 2^-23 of a border: deciding these by comparisons in 64 bits made 16384 x 8192 take 217 us.)
+//   A block whose scale is the largest one may be beyond it by any factor: eight steps round to the same value, and stay finite.
 template <int N>
-__device__ __forceinline__ void quantise4(const Scale4& s, const Factor4& f, int format, const float* x, uint32_t* q) {
-  float v[N];
-  bool look = false;
+__device__ __forceinline__ void quantise4(const Scale4& s, const Factor4& f, int format, const float* in, uint32_t* q) {
+  float v[N], x[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = in[i];
+  if (format == B2C_NVFP4 && s.code == 0x7Eu) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = fminf(fmaxf(x[i], -8.0f * s.step), 8.0f * s.step);
+  }
+  const f32x2 r = pair_of(s.r, s.r), neg = pair_of(-s.step, -s.step);
   if (format == B2C_MXFP4) {
-    const f32x2 r = pair_of(s.r, s.r);
 #pragma unroll
     for (int i = 0; i < N; i += 2) unpair(mul2(pair_of(x[i], x[i + 1]), r), &v[i], &v[i + 1]);
   } else if (f.few_bits) {
-    const f32x2 r = pair_of(s.r, s.r), neg = pair_of(-s.step, -s.step);
 #pragma unroll
     for (int i = 0; i < N; i += 2) {
       const f32x2 u = pair_of(x[i], x[i + 1]), q0 = mul2(u, r);
       unpair(fma2_of(fma2_of(q0, neg, u), r, q0), &v[i], &v[i + 1]);
     }
-    look = s.code == 0x7Eu;
   } else {
-    const f32x2 r = pair_of(s.r, s.r);
-    uint32_t near = 0xFFFFFu;
+    const f32x2 neg_lo = pair_of(-s.lo, -s.lo);
 #pragma unroll
     for (int i = 0; i < N; i += 2) {
-      unpair(mul2(pair_of(x[i], x[i + 1]), r), &v[i], &v[i + 1]);
-      // (0.2 is far from every border: zeros, and what is as small, need no look)
-      near = min(near, min((__float_as_uint(fmaxf(fabsf(v[i]), 0.2f)) + 4u) & 0xFFFFFu, (__float_as_uint(fmaxf(fabsf(v[i + 1]), 0.2f)) + 4u) & 0xFFFFFu));
+      const f32x2 u = pair_of(x[i], x[i + 1]);
+      float t[2], d[2];
+      unpair(mul2(u, r), &t[0], &t[1]);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) t[j] = __uint_as_float((__float_as_uint(t[j]) + 0x80000u) & 0xFFF00000u);
+      const f32x2 tt = pair_of(t[0], t[1]);
+      unpair(fma2_of(tt, neg_lo, fma2_of(tt, neg, u)), &d[0], &d[1]);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float side = __uint_as_float((__float_as_uint(d[j]) & 0x80000000u) | 0x3A800000u);  // +-2^-10
+        v[i + j] = d[j] == 0.0f ? t[j] : fmaf(fabsf(t[j]), side, t[j]);
+      }
     }
-    look = (near <= 8u || s.code == 0x7Eu) && s.r != 0.0f;
   }
 #pragma unroll
   for (int i = 0; i < N / 8; ++i) q[i] = cvt_e2m1x8(v + 8 * i);
   if constexpr (N == 4) q[0] = cvt_e2m1x4(v);
-  if (look) {
-    const double step = (double)scale_value(s.code, B2C_NVFP4) * (double)f.g;
-#pragma unroll
-    for (int i = 0; i < (N + 7) / 8; ++i) {
-      uint32_t w = 0;
-#pragma unroll
-      for (int j = 0; j < (N < 8 ? N : 8); ++j) w |= code4_exact(x[8 * i + j], step) << (4 * j);
-      q[i] = w;
-    }
-  }
   if (s.r == 0.0f) {
 #pragma unroll
     for (int i = 0; i < (N + 7) / 8; ++i) q[i] = 0;

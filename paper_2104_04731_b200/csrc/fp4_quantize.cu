@@ -76,31 +76,48 @@ __global__ void __launch_bounds__(kThreads) quantize4_kernel(const Quantize4Args
   }
 }
 
-// Any rows: the 16 elements of each lane are brought by 16 neighbouring lanes and change hands in shared memory; packed bytes leave the same way.
+// Runs one after another, `step` further at a time, without a division for each: row and place in the row.
+struct Walk {
+  int rows, rest, per_row;  // of a step
+  __device__ __forceinline__ Walk(int step, int n) : rows(step / n), rest(step % n), per_row(n) {}
+  __device__ __forceinline__ void next(long long* row, int* run) const {
+    *row += rows;
+    *run += rest;
+    if (*run >= per_row) {
+      *run -= per_row;
+      ++*row;
+    }
+  }
+};
+
+// Any rows: a warp has 32 runs, whose elements neighbouring lanes bring together (16 lanes a run) and exchange in shared memory; packed bytes
+// leave the same way.
 constexpr int kPitch = kRun + 1;
 template <typename T>
-__global__ void __launch_bounds__(kThreads) quantize4_any_kernel(const Quantize4Args a, const FastDiv per_row, const long long runs) {
+__global__ void __launch_bounds__(kThreads) quantize4_any_kernel(const Quantize4Args a, const FastDiv per_row, const long long runs, const bool words) {
   __shared__ float stage[kThreads / 32][32 * kPitch];
   pdl_wait();
   pdl_launch_dependents();
   const Factor4 f = load_factor4(a.global, a.format);
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, n = (int)per_row.d;
   float* mine = stage[threadIdx.x >> 5];
   uint8_t* bytes = reinterpret_cast<uint8_t*>(mine);
+  const Walk two(2, n), four(4, n);
+  // (rows * runs of a row may pass 32 bits: what is above 2^31 is divided the long way)
+  auto place = [&](long long id, long long* row, int* run) {
+    *row = id < (1ll << 31) ? (long long)per_row.div((uint32_t)id) : id / n;
+    *run = (int)(id - *row * n);
+  };
   for (long long first = (long long)blockIdx.x * kThreads + (threadIdx.x & ~31u); first < runs; first += (long long)gridDim.x * kThreads) {
-    const long long id = min(first + lane, runs - 1);
-    // (rows * runs of a row may pass 32 bits: the quotient of the part above 2^31 goes the long way)
-    const long long row = id < (1ll << 31) ? (long long)per_row.div((uint32_t)id) : id / per_row.d;
-    const int run = (int)(id - row * per_row.d);
-    const int left = first + lane < runs ? max(0, min(kRun, a.cols - run * kRun)) : 0;
-    const T* p = (const T*)a.x + row * a.ldx + run * kRun;
+    long long row;
+    int run;
+    place(first + (lane >> 4), &row, &run);
     float v[kRun];
 #pragma unroll
     for (int i = 0; i < kRun; ++i) {
-      const int from = 2 * i + (lane >> 4);
-      const T* src = (const T*)__shfl_sync(0xffffffffu, (unsigned long long)p, from);
-      const int n = __shfl_sync(0xffffffffu, left, from);
-      v[i] = (lane & 15) < n ? to_float<T>(src[lane & 15]) : 0.0f;
+      const int c = run * kRun + (lane & 15);
+      v[i] = row < a.rows && c < a.cols ? to_float<T>(((const T*)a.x)[row * a.ldx + c]) : 0.0f;
+      two.next(&row, &run);
     }
     __syncwarp();
 #pragma unroll
@@ -116,21 +133,34 @@ __global__ void __launch_bounds__(kThreads) quantize4_any_kernel(const Quantize4
     const Scale4 s = scale_of(m, f, a.format);
     uint32_t q[2];
     quantise4<kRun>(s, f, a.format, v, q);
-    __syncwarp();
-    *reinterpret_cast<uint2*>(bytes + 8 * lane) = make_uint2(q[0], q[1]);
-    __syncwarp();
-    const bool scales = left > 0 && (a.format == B2C_NVFP4 || (run & 1) == 0);
-    for (int j = 0; j < (a.map == nullptr ? 1 : a.copies); ++j) {
-      const long long to = a.map == nullptr ? row : (long long)a.map[row * a.copies + j];
-      const int n = to < 0 ? 0 : (left + 1) / 2;
-      uint8_t* dst = a.q + to * a.ldq + run * (kRun / 2);
+    place(first + lane, &row, &run);
+    const bool on = row < a.rows && run * kRun < a.cols, scales = on && (a.format == B2C_NVFP4 || (run & 1) == 0);
+    const int at = a.format == B2C_NVFP4 ? run : run >> 1;
+    if (a.map == nullptr) {
+      if (scales) a.scale[row * a.lds + at] = (uint8_t)s.code;
+      if (words && on && run * kRun + kRun <= a.cols) {
+        *reinterpret_cast<uint2*>(a.q + row * a.ldq + run * (kRun / 2)) = make_uint2(q[0], q[1]);
+      } else if (words && on) {
+        for (int i = 0; i < (a.cols - run * kRun + 1) / 2; ++i) a.q[row * a.ldq + run * (kRun / 2) + i] = (uint8_t)(q[i >> 2] >> (8 * (i & 3)));
+      } else if (!words) {
+        __syncwarp();
+        *reinterpret_cast<uint2*>(bytes + 8 * lane) = make_uint2(q[0], q[1]);
+        __syncwarp();
+        place(first + (lane >> 3), &row, &run);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int from = 4 * i + (lane >> 3);
-        uint8_t* d = (uint8_t*)__shfl_sync(0xffffffffu, (unsigned long long)dst, from);
-        if ((lane & 7) < __shfl_sync(0xffffffffu, n, from)) d[lane & 7] = bytes[8 * from + (lane & 7)];
+        for (int i = 0; i < 8; ++i) {
+          const int c = run * (kRun / 2) + (lane & 7);  // byte of the row
+          if (row < a.rows && 2 * c < a.cols) a.q[row * a.ldq + c] = bytes[32 * i + lane];
+          four.next(&row, &run);
+        }
       }
-      if (scales && to >= 0) a.scale[to * a.lds + (a.format == B2C_NVFP4 ? run : run >> 1)] = (uint8_t)s.code;
+    } else {  // rows of an expert layer are whole blocks and on the grid
+      for (int j = 0; j < a.copies; ++j) {
+        const long long to = on ? (long long)a.map[row * a.copies + j] : -1;
+        if (to < 0) continue;
+        *reinterpret_cast<uint2*>(a.q + to * a.ldq + run * (kRun / 2)) = make_uint2(q[0], q[1]);
+        if (scales) a.scale[to * a.lds + at] = (uint8_t)s.code;
+      }
     }
     __syncwarp();
   }
@@ -183,25 +213,51 @@ __global__ void __launch_bounds__(kThreads) dequantize4_kernel(const Dequantize4
   }
 }
 
-// Any rows: a byte, two values, a lane.
+// Any rows: eight columns a lane that begin on the 16-byte grid of y, where that is (the first and the last of a row are not whole), so that
+// stores are wide; their 4-bit values begin at any nibble of q.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) dequantize4_any_kernel(const Dequantize4Args a, const FastDiv per_row, const long long all) {
+__global__ void __launch_bounds__(kThreads) dequantize4_any_kernel(const Dequantize4Args a, const FastDiv per_row, const long long runs) {
   pdl_wait();
   pdl_launch_dependents();
   const float g = a.global != nullptr ? *a.global : 1.0f;
-  const int shift = a.format == B2C_MXFP4 ? 4 : 3;  // bytes in a block
-  for (long long id = (long long)blockIdx.x * kThreads + threadIdx.x; id < all; id += (long long)gridDim.x * kThreads) {
-    const long long row = id < (1ll << 31) ? (long long)per_row.div((uint32_t)id) : id / per_row.d;
-    const int at = (int)(id - row * per_row.d);
-    const uint32_t q = a.q[row * a.ldq + at];
-    const float s = scale_value(a.scale[row * a.lds + (at >> shift)], a.format);
+  const int shift = a.format == B2C_MXFP4 ? 5 : 4, n = (int)per_row.d;
+  const long long step = (long long)gridDim.x * kThreads;
+  for (long long id = (long long)blockIdx.x * kThreads + threadIdx.x; id < runs; id += step) {
+    const long long row = id < (1ll << 31) ? (long long)per_row.div((uint32_t)id) : id / n;
+    T* y = (T*)a.y + row * a.ldy;
+    const int behind = (int)((reinterpret_cast<uintptr_t>(y) & 15) / sizeof(T));  // columns that the row begins behind the grid
+    const int c0 = (int)(id - row * n) * 8 - (behind & 7);
+    const int lo = max(c0, 0), hi = min(c0 + 8, a.cols);
+    if (lo >= hi) continue;
+    const uint8_t* q = a.q + row * a.ldq;
+    const uint8_t* scale = a.scale + row * a.lds;
+    // the bytes of columns lo .. hi - 1, the first one's in the lowest
+    unsigned long long w = 0;
+#pragma unroll
+    for (int i = 0; i < 5; ++i)
+      if ((lo >> 1) + i <= (hi - 1) >> 1) w |= (unsigned long long)q[(lo >> 1) + i] << (8 * i);
+    const uint32_t nibbles = (uint32_t)(w >> (4 * (lo & 1)));
+    const float s0 = scale_value(scale[lo >> shift], a.format), s1 = scale_value(scale[(hi - 1) >> shift], a.format);
     uint32_t h[4];
-    cvt_f16x8(q * 0x01010101u, h);  // (of a word that the compiler sees to be a single byte, nvcc 12.9 made zeros)
-    float lo, hi;
-    unpack2<__half>(h[0], &lo, &hi);
-    T* dst = (T*)a.y + row * a.ldy + 2 * at;
-    dst[0] = from_float<T>(lo * s * g);
-    if (2 * at + 1 < a.cols) dst[1] = from_float<T>(hi * s * g);
+    cvt_f16x8(nibbles, h);
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack2<__half>(h[i], &v[2 * i], &v[2 * i + 1]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = v[i] * ((lo + i) >> shift == lo >> shift ? s0 : s1) * g;
+    if (hi - lo == 8) {
+      T* dst = y + lo;
+      if constexpr (sizeof(T) == 4) {
+        reinterpret_cast<float4*>(dst)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(dst)[1] = make_float4(v[4], v[5], v[6], v[7]);
+      } else {
+        *reinterpret_cast<uint4*>(dst) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (lo + i < hi) y[lo + i] = from_float<T>(v[i]);
+    }
   }
 }
 
@@ -213,13 +269,14 @@ template <typename T>
 cudaError_t launch_quantize(const Quantize4Args& a, cudaStream_t st) {
   // (an MX row has an even number of runs, so that the two halves of a block are neighbours in a warp)
   const long long per_row = a.format == B2C_MXFP4 ? (a.cols + 31ll) / 32 * 2 : (a.cols + 15ll) / 16, runs = a.rows * per_row;
-  const bool wide = on_grid(a.x, a.ldx * (long long)sizeof(T), a.rows, 16) && on_grid(a.q, a.ldq, a.map != nullptr ? 2 : a.rows, 8);
+  const bool words = on_grid(a.q, a.ldq, a.map != nullptr ? 2 : a.rows, 8);
+  const bool wide = on_grid(a.x, a.ldx * (long long)sizeof(T), a.rows, 16) && words;
   const long long blocks = (runs + kThreads - 1) / kThreads;
   const FastDiv div = make_fastdiv((uint32_t)per_row);
   // resident at once: 8 blocks of 256 threads an SM; all of them load one run ahead
   if (wide && a.cols % 32 == 0 && runs < (1ll << 30))
     return launch_pdl(quantize4_kernel<T>, dim3((unsigned)std::min<long long>(blocks, 8 * kNumSMs)), dim3(kThreads), 0, st, a, div, (unsigned)runs);
-  return launch_pdl(quantize4_any_kernel<T>, dim3((unsigned)std::min<long long>(blocks, 64 * kNumSMs)), dim3(kThreads), 0, st, a, div, runs);
+  return launch_pdl(quantize4_any_kernel<T>, dim3((unsigned)std::min<long long>(blocks, 64 * kNumSMs)), dim3(kThreads), 0, st, a, div, runs, words);
 }
 
 template <typename T>
@@ -230,9 +287,9 @@ cudaError_t launch_dequantize(const Dequantize4Args& a, cudaStream_t st) {
     return launch_pdl(dequantize4_kernel<T>, dim3((unsigned)std::min<long long>(blocks, 8 * kNumSMs)), dim3(kThreads), 0, st, a,
                       make_fastdiv((uint32_t)(a.cols / 8)), (unsigned)runs);
   }
-  const long long per_row = (a.cols + 1) / 2, all = a.rows * per_row, blocks = (all + kThreads - 1) / kThreads;
+  const long long per_row = (a.cols + 7ll + 7ll) / 8, runs = a.rows * per_row, blocks = (runs + kThreads - 1) / kThreads;  // (a row may begin inside a run)
   return launch_pdl(dequantize4_any_kernel<T>, dim3((unsigned)std::min<long long>(blocks, 64 * kNumSMs)), dim3(kThreads), 0, st, a,
-                    make_fastdiv((uint32_t)per_row), all);
+                    make_fastdiv((uint32_t)per_row), runs);
 }
 
 }  // namespace
