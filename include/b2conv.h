@@ -524,7 +524,7 @@ int b2c_fp4_experts(const b2c_fp4_experts_desc* desc, int64_t tokens, const void
                     const float* w1_global_dev, const float* h_global_dev, const float* w2_global_dev, void* y_dev, int64_t ldy,
                     void* workspace_dev, void* cuda_stream);
 
-/* As b2c_fp8_status and b2c_selftest_fp8_wait, of the 4-bit operators' kernels. */
+/* As b2c_fp8_status and b2c_selftest_fp8_wait, of the 4-bit operators' kernels (form 2: the expert layer of few tokens). */
 int b2c_fp4_status(int32_t* status);
 int b2c_selftest_fp4_wait(int form, void* cuda_stream);
 

@@ -14,7 +14,7 @@ SO = os.path.join(HERE, "libb2conv.so")
 SO_DEBUG = os.path.join(HERE, "libb2conv_debug.so")  # -DB2C_DEBUG_BOUNDS: bounds-checked kernels, workspace guard bands
 SOURCES = ["api.cpp", "planner.cpp", "tma.cpp", "layout.cu", "conv_mma.cu", "conv_mma_pair.cu", "mma_rate.cu", "conv_mma_window.cu", "conv_mma_plane.cu", "conv_mma_stream.cu",
            "fp8_api.cpp", "fp8_quantize.cu", "fp8_matmul.cu", "fp8_matmul_pair.cu", "route.cu",
-           "fp4_api.cpp", "fp4_quantize.cu", "fp4_matmul.cu", "fp4_matmul_pair.cu"]
+           "fp4_api.cpp", "fp4_quantize.cu", "fp4_matmul.cu", "fp4_matmul_pair.cu", "fp4_experts.cu"]
 
 
 def binding_path() -> str:

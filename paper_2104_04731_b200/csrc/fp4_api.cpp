@@ -18,7 +18,7 @@ int from_cuda(cudaError_t e) {
 
 // The workspace of an expert layer, in order; each part starts on a 256-byte boundary.
 struct ExpertsLayout {
-  size_t offsets, rows, sort, xq, xs, hq, hs, y, total;
+  size_t offsets, rows, sort, xq, xs, hq, hs, y, done, total;
 };
 int experts_layout(const b2c_fp4_experts_desc* d, int64_t tokens, ExpertsLayout* l) {
   if (!d || tokens < 0) return B2C_E_INVALID_ARG;
@@ -42,6 +42,7 @@ int experts_layout(const b2c_fp4_experts_desc* d, int64_t tokens, ExpertsLayout*
   l->hq = part(pairs * d->inter / 2);
   l->hs = part(pairs * fp4_scale_pitch(d->inter, d->format));
   l->y = part(pairs * d->hidden * 4);
+  l->done = part(4 * (((size_t)d->hidden + kTileM - 1) / kTileM));
   l->total = at;
   return B2C_OK;
 }
@@ -159,6 +160,38 @@ int b2c_fp4_experts(const b2c_fp4_experts_desc* d, int64_t tokens, const void* x
   cudaStream_t st = (cudaStream_t)cuda_stream;
   char* ws = (char*)workspace;
   const long long pairs = tokens * d->topk;
+  if (pairs <= kFewPairs && pairs <= 8ll * d->experts) {
+    Few4Args f = {};
+    f.x = x;
+    f.ldx = ldx;
+    f.ids = ids;
+    f.weights = weights;
+    f.w1 = (const uint8_t*)w1;
+    f.w1_scale = (const uint8_t*)w1_scale;
+    f.w2 = (const uint8_t*)w2;
+    f.w2_scale = (const uint8_t*)w2_scale;
+    f.ld1 = ld1;
+    f.ld2 = ld2;
+    f.x_global = x_global;
+    f.w1_global = w1_global;
+    f.h_global = h_global;
+    f.w2_global = w2_global;
+    f.hq = (uint8_t*)(ws + l.hq);
+    f.hs = (uint8_t*)(ws + l.hs);
+    f.ldhs = fp4_scale_pitch(d->inter, d->format);
+    f.part = (float*)(ws + l.y);
+    f.done = (int32_t*)(ws + l.done);
+    f.y = y;
+    f.ldy = ldy;
+    f.pairs = (int)pairs;
+    f.topk = d->topk;
+    f.experts = d->experts;
+    f.hidden = d->hidden;
+    f.inter = d->inter;
+    f.type = d->type;
+    f.format = d->format;
+    return launch_fp4_few_experts(f, st);
+  }
   int32_t* offsets = (int32_t*)(ws + l.offsets);
   int32_t* rows = (int32_t*)(ws + l.rows);
   rc = from_cuda(launch_route_sort(ids, pairs, d->experts, offsets, rows, nullptr, (int32_t*)(ws + l.sort), st));
@@ -235,8 +268,9 @@ int b2c_fp4_status(int32_t* status) {
 }
 
 int b2c_selftest_fp4_wait(int form, void* cuda_stream) {
-  if (form != 0 && form != 1) return B2C_E_INVALID_ARG;
-  return from_cuda(form == 0 ? fp4_rows_wait_selftest((cudaStream_t)cuda_stream) : fp4_pair_wait_selftest((cudaStream_t)cuda_stream));
+  if (form < 0 || form > 2) return B2C_E_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  return from_cuda(form == 0 ? fp4_rows_wait_selftest(st) : (form == 1 ? fp4_pair_wait_selftest(st) : fp4_few_wait_selftest(st)));
 }
 
 }  // extern "C"

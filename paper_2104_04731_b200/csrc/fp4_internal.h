@@ -69,11 +69,33 @@ struct Matmul4Args {
   int gated;  // y = quantise(silu(a . gate) * (a . up))
 };
 
+// The expert layer of few tokens (see fp4_experts.cu).
+constexpr int kFewPairs = 512;
+struct Few4Args {
+  const void* x;
+  long long ldx;
+  const int32_t* ids;
+  const float* weights;
+  const uint8_t *w1, *w1_scale, *w2, *w2_scale;
+  long long ld1, ld2;
+  const float *x_global, *w1_global, *h_global, *w2_global;
+  uint8_t *hq, *hs;  // [pairs][inter / 2], [pairs][ldhs]
+  long long ldhs;
+  float* part;       // [pairs][hidden]
+  int32_t* done;     // [128 columns of hidden]
+  void* y;
+  long long ldy;
+  int pairs, topk, experts, hidden, inter, type, format;
+};
+
 cudaError_t launch_fp4_quantize(const Quantize4Args& a, cudaStream_t st);
 cudaError_t launch_fp4_dequantize(const Dequantize4Args& a, cudaStream_t st);
 int launch_fp4_matmul(const Matmul4Args& a, cudaStream_t st);  // B2C_* code
 int launch_fp4_matmul_pair(const Matmul4Args& a, cudaStream_t st);  // its form for many rows
 cudaError_t fp4_pair_status(int* status);
+int launch_fp4_few_experts(const Few4Args& a, cudaStream_t st);
+cudaError_t fp4_few_status(int* status);
+cudaError_t fp4_few_wait_selftest(cudaStream_t st);
 int fp4_status_read_and_clear(int32_t* status);
 cudaError_t fp4_rows_wait_selftest(cudaStream_t st);
 cudaError_t fp4_pair_wait_selftest(cudaStream_t st);

@@ -342,12 +342,13 @@ int launch_fp4_matmul(const Matmul4Args& a, cudaStream_t st) {
 cudaError_t fp4_rows_wait_selftest(cudaStream_t st) { return launch_wait_selftest(st); }
 
 int fp4_status_read_and_clear(int32_t* status) {
-  int rows = 0, pair = 0;
+  int rows = 0, pair = 0, few = 0;
   cudaError_t e = cudaDeviceSynchronize();
   if (e == cudaSuccess) e = take_status(&rows);
   if (e == cudaSuccess) e = fp4_pair_status(&pair);
+  if (e == cudaSuccess) e = fp4_few_status(&few);
   if (e != cudaSuccess) return fail(e);
-  *status = rows != 0 ? rows : pair;
+  *status = rows != 0 ? rows : (pair != 0 ? pair : few);
   return B2C_OK;
 }
 

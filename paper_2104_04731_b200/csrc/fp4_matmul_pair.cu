@@ -20,7 +20,9 @@ constexpr int kPairThreads = 32 * (kEpiWarp0 + kEpiWarps);
 // 384 threads are launched with 168 registers each; a thread of the results holds 128 sums: 128 * 88 + 256 * 208 = 384 * 168.
 constexpr int kRegsSums = 208, kRegsRest = 88;
 constexpr int kABytes = kTileM * kStageRow;
-constexpr int kBoxBytes = 32 * 128;  // results of a warp on their way out: 32 rows of 128 bytes
+constexpr int kBoxRow = 64;
+constexpr int kBoxBytes = 32 * kBoxRow;  // results of a warp on their way out: 32 rows
+constexpr int kGroups = 2;               // groups of scales in shared memory
 // CTAS thread blocks share a tile of CTAS * 128 rows and TN columns.
 template <int CTAS, int TN>
 struct TileShape4 {
@@ -29,13 +31,13 @@ struct TileShape4 {
   static constexpr int kBoxRows = kBRows < kTileM ? kBRows : kTileM;
   static constexpr int kBBytes = kBRows * kStageRow;
   static constexpr int kColTiles = TN / kTileM;                      // of 128 columns
-  static constexpr int kScaleBytes = (1 + kColTiles) * kScaleTile;   // the block's A rows, all B rows
-  static constexpr int kStageBytes = kABytes + kBBytes + kScaleBytes;
-  static constexpr int kStages = CTAS == 1 ? 3 : (TN == 256 ? 5 : 6);
+  static constexpr int kScaleBytes = (1 + kColTiles) * kGroupTile;   // of a group: the block's A rows, all B rows
+  static constexpr int kStages = CTAS == 1 ? 3 : (TN == 256 ? 5 : 7);
   static constexpr int kBufs = TN == 256 ? 1 : 2;  // accumulators in tensor memory, beside the scales of two stages
   static constexpr int kScaleCols = 16 * (1 + kColTiles);
   static constexpr int kWarpCols = TN / 2;  // accumulator columns of a warp of results
-  static constexpr int kSmem = 1024 + kStages * kStageBytes + kEpiWarps * kBoxBytes;
+  static constexpr int kSmem = 1024 + kStages * (kABytes + kBBytes) + kGroups * kScaleBytes + kEpiWarps * kBoxBytes;
+  static_assert(kSmem <= 226 * 1024, "shared memory, some static beside it");
   static_assert(kBufs * TN + 2 * kScaleCols <= 512, "tensor memory");
 };
 
@@ -55,8 +57,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   constexpr int kStages = S::kStages, kBBytes = S::kBBytes;
   extern __shared__ uint8_t smem_raw[];
   __shared__ SharedCtl ctl;
-  __shared__ __align__(8) unsigned long long scales_full[8];  // a stage's scales have come (each block its own)
-  __shared__ __align__(8) unsigned long long turned[8];       // and are in place in all blocks (the leader's)
+  __shared__ __align__(8) unsigned long long scales_full[2][kGroups];  // a group's scales have come: of the A rows, of the B rows (each block its own)
+  __shared__ __align__(8) unsigned long long turned[kGroups];          // and are in place in all blocks (the leader's)
+  __shared__ __align__(8) unsigned long long scales_empty[kGroups];
   __shared__ int row_tiles_s;
 
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
@@ -66,15 +69,19 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   const uint32_t a_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t b_base = a_base + kStages * kABytes;
   const uint32_t s_base = b_base + kStages * kBBytes;
-  const uint32_t box_base = s_base + kStages * S::kScaleBytes;
+  const uint32_t box_base = s_base + kGroups * S::kScaleBytes;
 
   if (warp == 0) {
     if (lane < kStages) {
       // full[] is used in the leader only: one arrival (its producer) plus the bytes of both blocks
       mbar_init(smem_u32(&ctl.full[lane]), 1);
       mbar_init(smem_u32(&ctl.empty[lane]), 1);
-      mbar_init(smem_u32(&scales_full[lane]), 1);
+    }
+    if (lane < kGroups) {
+      mbar_init(smem_u32(&scales_full[0][lane]), 1);
+      mbar_init(smem_u32(&scales_full[1][lane]), 1);
       mbar_init(smem_u32(&turned[lane]), 2 * CTAS);
+      mbar_init(smem_u32(&scales_empty[lane]), 1);
     }
     if (lane == 8) {
       for (int b = 0; b < S::kBufs; ++b) {
@@ -114,6 +121,10 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   const int tiles = row_tiles * n_tiles;  // (fits: checked by the host)
   const int kb_all = (a.K + kFp4Stage - 1) / kFp4Stage;
 
+  // a tile's columns, 128 at a time: row of the B matrix, and which matrix
+  auto b_row = [&](const PairTile& p, int i) { return GATED ? p.nt * kTileM : p.nt * TN + i * kTileM; };
+  auto b_plane = [&](const PairTile& p, int i) { return GATED ? 2 * p.group + i : p.group; };
+
   if (warp < kEpiWarp0) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
     if (warp == 0) {
@@ -125,31 +136,22 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       for (int t = pair_id; t < tiles && alive; t += num_pairs) {
         const PairTile p = pair_tile<CTAS>(a, t, row_tiles, n_tiles);
         const int m = p.row0 + (int)rank * kTileM;
-        // the tile's columns, 128 at a time: row of the B matrix, and which matrix
-        auto b_row = [&](int i) { return GATED ? p.nt * kTileM : p.nt * TN + i * kTileM; };
-        auto b_plane = [&](int i) { return GATED ? 2 * p.group + i : p.group; };
         for (int kb = 0; kb < kb_all; ++kb) {
           if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.empty[s]), ph ^ 1u, &ctl, &g_wait_status))) {
             alive = false;
             break;
           }
-          const uint32_t sfull = smem_u32(&scales_full[s]), sdst = s_base + s * S::kScaleBytes;
-          mbar_arrive_expect_tx(sfull, S::kScaleBytes, on);
-          const int sx = scale_byte(kb, a.format);
-          tma_load_2d(sdst, &tmap_as, sx, m, sfull, on);
-#pragma unroll
-          for (int i = 0; i < S::kColTiles; ++i) tma_load_3d(sdst + (1 + i) * kScaleTile, &tmap_bs, sx, b_row(i), b_plane(i), sfull, on);
           const uint32_t full = CTAS == 2 ? map_to_rank(smem_u32(&ctl.full[s]), 0u) : smem_u32(&ctl.full[s]);
           if (rank == 0) mbar_arrive_expect_tx(smem_u32(&ctl.full[s]), (uint32_t)CTAS * (kABytes + kBBytes), on);
           const uint32_t dst = b_base + s * kBBytes;
           if constexpr (CTAS == 2) {
             tma_pair_load_2d(a_base + s * kABytes, &tmap_a, kb * kStageRow, m, full, on);
-            if constexpr (S::kColTiles == 2) tma_pair_load_3d(dst, &tmap_b, kb * kStageRow, b_row((int)rank), b_plane((int)rank), full, on);
+            if constexpr (S::kColTiles == 2) tma_pair_load_3d(dst, &tmap_b, kb * kStageRow, b_row(p, (int)rank), b_plane(p, (int)rank), full, on);
             else tma_pair_load_3d(dst, &tmap_b, kb * kStageRow, p.nt * TN + (int)rank * S::kBRows, p.group, full, on);
           } else {
             tma_load_2d(a_base + s * kABytes, &tmap_a, kb * kStageRow, m, full, on);
 #pragma unroll
-            for (int i = 0; i < S::kColTiles; ++i) tma_load_3d(dst + i * kTileM * kStageRow, &tmap_b, kb * kStageRow, b_row(i), b_plane(i), full, on);
+            for (int i = 0; i < S::kColTiles; ++i) tma_load_3d(dst + i * kTileM * kStageRow, &tmap_b, kb * kStageRow, b_row(p, i), b_plane(p, i), full, on);
           }
           if (++s == kStages) {
             s = 0;
@@ -164,13 +166,14 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         const uint32_t on = elect_one() ? 1u : 0u;
         const uint32_t idesc = make_idesc_f4(S::kRows, TN, a.format);
         const int groups4 = scale_groups(a.format);
-        int s = 0, buf = 0;
-        uint32_t ph = 0, bph = 0, ts_at = 0;
+        int s = 0, g = 0, buf = 0;
+        uint32_t ph = 0, gph = 0, bph = 0, ts_at = 0;
         bool alive = true;
         for (int t = pair_id; t < tiles && alive; t += num_pairs) {
           if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.tmem_empty[buf]), bph ^ 1u, &ctl, &g_wait_status))) break;
           for (int kb = 0; kb < kb_all; ++kb) {
-            if (!__all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&turned[s]), ph, &ctl, &g_wait_status)) ||
+            const int in = kb % kGroup;  // stage of the group
+            if ((in == 0 && !__all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&turned[g]), gph, &ctl, &g_wait_status))) ||
                 !__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.full[s]), ph, &ctl, &g_wait_status))) {
               alive = false;
               break;
@@ -178,13 +181,13 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const int ksteps = min(4, (a.K - kb * kFp4Stage + 63) / 64);
             // (copies and MMAs run in the order in which they are issued)
-            const uint32_t ts = tmem_scales + ts_at, scales = s_base + s * S::kScaleBytes;
+            const uint32_t ts = tmem_scales + ts_at, scales = s_base + g * S::kScaleBytes + (uint32_t)(512 * groups4 * in);
             ts_at = S::kScaleCols - ts_at;
             for (int j = 0; j < groups4; ++j) {
               copy_scales<CTAS>(ts + 4 * j, scales + 512 * j, on);
 #pragma unroll
               for (int i = 0; i < S::kColTiles; ++i)
-                copy_scales<CTAS>(ts + 16 + 4 * (j * S::kColTiles + i), scales + (1 + i) * kScaleTile + 512 * j, on);
+                copy_scales<CTAS>(ts + 16 + 4 * (j * S::kColTiles + i), scales + (1 + i) * kGroupTile + 512 * j, on);
             }
             mma_f4_stage<CTAS>(tmem_acc + buf * TN, make_smem_desc(a_base + s * kABytes, kStageRow), make_smem_desc(b_base + s * kBBytes, kStageRow), idesc,
                                ts, ts + 16, 4 * S::kColTiles, a.format, kb > 0, on, ksteps);
@@ -193,6 +196,14 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             if (++s == kStages) {
               s = 0;
               ph ^= 1u;
+            }
+            if (in == kGroup - 1 || kb == kb_all - 1) {
+              if constexpr (CTAS == 2) mma_commit_pair(smem_u32(&scales_empty[g]), on);
+              else mma_commit(smem_u32(&scales_empty[g]), on);
+              if (++g == kGroups) {
+                g = 0;
+                gph ^= 1u;
+              }
             }
           }
           if constexpr (CTAS == 2) mma_commit_pair(smem_u32(&ctl.tmem_full[buf]), on);
@@ -206,32 +217,62 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       pdl_launch_dependents();
       __syncwarp();
     } else {
-      // ---------------------------------------------------------------- scales turned round (both blocks)
-      int s = 0;
+      // ---------------------------------------------------------------- scales: copied and turned round (both blocks)
+      const uint32_t on = elect_one() ? 1u : 0u;
+      const int part = warp - 2;  // 0: A rows, 1: B rows
+      const uint32_t mine = s_base + part * kGroupTile;
+      // the walk of the copies, up to two groups ahead
+      int lt = pair_id, lkb = 0, lg = 0;
+      PairTile lp = {0, 0, 0, 0};
+      auto load_next = [&]() {
+        if (lt >= tiles) return;
+        if (lkb == 0) lp = pair_tile<CTAS>(a, lt, row_tiles, n_tiles);
+        const uint32_t full = smem_u32(&scales_full[part][lg]), dst = mine + lg * S::kScaleBytes;
+        const int width = group_row(a.format), x = lkb / kGroup * width;
+        mbar_arrive_expect_tx(full, (uint32_t)((part == 0 ? 1 : S::kColTiles) * kTileM * width), on);
+        if (part == 0) {
+          tma_load_2d(dst, &tmap_as, x, lp.row0 + (int)rank * kTileM, full, on);
+        } else {
+#pragma unroll
+          for (int i = 0; i < S::kColTiles; ++i) tma_load_3d(dst + i * kGroupTile, &tmap_bs, x, b_row(lp, i), b_plane(lp, i), full, on);
+        }
+        lg ^= 1;
+        lkb += kGroup;
+        if (lkb >= kb_all) {
+          lkb = 0;
+          lt += num_pairs;
+        }
+      };
+      static_assert(kGroups == 2, "the places of the walk");
+      load_next();
+      load_next();
+      int g = 0;
       uint32_t ph = 0;
-      bool alive = true;
+      bool alive = true, first = true;
       for (int t = pair_id; t < tiles && alive; t += num_pairs) {
-        for (int kb = 0; kb < kb_all; ++kb) {
-          if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&scales_full[s]), ph, &ctl, &g_wait_status))) {
+        for (int kb = 0; kb < kb_all; kb += kGroup) {
+          if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&scales_full[part][g]), ph, &ctl, &g_wait_status))) {
             alive = false;
             break;
           }
-          const uint32_t scales = s_base + s * S::kScaleBytes;
-          if (warp == 2) {
-            turn_scales(scales, kTileM, a.format, kb, lane);
-          } else {
-#pragma unroll
-            for (int i = 0; i < S::kColTiles; ++i) turn_scales(scales + (1 + i) * kScaleTile, kTileM, a.format, kb, lane);
-          }
+          turn_group(mine + g * S::kScaleBytes, kTileM, a.format, lane);
+          if (part == 1 && S::kColTiles == 2) turn_group(mine + g * S::kScaleBytes + kGroupTile, kTileM, a.format, lane);
           __syncwarp();
           if (lane == 0) {
-            if constexpr (CTAS == 2) mbar_arrive_leader(map_to_rank(smem_u32(&turned[s]), 0u));
-            else mbar_arrive(smem_u32(&turned[s]));
+            if constexpr (CTAS == 2) mbar_arrive_leader(map_to_rank(smem_u32(&turned[g]), 0u));
+            else mbar_arrive(smem_u32(&turned[g]));
           }
-          if (++s == kStages) {
-            s = 0;
-            ph ^= 1u;
+          g ^= 1;
+          // the other place, when the MMAs of its group (the one before) have ended: it was in use for as many turns as `ph` says
+          if (!first) {
+            if (lt < tiles && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&scales_empty[g]), g == 0 ? ph : ph ^ 1u, &ctl, &g_wait_status))) {
+              alive = false;
+              break;
+            }
+            load_next();
           }
+          first = false;
+          if (g == 0) ph ^= 1u;
         }
       }
       __syncwarp();
@@ -300,18 +341,18 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 #pragma unroll
         for (int i = 0; i < S::kWarpCols; ++i) v[i] *= alpha;
         const int n = p.nt * TN + half * S::kWarpCols, m0 = p.row0 + (int)rank * kTileM + quad * 32;
-        // 128 bytes of each of the warp's 32 rows go to shared memory (16-byte pieces, swizzled as the tensor map says).  From there, if
+        // 64 bytes of each of the warp's 32 rows go to shared memory (16-byte pieces, swizzled as the tensor map says).  From there, if
         // the copy engine can address the result and all 32 rows are this group's, in one copy, which runs beside the next tile; else by the
         // lanes.  The copy clips what lies past the last column in steps of 16 bytes: a box that the result ends in at another place is
         // left to the lanes.
-        constexpr int kCols = 128 / (int)sizeof(YT);
+        constexpr int kCols = kBoxRow / (int)sizeof(YT);
         const uint32_t box = box_base + (uint32_t)((warp - kEpiWarp0) * kBoxBytes);
 #pragma unroll
         for (int i = 0; i < S::kWarpCols; i += kCols) {
           if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
           __syncwarp();
 #pragma unroll
-          for (int c = 0; c < 8; ++c) {
+          for (int c = 0; c < kBoxRow / 16; ++c) {
             constexpr int kPer = 16 / (int)sizeof(YT);
             const float* u = v + i + c * kPer;
             uint32_t w[4];
@@ -320,7 +361,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
               if constexpr (sizeof(YT) == 4) w[j] = __float_as_uint(u[j]);
               else w[j] = pack2<YT>(u[2 * j], u[2 * j + 1]);
             }
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + (uint32_t)(lane * 128 + ((c ^ (lane & 7)) * 16))), "r"(w[0]),
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + (uint32_t)(lane * kBoxRow + ((c ^ ((lane >> 1) & 3)) * 16))), "r"(w[0]),
                          "r"(w[1]), "r"(w[2]), "r"(w[3])
                          : "memory");
           }
@@ -337,7 +378,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           } else {
             __syncwarp();
             if (ok && n + i < a.N)
-              store_box<YT>((YT*)a.y + (long long)m0 * a.ldy + n + i, a.ldy, box, min(32, p.row_end - m0), min(kCols, a.N - n - i), y_boxes, lane);
+              store_box<YT, kBoxRow>((YT*)a.y + (long long)m0 * a.ldy + n + i, a.ldy, box, min(32, p.row_end - m0), min(kCols, a.N - n - i), y_boxes, lane);
             __syncwarp();
           }
         }
@@ -379,15 +420,16 @@ int launch_pair(const Matmul4Args& a, cudaStream_t st) {
   const long long row_tiles = a.offsets ? a.rows / S::kRows + std::min(a.groups, a.rows) : (a.rows + S::kRows - 1) / S::kRows;
   if (row_tiles * n_tiles > 0x7FFFFFFFLL - kNumSMs) return B2C_E_UNSUPPORTED;
   const uint64_t bytes = a.K / 2, scales = fp4_scales(a.K, a.format), planes = (uint64_t)a.groups * (GATED ? 2 : 1);
+  const int width = group_row(a.format);
   CUtensorMap ta, tas, tb, tbs, ty;
   int rc = encode_tiled_2d(&ta, a.a, bytes, a.rows, a.rows > 1 ? a.lda : bytes, kStageRow, kTileM, 128);
-  if (rc == B2C_OK) rc = encode_tiled_2d(&tas, a.a_scale, scales, a.rows, a.rows > 1 ? a.lds : fp4_scale_pitch(a.K, a.format), kScaleRow, kTileM, 0);
+  if (rc == B2C_OK) rc = encode_tiled_2d(&tas, a.a_scale, scales, a.rows, a.rows > 1 ? a.lds : fp4_scale_pitch(a.K, a.format), width, kTileM, width);
   if (rc == B2C_OK) rc = encode_tiled_3d(&tb, a.b, bytes, a.N, planes, bytes, (uint64_t)a.N * bytes, kStageRow, S::kBoxRows, 128);
-  if (rc == B2C_OK) rc = encode_tiled_3d(&tbs, a.b_scale, scales, a.N, planes, a.ldbs, (uint64_t)a.N * a.ldbs, kScaleRow, kTileM, 0);
+  if (rc == B2C_OK) rc = encode_tiled_3d(&tbs, a.b_scale, scales, a.N, planes, a.ldbs, (uint64_t)a.N * a.ldbs, width, kTileM, width);
   if (rc != B2C_OK) return rc;
-  const bool y_boxes = boxes_of(a, (int)sizeof(YT));  // (of 128 bytes x 32 rows)
+  const bool y_boxes = boxes_of(a, (int)sizeof(YT));  // (of 64 bytes x 32 rows)
   ty = ta;
-  if (y_boxes) rc = encode_tiled_2d(&ty, a.y, (uint64_t)a.N * sizeof(YT), a.rows, a.rows > 1 ? (uint64_t)a.ldy * sizeof(YT) : ((uint64_t)a.N * sizeof(YT) + 15) / 16 * 16, 128, 32, 128);
+  if (y_boxes) rc = encode_tiled_2d(&ty, a.y, (uint64_t)a.N * sizeof(YT), a.rows, a.rows > 1 ? (uint64_t)a.ldy * sizeof(YT) : ((uint64_t)a.N * sizeof(YT) + 15) / 16 * 16, kBoxRow, 32, kBoxRow);
   if (rc != B2C_OK) return rc;
   static std::atomic<unsigned long long> configured{0};
   cudaError_t e = set_max_dynamic_smem_once(configured, (const void*)matmul4_pair_kernel<CTAS, TN, GATED, YT>, S::kSmem);

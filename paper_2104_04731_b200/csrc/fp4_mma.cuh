@@ -116,6 +116,43 @@ __device__ __forceinline__ void turn_scales(uint32_t base, int rows, int format,
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
+// Scales come for four stages at a time: 64 bytes (NV) or 32 (MX) of every row.  (The copy engine works by rows of a box: pieces of 16 bytes, a
+// stage's, took it as long as the 128-byte rows of the operands.)
+constexpr int kGroup = 4;
+constexpr int kGroupTile = 128 * 64;  // bytes of a group's scales of 128 rows
+inline __host__ __device__ int group_row(int format) { return format == B2C_MXFP4 ? 32 : 64; }
+
+// A group's scales of up to 128 rows, as a copy with the swizzle of that width left them, turned round in place: word w of all rows
+// becomes the 512 bytes at 512 w (NV: words 4 i .. 4 i + 3 are those of stage i, MX: 2 i and 2 i + 1).  A lane holds all of four rows, 32
+// apart.  Called by a whole warp; what follows in the asynchronous proxy sees it after the caller's barrier.
+template <int WORDS>
+__device__ __forceinline__ void turn_group_words(uint32_t base, int rows, int lane) {
+  uint32_t w[4][WORDS];
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const int r = 32 * g + lane, x = WORDS == 16 ? (r >> 1) & 3 : (r >> 2) & 1;
+#pragma unroll
+    for (int c = 0; c < WORDS / 4; ++c) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[g][4 * c + j] = 0;
+      if (32 * g < rows)
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(w[g][4 * c]), "=r"(w[g][4 * c + 1]), "=r"(w[g][4 * c + 2]), "=r"(w[g][4 * c + 3])
+                     : "r"(base + (uint32_t)(r * (4 * WORDS) + ((c ^ x) << 4)))
+                     : "memory");
+    }
+  }
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < WORDS; ++i)
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + (uint32_t)(512 * i + lane * 16)), "r"(w[0][i]), "r"(w[1][i]), "r"(w[2][i]), "r"(w[3][i]) : "memory");
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
+__device__ __forceinline__ void turn_group(uint32_t base, int rows, int format, int lane) {
+  if (format == B2C_MXFP4) turn_group_words<8>(base, rows, lane);
+  else turn_group_words<16>(base, rows, lane);
+}
+
 __device__ __forceinline__ float alpha_of(const Matmul4Args& a, int group) {
   return (a.alpha != nullptr ? a.alpha[group] : 1.0f) * (a.alpha2 != nullptr ? *a.alpha2 : 1.0f);
 }

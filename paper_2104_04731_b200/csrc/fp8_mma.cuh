@@ -246,21 +246,22 @@ __device__ __forceinline__ PairTile pair_tile(const Args& a, int t, int row_tile
   return p;
 }
 
-// A box of results in shared memory (32 rows of 128 bytes, swizzled) to rows of any alignment; called by a whole warp.  Rows one after
-// another, neighbouring lanes neighbouring columns; 16-bit results in words where a row starts on an odd one too.
+// A box of results in shared memory (32 rows of ROW bytes, 128 or 64, swizzled) to rows of any alignment; called by a whole warp.  Rows one
+// after another, neighbouring lanes neighbouring columns; 16-bit results in words where a row starts on an odd one too.
 // (Two-byte stores of a row a lane, 32 lines an instruction, made a product of 762 x 3937 x 608 take 46 us.)
-template <typename T>
+template <typename T, int ROW = 128>
 __device__ __forceinline__ void store_box(T* y, long long ldy, uint32_t box, int rows, int cols, bool wide, int lane) {
-  constexpr int kPer = 16 / (int)sizeof(T);
-  if (wide) {  // rows on the 16-byte grid, but not all of them: eight lanes a row
-    const int c = lane & 7;
+  constexpr int kPer = 16 / (int)sizeof(T), kPieces = ROW / 16, kAll = ROW / (int)sizeof(T);
+  auto swizzle = [](int r) { return ROW == 128 ? r & 7 : (r >> 1) & 3; };
+  if (wide) {  // rows on the 16-byte grid, but not all of them: a lane a piece of 16 bytes
+    const int c = lane % kPieces;
 #pragma unroll
-    for (int r0 = 0; r0 < 32; r0 += 4) {
-      const int r = r0 + (lane >> 3);
+    for (int r0 = 0; r0 < 32; r0 += 32 / kPieces) {
+      const int r = r0 + lane / kPieces;
       uint4 w;
       asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
                    : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
-                   : "r"(box + (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)))
+                   : "r"(box + (uint32_t)(r * ROW + ((c ^ swizzle(r)) << 4)))
                    : "memory");
       T* dst = y + r * ldy + c * kPer;
       if (r < rows && c * kPer + kPer <= cols) {
@@ -279,16 +280,16 @@ __device__ __forceinline__ void store_box(T* y, long long ldy, uint32_t box, int
   }
   for (int r = 0; r < rows; ++r) {
     T* dst = y + r * ldy;
-    const uint32_t line = box + (uint32_t)(r * 128);
-    auto at = [&](int byte) { return line + (uint32_t)((((byte >> 4) ^ (r & 7)) << 4) | (byte & 15)); };
+    const uint32_t line = box + (uint32_t)(r * ROW);
+    auto at = [&](int byte) { return line + (uint32_t)((((byte >> 4) ^ swizzle(r)) << 4) | (byte & 15)); };
     if constexpr (sizeof(T) == 4) {
       uint32_t w;
-      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(at(4 * lane)) : "memory");
+      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(at(4 * min(lane, kAll - 1))) : "memory");
       if (lane < cols) reinterpret_cast<uint32_t*>(dst)[lane] = w;
     } else {
       auto load = [&](int e) {
         uint16_t h;
-        asm volatile("ld.shared.b16 %0, [%1];" : "=h"(h) : "r"(at(2 * e)) : "memory");
+        asm volatile("ld.shared.b16 %0, [%1];" : "=h"(h) : "r"(at(2 * max(0, min(e, kAll - 1)))) : "memory");
         return (uint32_t)h;
       };
       auto one = [&](int e, uint32_t h) {
@@ -296,14 +297,14 @@ __device__ __forceinline__ void store_box(T* y, long long ldy, uint32_t box, int
       };
       const int odd = (int)(reinterpret_cast<uintptr_t>(dst) >> 1) & 1;
       const int e = 2 * lane - odd;  // this lane's word: elements e and e + 1
-      const uint32_t lo = load(max(e, 0)), hi = load(e + 1);
+      const uint32_t lo = load(e), hi = load(e + 1);
       if (e >= 0 && e + 1 < cols) {
         *reinterpret_cast<uint32_t*>(dst + e) = lo | (hi << 16);
       } else {
         one(e, lo);
         one(e + 1, hi);
       }
-      if (odd && lane == 31) one(63, load(63));
+      if (ROW == 128 && odd && lane == 31) one(63, load(63));
     }
   }
 }

@@ -108,7 +108,7 @@ def test_experts_limits_and_workspace(lib):
         assert n.value >= tokens * 2 * (128 + 16 + 64 + 16 + 4 * 256)
     assert sizes == sorted(sizes)
     assert lib.b2c_fp4_status(None) == BAD
-    assert lib.b2c_selftest_fp4_wait(2, None) == BAD
+    assert lib.b2c_selftest_fp4_wait(3, None) == BAD
 
 
 def refused(call, *args, code=BAD, **kw):
