@@ -20,8 +20,14 @@ namespace {
 constexpr int kTileRows = 16;  // tokens of a tile
 constexpr int kStages4 = 4;
 constexpr int kWBytes = kTileM * kStageRow, kXBytes = kTileRows * kStageRow;
-constexpr int kFewStage = kWBytes + kXBytes + 2 * kScaleTile;
-constexpr int kFewSmem = 1024 + kStages4 * kFewStage;  // (a block of either kernel beside one of the other on an SM)
+constexpr int kFewStage = kWBytes + kXBytes;
+// Scales of 16 rows, turned round: a word of all rows takes 256 bytes, of which the copy to tensor memory reads the next 256 too (lanes of no row).
+constexpr int kRowWord = 16 * 16;
+constexpr int kRowStage = 1536, kRowGroup = 4608;  // of a stage (first kernel), of a group (second): words of it, and one more
+static_assert(4 * kRowWord + kRowWord <= kRowStage && 16 * kRowWord + kRowWord <= kRowGroup && kRowGroup % 512 == 0, "scales of rows");
+// stages, two groups of scales of the weights, scales of the rows (a block of either kernel stands beside one of the other on an SM)
+constexpr int kUpSmem = 1024 + kStages4 * kFewStage + 2 * kGroupTile + kStages4 * kRowStage;
+constexpr int kDownSmem = 1024 + kStages4 * kFewStage + 2 * kGroupTile + 2 * kRowGroup;
 constexpr int kMaxTiles = kFewPairs + kFewPairs / kTileRows;
 static_assert(kMaxExperts * (kFewPairs / 32) * 4 <= kStages4 * kFewStage, "the bits of plan_few");
 constexpr int kAccCols = kTileRows, kFewScaleCols = 32;  // of a tile; of a stage: weights, rows
@@ -102,30 +108,26 @@ __device__ __forceinline__ void plan_few(FewPlan& plan, uint32_t* bits, const in
   __syncthreads();
 }
 
-// A box of weights to L2, ahead of the copy that takes it from there: what is under way from memory is then not bound by the ring (four
-// stages of all SMs are 11 MB; with 2 us of latency under load that was 5.3 TB/s).
-__device__ __forceinline__ void tma_prefetch_3d(const CUtensorMap* map, int c0, int c1, int c2, uint32_t on) {
-  asm volatile("{\n.reg .pred q;\nsetp.ne.b32 q, %4, 0;\n@q cp.async.bulk.prefetch.tensor.3d.L2.global [%0, {%1, %2, %3}];\n}" ::"l"(map), "r"(c0), "r"(c1),
-               "r"(c2), "r"(on)
-               : "memory");
-}
-constexpr int kPrefetch = 8;  // stages ahead of the copies
-
-// Barriers and tensor memory of a block; called by all threads.  `turners`: arrivals that say that a stage's scales (and rows) are in place.
+// Barriers and tensor memory of a block; called by all threads.  `turners`: warps that put a group's scales in place.
 struct FewCtl {
   SharedCtl ctl;
-  unsigned long long turned[kStages4];
+  unsigned long long rows[kStages4];                                // rows of a stage are in place (first kernel)
+  unsigned long long scales_full[2][2], scales_empty[2], turned[2];  // of a group of scales
 };
 __device__ __forceinline__ void setup_few(FewCtl& c, int warp, int lane, int turners) {
   if (warp == 0) {
     if (lane < kStages4) {
       mbar_init(smem_u32(&c.ctl.full[lane]), 1);
       mbar_init(smem_u32(&c.ctl.empty[lane]), 1);
-      mbar_init(smem_u32(&c.turned[lane]), turners);
+      mbar_init(smem_u32(&c.rows[lane]), 2);
     }
     if (lane < 2) {
       mbar_init(smem_u32(&c.ctl.tmem_full[lane]), 1);
       mbar_init(smem_u32(&c.ctl.tmem_empty[lane]), 4);
+      mbar_init(smem_u32(&c.scales_full[0][lane]), 1);
+      mbar_init(smem_u32(&c.scales_full[1][lane]), 1);
+      mbar_init(smem_u32(&c.scales_empty[lane]), 1);
+      mbar_init(smem_u32(&c.turned[lane]), turners);
     }
     if (lane == 8) c.ctl.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -151,29 +153,33 @@ __device__ __forceinline__ void teardown_few(FewCtl& c, int warp, uint32_t tmem)
   }
 }
 
-// The MMAs of all items of this block; called by warp 1 of either kernel.
-__device__ __forceinline__ void mma_few(FewCtl& c, uint32_t smem, uint32_t tmem, int items, int kb_all, int K, int format) {
+// The MMAs of all items of this block; called by warp 1 of either kernel.  row_scales(stage, group's place, stage of the group): where the scales
+// of the rows are, which in the first kernel (UP) are there with the rows.
+template <bool UP, typename F>
+__device__ __forceinline__ void mma_few(FewCtl& c, uint32_t smem, uint32_t scales, F row_scales, uint32_t tmem, int items, int kb_all, int K, int format) {
   const uint32_t on = elect_one() ? 1u : 0u;
   const uint32_t idesc = make_idesc_f4(kTileM, kTileRows, format);
   const int groups4 = scale_groups(format);
-  int s = 0, buf = 0;
-  uint32_t ph = 0, bph = 0, odd = 0;
+  int s = 0, g = 0, buf = 0;
+  uint32_t ph = 0, gph = 0, bph = 0, odd = 0;
   bool alive = true;
   for (int item = blockIdx.x; item < items && alive; item += gridDim.x) {
     if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&c.ctl.tmem_empty[buf]), bph ^ 1u, &c.ctl, &g_wait_status))) break;
     for (int kb = 0; kb < kb_all; ++kb) {
-      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&c.turned[s]), ph, &c.ctl, &g_wait_status)) ||
+      const int in = kb % kGroup;  // stage of the group
+      if ((in == 0 && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&c.turned[g]), gph, &c.ctl, &g_wait_status))) ||
+          (UP && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&c.rows[s]), ph, &c.ctl, &g_wait_status))) ||
           !__all_sync(0xffffffffu, mbar_wait(smem_u32(&c.ctl.full[s]), ph, &c.ctl, &g_wait_status))) {
         alive = false;
         break;
       }
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const uint32_t base = smem + s * kFewStage, scales = base + kWBytes + kXBytes;
+      const uint32_t base = smem + s * kFewStage, ws = scales + g * kGroupTile + (uint32_t)(512 * groups4 * in), xs = row_scales(s, g, in);
       const uint32_t ts = tmem + 2 * kAccCols + odd * kFewScaleCols;
       odd ^= 1u;
       for (int j = 0; j < groups4; ++j) {
-        copy_scales<1>(ts + 4 * j, scales + 512 * j, on);
-        copy_scales<1>(ts + 16 + 4 * j, scales + kScaleTile + 512 * j, on);
+        copy_scales<1>(ts + 4 * j, ws + 512 * j, on);
+        copy_scales<1>(ts + 16 + 4 * j, xs + kRowWord * j, on);
       }
       mma_f4_stage<1>(tmem + buf * kAccCols, make_smem_desc(base, kStageRow), make_smem_desc(base + kWBytes, kStageRow), idesc, ts, ts + 16, 4, format, kb > 0, on,
                       min(4, (K - kb * kFp4Stage + 63) / 64));
@@ -181,6 +187,11 @@ __device__ __forceinline__ void mma_few(FewCtl& c, uint32_t smem, uint32_t tmem,
       if (++s == kStages4) {
         s = 0;
         ph ^= 1u;
+      }
+      if (in == kGroup - 1 || kb == kb_all - 1) {
+        mma_commit(smem_u32(&c.scales_empty[g]), on);
+        g ^= 1;
+        if (g == 0) gph ^= 1u;
       }
     }
     mma_commit(smem_u32(&c.ctl.tmem_full[buf]), on);
@@ -190,22 +201,61 @@ __device__ __forceinline__ void mma_few(FewCtl& c, uint32_t smem, uint32_t tmem,
   __syncwarp();
 }
 
-// The scales of one operand, turned round; called by a warp.
-__device__ __forceinline__ void turn_few(FewCtl& c, uint32_t scales, int rows, int items, int kb_all, int format, int lane) {
-  int s = 0;
+// The scales of one operand (0: weights, 1: rows), copied two groups ahead and turned round; called by a warp.  load(item, group of the item, place,
+// barrier) issues the copies, turn(place) puts them in order.
+template <typename Load, typename Turn>
+__device__ __forceinline__ void scales_few(FewCtl& c, int part, int items, int kb_all, int lane, Load load, Turn turn, bool wait_first) {
+  int li = blockIdx.x, lgroup = 0, place = 0;
+  auto load_next = [&]() {
+    if (li >= items) return;
+    load(li, lgroup, place, smem_u32(&c.scales_full[part][place]));
+    place ^= 1;
+    if (++lgroup * kGroup >= kb_all) {
+      lgroup = 0;
+      li += gridDim.x;
+    }
+  };
+  if (wait_first) pdl_wait();
+  load_next();
+  load_next();
+  int g = 0;
   uint32_t ph = 0;
+  bool first = true;
   for (int item = blockIdx.x; item < items; item += gridDim.x) {
-    for (int kb = 0; kb < kb_all; ++kb) {
-      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&c.ctl.full[s]), ph, &c.ctl, &g_wait_status))) return;
-      turn_scales(scales + s * kFewStage, rows, format, kb, lane);
+    for (int kb = 0; kb < kb_all; kb += kGroup) {
+      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&c.scales_full[part][g]), ph, &c.ctl, &g_wait_status))) return;
+      turn(g);
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&c.turned[s]));
-      if (++s == kStages4) {
-        s = 0;
-        ph ^= 1u;
+      if (lane == 0) mbar_arrive(smem_u32(&c.turned[g]));
+      g ^= 1;
+      // the other place, when the MMAs of its group (the one before) have ended
+      if (!first && li < items) {
+        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&c.scales_empty[g]), g == 0 ? ph : ph ^ 1u, &c.ctl, &g_wait_status))) return;
+        load_next();
       }
+      first = false;
+      if (g == 0) ph ^= 1u;
     }
   }
+}
+
+// A group's scales of 16 rows, as a copy with the swizzle of their width left them, turned round in place: a word of all rows after another.
+__device__ __forceinline__ void turn_rows(uint32_t base, int format, int lane) {
+  uint32_t w[16];
+  const int r = lane & 15, pieces = format == B2C_MXFP4 ? 2 : 4, x = format == B2C_MXFP4 ? (r >> 2) & 1 : (r >> 1) & 3;
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    if (p < pieces)
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(w[4 * p]), "=r"(w[4 * p + 1]), "=r"(w[4 * p + 2]), "=r"(w[4 * p + 3])
+                   : "r"(base + (uint32_t)(r * 16 * pieces + ((p ^ x) << 4)))
+                   : "memory");
+  }
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (i < 4 * pieces && lane < 16) asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + (uint32_t)(kRowWord * i + r * 16)), "r"(w[i]) : "memory");
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
 // Eight neighbouring elements of a row of n as they lie in memory, zeros past its end; widened.
@@ -241,16 +291,18 @@ __device__ __forceinline__ void widen8(const Raw8<T>& r, float* v) {
 }
 
 constexpr int kQuantWarp0 = 8, kQuantWarps = 2 * kStages4, kUpThreads = 32 * (kQuantWarp0 + kQuantWarps);
+// (80 registers a thread, so that a block of the second kernel, of 256 threads with up to 96, has room beside it)
 template <typename T>
-__global__ void __launch_bounds__(kUpThreads, 1) experts4_up_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_ws, const Few4Args a) {
+__global__ void __maxnreg__(80) experts4_up_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_ws, const Few4Args a) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ FewCtl c;
   __shared__ FewPlan plan;
-  __shared__ float sums[2][kTileRows][kTileM];
+  __shared__ float sums[kTileRows][kTileM];
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
   const int lane = threadIdx.x & 31;
   const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  setup_few(c, warp, lane, 3);
+  const uint32_t ws = smem + kStages4 * kFewStage, xs0 = ws + 2 * kGroupTile;
+  setup_few(c, warp, lane, 1);
   if (warp == 0 && lane == 9) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_w) : "memory");
   if (warp == 0 && lane == 10) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_ws) : "memory");
   pdl_wait();
@@ -269,48 +321,20 @@ __global__ void __launch_bounds__(kUpThreads, 1) experts4_up_kernel(const __grid
   if (warp == 0) {
     // ---------------------------------------------------------------- copies of weights
     const uint32_t on = elect_one() ? 1u : 0u;
-    int ahead_item = blockIdx.x, ahead_kb = 0;
-    auto prefetch = [&]() {
-      if (ahead_item >= items) return;
-      const int t = ahead_item / n_tiles, n0 = (ahead_item - t * n_tiles) * cols, plane = 2 * plan.tile[t].expert;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        tma_prefetch_3d(&tmap_w, ahead_kb * kStageRow, n0, plane + h, on);
-        tma_prefetch_3d(&tmap_ws, scale_byte(ahead_kb, a.format), n0, plane + h, on);
-      }
-      if (++ahead_kb == kb_all) {
-        ahead_kb = 0;
-        ahead_item += gridDim.x;
-      }
-    };
-    int s = 0, i = 0;
+    int s = 0;
     uint32_t ph = 0;
     bool alive = true;
     for (int item = blockIdx.x; item < items && alive; item += gridDim.x) {
       const int t = item / n_tiles, n0 = (item - t * n_tiles) * cols, plane = 2 * plan.tile[t].expert;
-      for (int kb = 0; kb < kb_all; ++kb, ++i) {
+      for (int kb = 0; kb < kb_all; ++kb) {
         if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&c.ctl.empty[s]), ph ^ 1u, &c.ctl, &g_wait_status))) {
           alive = false;
           break;
         }
         const uint32_t full = smem_u32(&c.ctl.full[s]), dst = smem + s * kFewStage;
-        mbar_arrive_expect_tx(full, kWBytes + kScaleTile, on);
-        const int sx = scale_byte(kb, a.format);
+        mbar_arrive_expect_tx(full, kWBytes, on);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {  // gate, up
-          tma_load_3d(dst + kWBytes + kXBytes + h * (kScaleTile / 2), &tmap_ws, sx, n0, plane + h, full, on);
-          tma_load_3d(dst + h * (kWBytes / 2), &tmap_w, kb * kStageRow, n0, plane + h, full, on);
-        }
-        if (i < kStages4) {  // the first stages are not prefetched
-          if (++ahead_kb == kb_all) {
-            ahead_kb = 0;
-            ahead_item += gridDim.x;
-          }
-          if (i == kStages4 - 1)
-            for (int k = 0; k < kPrefetch; ++k) prefetch();
-        } else {
-          prefetch();
-        }
+        for (int h = 0; h < 2; ++h) tma_load_3d(dst + h * (kWBytes / 2), &tmap_w, kb * kStageRow, n0, plane + h, full, on);  // gate, up
         if (++s == kStages4) {
           s = 0;
           ph ^= 1u;
@@ -319,9 +343,21 @@ __global__ void __launch_bounds__(kUpThreads, 1) experts4_up_kernel(const __grid
     }
     __syncwarp();
   } else if (warp == 1) {
-    mma_few(c, smem, tmem, items, kb_all, a.hidden, a.format);
+    mma_few<true>(c, smem, ws, [&](int s, int, int) { return xs0 + (uint32_t)(s * kRowStage); }, tmem, items, kb_all, a.hidden, a.format);
   } else if (warp == 2) {
-    turn_few(c, smem + kWBytes + kXBytes, kTileM, items, kb_all, a.format, lane);
+    // ---------------------------------------------------------------- scales of weights
+    const uint32_t on = elect_one() ? 1u : 0u;
+    const int width = group_row(a.format);
+    scales_few(
+        c, 0, items, kb_all, lane,
+        [&](int item, int group, int place, uint32_t full) {
+          const int t = item / n_tiles, n0 = (item - t * n_tiles) * cols, plane = 2 * plan.tile[t].expert;
+          mbar_arrive_expect_tx(full, (uint32_t)(kTileM * width), on);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) tma_load_3d(ws + (uint32_t)(place * kGroupTile + h * 64 * width), &tmap_ws, group * width, n0, plane + h, full, on);
+        },
+        [&](int place) { turn_group(ws + (uint32_t)(place * kGroupTile), kTileM, a.format, lane); }, false);
+    __syncwarp();
   } else if (warp >= kQuantWarp0) {
     // ---------------------------------------------------------------- rows
     // A place of the ring has two warps, for its even and its odd rows: the latency of a warp's loads is spread over the stages between.  (A warp
@@ -331,7 +367,7 @@ __global__ void __launch_bounds__(kUpThreads, 1) experts4_up_kernel(const __grid
     // It takes two rows at a time, and the two after them, of this stage or of its next one, are on their way.
     const int s = (warp - kQuantWarp0) % kStages4, half = (warp - kQuantWarp0) / kStages4;
     const int per = a.format == B2C_MXFP4 ? 2 : 1;  // lanes of a block: 4 or 2
-    const uint32_t x = smem + s * kFewStage + kWBytes, xs = x + kXBytes + kScaleTile;
+    const uint32_t x = smem + s * kFewStage + kWBytes, xs = xs0 + s * kRowStage;
     Raw8<T> next[2];
     auto fetch = [&](const FewTile& t, int i, int r) {
 #pragma unroll
@@ -377,13 +413,13 @@ __global__ void __launch_bounds__(kUpThreads, 1) experts4_up_kernel(const __grid
           const int block = lane >> per;
           asm volatile("st.shared.b32 [%0], %1;" ::"r"(x + (uint32_t)(row * kStageRow + (((lane >> 2) ^ (row & 7)) << 4) + (lane & 3) * 4)), "r"(q) : "memory");
           if ((lane & ((1 << per) - 1)) == 0)
-            asm volatile("st.shared.b8 [%0], %1;" ::"r"(xs + (uint32_t)((block >> 2) * 512 + row * 16 + (block & 3))), "r"(sc.code) : "memory");
+            asm volatile("st.shared.b8 [%0], %1;" ::"r"(xs + (uint32_t)((block >> 2) * kRowWord + row * 16 + (block & 3))), "r"(sc.code) : "memory");
         }
       }
       if (done) {
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&c.turned[s]));
+        if (lane == 0) mbar_arrive(smem_u32(&c.rows[s]));
       }
     }
     __syncwarp();
@@ -405,17 +441,18 @@ __global__ void __launch_bounds__(kUpThreads, 1) experts4_up_kernel(const __grid
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&c.ctl.tmem_empty[buf]));
-      // gate sums are in lanes 0..63, up sums in 64..127; a slice of `sums` is written again two items later, and a barrier lies between
+      // gate sums are in lanes 0..63, up sums in 64..127
       const float alpha = xg * (a.w1_global != nullptr ? a.w1_global[t.expert] : 1.0f);
+      asm volatile("bar.sync 1, 128;" ::: "memory");  // (those of the item before have been read)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sums[buf][i][quad * 32 + lane] = v[i] * alpha;
+      for (int i = 0; i < 16; ++i) sums[i][quad * 32 + lane] = v[i] * alpha;
       asm volatile("bar.sync 1, 128;" ::: "memory");
       // half a warp takes a token: each lane four neighbouring columns
       const int l = lane & 15, n = n0 + 4 * l;
       for (int r = 2 * quad + (lane >> 4); r - (lane >> 4) < t.rows; r += 8) {
         float h[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = r < t.rows ? silu(sums[buf][r][4 * l + i]) * sums[buf][r][64 + 4 * l + i] : 0.0f;
+        for (int i = 0; i < 4; ++i) h[i] = r < t.rows ? silu(sums[r][4 * l + i]) * sums[r][64 + 4 * l + i] : 0.0f;
         uint32_t mx = max(max(abs_bits(h[0]), abs_bits(h[1])), max(abs_bits(h[2]), abs_bits(h[3])));
         mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
@@ -450,6 +487,7 @@ __global__ void __launch_bounds__(kDownThreads, 1)
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
   const int lane = threadIdx.x & 31;
   const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t ws = smem + kStages4 * kFewStage, xs0 = ws + 2 * kGroupTile;
   setup_few(c, warp, lane, 2);
   if (warp == 0 && lane == 9) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_w) : "memory");
   if (warp == 0 && lane == 10) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_ws) : "memory");
@@ -479,16 +517,12 @@ __global__ void __launch_bounds__(kDownThreads, 1)
     };
     auto load_w = [&](const At& p, int s) {
       const int t = p.item / n_tiles, n0 = (p.item - t * n_tiles) * cols;
-      const uint32_t full = smem_u32(&c.ctl.full[s]), dst = smem + s * kFewStage;
-      mbar_arrive_expect_tx(full, kWBytes + kScaleTile + kXBytes + kTileRows * kScaleRow, on);
-      tma_load_3d(dst + kWBytes + kXBytes, &tmap_ws, scale_byte(p.kb, a.format), n0, plan.tile[t].expert, full, on);
-      tma_load_3d(dst, &tmap_w, p.kb * kStageRow, n0, plan.tile[t].expert, full, on);
+      const uint32_t full = smem_u32(&c.ctl.full[s]);
+      mbar_arrive_expect_tx(full, kFewStage, on);
+      tma_load_3d(smem + s * kFewStage, &tmap_w, p.kb * kStageRow, n0, plan.tile[t].expert, full, on);
     };
     auto load_x = [&](const At& p, int s) {
-      const int row0 = plan.tile[p.item / n_tiles].row0;
-      const uint32_t full = smem_u32(&c.ctl.full[s]), dst = smem + s * kFewStage + kWBytes;
-      tma_load_2d(dst + kXBytes + kScaleTile, &tmap_xs, scale_byte(p.kb, a.format), row0, full, on);
-      tma_load_2d(dst, &tmap_x, p.kb * kStageRow, row0, full, on);
+      tma_load_2d(smem + s * kFewStage + kWBytes, &tmap_x, p.kb * kStageRow, plan.tile[p.item / n_tiles].row0, smem_u32(&c.ctl.full[s]), on);
     };
     const int ahead = min(kStages4, all);
     At w = {(int)blockIdx.x, 0}, x = w;
@@ -496,15 +530,6 @@ __global__ void __launch_bounds__(kDownThreads, 1)
       load_w(w, i);
       step(w);
     }
-    At far = w;
-    auto prefetch = [&]() {
-      if (far.item >= items) return;
-      const int t = far.item / n_tiles, n0 = (far.item - t * n_tiles) * cols;
-      tma_prefetch_3d(&tmap_w, far.kb * kStageRow, n0, plan.tile[t].expert, on);
-      tma_prefetch_3d(&tmap_ws, scale_byte(far.kb, a.format), n0, plan.tile[t].expert, on);
-      step(far);
-    };
-    for (int i = 0; i < kPrefetch; ++i) prefetch();
     pdl_wait();
     for (int i = 0; i < ahead; ++i) {
       load_x(x, i);
@@ -517,7 +542,6 @@ __global__ void __launch_bounds__(kDownThreads, 1)
       load_w(w, s);
       load_x(w, s);
       step(w);
-      prefetch();
       if (++s == kStages4) {
         s = 0;
         ph ^= 1u;
@@ -525,9 +549,31 @@ __global__ void __launch_bounds__(kDownThreads, 1)
     }
     __syncwarp();
   } else if (warp == 1) {
-    mma_few(c, smem, tmem, items, kb_all, a.inter, a.format);
+    const int words = scale_groups(a.format);
+    mma_few<false>(c, smem, ws, [&](int, int g, int in) { return xs0 + (uint32_t)(g * kRowGroup + kRowWord * words * in); }, tmem, items, kb_all, a.inter, a.format);
   } else if (warp < 4) {
-    turn_few(c, smem + kWBytes + kXBytes + (warp - 2) * kScaleTile, warp == 2 ? kTileM : kTileRows, items, kb_all, a.format, lane);
+    // ---------------------------------------------------------------- scales of weights, of rows
+    const uint32_t on = elect_one() ? 1u : 0u;
+    const int width = group_row(a.format);
+    if (warp == 2) {
+      scales_few(
+          c, 0, items, kb_all, lane,
+          [&](int item, int group, int place, uint32_t full) {
+            const int t = item / n_tiles, n0 = (item - t * n_tiles) * cols;
+            mbar_arrive_expect_tx(full, (uint32_t)(kTileM * width), on);
+            tma_load_3d(ws + (uint32_t)(place * kGroupTile), &tmap_ws, group * width, n0, plan.tile[t].expert, full, on);
+          },
+          [&](int place) { turn_group(ws + (uint32_t)(place * kGroupTile), kTileM, a.format, lane); }, false);
+    } else {
+      scales_few(
+          c, 1, items, kb_all, lane,
+          [&](int item, int group, int place, uint32_t full) {
+            mbar_arrive_expect_tx(full, (uint32_t)(kTileRows * width), on);
+            tma_load_2d(xs0 + (uint32_t)(place * kRowGroup), &tmap_xs, group * width, plan.tile[item / n_tiles].row0, full, on);
+          },
+          [&](int place) { turn_rows(xs0 + (uint32_t)(place * kRowGroup), a.format, lane); }, true);
+    }
+    __syncwarp();
   } else {
     // ---------------------------------------------------------------- rows of the slots, their sums by token
     pdl_wait();
@@ -620,22 +666,23 @@ int fail(cudaError_t e) {
 template <typename T>
 int launch(const Few4Args& a, cudaStream_t st) {
   const uint64_t b1 = a.hidden / 2, b2 = a.inter / 2, s1 = fp4_scales(a.hidden, a.format), s2 = fp4_scales(a.inter, a.format);
+  const int width = group_row(a.format);
   CUtensorMap w1, ws1, w2, ws2, x, xs;
   int rc = encode_tiled_3d(&w1, a.w1, b1, a.inter, 2ull * a.experts, b1, (uint64_t)a.inter * b1, kStageRow, 64, 128);
-  if (rc == B2C_OK) rc = encode_tiled_3d(&ws1, a.w1_scale, s1, a.inter, 2ull * a.experts, a.ld1, (uint64_t)a.inter * a.ld1, kScaleRow, 64, 0);
+  if (rc == B2C_OK) rc = encode_tiled_3d(&ws1, a.w1_scale, s1, a.inter, 2ull * a.experts, a.ld1, (uint64_t)a.inter * a.ld1, width, 64, width);
   if (rc == B2C_OK) rc = encode_tiled_3d(&w2, a.w2, b2, a.hidden, a.experts, b2, (uint64_t)a.hidden * b2, kStageRow, kTileM, 128);
-  if (rc == B2C_OK) rc = encode_tiled_3d(&ws2, a.w2_scale, s2, a.hidden, a.experts, a.ld2, (uint64_t)a.hidden * a.ld2, kScaleRow, kTileM, 0);
+  if (rc == B2C_OK) rc = encode_tiled_3d(&ws2, a.w2_scale, s2, a.hidden, a.experts, a.ld2, (uint64_t)a.hidden * a.ld2, width, kTileM, width);
   if (rc == B2C_OK) rc = encode_tiled_2d(&x, a.hq, b2, a.pairs, b2, kStageRow, kTileRows, 128);
-  if (rc == B2C_OK) rc = encode_tiled_2d(&xs, a.hs, s2, a.pairs, a.ldhs, kScaleRow, kTileRows, 0);
+  if (rc == B2C_OK) rc = encode_tiled_2d(&xs, a.hs, s2, a.pairs, a.ldhs, width, kTileRows, width);
   if (rc != B2C_OK) return rc;
   static std::atomic<unsigned long long> up{0}, down{0};
-  cudaError_t e = set_max_dynamic_smem_once(up, (const void*)experts4_up_kernel<T>, kFewSmem);
-  if (e == cudaSuccess) e = set_max_dynamic_smem_once(down, (const void*)experts4_down_kernel<T>, kFewSmem);
+  cudaError_t e = set_max_dynamic_smem_once(up, (const void*)experts4_up_kernel<T>, kUpSmem);
+  if (e == cudaSuccess) e = set_max_dynamic_smem_once(down, (const void*)experts4_down_kernel<T>, kDownSmem);
   // (as many tiles as experts or pairs at most, and one more for every 16 pairs)
   const long long tiles = std::min(a.experts, a.pairs) + a.pairs / kTileRows;
   auto grid = [&](long long n) { return dim3((unsigned)std::min<long long>(tiles * n, kNumSMs)); };
-  if (e == cudaSuccess) e = launch_pdl(experts4_up_kernel<T>, grid((a.inter + 63) / 64), dim3(kUpThreads), kFewSmem, st, w1, ws1, a);
-  if (e == cudaSuccess) e = launch_pdl(experts4_down_kernel<T>, grid((a.hidden + kTileM - 1) / kTileM), dim3(kDownThreads), kFewSmem, st, w2, ws2, x, xs, a);
+  if (e == cudaSuccess) e = launch_pdl(experts4_up_kernel<T>, grid((a.inter + 63) / 64), dim3(kUpThreads), kUpSmem, st, w1, ws1, a);
+  if (e == cudaSuccess) e = launch_pdl(experts4_down_kernel<T>, grid((a.hidden + kTileM - 1) / kTileM), dim3(kDownThreads), kDownSmem, st, w2, ws2, x, xs, a);
   return e == cudaSuccess ? B2C_OK : fail(e);
 }
 

@@ -22,10 +22,10 @@ struct RowsShape {
   static constexpr int kThreads = 64 + 32 * kEpiWarps;
   static constexpr int kWarpCols = kCols / (kEpiWarps / 4);
   static constexpr int kW = WT * kTileM * kStageRow, kX = NT * kStageRow;
-  static constexpr int kStageBytes = kW + kX + (WT + 1) * kScaleTile;
-  static constexpr int kCopied = kW + kX + WT * kScaleTile + NT * kScaleRow;
+  static constexpr int kStageBytes = kW + kX;
+  static constexpr int kScaleBytes = (WT + 1) * kGroupTile;  // of a group; two groups
   // two thread blocks share an SM where that leaves each three stages (228 KB, 1 KB of it kept for each block; the barriers are static)
-  static constexpr int kHalf = 113 * 1024 - 1024 - 1024, kWhole = 227 * 1024 - 1024 - 1024;
+  static constexpr int kHalf = 113 * 1024 - 1024 - 1024 - 2 * kScaleBytes, kWhole = 227 * 1024 - 1024 - 1024 - 2 * kScaleBytes;
   static constexpr int kPerSm = kHalf / kStageBytes >= 3 ? 2 : 1;
   static constexpr int kRing = kPerSm == 2 ? kHalf : kWhole;
   static constexpr int kStages = kRing / kStageBytes < 8 ? kRing / kStageBytes : 8;
@@ -33,7 +33,8 @@ struct RowsShape {
   static constexpr int kNeed = kCols + 2 * kScaleCols;
   static constexpr int kTmemCols = kNeed <= 128 ? 128 : (kNeed <= 256 ? 256 : 512);
   static constexpr int kPartBytes = kCols * kTileM * 4;  // sums, in the place of the stages
-  static constexpr int kSmem = 1024 + (kStages * kStageBytes > kPartBytes ? kStages * kStageBytes : kPartBytes);
+  static constexpr int kUsed = kStages * kStageBytes + 2 * kScaleBytes;
+  static constexpr int kSmem = 1024 + (kUsed > kPartBytes ? kUsed : kPartBytes);
   static_assert(kPerSm * kTmemCols <= 512, "tensor memory of the blocks of an SM");
 };
 
@@ -45,18 +46,24 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, RowsShape<NT, WT>
   constexpr int stages = S::kStages;
   extern __shared__ uint8_t smem_raw[];
   __shared__ SharedCtl ctl;
-  __shared__ __align__(8) unsigned long long turned[8];  // scales of a stage are in place
+  __shared__ __align__(8) unsigned long long scales_full[WT + 1][2], scales_empty[2];  // of a group of scales
+  __shared__ __align__(8) unsigned long long turned[2];                                // and when all of them are in place
   __shared__ RowTile tile;
 
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
   const int lane = threadIdx.x & 31;
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t s_base = smem_base + stages * S::kStageBytes;
   const int split = (int)gridDim.z, rank = (int)blockIdx.z;  // (a cluster is the blocks of one z run)
 
   if (warp == 0) {
     if (lane < stages) {
       mbar_init(smem_u32(&ctl.full[lane]), 1);
       mbar_init(smem_u32(&ctl.empty[lane]), 1);
+    }
+    if (lane < 2) {
+      for (int w = 0; w <= WT; ++w) mbar_init(smem_u32(&scales_full[w][lane]), 1);
+      mbar_init(smem_u32(&scales_empty[lane]), 1);
       mbar_init(smem_u32(&turned[lane]), WT + 1);
     }
     if (lane == 8) mbar_init(smem_u32(&ctl.tmem_full[0]), 1);
@@ -96,17 +103,12 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, RowsShape<NT, WT>
     const uint32_t leader = elect_one() ? 1u : 0u;
     auto load_w = [&](int kb, int s) {
       const uint32_t full = smem_u32(&ctl.full[s]), dst = smem_base + s * S::kStageBytes;
-      mbar_arrive_expect_tx(full, S::kCopied, leader);
+      mbar_arrive_expect_tx(full, S::kStageBytes, leader);
 #pragma unroll
-      for (int w = 0; w < WT; ++w) {
-        tma_load_3d(dst + S::kW + S::kX + w * kScaleTile, &tmap_ws, scale_byte(kb, a.format), n0, group * WT + w, full, leader);
-        tma_load_3d(dst + w * kTileM * kStageRow, &tmap_w, kb * kStageRow, n0, group * WT + w, full, leader);
-      }
+      for (int w = 0; w < WT; ++w) tma_load_3d(dst + w * kTileM * kStageRow, &tmap_w, kb * kStageRow, n0, group * WT + w, full, leader);
     };
     auto load_x = [&](int kb, int s) {
-      const uint32_t full = smem_u32(&ctl.full[s]), dst = smem_base + s * S::kStageBytes + S::kW;
-      tma_load_2d(dst + S::kX + WT * kScaleTile, &tmap_xs, scale_byte(kb, a.format), row0, full, leader);
-      tma_load_2d(dst, &tmap_x, kb * kStageRow, row0, full, leader);
+      tma_load_2d(smem_base + s * S::kStageBytes + S::kW, &tmap_x, kb * kStageRow, row0, smem_u32(&ctl.full[s]), leader);
     };
     const int ahead = early ? min(stages, kb1 - kb0) : 0;
     for (int i = 0; i < ahead; ++i) load_w(kb0 + i, i);
@@ -129,25 +131,33 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, RowsShape<NT, WT>
     const uint32_t leader = elect_one() ? 1u : 0u;
     const uint32_t idesc = make_idesc_f4(kTileM, NT, a.format);
     const int groups4 = scale_groups(a.format);
-    int s = 0;
-    uint32_t ph = 0;
+    int s = 0, g = 0;
+    uint32_t ph = 0, gph = 0;
     for (int kb = kb0; kb < kb1; ++kb) {
+      const int in = kb % kGroup;  // stage of the group (the first group may begin inside)
+      if (in == 0 || kb == kb0) {
+        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&turned[g]), gph, &ctl, &g_wait_status))) break;
+      }
       if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.full[s]), ph, &ctl, &g_wait_status))) break;
-      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&turned[s]), ph, &ctl, &g_wait_status))) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const int ksteps = min(4, (a.K - kb * kFp4Stage + 63) / 64);
-      const uint32_t base = smem_base + s * S::kStageBytes, scales = base + S::kW + S::kX;
+      const uint32_t base = smem_base + s * S::kStageBytes, scales = s_base + g * S::kScaleBytes + (uint32_t)(512 * groups4 * in);
       // (copies and MMAs run in the order in which they are issued)
       const uint32_t ts = tmem_scales + (uint32_t)((kb - kb0) & 1) * S::kScaleCols;
 #pragma unroll
       for (int w = 0; w <= WT; ++w)
-        for (int j = 0; j < groups4; ++j) copy_scales<1>(ts + 16 * w + 4 * j, scales + w * kScaleTile + 512 * j, leader);
+        for (int j = 0; j < groups4; ++j) copy_scales<1>(ts + 16 * w + 4 * j, scales + w * kGroupTile + 512 * j, leader);
       const uint64_t xdesc = make_smem_desc(base + S::kW, kStageRow);
 #pragma unroll
       for (int w = 0; w < WT; ++w)
         mma_f4_stage<1>(tmem_acc + w * NT, make_smem_desc(base + w * kTileM * kStageRow, kStageRow), xdesc, idesc, ts + 16 * w, ts + 16 * WT, 4, a.format,
                         kb > kb0, leader, ksteps);
       mma_commit(smem_u32(&ctl.empty[s]), leader);
+      if (in == kGroup - 1) {
+        mma_commit(smem_u32(&scales_empty[g]), leader);
+        g ^= 1;
+        if (g == 0) gph ^= 1u;
+      }
       if (kb == kb1 - 1) mma_commit(smem_u32(&ctl.tmem_full[0]), leader);
       if (++s == stages) {
         s = 0;
@@ -156,24 +166,47 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, RowsShape<NT, WT>
     }
     __syncwarp();
   } else {
+    // ---------------------------------------------------------------- scales: a warp has a tile of weights, the one after them the rows
+    const int part = warp - 2;
+    int lg = kb0 / kGroup, place = 0;  // next group to be copied, and where to
+    const int last = (kb1 - 1) / kGroup;
+    auto load_next = [&]() {
+      if (lg > last) return;
+      const uint32_t on = elect_one() ? 1u : 0u, full = smem_u32(&scales_full[part][place]), dst = s_base + place * S::kScaleBytes + part * kGroupTile;
+      const int width = group_row(a.format);
+      mbar_arrive_expect_tx(full, (uint32_t)((part < WT ? kTileM : NT) * width), on);
+      if (part < WT) tma_load_3d(dst, &tmap_ws, lg * width, n0, group * WT + part, full, on);
+      else tma_load_2d(dst, &tmap_xs, lg * width, row0, full, on);
+      ++lg;
+      place ^= 1;
+    };
+    if (part < WT) {
+      load_next();
+      load_next();
+    }
     if (early) {
       pdl_wait();
       pdl_launch_dependents();
     }
-    // ---------------------------------------------------------------- scales turned round: a warp has a tile of weights, the last one the rows
-    const int part = warp - 2;
     if (part <= WT) {
-      int s = 0;
+      if (part == WT) {
+        load_next();
+        load_next();
+      }
       uint32_t ph = 0;
-      for (int kb = kb0; kb < kb1; ++kb) {
-        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.full[s]), ph, &ctl, &g_wait_status))) break;
-        turn_scales(smem_base + s * S::kStageBytes + S::kW + S::kX + part * kScaleTile, part == WT ? NT : kTileM, a.format, kb, lane);
+      int g = 0;
+      for (int n = kb0 / kGroup; n <= last; ++n) {
+        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&scales_full[part][g]), ph, &ctl, &g_wait_status))) break;
+        turn_group(s_base + g * S::kScaleBytes + part * kGroupTile, part == WT ? NT : kTileM, a.format, lane);
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&turned[s]));
-        if (++s == stages) {
-          s = 0;
-          ph ^= 1u;
+        if (lane == 0) mbar_arrive(smem_u32(&turned[g]));
+        g ^= 1;
+        // the other place, when the MMAs of its group (the one before) have ended
+        if (n > kb0 / kGroup && lg <= last) {
+          if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&scales_empty[g]), g == 0 ? ph : ph ^ 1u, &ctl, &g_wait_status))) break;
+          load_next();
         }
+        if (g == 0) ph ^= 1u;
       }
       __syncwarp();
     }
@@ -280,16 +313,20 @@ int fail(cudaError_t e) {
   return B2C_E_CUDA;
 }
 
-// How many thread blocks share a tile's reduction: what counts is the SM with the most stages to fetch (tiles * split thread blocks over 148 SMs);
-// a cut costs the exchange of the partial sums, about as long as three stages, and more the larger the cluster.
-int choose_split(long long tiles, int kb_all, bool counted) {
+// How many thread blocks share a tile's reduction: what counts is the stages that a block fetches, one after another.  Blocks that share an SM are
+// a fifth slower each; a cut costs the exchange of the partial sums, about as long as two stages and one more for every block of the cluster.
+// Measured, us with 1, 2, 3, 4, 6 blocks a tile:
+//   1 x 8192 x 8192 (64 tiles of 32 stages) 17.3, 13.1, 11.8, 11.3, 16.7;   37 x 5136 x 4128 (41 of 17) 10.1, 8.9, 8.3, 9.0, 8.9;
+//   16 x 4096 x 4096 (32 of 16) 10.3, 8.5, 7.5, 6.9, 7.2;   128 x 4096 x 4096 (64 of 16) 11.2, 9.7, 9.8, 9.3, 16.2.
+int choose_split(long long tiles, int kb_all, int per_sm, bool counted) {
   if (!counted && tiles >= kNumSMs) return 1;  // (a guess of the tiles says nothing about the last wave)
   int best = 1;
   double least = 0;
   for (int s = 1; s <= kMaxSplit && 2 * s <= std::max(2, kb_all); ++s) {
     const int per = (kb_all + s - 1) / s;
     if ((kb_all + per - 1) / per != s) continue;  // (no thread block without work)
-    const double cost = (double)((tiles * s + kNumSMs - 1) / kNumSMs) * per + (s > 1 ? 2.5 + 0.5 * s : 0.0);
+    const long long blocks = tiles * s, waves = (blocks + kNumSMs * per_sm - 1) / (kNumSMs * per_sm);
+    const double cost = (double)waves * per * (per_sm > 1 && blocks > kNumSMs ? 1.2 : 1.0) + (s > 1 ? 1.5 + s : 0.0);
     if (s == 1 || cost < least) {
       best = s;
       least = cost;
@@ -307,14 +344,15 @@ int launch_rows(const Matmul4Args& a, cudaStream_t st) {
   if (row_tiles > 65535) return B2C_E_UNSUPPORTED;
   // (with groups the number of tiles is known on the device only: as many groups as there are rows may have some)
   const long long busy = (long long)n_tiles * (a.offsets ? std::max<long long>((a.rows + NT - 1) / NT, std::min(a.groups, a.rows)) : row_tiles);
-  const int split = choose_split(busy, kb_all, a.offsets == nullptr);
+  const int split = choose_split(busy, kb_all, S::kPerSm, a.offsets == nullptr);
   const int kb_per_split = (kb_all + split - 1) / split;
   const uint64_t bytes = a.K / 2, scales = fp4_scales(a.K, a.format), planes = (uint64_t)a.groups * WT;
+  const int width = group_row(a.format);
   CUtensorMap tw, tws, tx, txs;
   int rc = encode_tiled_3d(&tw, a.b, bytes, a.N, planes, bytes, (uint64_t)a.N * bytes, kStageRow, kTileM, 128);
-  if (rc == B2C_OK) rc = encode_tiled_3d(&tws, a.b_scale, scales, a.N, planes, a.ldbs, (uint64_t)a.N * a.ldbs, kScaleRow, kTileM, 0);
+  if (rc == B2C_OK) rc = encode_tiled_3d(&tws, a.b_scale, scales, a.N, planes, a.ldbs, (uint64_t)a.N * a.ldbs, width, kTileM, width);
   if (rc == B2C_OK) rc = encode_tiled_2d(&tx, a.a, bytes, a.rows, a.rows > 1 ? a.lda : bytes, kStageRow, NT, 128);
-  if (rc == B2C_OK) rc = encode_tiled_2d(&txs, a.a_scale, scales, a.rows, a.rows > 1 ? a.lds : fp4_scale_pitch(a.K, a.format), kScaleRow, NT, 0);
+  if (rc == B2C_OK) rc = encode_tiled_2d(&txs, a.a_scale, scales, a.rows, a.rows > 1 ? a.lds : fp4_scale_pitch(a.K, a.format), width, NT, width);
   if (rc != B2C_OK) return rc;
   static std::atomic<unsigned long long> configured{0};
   cudaError_t e = set_max_dynamic_smem_once(configured, (const void*)matmul4_rows_kernel<NT, WT>, S::kSmem);

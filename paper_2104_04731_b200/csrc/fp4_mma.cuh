@@ -2,8 +2,8 @@
 //
 // A stage is 256 elements of the reduction: 128 bytes of every row, four MMAs of depth 64.  The tensor core takes the scales from tensor
 // memory: lane r, column c of a group of four columns holds four consecutive scales of row 32 c + r, for all four quarters of the lanes alike.
-// In memory a row's scales follow each other, so 128 rows come as 128 pieces of 16 bytes; a warp turns them round in place (a lane has the pieces
-// of four rows, 32 apart, and every group of columns takes a word of each) and tcgen05.cp carries 512 bytes to four columns.
+// In memory a row's scales follow each other, so a copy brings pieces of 128 rows; a warp turns them round in place (a lane has the pieces of four
+// rows, 32 apart, and every group of columns takes a word of each) and tcgen05.cp carries 512 bytes to four columns.
 #pragma once
 
 #include "fp4_common.cuh"
@@ -14,8 +14,6 @@ namespace b2c {
 namespace {
 
 constexpr int kStageRow = kFp4Stage / 2;  // bytes
-constexpr int kScaleRow = 16;             // bytes of a row's scales that are copied for a stage (MX: of two)
-constexpr int kScaleTile = 128 * kScaleRow;
 
 // Instruction descriptor of kind::mxf4 and kind::mxf4nvf4: both operands E2M1 (code 1 at bits 7 and 10), N/8 at bit 17, kind of the scales (0 E4M3,
 // 1 E8M0) at bit 23, M/16 at bit 24; the half of a scale word that an MMA uses at bits 29 and 4.
@@ -77,43 +75,6 @@ __device__ __forceinline__ void mma_f4_stage(uint32_t d_tmem, uint64_t adesc, ui
     else B2C_F4_STAGE("2", "mxf4nvf4.block_scale.scale_vec::4X", sa + 4, sa + 8, sa + 12, sb + b_cols, sb + 2 * b_cols, sb + 3 * b_cols, idesc);
   }
 #undef B2C_F4_STAGE
-}
-
-// Byte of a row of scales that the copy for stage kb starts at: on the copy engine's 16-byte grid.
-__device__ __forceinline__ int scale_byte(int kb, int format) { return format == B2C_MXFP4 ? (kb >> 1) * kScaleRow : kb * kScaleRow; }
-
-// The copied scales of up to 128 rows, turned round in place; called by a whole warp.  What follows in the asynchronous proxy sees it
-// after the caller's barrier.
-__device__ __forceinline__ void turn_scales(uint32_t base, int rows, int format, int kb, int lane) {
-  if (format == B2C_MXFP4) {
-    uint32_t lo[4], hi[4];
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      lo[g] = hi[g] = 0;
-      if (32 * g < rows)
-        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(lo[g]), "=r"(hi[g]) : "r"(base + (uint32_t)((32 * g + lane) * kScaleRow + (kb & 1) * 8)) : "memory");
-    }
-    __syncwarp();
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + (uint32_t)(lane * 16)), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + (uint32_t)(512 + lane * 16)), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
-  } else {
-    uint32_t w[4][4];
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[g][j] = 0;
-      if (32 * g < rows)
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(w[g][0]), "=r"(w[g][1]), "=r"(w[g][2]), "=r"(w[g][3])
-                     : "r"(base + (uint32_t)((32 * g + lane) * kScaleRow))
-                     : "memory");
-    }
-    __syncwarp();
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + (uint32_t)(512 * j + lane * 16)), "r"(w[0][j]), "r"(w[1][j]), "r"(w[2][j]), "r"(w[3][j]) : "memory");
-  }
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
 // Scales come for four stages at a time: 64 bytes (NV) or 32 (MX) of every row.  (The copy engine works by rows of a box: pieces of 16 bytes, a
