@@ -108,18 +108,17 @@ __device__ __forceinline__ void plan_few(FewPlan& plan, uint32_t* bits, const in
   __syncthreads();
 }
 
-// Barriers and tensor memory of a block; called by all threads.  `turners`: warps that put a group's scales in place.
+// Barriers and tensor memory of a block; called by all threads.  `fillers`: warps that fill a stage (the copies' one among them),
+// `turners`: warps that put a group's scales in place.
 struct FewCtl {
   SharedCtl ctl;
-  unsigned long long rows[kStages4];                                // rows of a stage are in place (first kernel)
   unsigned long long scales_full[2][2], scales_empty[2], turned[2];  // of a group of scales
 };
-__device__ __forceinline__ void setup_few(FewCtl& c, int warp, int lane, int turners) {
+__device__ __forceinline__ void setup_few(FewCtl& c, int warp, int lane, int fillers, int turners) {
   if (warp == 0) {
     if (lane < kStages4) {
-      mbar_init(smem_u32(&c.ctl.full[lane]), 1);
+      mbar_init(smem_u32(&c.ctl.full[lane]), fillers);
       mbar_init(smem_u32(&c.ctl.empty[lane]), 1);
-      mbar_init(smem_u32(&c.rows[lane]), 2);
     }
     if (lane < 2) {
       mbar_init(smem_u32(&c.ctl.tmem_full[lane]), 1);
@@ -154,12 +153,11 @@ __device__ __forceinline__ void teardown_few(FewCtl& c, int warp, uint32_t tmem)
 }
 
 // The MMAs of all items of this block; called by warp 1 of either kernel.  row_scales(stage, group's place, stage of the group): where the scales
-// of the rows are, which in the first kernel (UP) are there with the rows.
-template <bool UP, typename F>
-__device__ __forceinline__ void mma_few(FewCtl& c, uint32_t smem, uint32_t scales, F row_scales, uint32_t tmem, int items, int kb_all, int K, int format) {
+// of the rows are.
+template <int FORMAT, typename F>
+__device__ __forceinline__ void mma_few(FewCtl& c, uint32_t smem, uint32_t scales, F row_scales, uint32_t tmem, int items, int kb_all, int K) {
   const uint32_t on = elect_one() ? 1u : 0u;
-  const uint32_t idesc = make_idesc_f4(kTileM, kTileRows, format);
-  const int groups4 = scale_groups(format);
+  const uint32_t idesc = make_idesc_f4(kTileM, kTileRows, FORMAT);
   int s = 0, g = 0, buf = 0;
   uint32_t ph = 0, gph = 0, bph = 0, odd = 0;
   bool alive = true;
@@ -168,21 +166,18 @@ __device__ __forceinline__ void mma_few(FewCtl& c, uint32_t smem, uint32_t scale
     for (int kb = 0; kb < kb_all; ++kb) {
       const int in = kb % kGroup;  // stage of the group
       if ((in == 0 && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&c.turned[g]), gph, &c.ctl, &g_wait_status))) ||
-          (UP && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&c.rows[s]), ph, &c.ctl, &g_wait_status))) ||
           !__all_sync(0xffffffffu, mbar_wait(smem_u32(&c.ctl.full[s]), ph, &c.ctl, &g_wait_status))) {
         alive = false;
         break;
       }
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const uint32_t base = smem + s * kFewStage, ws = scales + g * kGroupTile + (uint32_t)(512 * groups4 * in), xs = row_scales(s, g, in);
+      const uint32_t base = smem + s * kFewStage, ws = scales + g * kGroupTile + (uint32_t)(512 * stage_words(FORMAT) * in);
       const uint32_t ts = tmem + 2 * kAccCols + odd * kFewScaleCols;
       odd ^= 1u;
-      for (int j = 0; j < groups4; ++j) {
-        copy_scales<1>(ts + 4 * j, ws + 512 * j, on);
-        copy_scales<1>(ts + 16 + 4 * j, xs + kRowWord * j, on);
-      }
-      mma_f4_stage<1>(tmem + buf * kAccCols, make_smem_desc(base, kStageRow), make_smem_desc(base + kWBytes, kStageRow), idesc, ts, ts + 16, 4, format, kb > 0, on,
-                      min(4, (K - kb * kFp4Stage + 63) / 64));
+      copy_scales<1, FORMAT, 512>(ts, ws, 4, on);
+      copy_scales<1, FORMAT, kRowWord>(ts + 16, row_scales(s, g, in), 4, on);
+      mma_f4_stage<1, FORMAT>(tmem + buf * kAccCols, make_smem_desc(base, kStageRow), make_smem_desc(base + kWBytes, kStageRow), idesc, ts, ts + 16, 4, kb > 0, on,
+                              min(4, (K - kb * kFp4Stage + 63) / 64));
       mma_commit(smem_u32(&c.ctl.empty[s]), on);
       if (++s == kStages4) {
         s = 0;
@@ -302,7 +297,7 @@ __global__ void __maxnreg__(80) experts4_up_kernel(const __grid_constant__ CUten
   const int lane = threadIdx.x & 31;
   const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t ws = smem + kStages4 * kFewStage, xs0 = ws + 2 * kGroupTile;
-  setup_few(c, warp, lane, 1);
+  setup_few(c, warp, lane, 1 + kQuantWarps / kStages4, 1);
   if (warp == 0 && lane == 9) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_w) : "memory");
   if (warp == 0 && lane == 10) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_ws) : "memory");
   pdl_wait();
@@ -343,7 +338,9 @@ __global__ void __maxnreg__(80) experts4_up_kernel(const __grid_constant__ CUten
     }
     __syncwarp();
   } else if (warp == 1) {
-    mma_few<true>(c, smem, ws, [&](int s, int, int) { return xs0 + (uint32_t)(s * kRowStage); }, tmem, items, kb_all, a.hidden, a.format);
+    auto row_scales = [&](int s, int, int) { return xs0 + (uint32_t)(s * kRowStage); };
+    if (a.format == B2C_MXFP4) mma_few<B2C_MXFP4>(c, smem, ws, row_scales, tmem, items, kb_all, a.hidden);
+    else mma_few<B2C_NVFP4>(c, smem, ws, row_scales, tmem, items, kb_all, a.hidden);
   } else if (warp == 2) {
     // ---------------------------------------------------------------- scales of weights
     const uint32_t on = elect_one() ? 1u : 0u;
@@ -419,7 +416,7 @@ __global__ void __maxnreg__(80) experts4_up_kernel(const __grid_constant__ CUten
       if (done) {
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&c.rows[s]));
+        if (lane == 0) mbar_arrive(smem_u32(&c.ctl.full[s]));
       }
     }
     __syncwarp();
@@ -488,7 +485,7 @@ __global__ void __launch_bounds__(kDownThreads, 1)
   const int lane = threadIdx.x & 31;
   const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t ws = smem + kStages4 * kFewStage, xs0 = ws + 2 * kGroupTile;
-  setup_few(c, warp, lane, 2);
+  setup_few(c, warp, lane, 1, 2);
   if (warp == 0 && lane == 9) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_w) : "memory");
   if (warp == 0 && lane == 10) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_ws) : "memory");
   if (warp == 0 && lane == 11) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_x) : "memory");
@@ -549,8 +546,10 @@ __global__ void __launch_bounds__(kDownThreads, 1)
     }
     __syncwarp();
   } else if (warp == 1) {
-    const int words = scale_groups(a.format);
-    mma_few<false>(c, smem, ws, [&](int, int g, int in) { return xs0 + (uint32_t)(g * kRowGroup + kRowWord * words * in); }, tmem, items, kb_all, a.inter, a.format);
+    const int stage = kRowWord * stage_words(a.format);
+    auto row_scales = [&](int, int g, int in) { return xs0 + (uint32_t)(g * kRowGroup + stage * in); };
+    if (a.format == B2C_MXFP4) mma_few<B2C_MXFP4>(c, smem, ws, row_scales, tmem, items, kb_all, a.inter);
+    else mma_few<B2C_NVFP4>(c, smem, ws, row_scales, tmem, items, kb_all, a.inter);
   } else if (warp < 4) {
     // ---------------------------------------------------------------- scales of weights, of rows
     const uint32_t on = elect_one() ? 1u : 0u;

@@ -130,40 +130,43 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, RowsShape<NT, WT>
     // ---------------------------------------------------------------- scales to tensor memory, MMA issue
     const uint32_t leader = elect_one() ? 1u : 0u;
     const uint32_t idesc = make_idesc_f4(kTileM, NT, a.format);
-    const int groups4 = scale_groups(a.format);
-    int s = 0, g = 0;
-    uint32_t ph = 0, gph = 0;
-    for (int kb = kb0; kb < kb1; ++kb) {
-      const int in = kb % kGroup;  // stage of the group (the first group may begin inside)
-      if (in == 0 || kb == kb0) {
-        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&turned[g]), gph, &ctl, &g_wait_status))) break;
-      }
-      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.full[s]), ph, &ctl, &g_wait_status))) break;
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const int ksteps = min(4, (a.K - kb * kFp4Stage + 63) / 64);
-      const uint32_t base = smem_base + s * S::kStageBytes, scales = s_base + g * S::kScaleBytes + (uint32_t)(512 * groups4 * in);
-      // (copies and MMAs run in the order in which they are issued)
-      const uint32_t ts = tmem_scales + (uint32_t)((kb - kb0) & 1) * S::kScaleCols;
+    auto run = [&](auto format) {
+      constexpr int FORMAT = decltype(format)::value;
+      int s = 0, g = 0;
+      uint32_t ph = 0, gph = 0;
+      for (int kb = kb0; kb < kb1; ++kb) {
+        const int in = kb % kGroup;  // stage of the group (the first group may begin inside)
+        if (in == 0 || kb == kb0) {
+          if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&turned[g]), gph, &ctl, &g_wait_status))) break;
+        }
+        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.full[s]), ph, &ctl, &g_wait_status))) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const int ksteps = min(4, (a.K - kb * kFp4Stage + 63) / 64);
+        const uint32_t base = smem_base + s * S::kStageBytes, scales = s_base + g * S::kScaleBytes + (uint32_t)(512 * stage_words(FORMAT) * in);
+        // (copies and MMAs run in the order in which they are issued)
+        const uint32_t ts = tmem_scales + (uint32_t)((kb - kb0) & 1) * S::kScaleCols;
 #pragma unroll
-      for (int w = 0; w <= WT; ++w)
-        for (int j = 0; j < groups4; ++j) copy_scales<1>(ts + 16 * w + 4 * j, scales + w * kGroupTile + 512 * j, leader);
-      const uint64_t xdesc = make_smem_desc(base + S::kW, kStageRow);
+        for (int w = 0; w <= WT; ++w) copy_scales<1, FORMAT, 512>(ts + 16 * w, scales + w * kGroupTile, 4, leader);
+        const uint64_t xdesc = make_smem_desc(base + S::kW, kStageRow);
 #pragma unroll
-      for (int w = 0; w < WT; ++w)
-        mma_f4_stage<1>(tmem_acc + w * NT, make_smem_desc(base + w * kTileM * kStageRow, kStageRow), xdesc, idesc, ts + 16 * w, ts + 16 * WT, 4, a.format,
-                        kb > kb0, leader, ksteps);
-      mma_commit(smem_u32(&ctl.empty[s]), leader);
-      if (in == kGroup - 1) {
-        mma_commit(smem_u32(&scales_empty[g]), leader);
-        g ^= 1;
-        if (g == 0) gph ^= 1u;
+        for (int w = 0; w < WT; ++w)
+          mma_f4_stage<1, FORMAT>(tmem_acc + w * NT, make_smem_desc(base + w * kTileM * kStageRow, kStageRow), xdesc, idesc, ts + 16 * w, ts + 16 * WT, 4, kb > kb0,
+                                  leader, ksteps);
+        mma_commit(smem_u32(&ctl.empty[s]), leader);
+        if (in == kGroup - 1) {
+          mma_commit(smem_u32(&scales_empty[g]), leader);
+          g ^= 1;
+          if (g == 0) gph ^= 1u;
+        }
+        if (kb == kb1 - 1) mma_commit(smem_u32(&ctl.tmem_full[0]), leader);
+        if (++s == stages) {
+          s = 0;
+          ph ^= 1u;
+        }
       }
-      if (kb == kb1 - 1) mma_commit(smem_u32(&ctl.tmem_full[0]), leader);
-      if (++s == stages) {
-        s = 0;
-        ph ^= 1u;
-      }
-    }
+    };
+    if (a.format == B2C_MXFP4) run(std::integral_constant<int, B2C_MXFP4>());
+    else run(std::integral_constant<int, B2C_NVFP4>());
     __syncwarp();
   } else {
     // ---------------------------------------------------------------- scales: a warp has a tile of weights, the one after them the rows

@@ -165,54 +165,55 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       if (rank == 0) {
         const uint32_t on = elect_one() ? 1u : 0u;
         const uint32_t idesc = make_idesc_f4(S::kRows, TN, a.format);
-        const int groups4 = scale_groups(a.format);
-        int s = 0, g = 0, buf = 0;
-        uint32_t ph = 0, gph = 0, bph = 0, ts_at = 0;
-        bool alive = true;
-        for (int t = pair_id; t < tiles && alive; t += num_pairs) {
-          if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.tmem_empty[buf]), bph ^ 1u, &ctl, &g_wait_status))) break;
-          for (int kb = 0; kb < kb_all; ++kb) {
-            const int in = kb % kGroup;  // stage of the group
-            if ((in == 0 && !__all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&turned[g]), gph, &ctl, &g_wait_status))) ||
-                !__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.full[s]), ph, &ctl, &g_wait_status))) {
-              alive = false;
-              break;
-            }
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const int ksteps = min(4, (a.K - kb * kFp4Stage + 63) / 64);
-            // (copies and MMAs run in the order in which they are issued)
-            const uint32_t ts = tmem_scales + ts_at, scales = s_base + g * S::kScaleBytes + (uint32_t)(512 * groups4 * in);
-            ts_at = S::kScaleCols - ts_at;
-            for (int j = 0; j < groups4; ++j) {
-              copy_scales<CTAS>(ts + 4 * j, scales + 512 * j, on);
+        auto run = [&](auto format) {
+          constexpr int FORMAT = decltype(format)::value;
+          int s = 0, g = 0, buf = 0;
+          uint32_t ph = 0, gph = 0, bph = 0, ts_at = 0;
+          bool alive = true;
+          for (int t = pair_id; t < tiles && alive; t += num_pairs) {
+            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.tmem_empty[buf]), bph ^ 1u, &ctl, &g_wait_status))) break;
+            for (int kb = 0; kb < kb_all; ++kb) {
+              const int in = kb % kGroup;  // stage of the group
+              if ((in == 0 && !__all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&turned[g]), gph, &ctl, &g_wait_status))) ||
+                  !__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.full[s]), ph, &ctl, &g_wait_status))) {
+                alive = false;
+                break;
+              }
+              asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+              const int ksteps = min(4, (a.K - kb * kFp4Stage + 63) / 64);
+              // (copies and MMAs run in the order in which they are issued)
+              const uint32_t ts = tmem_scales + ts_at, scales = s_base + g * S::kScaleBytes + (uint32_t)(512 * stage_words(FORMAT) * in);
+              ts_at = S::kScaleCols - ts_at;
+              copy_scales<CTAS, FORMAT, 512>(ts, scales, 4, on);
 #pragma unroll
-              for (int i = 0; i < S::kColTiles; ++i)
-                copy_scales<CTAS>(ts + 16 + 4 * (j * S::kColTiles + i), scales + (1 + i) * kGroupTile + 512 * j, on);
-            }
-            mma_f4_stage<CTAS>(tmem_acc + buf * TN, make_smem_desc(a_base + s * kABytes, kStageRow), make_smem_desc(b_base + s * kBBytes, kStageRow), idesc,
-                               ts, ts + 16, 4 * S::kColTiles, a.format, kb > 0, on, ksteps);
-            if constexpr (CTAS == 2) mma_commit_pair(smem_u32(&ctl.empty[s]), on);
-            else mma_commit(smem_u32(&ctl.empty[s]), on);
-            if (++s == kStages) {
-              s = 0;
-              ph ^= 1u;
-            }
-            if (in == kGroup - 1 || kb == kb_all - 1) {
-              if constexpr (CTAS == 2) mma_commit_pair(smem_u32(&scales_empty[g]), on);
-              else mma_commit(smem_u32(&scales_empty[g]), on);
-              if (++g == kGroups) {
-                g = 0;
-                gph ^= 1u;
+              for (int i = 0; i < S::kColTiles; ++i) copy_scales<CTAS, FORMAT, 512>(ts + 16 + 4 * i, scales + (1 + i) * kGroupTile, 4 * S::kColTiles, on);
+              mma_f4_stage<CTAS, FORMAT>(tmem_acc + buf * TN, make_smem_desc(a_base + s * kABytes, kStageRow), make_smem_desc(b_base + s * kBBytes, kStageRow), idesc,
+                                         ts, ts + 16, 4 * S::kColTiles, kb > 0, on, ksteps);
+              if constexpr (CTAS == 2) mma_commit_pair(smem_u32(&ctl.empty[s]), on);
+              else mma_commit(smem_u32(&ctl.empty[s]), on);
+              if (++s == kStages) {
+                s = 0;
+                ph ^= 1u;
+              }
+              if (in == kGroup - 1 || kb == kb_all - 1) {
+                if constexpr (CTAS == 2) mma_commit_pair(smem_u32(&scales_empty[g]), on);
+                else mma_commit(smem_u32(&scales_empty[g]), on);
+                if (++g == kGroups) {
+                  g = 0;
+                  gph ^= 1u;
+                }
               }
             }
+            if constexpr (CTAS == 2) mma_commit_pair(smem_u32(&ctl.tmem_full[buf]), on);
+            else mma_commit(smem_u32(&ctl.tmem_full[buf]), on);
+            if (++buf == S::kBufs) {
+              buf = 0;
+              bph ^= 1u;
+            }
           }
-          if constexpr (CTAS == 2) mma_commit_pair(smem_u32(&ctl.tmem_full[buf]), on);
-          else mma_commit(smem_u32(&ctl.tmem_full[buf]), on);
-          if (++buf == S::kBufs) {
-            buf = 0;
-            bph ^= 1u;
-          }
-        }
+        };
+        if (a.format == B2C_MXFP4) run(std::integral_constant<int, B2C_MXFP4>());
+        else run(std::integral_constant<int, B2C_NVFP4>());
       }
       pdl_launch_dependents();
       __syncwarp();

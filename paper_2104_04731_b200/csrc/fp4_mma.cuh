@@ -26,22 +26,48 @@ constexpr uint32_t kUpperScales = (2u << 29) | (2u << 4);
 __device__ __forceinline__ uint64_t make_scale_desc(uint32_t addr) {
   return (uint64_t)((addr & 0x3FFFF) >> 4) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);
 }
-// 512 bytes at `addr` to four columns of tensor memory; with CTAS == 2 in both blocks of the pair, each from its own shared memory.
-template <int CTAS>
-__device__ __forceinline__ void copy_scales(uint32_t taddr, uint32_t addr, uint32_t on) {
+// A stage's scales of 128 rows to tensor memory: NV four, MX two times 512 bytes, `step` bytes apart, to four columns each, `columns` apart; with
+// CTAS == 2 in both blocks of the pair, each from its own shared memory.  One asm block, so that the predicate is formed once and the
+// instructions go out back to back: issuing them is what the tensor core waits for where the tiles are small.
+template <int CTAS, int FORMAT, int STEP>
+__device__ __forceinline__ void copy_scales(uint32_t taddr, uint32_t addr, int columns, uint32_t on) {
   const uint64_t desc = make_scale_desc(addr);
-  if constexpr (CTAS == 1)
-    asm volatile("{\n.reg .pred q;\nsetp.ne.b32 q, %2, 0;\n@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n}" ::"r"(taddr), "l"(desc), "r"(on) : "memory");
-  else
-    asm volatile("{\n.reg .pred q;\nsetp.ne.b32 q, %2, 0;\n@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n}" ::"r"(taddr), "l"(desc), "r"(on) : "memory");
+#define B2C_CP4(GROUP)                                                                                     \
+  asm volatile(                                                                                            \
+      "{\n.reg .pred q;\n.reg .b32 t1, t2, t3;\n.reg .b64 d1, d2, d3;\nsetp.ne.b32 q, %2, 0;\n"            \
+      "add.u32 t1, %0, %3;\nadd.u32 t2, t1, %3;\nadd.u32 t3, t2, %3;\n"                                    \
+      "add.u64 d1, %1, %4;\nadd.u64 d2, d1, %4;\nadd.u64 d3, d2, %4;\n"                                    \
+      "@q tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [%0], %1;\n"                                      \
+      "@q tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [t1], d1;\n"                                      \
+      "@q tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [t2], d2;\n"                                      \
+      "@q tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [t3], d3;\n}" ::"r"(taddr),                       \
+      "l"(desc), "r"(on), "r"(columns), "n"(STEP >> 4)                                                     \
+      : "memory")
+#define B2C_CP2(GROUP)                                                                                     \
+  asm volatile(                                                                                            \
+      "{\n.reg .pred q;\n.reg .b32 t1;\n.reg .b64 d1;\nsetp.ne.b32 q, %2, 0;\n"                           \
+      "add.u32 t1, %0, %3;\nadd.u64 d1, %1, %4;\n"                                                         \
+      "@q tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [%0], %1;\n"                                      \
+      "@q tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [t1], d1;\n}" ::"r"(taddr),                       \
+      "l"(desc), "r"(on), "r"(columns), "n"(STEP >> 4)                                                     \
+      : "memory")
+  if constexpr (FORMAT == B2C_MXFP4) {
+    if constexpr (CTAS == 1) B2C_CP2("1");
+    else B2C_CP2("2");
+  } else {
+    if constexpr (CTAS == 1) B2C_CP4("1");
+    else B2C_CP4("2");
+  }
+#undef B2C_CP4
+#undef B2C_CP2
 }
-inline __host__ __device__ int scale_groups(int format) { return format == B2C_MXFP4 ? 2 : 4; }  // of four columns, a stage and 128 rows
+__host__ __device__ constexpr int stage_words(int format) { return format == B2C_MXFP4 ? 2 : 4; }  // groups of four columns, of a stage and 128 rows
 
 // One stage: `ksteps` (1..4) MMAs over consecutive 32-byte slices; the first overwrites unless `accumulate`.  Scales of the A rows at
 // sa, a group of four columns for one MMA (NV) or two (MX); of the B rows at sb, groups b_cols columns apart.
-template <int CTAS>
+template <int CTAS, int FORMAT>
 __device__ __forceinline__ void mma_f4_stage(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t b_cols,
-                                             int format, uint32_t accumulate, uint32_t on, int ksteps) {
+                                             uint32_t accumulate, uint32_t on, int ksteps) {
 #define B2C_F4_STAGE(GROUP, KIND, SA1, SA2, SA3, SB1, SB2, SB3, ID1)                                              \
   asm volatile(                                                                                                   \
       "{\n"                                                                                                       \
@@ -67,11 +93,11 @@ __device__ __forceinline__ void mma_f4_stage(uint32_t d_tmem, uint64_t adesc, ui
       "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(on), "r"(ksteps), "r"(sa), "r"(sb), "r"(ID1),      \
       "r"(SA1), "r"(SB1), "r"(SA2), "r"(SB2), "r"(SA3), "r"(SB3)                                                  \
       : "memory")
-  if (format == B2C_MXFP4) {
-    if (CTAS == 1) B2C_F4_STAGE("1", "mxf4.block_scale.scale_vec::2X", sa, sa + 4, sa + 4, sb, sb + b_cols, sb + b_cols, idesc | kUpperScales);
+  if constexpr (FORMAT == B2C_MXFP4) {
+    if constexpr (CTAS == 1) B2C_F4_STAGE("1", "mxf4.block_scale.scale_vec::2X", sa, sa + 4, sa + 4, sb, sb + b_cols, sb + b_cols, idesc | kUpperScales);
     else B2C_F4_STAGE("2", "mxf4.block_scale.scale_vec::2X", sa, sa + 4, sa + 4, sb, sb + b_cols, sb + b_cols, idesc | kUpperScales);
   } else {
-    if (CTAS == 1) B2C_F4_STAGE("1", "mxf4nvf4.block_scale.scale_vec::4X", sa + 4, sa + 8, sa + 12, sb + b_cols, sb + 2 * b_cols, sb + 3 * b_cols, idesc);
+    if constexpr (CTAS == 1) B2C_F4_STAGE("1", "mxf4nvf4.block_scale.scale_vec::4X", sa + 4, sa + 8, sa + 12, sb + b_cols, sb + 2 * b_cols, sb + 3 * b_cols, idesc);
     else B2C_F4_STAGE("2", "mxf4nvf4.block_scale.scale_vec::4X", sa + 4, sa + 8, sa + 12, sb + b_cols, sb + 2 * b_cols, sb + 3 * b_cols, idesc);
   }
 #undef B2C_F4_STAGE
