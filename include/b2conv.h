@@ -510,7 +510,8 @@ int b2c_fp4_matmul(const b2c_fp4_matmul_desc* desc, int64_t rows, const void* a_
  * w1_dev: [experts][2][inter][hidden / 2] bytes, gate then up, its scales [experts][2][inter] rows ld_w1_scale_bytes apart; w2_dev:
  * [experts][hidden][inter / 2], scales [experts][hidden] rows ld_w2_scale_bytes apart; matrices dense, all 16-byte aligned, distances multiples of
  * 16.  hidden and inter are multiples of 32.  The factors are fp32 on the device, one for x and h, [experts] for the weights; each may be
- * NULL (1), and is for B2C_MXFP4.  h is not rounded before it is quantised; the rows of the slots and their weighted sum are formed in
+ * NULL (1), and is for B2C_MXFP4.  h is not rounded before it is quantised (in fp32: a border
+ * between two results may be off by 3 * 2^-24 of itself, as h is by its sums' errors); the rows of the slots and their weighted sum are formed in
  * fp32, in the order of the slots, and rounded once.  ids outside 0..experts-1 add nothing.  workspace_dev: as there, of
  * b2c_fp4_experts_workspace_bytes bytes. */
 typedef struct {

@@ -166,5 +166,50 @@ __device__ __forceinline__ Scale4 scale_of(uint32_t amax, const Factor4& f, int 
 
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
+// The hidden rows of an expert layer are quantised from values that are off by the errors of their sums, so the 64 bits and residuals that
+// decide borders exactly have nothing to decide: scale and quotients are formed in fp32 (a border moves by 3 units of the last place).
+__device__ __forceinline__ float quick_inv_6g(const float* p, int format) {
+  if (p == nullptr || format != B2C_NVFP4) return 1.0f / 6.0f;
+  return __frcp_rn(6.0f * fminf(fmaxf(*p, 0x1p-100f), 0x1p100f));
+}
+__device__ __forceinline__ Scale4 quick_scale(uint32_t amax, float inv_6g, int format) {
+  if (format == B2C_MXFP4) return scale_mx(amax);
+  Scale4 s;
+  const bool fine = amax < kInfBits;
+  s.code = fine ? (uint32_t)__nv_cvt_float_to_fp8(__uint_as_float(amax) * inv_6g, __NV_SATFINITE, __NV_E4M3) : 0x7Fu;
+  const float t = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)s.code, __NV_E4M3)));
+  s.r = fine && s.code != 0 ? __fdividef(6.0f * inv_6g, t) : 0.0f;  // (inv_6g is 2^-103 to 2^98, t 2^-9 to 448)
+  s.step = s.lo = 0.0f;
+  return s;
+}
+template <int N>
+__device__ __forceinline__ void quick_quantise4(const Scale4& s, const float* x, uint32_t* q) {
+  float v[N];
+  const f32x2 r = pair_of(s.r, s.r);
+#pragma unroll
+  for (int i = 0; i < N; i += 2) unpair(mul2(pair_of(x[i], x[i + 1]), r), &v[i], &v[i + 1]);
+#pragma unroll
+  for (int i = 0; i < N / 8; ++i) q[i] = cvt_e2m1x8(v + 8 * i);
+  if constexpr (N == 4) q[0] = cvt_e2m1x4(v);
+  if (s.r == 0.0f) {
+#pragma unroll
+    for (int i = 0; i < (N + 7) / 8; ++i) q[i] = 0;
+  }
+}
+// The largest magnitude of three; NaN if one is.
+__device__ __forceinline__ float max_abs3(float a, float b, float c) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// silu as in the 8-bit layer, with e^-|v| as a power of two from one rounded product: it is off by |v| 2^-24 of itself more, and silu with it where v
+// is negative; v^2 e^-|v| 2^-24 is 0.6 units of 2^-24 at most.  Eight operations, two of them on the unit of 16 results a cycle.
+__device__ __forceinline__ float quick_silu(float v) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(v) * -1.44269504f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+  return (v < 0.0f ? v * e : v) * r;
+}
+
 }  // namespace
 }  // namespace b2c

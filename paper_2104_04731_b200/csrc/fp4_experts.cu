@@ -303,7 +303,9 @@ __global__ void __maxnreg__(80) experts4_up_kernel(const __grid_constant__ CUten
   pdl_wait();
   pdl_launch_dependents();
   Factor4 f = {};  // of what this warp quantises
-  if (warp >= 4) f = load_factor4(warp >= kQuantWarp0 ? a.x_global : a.h_global, a.format);
+  float inv_6g = 0.0f;
+  if (warp >= kQuantWarp0) f = load_factor4(a.x_global, a.format);
+  else if (warp >= 4) inv_6g = quick_inv_6g(a.h_global, a.format);
   plan_few(plan, reinterpret_cast<uint32_t*>(smem_raw + (smem - smem_u32(smem_raw))), a.ids, a.pairs, a.experts);
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = __shfl_sync(0xffffffffu, c.ctl.tmem_base, 0);
@@ -449,14 +451,14 @@ __global__ void __maxnreg__(80) experts4_up_kernel(const __grid_constant__ CUten
       for (int r = 2 * quad + (lane >> 4); r - (lane >> 4) < t.rows; r += 8) {
         float h[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = r < t.rows ? silu(sums[r][4 * l + i]) * sums[r][64 + 4 * l + i] : 0.0f;
+        for (int i = 0; i < 4; ++i) h[i] = r < t.rows ? quick_silu(sums[r][4 * l + i]) * sums[r][64 + 4 * l + i] : 0.0f;
         uint32_t mx = max(max(abs_bits(h[0]), abs_bits(h[1])), max(abs_bits(h[2]), abs_bits(h[3])));
         mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
         if (a.format == B2C_MXFP4) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-        const Scale4 s = scale_of(mx, f, a.format);
+        const Scale4 s = quick_scale(mx, inv_6g, a.format);
         uint32_t q;
-        quantise4<4>(s, f, a.format, h, &q);
+        quick_quantise4<4>(s, h, &q);
         if (ok && r < t.rows && n < a.inter) {  // (inter is a multiple of 32)
           const long long row = t.row0 + r;
           *reinterpret_cast<uint16_t*>(a.hq + row * (a.inter / 2) + n / 2) = (uint16_t)q;

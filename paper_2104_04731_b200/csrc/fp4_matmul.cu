@@ -252,8 +252,8 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, RowsShape<NT, WT>
     const int rows = min(NT, tile.row_end - row0);
     const int n = n0 + 4 * lane;
     const float alpha = alpha_of(a, group);
-    Factor4 f;
-    if constexpr (WT == 2) f = load_factor4(a.y_global, a.format);
+    float inv_6g = 0.0f;
+    if constexpr (WT == 2) inv_6g = quick_inv_6g(a.y_global, a.format);
     // (code that runs once or twice is paid for when it is fetched, not when it runs)
 #pragma unroll 1
     for (int j = rank + split * warp; j < rows; j += split * (S::kThreads / 32)) {
@@ -290,14 +290,14 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, RowsShape<NT, WT>
         }
       } else {
         // a block of 16 (32) columns is four (eight) neighbouring lanes
-        const float h[4] = {silu(v[0].x) * v[1].x, silu(v[0].y) * v[1].y, silu(v[0].z) * v[1].z, silu(v[0].w) * v[1].w};
+        const float h[4] = {quick_silu(v[0].x) * v[1].x, quick_silu(v[0].y) * v[1].y, quick_silu(v[0].z) * v[1].z, quick_silu(v[0].w) * v[1].w};
         uint32_t mx = max(max(abs_bits(h[0]), abs_bits(h[1])), max(abs_bits(h[2]), abs_bits(h[3])));
         mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
         if (a.format == B2C_MXFP4) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-        const Scale4 s = scale_of(mx, f, a.format);
+        const Scale4 s = quick_scale(mx, inv_6g, a.format);
         uint32_t q;
-        quantise4<4>(s, f, a.format, h, &q);
+        quick_quantise4<4>(s, h, &q);
         if (n < a.N) {  // (N is a multiple of 32)
           *reinterpret_cast<uint16_t*>((uint8_t*)a.y + row * a.ldy + n / 2) = (uint16_t)q;
           const int block = fp4_block(a.format);
@@ -373,8 +373,9 @@ int launch_rows_of(const Matmul4Args& a, cudaStream_t st) {
 }  // namespace
 
 int launch_fp4_matmul(const Matmul4Args& a, cudaStream_t st) {
-  const int rows = a.offsets ? (int)(((long long)a.rows + a.groups - 1) / a.groups) : a.rows;  // of a group, on average
-  if (rows > 128) return launch_fp4_matmul_pair(a, st);
+  int rows = a.offsets ? (int)(((long long)a.rows + a.groups - 1) / a.groups) : a.rows;  // of a group, on average
+  if (a.offsets) rows += rows / 2;
+  if (rows > (a.offsets ? 64 : 128)) return launch_fp4_matmul_pair(a, st);
   if (rows <= 16) return launch_rows_of<16>(a, st);
   if (rows <= 32) return launch_rows_of<32>(a, st);
   return launch_rows_of<64>(a, st);

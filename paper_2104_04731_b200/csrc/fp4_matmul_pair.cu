@@ -286,8 +286,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     const uint32_t leader_empty = CTAS == 2 ? map_to_rank(smem_u32(&ctl.tmem_empty[0]), 0u) : smem_u32(&ctl.tmem_empty[0]);
     const uint32_t taddr0 = tmem_acc + ((uint32_t)(quad * 32) << 16);
     const int in_tile = quad * 32 + lane;
-    Factor4 f;
-    if constexpr (GATED) f = load_factor4(a.y_global, a.format);
+    float inv_6g = 0.0f;
+    if constexpr (GATED) inv_6g = quick_inv_6g(a.y_global, a.format);
     int buf = 0;
     uint32_t bph = 0;
     bool ok = true;
@@ -316,20 +316,22 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       if constexpr (GATED) {
         const int n = p.nt * kTileM + half * 64;
 #pragma unroll
-        for (int i = 0; i < 64; ++i) v[i] = silu(v[i] * alpha) * (v[64 + i] * alpha);
+        for (int i = 0; i < 64; ++i) v[i] = quick_silu(v[i] * alpha) * (v[64 + i] * alpha);
         uint8_t* y = (uint8_t*)a.y + m * a.ldy + n / 2;
         const bool on = ok && m < p.row_end;
 #pragma unroll
         for (int c = 0; c < 64; c += 32) {
-          uint32_t mx[2] = {0, 0}, q[4];
+          float top[2] = {0.0f, 0.0f};
+          uint32_t q[4];
 #pragma unroll
-          for (int i = 0; i < 32; ++i) mx[i >> 4] = max(mx[i >> 4], abs_bits(v[c + i]));
+          for (int i = 0; i < 32; i += 2) top[i >> 4] = max_abs3(top[i >> 4], v[c + i], v[c + i + 1]);
+          uint32_t mx[2] = {abs_bits(top[0]), abs_bits(top[1])};
           if (a.format == B2C_MXFP4) mx[0] = mx[1] = max(mx[0], mx[1]);
           Scale4 s[2];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            s[i] = scale_of(mx[i], f, a.format);
-            quantise4<16>(s[i], f, a.format, v + c + 16 * i, q + 2 * i);
+            s[i] = quick_scale(mx[i], inv_6g, a.format);
+            quick_quantise4<16>(s[i], v + c + 16 * i, q + 2 * i);
           }
           if (on && n + c < a.N) {  // (N is a multiple of 32, ldy of 16)
             *reinterpret_cast<uint4*>(y + c / 2) = make_uint4(q[0], q[1], q[2], q[3]);

@@ -127,14 +127,16 @@ def experts(x, ids, weights, w1, s1, w2, s2, fmt, out_dtype, gx=1.0, g1=None, gh
         dg, du = ((sum_error(H) + 2.0 ** -23) * abs(f1) * (xq[token].abs() @ values(w1[e, j], s1[e, j], fmt).abs().t()) for j in (0, 1))
         sg = gate * torch.sigmoid(gate)
         h = sg * up
-        # |silu'| <= 1.1; the logistic function in fp32 is off by a few units (8 taken), the products by one each
-        dh = 1.1 * dg * up.abs() + (sg.abs() + 1.1 * dg) * du + 10 * 2.0 ** -24 * h.abs()
+        # |silu'| <= 1.1; the logistic function in fp32 is off by a few units (8 taken), the products by one each, and e^-|v| by |v| units more
+        # (of the exponent's rounding), which for a negative v is |v| units of silu
+        # itself; the quotients of the quantisation by 3 (step, its reciprocal, product)
+        dh = 1.1 * dg * up.abs() + (sg.abs() + 1.1 * dg) * du + (13 + 1.1 * gate.abs()) * 2.0 ** -24 * h.abs()
         amax, damax = block_amax(h, fmt), block_amax(dh, fmt)
         scale = scales_of(amax, fmt, gh)
         mid = rounded(h, scale, fmt, gh) * spread(scale, I, fmt) * gh
         dq = torch.zeros_like(mid)
         for u in (-1, 1):
-            other = scales_of((amax + u * damax).clamp_min(0.0), fmt, gh)
+            other = scales_of((amax + u * (damax + 3 * 2.0 ** -24 * amax)).clamp_min(0.0), fmt, gh)
             for s in (scale, other):
                 for d in (-1, 0, 1):
                     dq = torch.maximum(dq, (rounded(h + d * dh, s, fmt, gh) * spread(s, I, fmt) * gh - mid).abs())
