@@ -92,6 +92,7 @@ cudaError_t launch_fp4_quantize(const Quantize4Args& a, cudaStream_t st);
 cudaError_t launch_fp4_dequantize(const Dequantize4Args& a, cudaStream_t st);
 int launch_fp4_matmul(const Matmul4Args& a, cudaStream_t st);  // B2C_* code
 int launch_fp4_matmul_pair(const Matmul4Args& a, cudaStream_t st);  // its form for many rows
+long long fp4_pair_ns(const Matmul4Args& a);  // what it takes without groups, about
 cudaError_t fp4_pair_status(int* status);
 int launch_fp4_few_experts(const Few4Args& a, cudaStream_t st);
 cudaError_t fp4_few_status(int* status);

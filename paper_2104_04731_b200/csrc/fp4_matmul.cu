@@ -321,13 +321,14 @@ int fail(cudaError_t e) {
 // Measured, us with 1, 2, 3, 4, 6 blocks a tile:
 //   1 x 8192 x 8192 (64 tiles of 32 stages) 17.3, 13.1, 11.8, 11.3, 16.7;   37 x 5136 x 4128 (41 of 17) 10.1, 8.9, 8.3, 9.0, 8.9;
 //   16 x 4096 x 4096 (32 of 16) 10.3, 8.5, 7.5, 6.9, 7.2;   128 x 4096 x 4096 (64 of 16) 11.2, 9.7, 9.8, 9.3, 16.2.
-int choose_split(long long tiles, int kb_all, int per_sm, bool counted) {
+int choose_split(long long tiles, int kb_all, int per_sm, bool counted, double* stages = nullptr) {
   if (!counted && tiles >= kNumSMs) return 1;  // (a guess of the tiles says nothing about the last wave)
   int best = 1;
   double least = 0;
   for (int s = 1; s <= kMaxSplit && 2 * s <= std::max(2, kb_all); ++s) {
     const int per = (kb_all + s - 1) / s;
     if ((kb_all + per - 1) / per != s) continue;  // (no thread block without work)
+    if (s > 4 && tiles * s > kNumSMs) break;  // (300 x 1024 x 8192, 40 tiles: 15.2 us by seven)
     const long long blocks = tiles * s, waves = (blocks + kNumSMs * per_sm - 1) / (kNumSMs * per_sm);
     const double cost = (double)waves * per * (per_sm > 1 && blocks > kNumSMs ? 1.2 : 1.0) + (s > 1 ? 1.5 + s : 0.0);
     if (s == 1 || cost < least) {
@@ -335,6 +336,7 @@ int choose_split(long long tiles, int kb_all, int per_sm, bool counted) {
       least = cost;
     }
   }
+  if (stages != nullptr) *stages = least;
   return best;
 }
 
@@ -373,9 +375,21 @@ int launch_rows_of(const Matmul4Args& a, cudaStream_t st) {
 }  // namespace
 
 int launch_fp4_matmul(const Matmul4Args& a, cudaStream_t st) {
-  int rows = a.offsets ? (int)(((long long)a.rows + a.groups - 1) / a.groups) : a.rows;  // of a group, on average
-  if (a.offsets) rows += rows / 2;
-  if (rows > (a.offsets ? 64 : 128)) return launch_fp4_matmul_pair(a, st);
+  int rows = a.rows;
+  if (a.offsets) {
+    // half as many rows again as a group has on average: a second tile of a group reads its weights again (256 tokens, 4 of 64 experts, 16 rows
+    // a group: 89 us by tiles of 16, 74 of 32; 64 rows a group: 113 us by tiles of 64 here, 81 by those of 128 there)
+    rows = (int)(((long long)a.rows + a.groups - 1) / a.groups);
+    rows += rows / 2;
+    if (rows > 64) return launch_fp4_matmul_pair(a, st);
+  } else if (rows > 64) {
+    // 5.4 us and 0.3 for every stage that a block fetches: with few tiles and a long reduction the cut is worth more than larger tiles (us here and
+    // there: 128 x 2048 x 8192 8.8 and 12.3, 100 x 4096 x 4096 8.8 and 8.4)
+    const long long tiles = (long long)((a.N + kTileM - 1) / kTileM) * ((rows + 63) / 64);
+    double stages = 0;
+    choose_split(tiles, (a.K + kFp4Stage - 1) / kFp4Stage, RowsShape<64, 1>::kPerSm, true, &stages);
+    if (5400 + 300 * stages > (double)fp4_pair_ns(a)) return launch_fp4_matmul_pair(a, st);
+  }
   if (rows <= 16) return launch_rows_of<16>(a, st);
   if (rows <= 32) return launch_rows_of<32>(a, st);
   return launch_rows_of<64>(a, st);

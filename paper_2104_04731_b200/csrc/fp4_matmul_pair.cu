@@ -32,7 +32,7 @@ struct TileShape4 {
   static constexpr int kBBytes = kBRows * kStageRow;
   static constexpr int kColTiles = TN / kTileM;                      // of 128 columns
   static constexpr int kScaleBytes = (1 + kColTiles) * kGroupTile;   // of a group: the block's A rows, all B rows
-  static constexpr int kStages = CTAS == 1 ? 3 : (TN == 256 ? 5 : 7);
+  static constexpr int kStages = CTAS == 1 ? (TN == 256 ? 3 : 5) : (TN == 256 ? 5 : 7);
   static constexpr int kBufs = TN == 256 ? 1 : 2;  // accumulators in tensor memory, beside the scales of two stages
   static constexpr int kScaleCols = 16 * (1 + kColTiles);
   static constexpr int kWarpCols = TN / 2;  // accumulator columns of a warp of results
@@ -468,13 +468,29 @@ int launch_type(const Matmul4Args& a, cudaStream_t st) {
   return launch_pair<CTAS, TN, false, __nv_bfloat16>(a, st);
 }
 
+// Nanoseconds by tiles of 128 x 128 on one SM, and by those of 256 x 256 on a pair: the small ones where the large ones are fewer than the pairs.
+// Measured, us small / large: 384 x 4096 x 4096 9.3 / 11.6, 300 x 1024 x 8192 12.3 / 16.2, 1000 x 1024 x 1024 5.3 / 7.4,
+// 4096 x 512 x 4096 9.3 / 11.7;   768 x 4096 x 4096 14.1 / 12.6, 512 x 8192 x 8192 24.1 / 19.8, 2048 x 2048 x 2048 9.4 / 9.4.
+long long small_ns(const Matmul4Args& a) {
+  const long long tiles = (long long)((a.N + 127) / 128) * ((a.rows + 127) / 128), kb = (a.K + kFp4Stage - 1) / kFp4Stage;
+  const long long waves = (tiles + kNumSMs - 1) / kNumSMs;
+  return 4300 + waves * kb * (waves > 1 ? 300 : 250);
+}
+long long large_ns(const Matmul4Args& a) {
+  const long long tiles = (long long)((a.N + 255) / 256) * ((a.rows + 255) / 256), kb = (a.K + kFp4Stage - 1) / kFp4Stage;
+  return 5400 + (tiles + kNumSMs / 2 - 1) / (kNumSMs / 2) * (330 * kb + 700);
+}
+
 }  // namespace
+
+long long fp4_pair_ns(const Matmul4Args& a) { return std::min(small_ns(a), large_ns(a)); }
 
 int launch_fp4_matmul_pair(const Matmul4Args& a, cudaStream_t st) {
   const int rows = a.offsets ? (int)(((long long)a.rows + a.groups - 1) / a.groups) : a.rows;
+  // Half a tile of every group is empty: 64 rows of a tile of its own, 128 of a pair's.  At 240 rows of a group within 5 % either way.
   if (a.gated) return rows <= 768 ? launch_pair<1, 256, true, uint8_t>(a, st) : launch_pair<2, 256, true, uint8_t>(a, st);
   if (a.offsets) return rows <= 768 ? launch_type<1, 256>(a, st) : launch_type<2, 256>(a, st);
-  return launch_type<2, 256>(a, st);
+  return small_ns(a) < large_ns(a) ? launch_type<1, 128>(a, st) : launch_type<2, 256>(a, st);
 }
 
 cudaError_t fp4_pair_wait_selftest(cudaStream_t st) { return launch_wait_selftest(st); }
