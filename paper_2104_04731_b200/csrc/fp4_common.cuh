@@ -135,21 +135,19 @@ __device__ __forceinline__ void quantise4(const Scale4& s, const Factor4& f, int
       unpair(fma2_of(fma2_of(q0, neg, u), r, q0), &v[i], &v[i + 1]);
     }
   } else {
-    const f32x2 neg_lo = pair_of(-s.lo, -s.lo);
+    // t is the quotient rounded to four bits (Veltkamp's sum again); d, as large as it may be, goes through a saturating sum: 0, 1/2 or 1 by its
+    // sign.  All of it on the unit of the multiplications, which has twice the rate of that of comparisons.
+    const f32x2 neg_lo = pair_of(-s.lo, -s.lo), split = pair_of(1048577.0f, 1048577.0f), zero = pair_of(0.0f, 0.0f);
+    const float large = fminf(s.r * 0x1p40f, 0x1p127f);  // (d is 2^-33 steps at least, or 0)
 #pragma unroll
     for (int i = 0; i < N; i += 2) {
-      const f32x2 u = pair_of(x[i], x[i + 1]);
-      float t[2], d[2];
-      unpair(mul2(u, r), &t[0], &t[1]);
+      // (products as sums with 0: ptxas joins a packed product and the difference behind it to one operation, although both say .rn)
+      const f32x2 u = pair_of(x[i], x[i + 1]), q0 = fma2_of(u, r, zero), c = fma2_of(q0, split, zero), t = sub2(c, sub2(c, q0));
+      float tt[2], d[2];
+      unpair(t, &tt[0], &tt[1]);
+      unpair(fma2_of(t, neg_lo, fma2_of(t, neg, u)), &d[0], &d[1]);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) t[j] = __uint_as_float((__float_as_uint(t[j]) + 0x80000u) & 0xFFF00000u);
-      const f32x2 tt = pair_of(t[0], t[1]);
-      unpair(fma2_of(tt, neg_lo, fma2_of(tt, neg, u)), &d[0], &d[1]);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float side = __uint_as_float((__float_as_uint(d[j]) & 0x80000000u) | 0x3A800000u);  // +-2^-10
-        v[i + j] = d[j] == 0.0f ? t[j] : fmaf(fabsf(t[j]), side, t[j]);
-      }
+      for (int j = 0; j < 2; ++j) v[i + j] = fmaf(fabsf(tt[j]), fmaf(__saturatef(fmaf(d[j], large, 0.5f)), 0x1p-9f, -0x1p-10f), tt[j]);
     }
   }
 #pragma unroll

@@ -90,8 +90,29 @@ struct Walk {
   }
 };
 
-// Any rows: a warp has 32 runs, whose elements neighbouring lanes bring together (16 lanes a run) and exchange in shared memory; packed bytes
-// leave the same way.
+// 16 elements of a 16-bit type from any address: the words that hold them (each has at least one of them, so none is outside the tensor's
+// memory), shifted where the first begins inside one; zeros from element n on.
+template <typename T>
+__device__ __forceinline__ Raw16<T> load_run16(const T* p, int n) {
+  Raw16<T> r = {};
+  if (n <= 0) return r;
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)3);
+  const int odd = (int)(reinterpret_cast<uintptr_t>(p) >> 1) & 1, words = (min(n, kRun) + odd + 1) >> 1;
+  uint32_t u[9];
+#pragma unroll
+  for (int i = 0; i < 9; ++i) u[i] = i < words ? w[i] : 0u;
+  uint32_t* out = reinterpret_cast<uint32_t*>(&r);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    out[i] = __funnelshift_r(u[i], u[i + 1], 16 * odd);
+    const int left = n - 2 * i;
+    if (left < 2) out[i] &= left == 1 ? 0xFFFFu : 0u;
+  }
+  return r;
+}
+
+// Any rows.  fp32: a warp has 32 runs, whose elements neighbouring lanes bring together (16 lanes a run) and exchange in shared memory; 16-bit types:
+// a lane loads its own run in words.  Packed bytes go through shared memory to neighbouring lanes where rows of q do not lie on the grid.
 constexpr int kPitch = kRun + 1;
 template <typename T>
 __global__ void __launch_bounds__(kThreads) quantize4_any_kernel(const Quantize4Args a, const FastDiv per_row, const long long runs, const bool words) {
@@ -111,23 +132,30 @@ __global__ void __launch_bounds__(kThreads) quantize4_any_kernel(const Quantize4
   for (long long first = (long long)blockIdx.x * kThreads + (threadIdx.x & ~31u); first < runs; first += (long long)gridDim.x * kThreads) {
     long long row;
     int run;
-    place(first + (lane >> 4), &row, &run);
     float v[kRun];
-#pragma unroll
-    for (int i = 0; i < kRun; ++i) {
-      const int c = run * kRun + (lane & 15);
-      v[i] = row < a.rows && c < a.cols ? to_float<T>(((const T*)a.x)[row * a.ldx + c]) : 0.0f;
-      two.next(&row, &run);
-    }
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < kRun; ++i) mine[(2 * i + (lane >> 4)) * kPitch + (lane & 15)] = v[i];
-    __syncwarp();
     uint32_t m = 0;
+    if constexpr (sizeof(T) == 2) {
+      place(first + lane, &row, &run);
+      const Raw16<T> raw = load_run16<T>((const T*)a.x + row * a.ldx + run * kRun, row < a.rows ? a.cols - run * kRun : 0);
+      m = raw_amax(raw);
+      widen16<T>(raw, v);
+    } else {
+      place(first + (lane >> 4), &row, &run);
 #pragma unroll
-    for (int i = 0; i < kRun; ++i) {
-      v[i] = mine[lane * kPitch + i];
-      m = max(m, abs_bits(v[i]));
+      for (int i = 0; i < kRun; ++i) {
+        const int c = run * kRun + (lane & 15);
+        v[i] = row < a.rows && c < a.cols ? ((const float*)a.x)[row * a.ldx + c] : 0.0f;
+        two.next(&row, &run);
+      }
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) mine[(2 * i + (lane >> 4)) * kPitch + (lane & 15)] = v[i];
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) {
+        v[i] = mine[lane * kPitch + i];
+        m = max(m, abs_bits(v[i]));
+      }
     }
     if (a.format == B2C_MXFP4) m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
     const Scale4 s = scale_of(m, f, a.format);
@@ -199,8 +227,7 @@ __global__ void __launch_bounds__(kThreads) dequantize4_kernel(const Dequantize4
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         unpack2<__half>(h[j], &v[2 * j], &v[2 * j + 1]);
-        v[2 * j] = v[2 * j] * s * g;
-        v[2 * j + 1] = v[2 * j + 1] * s * g;
+        unpair(mul2(mul2(pair_of(v[2 * j], v[2 * j + 1]), pair_of(s, s)), pair_of(g, g)), &v[2 * j], &v[2 * j + 1]);
       }
       T* dst = (T*)a.y + (long long)row * a.ldy + 8 * run;
       if constexpr (sizeof(T) == 4) {
@@ -231,12 +258,12 @@ __global__ void __launch_bounds__(kThreads) dequantize4_any_kernel(const Dequant
     if (lo >= hi) continue;
     const uint8_t* q = a.q + row * a.ldq;
     const uint8_t* scale = a.scale + row * a.lds;
-    // the bytes of columns lo .. hi - 1, the first one's in the lowest
-    unsigned long long w = 0;
-#pragma unroll
-    for (int i = 0; i < 5; ++i)
-      if ((lo >> 1) + i <= (hi - 1) >> 1) w |= (unsigned long long)q[(lo >> 1) + i] << (8 * i);
-    const uint32_t nibbles = (uint32_t)(w >> (4 * (lo & 1)));
+    // the words that hold columns lo .. hi - 1 (each has at least one of them, so none is outside the tensor's memory)
+    const uint8_t* from = q + (lo >> 1);
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(from) & ~(uintptr_t)3);
+    const bool two = reinterpret_cast<uintptr_t>(q + ((hi - 1) >> 1)) >= reinterpret_cast<uintptr_t>(w + 1);
+    const uint32_t w0 = w[0], w1 = two ? w[1] : 0u;
+    const uint32_t nibbles = __funnelshift_r(w0, w1, (int)(reinterpret_cast<uintptr_t>(from) & 3) * 8 + 4 * (lo & 1));
     const float s0 = scale_value(scale[lo >> shift], a.format), s1 = scale_value(scale[(hi - 1) >> shift], a.format);
     uint32_t h[4];
     cvt_f16x8(nibbles, h);
