@@ -14,18 +14,27 @@ constexpr uint32_t kInfBits = 0x7F800000u;
 // The tensor's factor, and what is formed of it once a thread.
 struct Factor4 {
   float g;
-  bool few_bits;  // 17 at most: scale * g is exact in fp32, and so are its products with the borders between 4-bit values
-  double inv_6g;
+  bool few_bits;             // 17 at most: scale * g is exact in fp32, and so are its products with the borders between 4-bit values
+  float six, six_lo, inv_6;  // 6 g as the sum of two, and its reciprocal
 };
 __device__ __forceinline__ Factor4 load_factor4(const float* p, int format) {
-  Factor4 f = {1.0f, true, 1.0 / 6.0};
-  if (p != nullptr && format == B2C_NVFP4) {
-    f.g = fminf(fmaxf(*p, 0x1p-100f), 0x1p100f);
-    f.few_bits = (__float_as_uint(f.g) & 0x7Fu) == 0;
-    f.inv_6g = 1.0 / (6.0 * (double)f.g);
-  }
+  Factor4 f;
+  f.g = p != nullptr && format == B2C_NVFP4 ? fminf(fmaxf(*p, 0x1p-100f), 0x1p100f) : 1.0f;
+  f.few_bits = (__float_as_uint(f.g) & 0x7Fu) == 0;
+  f.six = 6.0f * f.g;
+  f.six_lo = fmaf(6.0f, f.g, -f.six);  // (26 bits in all: exact)
+  f.inv_6 = __frcp_rn(f.six);
   return f;
 }
+
+// A number on the same side as the quotient x / (hi + lo) of every border with few bits: t, which is the quotient q (good to some units) rounded to
+// BITS bits, as all borders are such numbers, moved by 2^-10 of itself (less than to the next one) to where x - t * (hi + lo) says.
+// x - t * hi is exact where it is small, and the rounding of the last sum keeps its sign.  `large` makes every d but 0 more than 1/2: d is 2^-33
+// of the divisor at least.  All of it on the unit of the multiplications, which has twice the rate of that of comparisons.
+__device__ __forceinline__ float side_of(float t, float d, float large) {
+  return fmaf(fabsf(t), fmaf(__saturatef(fmaf(d, large, 0.5f)), 0x1p-9f, -0x1p-10f), t);
+}
+__device__ __forceinline__ float large_of(float inverse) { return fminf(inverse * 0x1p40f, 0x1p127f); }
 
 // Scale of a block.  amax: bits of its largest magnitude (as whole numbers these are ordered as the magnitudes, and NaN is the largest).
 struct Scale4 {
@@ -44,24 +53,23 @@ __device__ __forceinline__ Scale4 scale_mx(uint32_t amax) {
   s.step = s.lo = 0.0f;
   return s;
 }
-// NV: the E4M3 value nearest to the real quotient amax / (6 g).  p is that quotient within 2^-52 of itself.  A border t between two E4M3
-// values has 5 bits, so t * 6 g has 31 at most, and amax, of 24, is that product or differs from it by 2^-31 or more of itself: rounded to 41
-// bits (the sum that does it is Veltkamp's: T. J. Dekker, A floating-point technique for extending the available precision, Numer. Math. 18,
-// 1971) p is on a border where the quotient is, and on its side of it elsewhere.  To fp32 it goes with its last bit set if anything was cut
-// off, which the rounding to four bits then sees.
+// NV: the E4M3 value nearest to the real quotient amax / (6 g).  A border between two E4M3 values has 5 bits (t is rounded to them by Veltkamp's
+// sum: T. J. Dekker, A floating-point technique for extending the available precision, Numer. Math. 18, 1971), so its product with 6 g has 31 at
+// most, and amax is that product or differs from it by 2^-31 or more of itself.
 __device__ __forceinline__ Scale4 scale_nv(uint32_t amax, const Factor4& f) {
   Scale4 s;
-  const double p = __dmul_rn((double)__uint_as_float(amax), f.inv_6g);
-  const double c = __dmul_rn(p, 4097.0);
-  const double hi = __dsub_rn(c, __dsub_rn(c, p));
-  float v = __double2float_rz(hi);
-  if ((double)v != hi) v = __uint_as_float(__float_as_uint(v) | 1u);
+  const float a = __uint_as_float(amax), p = fminf(a * f.inv_6, 512.0f);
+  const float c = __fmul_rn(p, 524289.0f), t = __fsub_rn(c, __fsub_rn(c, p));
+  const float v = side_of(t, fmaf(-t, f.six_lo, fmaf(-t, f.six, a)), large_of(f.inv_6));
   const bool fine = amax < kInfBits;
   s.code = fine ? (uint32_t)__nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3) : 0x7Fu;
-  const float t = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)s.code, __NV_E4M3)));
-  s.step = t * f.g;
-  s.lo = fmaf(t, f.g, -s.step);  // (28 bits in all: exact)
-  s.r = fine && s.code != 0 ? __frcp_rn(s.step) : 0.0f;
+  const float e = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)s.code, __NV_E4M3)));
+  s.step = e * f.g;
+  s.lo = fmaf(e, f.g, -s.step);  // (28 bits in all: exact)
+  float r;
+  if (f.few_bits) r = __frcp_rn(s.step);
+  else asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s.step));
+  s.r = fine && s.code != 0 ? r : 0.0f;
   return s;
 }
 __device__ __forceinline__ float scale_value(uint32_t code, int format) {
@@ -110,10 +118,8 @@ __device__ __forceinline__ void cvt_f16x8(uint32_t q, uint32_t* h) {
 //   NV, few_bits: the correctly rounded quotient by Markstein's residual step (see quantize2).  Every product of the step with a border t has 24
 // bits at most, so x is either that product, and the quotient t itself, or differs from it by a unit of x's last place, more than half a
 // unit of t's: the rounded quotient is on the same side.
-//   NV else: x times the rounded reciprocal says which number t of four bits the quotient is next to; all borders are such numbers.  On which side
-// of t it is says the sign of x - t * step: the step is hi + lo, x - t * hi is exact where it is small, and the rounding of the last
-// sum keeps its sign.  What is converted is t, moved to that side.  (Factors that come from a largest value of few bits put one number
-// in 200 within 2^-23 of a border: deciding these by comparisons in 64 bits made 16384 x 8192 take 217 us.)
+//   NV else: by side_of, with four bits.  (Factors that come from a largest value of few bits put one number in 200 within 2^-23 of a border:
+// deciding these by comparisons in 64 bits made 16384 x 8192 take 217 us.)
 //   A block whose scale is the largest one may be beyond it by any factor: eight steps round to the same value, and stay finite.
 template <int N>
 __device__ __forceinline__ void quantise4(const Scale4& s, const Factor4& f, int format, const float* in, uint32_t* q) {
@@ -135,10 +141,8 @@ __device__ __forceinline__ void quantise4(const Scale4& s, const Factor4& f, int
       unpair(fma2_of(fma2_of(q0, neg, u), r, q0), &v[i], &v[i + 1]);
     }
   } else {
-    // t is the quotient rounded to four bits (Veltkamp's sum again); d, as large as it may be, goes through a saturating sum: 0, 1/2 or 1 by its
-    // sign.  All of it on the unit of the multiplications, which has twice the rate of that of comparisons.
     const f32x2 neg_lo = pair_of(-s.lo, -s.lo), split = pair_of(1048577.0f, 1048577.0f), zero = pair_of(0.0f, 0.0f);
-    const float large = fminf(s.r * 0x1p40f, 0x1p127f);  // (d is 2^-33 steps at least, or 0)
+    const float large = large_of(s.r);
 #pragma unroll
     for (int i = 0; i < N; i += 2) {
       // (products as sums with 0: ptxas joins a packed product and the difference behind it to one operation, although both say .rn)
@@ -147,7 +151,7 @@ __device__ __forceinline__ void quantise4(const Scale4& s, const Factor4& f, int
       unpair(t, &tt[0], &tt[1]);
       unpair(fma2_of(t, neg_lo, fma2_of(t, neg, u)), &d[0], &d[1]);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) v[i + j] = fmaf(fabsf(tt[j]), fmaf(__saturatef(fmaf(d[j], large, 0.5f)), 0x1p-9f, -0x1p-10f), tt[j]);
+      for (int j = 0; j < 2; ++j) v[i + j] = side_of(tt[j], d[j], large);
     }
   }
 #pragma unroll

@@ -44,24 +44,49 @@ __device__ __forceinline__ void store_run(const Quantize4Args& a, long long row,
   }
 }
 
-// Rows on the grid of 16-byte loads and 8-byte stores, whole blocks of 32: a lane has 16 elements, and those of the next turn are under
-// way while these are converted.
-template <typename T>
+// 32 bytes at once, from a 32-byte boundary.
+__device__ __forceinline__ void load_8_words(const void* p, uint32_t* w) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+               : "l"(p)
+               : "memory");
+}
+__device__ __forceinline__ void store_8_words(void* p, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+
+// Rows on the grid of 32-byte loads and 8-byte stores, whole blocks of 32: a lane has 16 elements, and those of the next turn are under
+// way while these are converted.  FLAT: all rows follow each other without a gap, as one.  What bounds it are instructions as much as bytes.
+template <typename T, bool FLAT>
 __global__ void __launch_bounds__(kThreads) quantize4_kernel(const Quantize4Args a, const FastDiv per_row, const unsigned runs) {
   pdl_wait();
   pdl_launch_dependents();
   const Factor4 f = load_factor4(a.global, a.format);
   const unsigned step = gridDim.x * kThreads;
   unsigned id = blockIdx.x * kThreads + threadIdx.x;
+  struct Place {
+    unsigned row, run;
+  };
+  auto place = [&](unsigned i) {
+    if (FLAT) return Place{0u, i};
+    const unsigned row = per_row.div(i);
+    return Place{row, i - row * per_row.d};
+  };
   Raw16<T> next = {};
+  Place at = {0, 0}, at_next = {0, 0};
   auto fetch = [&](unsigned i) {
     if (i >= runs) return;
-    const unsigned row = per_row.div(i);
-    next = load_raw16<T>((const T*)a.x + (long long)row * a.ldx + (i - row * per_row.d) * kRun);
+    at_next = place(i);
+    const T* p = (const T*)a.x + (FLAT ? 0ll : (long long)at_next.row * a.ldx) + (long long)at_next.run * kRun;
+    uint32_t* w = reinterpret_cast<uint32_t*>(&next);
+    load_8_words(p, w);
+    if constexpr (sizeof(T) == 4) load_8_words(p + 8, w + 8);
   };
   fetch(id);
   for (unsigned first = blockIdx.x * kThreads; first < runs; first += step, id += step) {  // (the same for all lanes of a warp)
     const Raw16<T> raw = next;
+    at = at_next;
     fetch(id + step);
     uint32_t m = raw_amax(raw);
     if (a.format == B2C_MXFP4) m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));  // (runs are a multiple of two: a block's lanes both have some)
@@ -71,8 +96,13 @@ __global__ void __launch_bounds__(kThreads) quantize4_kernel(const Quantize4Args
     widen16<T>(raw, v);
     uint32_t q[2];
     quantise4<kRun>(s, f, a.format, v, q);
-    const unsigned row = per_row.div(id);
-    store_run(a, row, (int)(id - row * per_row.d), s, q);
+    if (FLAT) {
+      *reinterpret_cast<uint2*>(a.q + (long long)id * (kRun / 2)) = make_uint2(q[0], q[1]);
+      if (a.format == B2C_NVFP4) a.scale[id] = (uint8_t)s.code;
+      else if ((id & 1) == 0) a.scale[id >> 1] = (uint8_t)s.code;
+    } else {
+      store_run(a, at.row, (int)at.run, s, q);
+    }
   }
 }
 
@@ -194,48 +224,57 @@ __global__ void __launch_bounds__(kThreads) quantize4_any_kernel(const Quantize4
   }
 }
 
-// Eight values a lane, a 16-byte store of a 16-bit type.
-template <typename T>
+// 16 values a lane, stored 32 bytes at once; FLAT as above.
+template <typename T, bool FLAT>
 __global__ void __launch_bounds__(kThreads) dequantize4_kernel(const Dequantize4Args a, const FastDiv per_row, const unsigned runs) {
   pdl_wait();
   pdl_launch_dependents();
   const float g = a.global != nullptr ? *a.global : 1.0f;
-  const int shift = a.format == B2C_MXFP4 ? 2 : 1;  // runs of eight in a block
+  const int shift = a.format == B2C_MXFP4 ? 1 : 0;  // runs of 16 in a block
   constexpr int kAhead = 4;
   const unsigned step = gridDim.x * kThreads;
   for (unsigned id0 = blockIdx.x * kThreads + threadIdx.x; id0 < runs; id0 += kAhead * step) {
-    uint32_t q[kAhead], code[kAhead];
+    uint2 q[kAhead];
+    uint32_t code[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const unsigned id = id0 + i * step;
-      q[i] = code[i] = 0;
+      q[i] = make_uint2(0, 0);
+      code[i] = 0;
       if (id < runs && id >= id0) {
-        const unsigned row = per_row.div(id), run = id - row * per_row.d;
-        q[i] = *reinterpret_cast<const uint32_t*>(a.q + (long long)row * a.ldq + 4 * run);
-        code[i] = a.scale[(long long)row * a.lds + (run >> shift)];
+        const unsigned row = FLAT ? 0u : per_row.div(id), run = id - row * per_row.d;
+        q[i] = *reinterpret_cast<const uint2*>(a.q + (FLAT ? 0ll : (long long)row * a.ldq) + 8ll * run);
+        code[i] = a.scale[(FLAT ? 0ll : (long long)row * a.lds) + (run >> shift)];
       }
     }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const unsigned id = id0 + i * step;
       if (id >= runs || id < id0) continue;
-      const unsigned row = per_row.div(id), run = id - row * per_row.d;
+      const unsigned row = FLAT ? 0u : per_row.div(id), run = id - row * per_row.d;
       const float s = scale_value(code[i], a.format);
-      uint32_t h[4];
-      cvt_f16x8(q[i], h);
-      float v[8];
+      T* dst = (T*)a.y + (FLAT ? 0ll : (long long)row * a.ldy) + 16ll * run;
+      const uint32_t both[2] = {q[i].x, q[i].y};
+      uint32_t out[4 * sizeof(T)];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        unpack2<__half>(h[j], &v[2 * j], &v[2 * j + 1]);
-        unpair(mul2(mul2(pair_of(v[2 * j], v[2 * j + 1]), pair_of(s, s)), pair_of(g, g)), &v[2 * j], &v[2 * j + 1]);
+      for (int p = 0; p < 2; ++p) {
+        uint32_t h[4];
+        cvt_f16x8(both[p], h);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float lo, hi;
+          unpack2<__half>(h[j], &lo, &hi);
+          unpair(mul2(mul2(pair_of(lo, hi), pair_of(s, s)), pair_of(g, g)), &lo, &hi);
+          if constexpr (sizeof(T) == 4) {
+            out[8 * p + 2 * j] = __float_as_uint(lo);
+            out[8 * p + 2 * j + 1] = __float_as_uint(hi);
+          } else {
+            out[4 * p + j] = pack2<T>(lo, hi);
+          }
+        }
       }
-      T* dst = (T*)a.y + (long long)row * a.ldy + 8 * run;
-      if constexpr (sizeof(T) == 4) {
-        reinterpret_cast<float4*>(dst)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(dst)[1] = make_float4(v[4], v[5], v[6], v[7]);
-      } else {
-        *reinterpret_cast<uint4*>(dst) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
-      }
+      store_8_words(dst, out);
+      if constexpr (sizeof(T) == 4) store_8_words(dst + 8, out + 8);
     }
   }
 }
@@ -297,22 +336,29 @@ cudaError_t launch_quantize(const Quantize4Args& a, cudaStream_t st) {
   // (an MX row has an even number of runs, so that the two halves of a block are neighbours in a warp)
   const long long per_row = a.format == B2C_MXFP4 ? (a.cols + 31ll) / 32 * 2 : (a.cols + 15ll) / 16, runs = a.rows * per_row;
   const bool words = on_grid(a.q, a.ldq, a.map != nullptr ? 2 : a.rows, 8);
-  const bool wide = on_grid(a.x, a.ldx * (long long)sizeof(T), a.rows, 16) && words;
+  const bool wide = on_grid(a.x, a.ldx * (long long)sizeof(T), a.rows, 32) && words && a.cols % 32 == 0 && runs < (1ll << 30);
   const long long blocks = (runs + kThreads - 1) / kThreads;
   const FastDiv div = make_fastdiv((uint32_t)per_row);
-  // resident at once: 8 blocks of 256 threads an SM; all of them load one run ahead
-  if (wide && a.cols % 32 == 0 && runs < (1ll << 30))
-    return launch_pdl(quantize4_kernel<T>, dim3((unsigned)std::min<long long>(blocks, 8 * kNumSMs)), dim3(kThreads), 0, st, a, div, (unsigned)runs);
+  if (wide) {
+    const bool flat = a.map == nullptr && (a.rows <= 1 || (a.ldx == a.cols && 2 * a.ldq == a.cols && a.lds == fp4_scales(a.cols, a.format)));
+    // resident at once: 4 or 5 blocks of 256 threads an SM; each loads one run ahead
+    const dim3 grid((unsigned)std::min<long long>(blocks, 8 * kNumSMs));
+    return flat ? launch_pdl(quantize4_kernel<T, true>, grid, dim3(kThreads), 0, st, a, div, (unsigned)runs)
+                : launch_pdl(quantize4_kernel<T, false>, grid, dim3(kThreads), 0, st, a, div, (unsigned)runs);
+  }
   return launch_pdl(quantize4_any_kernel<T>, dim3((unsigned)std::min<long long>(blocks, 64 * kNumSMs)), dim3(kThreads), 0, st, a, div, runs, words);
 }
 
 template <typename T>
 cudaError_t launch_dequantize(const Dequantize4Args& a, cudaStream_t st) {
-  const bool wide = on_grid(a.y, a.ldy * (long long)sizeof(T), a.rows, 16) && on_grid(a.q, a.ldq, a.rows, 4);
-  if (wide && a.cols % 8 == 0 && a.rows * (a.cols / 8) < (1ll << 30)) {
-    const long long runs = a.rows * (a.cols / 8), blocks = (runs + kThreads - 1) / kThreads;
-    return launch_pdl(dequantize4_kernel<T>, dim3((unsigned)std::min<long long>(blocks, 8 * kNumSMs)), dim3(kThreads), 0, st, a,
-                      make_fastdiv((uint32_t)(a.cols / 8)), (unsigned)runs);
+  const bool wide = on_grid(a.y, a.ldy * (long long)sizeof(T), a.rows, 32) && on_grid(a.q, a.ldq, a.rows, 8);
+  if (wide && a.cols % 16 == 0 && a.rows * (a.cols / 16) < (1ll << 30)) {
+    const long long runs = a.rows * (a.cols / 16), blocks = (runs + kThreads - 1) / kThreads;
+    const bool flat = a.rows <= 1 || (a.ldy == a.cols && 2 * a.ldq == a.cols && a.lds * fp4_block(a.format) == a.cols);
+    const FastDiv div = make_fastdiv((uint32_t)(a.cols / 16));
+    const dim3 grid((unsigned)std::min<long long>(blocks, 8 * kNumSMs));
+    return flat ? launch_pdl(dequantize4_kernel<T, true>, grid, dim3(kThreads), 0, st, a, div, (unsigned)runs)
+                : launch_pdl(dequantize4_kernel<T, false>, grid, dim3(kThreads), 0, st, a, div, (unsigned)runs);
   }
   const long long per_row = (a.cols + 7ll + 7ll) / 8, runs = a.rows * per_row, blocks = (runs + kThreads - 1) / kThreads;  // (a row may begin inside a run)
   return launch_pdl(dequantize4_any_kernel<T>, dim3((unsigned)std::min<long long>(blocks, 64 * kNumSMs)), dim3(kThreads), 0, st, a,
