@@ -446,3 +446,269 @@ def test_experts_no_tokens(lib):
     w = layer(lib, 64, 32, 2, MX, 1)
     x = torch.zeros(0, 64, device="cuda")
     run_experts(lib, x, torch.zeros(0, 1, dtype=torch.int32, device="cuda"), torch.zeros(0, 1, device="cuda"), w, MX)
+
+
+def test_layer_from_route_and_its_parts(lib):
+    """Router, sort, quantisation, products of groups and weighted sum in a row, and the expert layer on the same route."""
+    T, E, K, H, I, fmt = 90, 16, 4, 256, 256, NV
+    w = layer(lib, H, I, E, fmt, 21)
+    w1, s1, f1, w2, s2, f2 = w
+    g = gen(22)
+    logits = torch.randn(T, E, generator=g, device="cuda")
+    weights, ids = torch.empty(T, K, device="cuda"), torch.empty(T, K, dtype=torch.int32, device="cuda")
+    lib.route(lib.make_route_desc(E, K, score=lib.SCORE_SIGMOID), logits, weights, ids)
+    x = torch.randn(T, H, generator=g, device="cuda").bfloat16()
+    gx, gh = factor(6 / 2688), factor(9 / 2688)
+    y = run_experts(lib, x, ids, weights, w, fmt, gx, gh)
+    check_experts(y, x, ids, weights, w, fmt, gx, gh)
+
+    offsets = torch.empty(E + 1, dtype=torch.int32, device="cuda")
+    rows, order = (torch.empty(T * K, dtype=torch.int32, device="cuda") for _ in range(2))
+    lib.route_sort(ids, E, offsets, rows, order, torch.empty(1 << 16, dtype=torch.uint8, device="cuda"))
+    xq, xs = lib.fp4_empty(T * K, H, fmt)
+    lib.fp4_quantize(x[order.long() // K], xq, xs, global_scale=gx)
+    gate_up = torch.empty(T * K, 2 * I, device="cuda")
+    both = s1.view(torch.uint8).reshape(E, 2 * I, -1)  # (a copy without gaps: rows of 16 scales)
+    lib.fp4_matmul(xq, xs, w1.reshape(E, 2 * I, -1), both.view(s1.dtype), gate_up, alpha=f1 * gx, offsets=offsets)
+    h = torch.nn.functional.silu(gate_up[:, :I]) * gate_up[:, I:]
+    hq, hs = lib.fp4_empty(T * K, I, fmt)
+    lib.fp4_quantize(h, hq, hs, global_scale=gh)
+    parts = torch.empty(T * K, H, device="cuda")
+    lib.fp4_matmul(hq, hs, w2, s2, parts, alpha=f2 * gh, offsets=offsets)
+    out = torch.empty_like(x)
+    lib.route_combine(parts, rows.reshape(T, K), weights, out)
+    check_experts(out, x, ids, weights, w, fmt, gx, gh)
+
+
+@FMT
+def test_linear_layer(lib, fmt):
+    """Weights and activations quantised and multiplied: as near to the product in 16 bits as 4 bits are."""
+    g = gen(23)
+    x, w = torch.randn(50, 1024, generator=g, device="cuda").bfloat16(), (torch.randn(300, 1024, generator=g, device="cuda") / 32).bfloat16()
+    fx, fw = (None, None) if fmt == MX else ((v.abs().amax().float() / 2688).reshape(1) for v in (x, w))
+    (xq, xs), (wq, ws) = lib.fp4_empty(50, 1024, fmt), lib.fp4_empty(300, 1024, fmt)
+    lib.fp4_quantize(x, xq, xs, global_scale=fx)
+    lib.fp4_quantize(w, wq, ws, global_scale=fw)
+    y = torch.empty(50, 300, device="cuda", dtype=torch.bfloat16)
+    lib.fp4_matmul(xq, xs, wq, ws, y, alpha=None if fmt == MX else fx * fw)
+    want = x.double() @ w.double().t()
+    # a value is off by a sixth of its block's largest at most (steps of a third of that, where nothing is beyond 6), NV by a sixteenth more
+    # (its scale's rounding); normal values have their block's largest at 2 to 3 standard deviations, most steps are smaller, and errors of different
+    # signs add up as the products do: a quarter of the size of the result covers two such operands
+    assert float((y.double() - want).norm() / want.norm()) < 0.25
+
+
+# ---- streams, graphs, sizes ------------------------------------------------------------------------------------------------------
+
+@FMT
+@pytest.mark.parametrize("rows", [3, 100, 400])
+def test_matmul_streams_and_graph(lib, rows, fmt):
+    """Two calls at once on two streams; a captured call replayed on new inputs."""
+    K, N = 1024, 500
+    sets = [(*operands(lib, rows, K, fmt, 30 + i), *operands(lib, N, K, fmt, 40 + i), torch.zeros(rows, N, device="cuda")) for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for st, (qa, sa, qb, sb, y) in zip(streams, sets):
+            lib.fp4_matmul(qa, sa, qb, sb, y, stream=st)
+    torch.cuda.synchronize()
+    for qa, sa, qb, sb, y in sets:
+        check_matmul(y, qa, sa, qb, sb, fmt)
+    qa, sa, qb, sb, y = sets[0]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lib.fp4_matmul(qa, sa, qb, sb, y)
+        lib.fp4_matmul(qa, sa, qb, sb, y)
+    qa.copy_(sets[1][0])
+    sa.view(torch.uint8).copy_(sets[1][1].view(torch.uint8))
+    y.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    check_matmul(y, qa, sa, qb, sb, fmt)
+    assert lib.fp4_status() == lib.OK
+
+
+@FMT
+def test_quantize_stream_and_graph(lib, fmt):
+    x = torch.randn(33, 512, generator=gen(31), device="cuda").bfloat16()
+    q, s = lib.fp4_empty(33, 512, fmt)
+    y = torch.empty_like(x)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    lib.fp4_quantize(x, q, s, stream=st)
+    lib.fp4_dequantize(q, s, y, stream=st)
+    torch.cuda.synchronize()
+    check_quantize(x, fmt, q, s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lib.fp4_quantize(x, q, s)
+        lib.fp4_dequantize(q, s, y)
+    x.copy_(torch.randn(33, 512, generator=gen(32), device="cuda"))
+    graph.replay()
+    torch.cuda.synchronize()
+    check_quantize(x, fmt, q, s)
+    assert bool((y.double() == ref.values(q, s, fmt, 512).to(y.dtype).double()).all())
+
+
+@FMT
+@pytest.mark.parametrize("tokens", [3, 60, 600])
+def test_experts_graph(lib, tokens, fmt):
+    """Two captured layers that share a workspace, replayed with other routes."""
+    E, K, H, I = 16, 2, 256, 128
+    x = torch.randn(tokens, H, generator=gen(33), device="cuda").bfloat16()
+    ws = torch.empty(lib.fp4_experts_workspace_bytes(H, I, E, K, tokens, fmt), dtype=torch.uint8, device="cuda")
+    ids, weights = routes(tokens, E, K, 34)
+    nets = [(layer(lib, H, I, E, fmt, 35 + i), torch.empty_like(x)) for i in range(2)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for (w1, s1, f1, w2, s2, f2), y in nets:
+            lib.fp4_experts(x, ids, weights, w1, s1, w2, s2, y, ws, w1_global=f1, w2_global=f2)
+    for seed in (1, 2):
+        i2, w2_ = routes(tokens, E, K, seed)
+        ids.copy_(i2)
+        weights.copy_(w2_)
+        for _ in range(2):
+            graph.replay()
+        torch.cuda.synchronize()
+        for w, y in nets:
+            check_experts(y, x, ids, weights, w, fmt)
+    assert lib.fp4_status() == lib.OK
+
+
+@pytest.mark.parametrize("tokens", [2, 40])
+def test_experts_two_streams(lib, tokens):
+    """Two layers at once, each with a workspace of its own, and a large product on a third stream."""
+    E, K, H, I, fmt = 16, 4, 512, 256, MX
+    nets = []
+    for i in range(2):
+        x = torch.randn(tokens, H, generator=gen(50 + i), device="cuda").bfloat16()
+        ws = torch.empty(lib.fp4_experts_workspace_bytes(H, I, E, K, tokens, fmt), dtype=torch.uint8, device="cuda")
+        nets.append((x, *routes(tokens, E, K, 52 + i), layer(lib, H, I, E, fmt, 54 + i), torch.empty_like(x), ws, torch.cuda.Stream()))
+    qa, sa = operands(lib, 2000, 2048, NV, 56)
+    qb, sb = operands(lib, 2000, 2048, NV, 57)
+    big, third = torch.empty(2000, 2000, device="cuda"), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        lib.fp4_matmul(qa, sa, qb, sb, big, stream=third)
+        for x, ids, weights, (w1, s1, f1, w2, s2, f2), y, ws, st in nets:
+            lib.fp4_experts(x, ids, weights, w1, s1, w2, s2, y, ws, stream=st)
+    torch.cuda.synchronize()
+    for x, ids, weights, w, y, ws, st in nets:
+        check_experts(y, x, ids, weights, w, fmt)
+    check_matmul(big, qa, sa, qb, sb, NV)
+    assert lib.fp4_status() == lib.OK
+
+
+@FMT
+@pytest.mark.parametrize("T,experts,topk", [(128, 64, 4), (129, 64, 4), (64, 8, 1), (65, 8, 1), (16, 1024, 32), (512, 1024, 1), (171, 700, 3)])
+def test_experts_at_the_border_of_few(lib, T, experts, topk, fmt):
+    """As many pairs as the two kernels for few tokens take, and one token more; very many experts."""
+    w = layer(lib, 64, 32, experts, fmt, T)
+    x = torch.randn(T, 64, generator=gen(T), device="cuda").half()
+    ids, weights = routes(T, experts, topk, T)
+    y = run_experts(lib, x, ids, weights, w, fmt, extra=256)
+    check_experts(y, x, ids, weights, w, fmt)
+
+
+def test_experts_strides(lib):
+    """Rows of x and y further apart and off the 16-byte grid; every other token of a larger batch."""
+    w = layer(lib, 160, 96, 6, NV, 60)
+    w1, s1, f1, w2, s2, f2 = w
+    for T in (3, 90):
+        base = torch.randn(2 * T, 167, generator=gen(61), device="cuda").bfloat16()
+        x = base[::2, 3:163]
+        ids, weights = routes(T, 6, 2, 62)
+        whole = torch.full((T, 171), 9.0, device="cuda", dtype=torch.bfloat16)
+        y = whole[:, 5:165]
+        ws = torch.empty(lib.fp4_experts_workspace_bytes(160, 96, 6, 2, T, NV), dtype=torch.uint8, device="cuda")
+        lib.fp4_experts(x, ids, weights, w1, s1, w2, s2, y, ws, w1_global=f1, w2_global=f2)
+        check_experts(y, x, ids, weights, w, NV)
+        assert bool((whole[:, :5] == 9.0).all()) and bool((whole[:, 165:] == 9.0).all())
+
+
+@pytest.mark.parametrize("T", [2, 200])
+def test_experts_nan(lib, T):
+    """A token with a NaN has a NaN everywhere (its block's scale has none), the others do not; an infinity likewise."""
+    w = layer(lib, 128, 64, 4, MX, 63)
+    x = torch.randn(T, 128, generator=gen(64), device="cuda")
+    x[T - 1, 5] = math.nan
+    if T > 2:
+        x[7, 100] = math.inf
+    ids, weights = routes(T, 4, 2, 65)
+    y = run_experts(lib, x, ids, weights, w, MX)
+    bad = torch.zeros(T, dtype=torch.bool, device="cuda")
+    bad[T - 1] = True
+    if T > 2:
+        bad[7] = True
+    assert bool((y.isnan().all(1) == bad).all()) and bool((y.isnan().any(1) == bad).all())
+
+
+@FMT
+def test_many_groups(lib, fmt):
+    """1024 groups of which a few have a row or two."""
+    G, N, K = 1024, 40, 96
+    count = torch.zeros(G, dtype=torch.long)
+    count[[0, 5, 511, 512, 1023]] = torch.tensor([1, 2, 1, 3, 2])
+    offsets = torch.nn.functional.pad(count.cumsum(0), (1, 0)).int().cuda()
+    rows = int(count.sum())
+    qa, sa = operands(lib, rows, K, fmt, 66)
+    qb, sb = operands(lib, N, K, fmt, 67, (G,))
+    y = torch.zeros(rows, N, device="cuda")
+    lib.fp4_matmul(qa, sa, qb, sb, y, offsets=offsets)
+    at = offsets.tolist()
+    for e in (0, 5, 511, 512, 1023):
+        check_matmul(y[at[e]:at[e + 1]], qa[at[e]:at[e + 1]], sa[at[e]:at[e + 1]], qb[e], sb[e], fmt)
+
+
+@FMT
+@pytest.mark.parametrize("rows", [1, 70, 260])
+def test_long_reduction(lib, rows, fmt):
+    qa, sa = operands(lib, rows, 40000, fmt, 68)
+    qb, sb = operands(lib, 130, 40000, fmt, 69)
+    y = torch.zeros(rows, 130, device="cuda")
+    lib.fp4_matmul(qa, sa, qb, sb, y)
+    check_matmul(y, qa, sa, qb, sb, fmt)
+
+
+@FMT
+@pytest.mark.parametrize("cols", [512, 333])
+def test_offsets_past_32_bits(lib, cols, fmt):
+    """Rows more than 2^31 elements and bytes apart."""
+    far = (1 << 31) + 96
+    x = torch.zeros(far + cols, dtype=torch.bfloat16, device="cuda").as_strided((2, cols), (far, 1))
+    x.copy_(torch.randn(2, cols, generator=gen(70), device="cuda"))
+    q = torch.zeros(far + cols, dtype=torch.uint8, device="cuda").as_strided((2, (cols + 1) // 2), (far, 1))
+    s = torch.zeros(far + cols, dtype=torch.uint8, device="cuda").as_strided((2, ref.nb(cols, fmt)), (far, 1)).view(ref.SCALE[fmt])
+    lib.fp4_quantize(x, q, s)
+    check_quantize(x, fmt, q, s)
+    y = torch.zeros(far + cols, dtype=torch.bfloat16, device="cuda").as_strided((2, cols), (far, 1))
+    lib.fp4_dequantize(q, s, y)
+    assert bool((y.double() == ref.values(q, s, fmt, cols).to(y.dtype).double()).all())
+    if cols == 512:
+        b, sb = operands(lib, 100, 512, fmt, 71)
+        out = torch.zeros(far + cols, dtype=torch.bfloat16, device="cuda").as_strided((2, 100), (far, 1))
+        lib.fp4_matmul(q, s, b, sb, out)
+        check_matmul(out, q, s, b, sb, fmt)
+
+
+def test_very_many_rows(lib):
+    """Very many short rows of an odd width."""
+    x = torch.randn(1 << 12, 33, generator=gen(72), device="cuda").bfloat16()
+    rows = 1 << 20
+    big = x.repeat(rows >> 12, 1)
+    q, s = torch.zeros(rows, 17, dtype=torch.uint8, device="cuda"), torch.zeros(rows, 3, dtype=torch.uint8, device="cuda").view(ref.SCALE[NV])
+    lib.fp4_quantize(big, q, s)
+    check_quantize(x, NV, q[-(1 << 12):], s[-(1 << 12):])
+    assert torch.equal(q[:1 << 12], q[-(1 << 12):]) and torch.equal(s.view(torch.uint8)[:1 << 12], s.view(torch.uint8)[-(1 << 12):])
+
+
+@pytest.mark.parametrize("form", [0, 1, 2])
+def test_bounded_wait(lib, form):
+    """A wait that cannot end gives up and is reported once; the device goes on."""
+    lib.selftest_fp4_wait(form)
+    assert lib.fp4_status() == lib.E_TIMEOUT
+    assert lib.fp4_status() == lib.OK
+    x = torch.ones(1, 32, device="cuda")
+    q, s = lib.fp4_empty(1, 32, lib.MXFP4)
+    lib.fp4_quantize(x, q, s)
+    check_quantize(x, MX, q, s)
