@@ -160,7 +160,9 @@ int b2c_fp4_experts(const b2c_fp4_experts_desc* d, int64_t tokens, const void* x
   cudaStream_t st = (cudaStream_t)cuda_stream;
   char* ws = (char*)workspace;
   const long long pairs = tokens * d->topk;
-  if (pairs <= kFewPairs && pairs <= 8ll * d->experts) {
+  // Two kernels where an expert has few rows (its tiles are 16 rows wide, and are quantised again for every tile of columns): us by them and by
+  // the five launches below, of 2048 x 1024, 4 of 64 experts: 1 token 13 and 18, 16 37 and 43, 64 57 and 58, 100 70 and 63.
+  if (pairs <= kFewPairs && pairs <= 4ll * d->experts) {
     Few4Args f = {};
     f.x = x;
     f.ldx = ldx;

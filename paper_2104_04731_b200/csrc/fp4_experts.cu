@@ -8,7 +8,7 @@
 //
 // First kernel: 64 gate rows and the 64 up rows of the same columns are one tile of weights.  Four warps quantise the rows of the tile as the
 // stages go by, into the place and order that the tensor core reads; every block of an expert does that again, beside its copies.
-// Second kernel: its blocks start beside those of the first, sort, and fetch weights until the rows are there.  A slot's row goes to
+// Second kernel: its blocks start where those of the first have ended, sort, and fetch weights until all rows are there.  A slot's row goes to
 // memory in fp32; the block that finishes the last tile of 128 columns sums them by token, in the order of the slots (no sum depends on who is
 // last).
 #include "fp4_mma.cuh"
@@ -18,14 +18,15 @@ namespace b2c {
 namespace {
 
 constexpr int kTileRows = 16;  // tokens of a tile
-constexpr int kStages4 = 4;
+constexpr int kStages4 = 8;
 constexpr int kWBytes = kTileM * kStageRow, kXBytes = kTileRows * kStageRow;
 constexpr int kFewStage = kWBytes + kXBytes;
 // Scales of 16 rows, turned round: a word of all rows takes 256 bytes, of which the copy to tensor memory reads the next 256 too (lanes of no row).
 constexpr int kRowWord = 16 * 16;
 constexpr int kRowStage = 1536, kRowGroup = 4608;  // of a stage (first kernel), of a group (second): words of it, and one more
 static_assert(4 * kRowWord + kRowWord <= kRowStage && 16 * kRowWord + kRowWord <= kRowGroup && kRowGroup % 512 == 0, "scales of rows");
-// stages, two groups of scales of the weights, scales of the rows (a block of either kernel stands beside one of the other on an SM)
+// Stages, two groups of scales of the weights, scales of the rows.  An SM has room for one block of either kernel.  (With half the stages a block of the
+// second stood beside one of the first and fetched weights ahead, but fewer bytes were under way: 32 tokens, 4 of 64 experts, 46 us instead of 43.)
 constexpr int kUpSmem = 1024 + kStages4 * kFewStage + 2 * kGroupTile + kStages4 * kRowStage;
 constexpr int kDownSmem = 1024 + kStages4 * kFewStage + 2 * kGroupTile + 2 * kRowGroup;
 constexpr int kMaxTiles = kFewPairs + kFewPairs / kTileRows;
@@ -286,9 +287,8 @@ __device__ __forceinline__ void widen8(const Raw8<T>& r, float* v) {
 }
 
 constexpr int kQuantWarp0 = 8, kQuantWarps = 2 * kStages4, kUpThreads = 32 * (kQuantWarp0 + kQuantWarps);
-// (80 registers a thread, so that a block of the second kernel, of 256 threads with up to 96, has room beside it)
 template <typename T>
-__global__ void __maxnreg__(80) experts4_up_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_ws, const Few4Args a) {
+__global__ void __launch_bounds__(kUpThreads, 1) experts4_up_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_ws, const Few4Args a) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ FewCtl c;
   __shared__ FewPlan plan;
@@ -475,6 +475,49 @@ __global__ void __maxnreg__(80) experts4_up_kernel(const __grid_constant__ CUten
 }
 
 constexpr int kDownThreads = 256;
+// The weighted sums of 128 columns, by four warps: a warp takes N tokens at a time, a lane four neighbouring columns.  All loads of S slots of
+// these tokens come first, so that their latency is waited for once (with 60 tokens of two slots, two tokens at a time took 6 us).
+template <typename T, int N, int S>
+__device__ __forceinline__ void sum_tokens(const Few4Args& a, const FewPlan& plan, int nt, int quad, int lane) {
+  const int tokens = a.pairs / a.topk, col = nt * kTileM + 4 * lane;
+  const bool on = col < a.hidden;  // (hidden is a multiple of 32)
+  T* y = (T*)a.y + col;
+#pragma unroll 1
+  for (int t0 = N * quad; t0 < tokens; t0 += 4 * N) {
+    float4 sum[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 1
+    for (int j0 = 0; j0 < a.topk; j0 += S) {
+      float4 part[N][S];
+      float w[N][S];
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < S; ++j) {
+          const int p = (t0 + i) * a.topk + j0 + j;
+          const int at = t0 + i < tokens && j0 + j < a.topk ? plan.place[p] : -1;
+          part[i][j] = at >= 0 && on ? __ldcg(reinterpret_cast<const float4*>(a.part + (long long)at * a.hidden + col)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          w[i][j] = at >= 0 ? a.weights[p] : 0.0f;
+        }
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < S; ++j) {
+          sum[i].x = fmaf(w[i][j], part[i][j].x, sum[i].x);
+          sum[i].y = fmaf(w[i][j], part[i][j].y, sum[i].y);
+          sum[i].z = fmaf(w[i][j], part[i][j].z, sum[i].z);
+          sum[i].w = fmaf(w[i][j], part[i][j].w, sum[i].w);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float out[4] = {sum[i].x, sum[i].y, sum[i].z, sum[i].w};
+      if (t0 + i < tokens && on) store4<T>(y + (t0 + i) * a.ldy, out, 4);
+    }
+  }
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kDownThreads, 1)
     experts4_down_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_ws, const __grid_constant__ CUtensorMap tmap_x,
@@ -614,42 +657,13 @@ __global__ void __launch_bounds__(kDownThreads, 1)
       asm volatile("bar.sync 1, 128;" ::: "memory");
       if (last) {
         __threadfence();
-        // a warp takes two tokens, a lane four neighbouring columns; loads of four slots of both at a time, so that their latency is
-        // waited for once
-        const int tokens = a.pairs / a.topk, col = nt * cols + 4 * lane;
-        const bool on = col < a.hidden;  // (hidden is a multiple of 32)
-        for (int t0 = 2 * quad; t0 < tokens; t0 += 8) {
-          float4 sum[2];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) sum[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          for (int j0 = 0; j0 < a.topk; j0 += 4) {
-            float4 part[2][4];
-            float w[2][4];
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const int p = (t0 + i) * a.topk + j0 + j;
-                const int at = t0 + i < tokens && j0 + j < a.topk ? plan.place[p] : -1;
-                part[i][j] = at >= 0 && on ? __ldcg(reinterpret_cast<const float4*>(a.part + (long long)at * a.hidden + col)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                w[i][j] = at >= 0 ? a.weights[p] : 0.0f;
-              }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                sum[i].x = fmaf(w[i][j], part[i][j].x, sum[i].x);
-                sum[i].y = fmaf(w[i][j], part[i][j].y, sum[i].y);
-                sum[i].z = fmaf(w[i][j], part[i][j].z, sum[i].z);
-                sum[i].w = fmaf(w[i][j], part[i][j].w, sum[i].w);
-              }
-          }
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float out[4] = {sum[i].x, sum[i].y, sum[i].z, sum[i].w};
-            if (t0 + i < tokens && on) store4<T>(y + (t0 + i) * a.ldy + col, out, 4);
-          }
-        }
+        // (a token or two a warp by short code: fetching that of 16 loads costs a microsecond)
+        const int tokens = a.pairs / a.topk;
+        if (tokens <= 4) sum_tokens<T, 1, 4>(a, plan, nt, quad, lane);
+        else if (tokens <= 8) sum_tokens<T, 2, 4>(a, plan, nt, quad, lane);
+        else if (a.topk == 1) sum_tokens<T, 16, 1>(a, plan, nt, quad, lane);
+        else if (a.topk == 2) sum_tokens<T, 8, 2>(a, plan, nt, quad, lane);
+        else sum_tokens<T, 4, 4>(a, plan, nt, quad, lane);
       }
     }
     __syncwarp();

@@ -600,7 +600,7 @@ def test_experts_two_streams(lib, tokens):
 
 
 @FMT
-@pytest.mark.parametrize("T,experts,topk", [(128, 64, 4), (129, 64, 4), (64, 8, 1), (65, 8, 1), (16, 1024, 32), (512, 1024, 1), (171, 700, 3)])
+@pytest.mark.parametrize("T,experts,topk", [(64, 64, 4), (65, 64, 4), (128, 64, 4), (129, 64, 4), (32, 8, 1), (33, 8, 1), (16, 1024, 32), (512, 1024, 1), (171, 700, 3)])
 def test_experts_at_the_border_of_few(lib, T, experts, topk, fmt):
     """As many pairs as the two kernels for few tokens take, and one token more; very many experts."""
     w = layer(lib, 64, 32, experts, fmt, T)
