@@ -160,22 +160,54 @@ __global__ void __launch_bounds__(kThreads) quantize4_any_kernel(const Quantize4
     *run = (int)(id - *row * n);
   };
   for (long long first = (long long)blockIdx.x * kThreads + (threadIdx.x & ~31u); first < runs; first += (long long)gridDim.x * kThreads) {
-    long long row;
-    int run;
+    long long row0, row;
+    int run0, run;
+    place(first, &row0, &run0);
+    const bool whole = (run0 + 32) * kRun <= a.cols;  // all of one row, and whole
     float v[kRun];
     uint32_t m = 0;
     if constexpr (sizeof(T) == 2) {
-      place(first + lane, &row, &run);
-      const Raw16<T> raw = load_run16<T>((const T*)a.x + row * a.ldx + run * kRun, row < a.rows ? a.cols - run * kRun : 0);
+      Raw16<T> raw;
+      if (whole) {  // the words that hold the 512 elements, a lane's eight or nine of them in turn
+        const T* p = (const T*)a.x + row0 * a.ldx + run0 * kRun;
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)3);
+        const int odd = (int)(reinterpret_cast<uintptr_t>(p) >> 1) & 1;
+        uint32_t* words4 = reinterpret_cast<uint32_t*>(mine);
+        uint32_t u[9];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = w[32 * i + lane];
+        u[8] = odd && lane == 0 ? w[256] : 0u;
+        __syncwarp();
+        // (a word more for every eight, so that lanes eight words apart meet in different banks)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) words4[(32 * i + lane) + (32 * i + lane) / 8] = u[i];
+        if (lane == 0) words4[256 + 32] = u[8];
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 9; ++i) u[i] = words4[9 * lane + i + i / 8];
+        uint32_t* out = reinterpret_cast<uint32_t*>(&raw);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[i] = __funnelshift_r(u[i], u[i + 1], 16 * odd);
+        __syncwarp();
+      } else {
+        place(first + lane, &row, &run);
+        raw = load_run16<T>((const T*)a.x + row * a.ldx + run * kRun, row < a.rows ? a.cols - run * kRun : 0);
+      }
       m = raw_amax(raw);
       widen16<T>(raw, v);
     } else {
-      place(first + (lane >> 4), &row, &run);
+      if (whole) {
+        const float* p = (const float*)a.x + row0 * a.ldx + run0 * kRun + lane;
 #pragma unroll
-      for (int i = 0; i < kRun; ++i) {
-        const int c = run * kRun + (lane & 15);
-        v[i] = row < a.rows && c < a.cols ? ((const float*)a.x)[row * a.ldx + c] : 0.0f;
-        two.next(&row, &run);
+        for (int i = 0; i < kRun; ++i) v[i] = p[32 * i];
+      } else {
+        place(first + (lane >> 4), &row, &run);
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
+          const int c = run * kRun + (lane & 15);
+          v[i] = row < a.rows && c < a.cols ? ((const float*)a.x)[row * a.ldx + c] : 0.0f;
+          two.next(&row, &run);
+        }
       }
       __syncwarp();
 #pragma unroll
@@ -191,7 +223,9 @@ __global__ void __launch_bounds__(kThreads) quantize4_any_kernel(const Quantize4
     const Scale4 s = scale_of(m, f, a.format);
     uint32_t q[2];
     quantise4<kRun>(s, f, a.format, v, q);
-    place(first + lane, &row, &run);
+    row = row0;
+    run = run0 + lane;
+    if (!whole) place(first + lane, &row, &run);
     const bool on = row < a.rows && run * kRun < a.cols, scales = on && (a.format == B2C_NVFP4 || (run & 1) == 0);
     const int at = a.format == B2C_NVFP4 ? run : run >> 1;
     if (a.map == nullptr) {
@@ -204,6 +238,13 @@ __global__ void __launch_bounds__(kThreads) quantize4_any_kernel(const Quantize4
         __syncwarp();
         *reinterpret_cast<uint2*>(bytes + 8 * lane) = make_uint2(q[0], q[1]);
         __syncwarp();
+        if (whole) {
+          uint8_t* d = a.q + row0 * a.ldq + run0 * (kRun / 2) + lane;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) d[32 * i] = bytes[32 * i + lane];
+          __syncwarp();
+          continue;
+        }
         place(first + (lane >> 3), &row, &run);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -309,8 +350,10 @@ __global__ void __launch_bounds__(kThreads) dequantize4_any_kernel(const Dequant
     float v[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) unpack2<__half>(h[i], &v[2 * i], &v[2 * i + 1]);
+    const int first = (((lo >> shift) + 1) << shift) - lo;  // columns of the block that the run begins in
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = v[i] * ((lo + i) >> shift == lo >> shift ? s0 : s1) * g;
+    for (int i = 0; i < 8; i += 2)
+      unpair(mul2(mul2(pair_of(v[i], v[i + 1]), pair_of(i < first ? s0 : s1, i + 1 < first ? s0 : s1)), pair_of(g, g)), &v[i], &v[i + 1]);
     if (hi - lo == 8) {
       T* dst = y + lo;
       if constexpr (sizeof(T) == 4) {
@@ -346,7 +389,8 @@ cudaError_t launch_quantize(const Quantize4Args& a, cudaStream_t st) {
     return flat ? launch_pdl(quantize4_kernel<T, true>, grid, dim3(kThreads), 0, st, a, div, (unsigned)runs)
                 : launch_pdl(quantize4_kernel<T, false>, grid, dim3(kThreads), 0, st, a, div, (unsigned)runs);
   }
-  return launch_pdl(quantize4_any_kernel<T>, dim3((unsigned)std::min<long long>(blocks, 64 * kNumSMs)), dim3(kThreads), 0, st, a, div, runs, words);
+  // (as many blocks as are resident: what a thread does before its first run is as much as a run)
+  return launch_pdl(quantize4_any_kernel<T>, dim3((unsigned)std::min<long long>(blocks, 8 * kNumSMs)), dim3(kThreads), 0, st, a, div, runs, words);
 }
 
 template <typename T>
@@ -361,6 +405,7 @@ cudaError_t launch_dequantize(const Dequantize4Args& a, cudaStream_t st) {
                 : launch_pdl(dequantize4_kernel<T, false>, grid, dim3(kThreads), 0, st, a, div, (unsigned)runs);
   }
   const long long per_row = (a.cols + 7ll + 7ll) / 8, runs = a.rows * per_row, blocks = (runs + kThreads - 1) / kThreads;  // (a row may begin inside a run)
+  // (more blocks than are resident: new ones hide the latency of a run's loads, 16384 x 8191 bf16 105 us instead of 125)
   return launch_pdl(dequantize4_any_kernel<T>, dim3((unsigned)std::min<long long>(blocks, 64 * kNumSMs)), dim3(kThreads), 0, st, a,
                     make_fastdiv((uint32_t)per_row), runs);
 }
