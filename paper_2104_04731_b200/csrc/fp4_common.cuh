@@ -115,7 +115,7 @@ __device__ __forceinline__ void cvt_f16x8(uint32_t q, uint32_t* h) {
 
 // N (4, 8 or 16) values of one block to 4 bits each, as if x / (scale * g) had been rounded as a real number.
 //   MX: multiplication by a power of two.
-//   NV, few_bits: the correctly rounded quotient by Markstein's residual step (see quantize2).  Every product of the step with a border t has 24
+//   NV, few_bits: the correctly rounded quotient by Markstein's residual step (as in quantize2 of the 8-bit operators).  Every product of the step with a border t has 24
 // bits at most, so x is either that product, and the quotient t itself, or differs from it by a unit of x's last place, more than half a
 // unit of t's: the rounded quotient is on the same side.
 //   NV else: by side_of, with four bits.  (Factors that come from a largest value of few bits put one number in 200 within 2^-23 of a border:
@@ -168,8 +168,8 @@ __device__ __forceinline__ Scale4 scale_of(uint32_t amax, const Factor4& f, int 
 
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
-// The hidden rows of an expert layer are quantised from values that are off by the errors of their sums, so the 64 bits and residuals that
-// decide borders exactly have nothing to decide: scale and quotients are formed in fp32 (a border moves by 3 units of the last place).
+// The hidden rows of an expert layer are quantised from values that are off by the errors of their sums, so the residuals that decide
+// borders exactly have nothing to decide: scale and quotients are formed in fp32 (a border moves by 3 units of the last place).
 __device__ __forceinline__ float quick_inv_6g(const float* p, int format) {
   if (p == nullptr || format != B2C_NVFP4) return 1.0f / 6.0f;
   return __frcp_rn(6.0f * fminf(fmaxf(*p, 0x1p-100f), 0x1p100f));

@@ -6,11 +6,14 @@
 // block an SM walks over the items (up to 16 rows of an expert, 128 weight rows), and the copies of weights run ahead over the items' ends.
 // The weights are on the accumulator's rows, the tokens are its columns.
 //
-// First kernel: 64 gate rows and the 64 up rows of the same columns are one tile of weights.  Four warps quantise the rows of the tile as the
+// First kernel: 64 gate rows and the 64 up rows of the same columns are one tile of weights.  Eight warps quantise the rows of the tile as the
 // stages go by, into the place and order that the tensor core reads; every block of an expert does that again, beside its copies.
 // Second kernel: its blocks start where those of the first have ended, sort, and fetch weights until all rows are there.  A slot's row goes to
 // memory in fp32; the block that finishes the last tile of 128 columns sums them by token, in the order of the slots (no sum depends on who is
 // last).
+//
+// 2048 x 1024, 4 of 64 experts: 16 tokens NV 37 us (145 MB; 22.5 at the rate of a copy), one token MX 13: of these 13 some 1.5 us are the plan, 2 the way
+// of the first weights and rows, 2 the MMAs of eight stages, each kernel.
 #include "fp4_mma.cuh"
 
 namespace b2c {

@@ -1,11 +1,12 @@
 // Products of 4-bit matrices on the tensor core: the kernel for few rows, and the choice between the two.
 //
 // With few rows the weights are the bytes, and the tensor core's 128 accumulator rows are given to them (the axes are swapped): a
-// thread block owns 128 weight rows and 16 to 128 activation rows.  What bounds it is how many bytes are in flight: the reduction is cut over
-// the blocks of a cluster until all SMs have a share, and the partial sums meet in distributed shared memory, in a fixed order.
+// thread block owns 128 weight rows and 16, 32 or 64 activation rows.  What bounds it is the way from the launch to the first sums and how many bytes
+// are in flight: the reduction is cut over the blocks of a cluster until all SMs have a share, and the partial sums meet in distributed shared
+// memory, in a fixed order.  1 x 8192 x 8192 NV: 10.8 us, 3.5 TB/s (37.8 MB; 5.9 at the rate of a copy);  37 x 5136 x 4128: 7.9.
 //
-// Roles: warp 0 copies (TMA), warp 1 carries the scales to tensor memory and issues the MMAs, the others turn the scales round (see
-// fp4_mma.cuh) and take the sums out of tensor memory when all stages have been added there.
+// Roles: warp 0 copies (TMA), warp 1 carries the scales to tensor memory and issues the MMAs, the others copy the scales and turn them round (a
+// warp an operand, see fp4_mma.cuh) and take the sums out of tensor memory when all stages have been added there.
 #include "fp4_mma.cuh"
 
 namespace b2c {

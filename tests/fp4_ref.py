@@ -127,9 +127,9 @@ def experts(x, ids, weights, w1, s1, w2, s2, fmt, out_dtype, gx=1.0, g1=None, gh
         dg, du = ((sum_error(H) + 2.0 ** -23) * abs(f1) * (xq[token].abs() @ values(w1[e, j], s1[e, j], fmt).abs().t()) for j in (0, 1))
         sg = gate * torch.sigmoid(gate)
         h = sg * up
-        # |silu'| <= 1.1; the logistic function in fp32 is off by a few units (8 taken), the products by one each, and e^-|v| by |v| units more
-        # (of the exponent's rounding), which for a negative v is |v| units of silu
-        # itself; the quotients of the quantisation by 3 (step, its reciprocal, product)
+        # |silu'| <= 1.1.  In units of 2^-24 of h: 8 for the logistic function (its power, sum, reciprocal), 2 for the products with it and with
+        # up, 3 for the quotient of the quantisation (step, its reciprocal, product); and 1.1 |gate| for the rounded exponent of e^-|gate|, which
+        # is a relative error of that power and for negative gates of silu itself
         dh = 1.1 * dg * up.abs() + (sg.abs() + 1.1 * dg) * du + (13 + 1.1 * gate.abs()) * 2.0 ** -24 * h.abs()
         amax, damax = block_amax(h, fmt), block_amax(dh, fmt)
         scale = scales_of(amax, fmt, gh)
