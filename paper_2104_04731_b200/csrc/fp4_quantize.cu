@@ -3,7 +3,7 @@
 //
 // 16384 x 8192 bf16 to NV and back 129 us, 688 MB, 5.3 TB/s (106 at the rate of a copy): the way back moves its bytes at nearly that rate (8192 x
 // 8192 32 us, 172 MB), the way there is bound by instructions, some 14 for every element, half of them for the exact side of the borders.
-// Rows off the 16-byte grid: 8203 x 5137 fp32 and back 84 us (59), 16384 x 8191 bf16 and back 215 (106).
+// Rows off the 16-byte grid: 8203 x 5137 fp32 and back 81 us (59), 16384 x 8191 bf16 and back 198 (106).
 #include "fp4_common.cuh"
 
 namespace b2c {
@@ -242,10 +242,16 @@ __global__ void __launch_bounds__(kThreads) quantize4_any_kernel(const Quantize4
         __syncwarp();
         *reinterpret_cast<uint2*>(bytes + 8 * lane) = make_uint2(q[0], q[1]);
         __syncwarp();
-        if (whole) {
-          uint8_t* d = a.q + row0 * a.ldq + run0 * (kRun / 2) + lane;
+        if (whole) {  // 256 bytes: words on their grid, shifted together, and up to three bytes before and behind them
+          uint8_t* d = a.q + row0 * a.ldq + run0 * (kRun / 2);
+          const int head = (int)(-reinterpret_cast<uintptr_t>(d) & 3), inner = head == 0 ? 64 : 63;
+          const uint32_t* from = reinterpret_cast<const uint32_t*>(mine);
+          uint32_t* to = reinterpret_cast<uint32_t*>(d + head);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) d[32 * i] = bytes[32 * i + lane];
+          for (int i = 0; i < 64; i += 32)
+            if (i + lane < inner) to[i + lane] = __funnelshift_r(from[i + lane], from[i + lane + 1], 8 * head);
+          const int at = lane < head ? lane : 252 + lane;  // (the four lanes of either end)
+          if (head != 0 && lane < 4) d[at] = bytes[at];
           __syncwarp();
           continue;
         }
@@ -324,51 +330,60 @@ __global__ void __launch_bounds__(kThreads) dequantize4_kernel(const Dequantize4
   }
 }
 
-// Any rows: eight columns a lane that begin on the 16-byte grid of y, where that is (the first and the last of a row are not whole), so that
-// stores are wide; their 4-bit values begin at any nibble of q.
+// Any rows: 32 bytes of y a lane that begin on the 32-byte grid, where that is (the first and the last of a row are not whole), so that a
+// store is whole sectors; their 4-bit values begin at any nibble of q.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) dequantize4_any_kernel(const Dequantize4Args a, const FastDiv per_row, const long long runs) {
   pdl_wait();
   pdl_launch_dependents();
+  constexpr int E = 32 / (int)sizeof(T);  // columns: 8 or 16, of two blocks at most
   const float g = a.global != nullptr ? *a.global : 1.0f;
   const int shift = a.format == B2C_MXFP4 ? 5 : 4, n = (int)per_row.d;
   const long long step = (long long)gridDim.x * kThreads;
   for (long long id = (long long)blockIdx.x * kThreads + threadIdx.x; id < runs; id += step) {
     const long long row = id < (1ll << 31) ? (long long)per_row.div((uint32_t)id) : id / n;
     T* y = (T*)a.y + row * a.ldy;
-    const int behind = (int)((reinterpret_cast<uintptr_t>(y) & 15) / sizeof(T));  // columns that the row begins behind the grid
-    const int c0 = (int)(id - row * n) * 8 - (behind & 7);
-    const int lo = max(c0, 0), hi = min(c0 + 8, a.cols);
+    const int behind = (int)((reinterpret_cast<uintptr_t>(y) & 31) / sizeof(T));  // columns that the row begins behind the grid
+    const int c0 = (int)(id - row * n) * E - behind;
+    const int lo = max(c0, 0), hi = min(c0 + E, a.cols);
     if (lo >= hi) continue;
     const uint8_t* q = a.q + row * a.ldq;
     const uint8_t* scale = a.scale + row * a.lds;
     // the words that hold columns lo .. hi - 1 (each has at least one of them, so none is outside the tensor's memory)
     const uint8_t* from = q + (lo >> 1);
     const uint32_t* w = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(from) & ~(uintptr_t)3);
-    const bool two = reinterpret_cast<uintptr_t>(q + ((hi - 1) >> 1)) >= reinterpret_cast<uintptr_t>(w + 1);
-    const uint32_t w0 = w[0], w1 = two ? w[1] : 0u;
-    const uint32_t nibbles = __funnelshift_r(w0, w1, (int)(reinterpret_cast<uintptr_t>(from) & 3) * 8 + 4 * (lo & 1));
-    const float s0 = scale_value(scale[lo >> shift], a.format), s1 = scale_value(scale[(hi - 1) >> shift], a.format);
-    uint32_t h[4];
-    cvt_f16x8(nibbles, h);
-    float v[8];
+    const int words = (int)((reinterpret_cast<uintptr_t>(q + ((hi - 1) >> 1)) - reinterpret_cast<uintptr_t>(w)) >> 2) + 1;
+    uint32_t u[E / 8 + 1];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) unpack2<__half>(h[i], &v[2 * i], &v[2 * i + 1]);
+    for (int i = 0; i <= E / 8; ++i) u[i] = i < words ? w[i] : 0u;
+    const uint32_t code0 = scale[lo >> shift], code1 = scale[(hi - 1) >> shift];
+    const int bits = (int)(reinterpret_cast<uintptr_t>(from) & 3) * 8 + 4 * (lo & 1);
+    const float s0 = scale_value(code0, a.format), s1 = scale_value(code1, a.format);
     const int first = (((lo >> shift) + 1) << shift) - lo;  // columns of the block that the run begins in
+    float v[E];
 #pragma unroll
-    for (int i = 0; i < 8; i += 2)
-      unpair(mul2(mul2(pair_of(v[i], v[i + 1]), pair_of(i < first ? s0 : s1, i + 1 < first ? s0 : s1)), pair_of(g, g)), &v[i], &v[i + 1]);
-    if (hi - lo == 8) {
-      T* dst = y + lo;
-      if constexpr (sizeof(T) == 4) {
-        reinterpret_cast<float4*>(dst)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(dst)[1] = make_float4(v[4], v[5], v[6], v[7]);
-      } else {
-        *reinterpret_cast<uint4*>(dst) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+    for (int p = 0; p < E / 8; ++p) {
+      uint32_t h[4];
+      cvt_f16x8(__funnelshift_r(u[p], u[p + 1], bits), h);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = 8 * p + 2 * j;
+        float x0, x1;
+        unpack2<__half>(h[j], &x0, &x1);
+        unpair(mul2(mul2(pair_of(x0, x1), pair_of(i < first ? s0 : s1, i + 1 < first ? s0 : s1)), pair_of(g, g)), &v[i], &v[i + 1]);
       }
+    }
+    if (hi - lo == E) {
+      uint32_t out[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (sizeof(T) == 4) out[i] = __float_as_uint(v[i]);
+        else out[i] = pack2<T>(v[2 * i], v[2 * i + 1]);
+      }
+      store_8_words(y + lo, out);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < E; ++i)
         if (lo + i < hi) y[lo + i] = from_float<T>(v[i]);
     }
   }
@@ -408,8 +423,9 @@ cudaError_t launch_dequantize(const Dequantize4Args& a, cudaStream_t st) {
     return flat ? launch_pdl(dequantize4_kernel<T, true>, grid, dim3(kThreads), 0, st, a, div, (unsigned)runs)
                 : launch_pdl(dequantize4_kernel<T, false>, grid, dim3(kThreads), 0, st, a, div, (unsigned)runs);
   }
-  const long long per_row = (a.cols + 7ll + 7ll) / 8, runs = a.rows * per_row, blocks = (runs + kThreads - 1) / kThreads;  // (a row may begin inside a run)
-  // (more blocks than are resident: new ones hide the latency of a run's loads, 16384 x 8191 bf16 105 us instead of 125)
+  constexpr long long E = 32 / sizeof(T);
+  const long long per_row = (a.cols + E - 1 + E - 1) / E, runs = a.rows * per_row, blocks = (runs + kThreads - 1) / kThreads;  // (a row may begin inside a run)
+  // (more blocks than are resident: 16384 x 8191 bf16 there and back 198 us; by 16 an SM 200, by 256 204)
   return launch_pdl(dequantize4_any_kernel<T>, dim3((unsigned)std::min<long long>(blocks, 64 * kNumSMs)), dim3(kThreads), 0, st, a,
                     make_fastdiv((uint32_t)per_row), runs);
 }
