@@ -7,10 +7,13 @@
 // memory, twelve a stage (NV) beside MMAs of 512 cycles (without them, a wrong result, 190 us), and the drain at a tile's end.
 // Tried and slower: copies of a stage's scales issued before the MMAs of the stage before it (240 us), a ring of scales for every stage (256).
 //
+// With many groups of rows and a long reduction the axes are swapped: the weights are the A operand, and a tile has as many columns as its group has
+// rows left, in steps of 32, so that a group's last tile costs what it holds (32 groups, 8192 x 2048 x 4096: 43 us for 47).
+//
 // Roles in each block: warp 0 copies, warp 1 of the leader carries scales to tensor memory (in both blocks) and issues the MMAs, warp 2
-// copies the scales of the A rows and turns them round, warp 3 those of the B rows, which both blocks need for all columns; warps 4-11 take results out, 32 rows x
-// half of the columns each.  The gated form takes 128 gate rows and the 128 up rows of the same columns as one B tile: a thread reads
-// both parts of its columns, so activation and quantisation happen in registers.
+// copies the scales of the A operand and turns them round, warp 3 those of the B operand, which both blocks need for all columns; warps 4-11 take
+// results out, 32 rows x half of the columns each.  The gated form takes 128 gate rows and the 128 up rows of the same columns as one B tile: a
+// thread reads both parts of its columns, so activation and quantisation happen in registers.
 #include "fp4_mma.cuh"
 
 namespace b2c {
@@ -26,6 +29,10 @@ constexpr int kABytes = kTileM * kStageRow;
 constexpr int kBoxRow = 64;
 constexpr int kBoxBytes = 32 * kBoxRow;  // results of a warp on their way out: 32 rows
 constexpr int kGroups = 2;               // groups of scales in shared memory
+// Which operand has the accumulator's rows.  The rows of a, and a tile's columns are rows of b; gated, 128 gate rows and the 128 up rows of the same
+// columns.  Or the weights (groups): the rows of a group are the tile's columns then, as many of them, in steps of 32, as there are.
+enum Form { kRowsFirst, kGated, kWeightsFirst };
+constexpr int kTokenBox = 32;  // rows of a copy where their number varies
 // CTAS thread blocks share a tile of CTAS * 128 rows and TN columns.
 template <int CTAS, int TN>
 struct TileShape4 {
@@ -51,12 +58,14 @@ __device__ __forceinline__ void mbar_arrive_leader(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
-template <int CTAS, int TN, bool GATED, typename YT>
+template <int CTAS, int TN, int FORM, typename YT>
 __global__ void __launch_bounds__(kPairThreads, 1)
     matmul4_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_as, const __grid_constant__ CUtensorMap tmap_b,
                         const __grid_constant__ CUtensorMap tmap_bs, const __grid_constant__ CUtensorMap tmap_y, const Matmul4Args a, const bool y_boxes) {
   using S = TileShape4<CTAS, TN>;
-  static_assert(!GATED || TN == 256, "a block of 128 columns is gate and up");
+  constexpr bool TURNED = FORM == kWeightsFirst, GATED = FORM == kGated;
+  static_assert(!TURNED || (CTAS == 2 && TN == 256), "pairs");
+  static_assert(!GATED || (CTAS == 1 && TN == 256), "a block of 128 columns is gate and up");
   constexpr int kStages = S::kStages, kBBytes = S::kBBytes;
   extern __shared__ uint8_t smem_raw[];
   __shared__ SharedCtl ctl;
@@ -124,9 +133,11 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   const int tiles = row_tiles * n_tiles;  // (fits: checked by the host)
   const int kb_all = (a.K + kFp4Stage - 1) / kFp4Stage;
 
-  // a tile's columns, 128 at a time: row of the B matrix, and which matrix
+  // rows first: a tile's columns, 128 at a time: row of the B matrix, and which matrix
   auto b_row = [&](const PairTile& p, int i) { return GATED ? p.nt * kTileM : p.nt * TN + i * kTileM; };
   auto b_plane = [&](const PairTile& p, int i) { return GATED ? 2 * p.group + i : p.group; };
+  // weights first: rows of a tile, which are columns of the MMA
+  auto width_of = [&](const PairTile& p) { return (min(S::kRows, p.row_end - p.row0) + kTokenBox - 1) / kTokenBox * kTokenBox; };
 
   if (warp < kEpiWarp0) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
@@ -139,19 +150,25 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       for (int t = pair_id; t < tiles && alive; t += num_pairs) {
         const PairTile p = pair_tile<CTAS>(a, t, row_tiles, n_tiles);
         const int m = p.row0 + (int)rank * kTileM;
+        const int per = width_of(p) / 2, boxes = (per + kTokenBox - 1) / kTokenBox, token0 = p.row0 + (int)rank * per;  // (of each block)
         for (int kb = 0; kb < kb_all; ++kb) {
           if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.empty[s]), ph ^ 1u, &ctl, &g_wait_status))) {
             alive = false;
             break;
           }
           const uint32_t full = CTAS == 2 ? map_to_rank(smem_u32(&ctl.full[s]), 0u) : smem_u32(&ctl.full[s]);
-          if (rank == 0) mbar_arrive_expect_tx(smem_u32(&ctl.full[s]), (uint32_t)CTAS * (kABytes + kBBytes), on);
           const uint32_t dst = b_base + s * kBBytes;
-          if constexpr (CTAS == 2) {
+          if constexpr (TURNED) {
+            if (rank == 0) mbar_arrive_expect_tx(smem_u32(&ctl.full[s]), 2u * (kABytes + (uint32_t)(boxes * kTokenBox * kStageRow)), on);
+            const int n = p.nt * TN + (int)rank * kTileM;
+            tma_pair_load_3d(a_base + s * kABytes, &tmap_b, kb * kStageRow, n, p.group, full, on);
+            for (int i = 0; i < boxes; ++i) tma_pair_load_2d(dst + i * kTokenBox * kStageRow, &tmap_a, kb * kStageRow, token0 + i * kTokenBox, full, on);
+          } else if constexpr (CTAS == 2) {
+            if (rank == 0) mbar_arrive_expect_tx(smem_u32(&ctl.full[s]), 2u * (kABytes + kBBytes), on);
             tma_pair_load_2d(a_base + s * kABytes, &tmap_a, kb * kStageRow, m, full, on);
-            if constexpr (S::kColTiles == 2) tma_pair_load_3d(dst, &tmap_b, kb * kStageRow, b_row(p, (int)rank), b_plane(p, (int)rank), full, on);
-            else tma_pair_load_3d(dst, &tmap_b, kb * kStageRow, p.nt * TN + (int)rank * S::kBRows, p.group, full, on);
+            tma_pair_load_3d(dst, &tmap_b, kb * kStageRow, p.nt * TN + (int)rank * S::kBRows, p.group, full, on);
           } else {
+            mbar_arrive_expect_tx(full, kABytes + kBBytes, on);
             tma_load_2d(a_base + s * kABytes, &tmap_a, kb * kStageRow, m, full, on);
 #pragma unroll
             for (int i = 0; i < S::kColTiles; ++i) tma_load_3d(dst + i * kTileM * kStageRow, &tmap_b, kb * kStageRow, b_row(p, i), b_plane(p, i), full, on);
@@ -167,13 +184,15 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       // ---------------------------------------------------------------- scales to tensor memory, MMA issue (leader)
       if (rank == 0) {
         const uint32_t on = elect_one() ? 1u : 0u;
-        const uint32_t idesc = make_idesc_f4(S::kRows, TN, a.format);
         auto run = [&](auto format) {
           constexpr int FORMAT = decltype(format)::value;
           int s = 0, g = 0, buf = 0;
           uint32_t ph = 0, gph = 0, bph = 0, ts_at = 0;
           bool alive = true;
           for (int t = pair_id; t < tiles && alive; t += num_pairs) {
+            int width = TN;
+            if constexpr (TURNED) width = width_of(pair_tile<CTAS>(a, t, row_tiles, n_tiles));
+            const uint32_t idesc = make_idesc_f4(S::kRows, width, FORMAT);
             if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.tmem_empty[buf]), bph ^ 1u, &ctl, &g_wait_status))) break;
             for (int kb = 0; kb < kb_all; ++kb) {
               const int in = kb % kGroup;  // stage of the group
@@ -189,7 +208,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
               ts_at = S::kScaleCols - ts_at;
               copy_scales<CTAS, FORMAT, 512>(ts, scales, 4, on);
 #pragma unroll
-              for (int i = 0; i < S::kColTiles; ++i) copy_scales<CTAS, FORMAT, 512>(ts + 16 + 4 * i, scales + (1 + i) * kGroupTile, 4 * S::kColTiles, on);
+              for (int i = 0; i < S::kColTiles; ++i)
+                if (i * kTileM < width) copy_scales<CTAS, FORMAT, 512>(ts + 16 + 4 * i, scales + (1 + i) * kGroupTile, 4 * S::kColTiles, on);
               mma_f4_stage<CTAS, FORMAT>(tmem_acc + buf * TN, make_smem_desc(a_base + s * kABytes, kStageRow), make_smem_desc(b_base + s * kBBytes, kStageRow), idesc,
                                          ts, ts + 16, 4 * S::kColTiles, kb > 0, on, ksteps);
               if constexpr (CTAS == 2) mma_commit_pair(smem_u32(&ctl.empty[s]), on);
@@ -234,7 +254,14 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         const uint32_t full = smem_u32(&scales_full[part][lg]), dst = mine + lg * S::kScaleBytes;
         const int width = group_row(a.format), x = lkb / kGroup * width;
         mbar_arrive_expect_tx(full, (uint32_t)((part == 0 ? 1 : S::kColTiles) * kTileM * width), on);
-        if (part == 0) {
+        if constexpr (TURNED) {
+          if (part == 1) {
+#pragma unroll
+            for (int i = 0; i < S::kColTiles; ++i) tma_load_2d(dst + i * kGroupTile, &tmap_as, x, lp.row0 + i * kTileM, full, on);
+          } else {
+            tma_load_3d(dst, &tmap_bs, x, lp.nt * TN + (int)rank * kTileM, lp.group, full, on);
+          }
+        } else if (part == 0) {
           tma_load_2d(dst, &tmap_as, x, lp.row0 + (int)rank * kTileM, full, on);
         } else {
 #pragma unroll
@@ -300,11 +327,12 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       // (voted, so that the lanes are together at the warp-wide loads; a wait that gave up does not leave the loop)
       ok = ok && __all_sync(0xffffffffu, mbar_wait_inline(smem_u32(&ctl.tmem_full[buf]), bph, &ctl, &g_wait_status));
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      // gated: 64 gate columns, then the up columns of the same 64;  weights first: half of the tile's rows, rounded to 32 (what lies behind
+      // them is read and not used)
+      const int mine = TURNED ? (width_of(p) / 2 + 31) / 32 * 32 : S::kWarpCols, c0 = half * mine;
       float v[S::kWarpCols];
-      // gated: 64 gate columns, then the up columns of the same 64
 #pragma unroll
-      for (int c = 0; c < S::kWarpCols; c += 64)
-        tmem_ld64(taddr0 + (uint32_t)(buf * TN + (GATED ? half * 64 + c * 2 : half * S::kWarpCols + c)), reinterpret_cast<int32_t*>(v + c));
+      for (int c = 0; c < S::kWarpCols; c += 64) tmem_ld64(taddr0 + (uint32_t)(buf * TN + (GATED ? half * 64 + c * 2 : c0 + c)), reinterpret_cast<int32_t*>(v + c));
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
       if (lane == 0) {
@@ -315,8 +343,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         buf = 0;
         bph ^= 1u;
       }
-      const long long m = (long long)p.row0 + (int)rank * kTileM + in_tile;
       if constexpr (GATED) {
+        const long long m = (long long)p.row0 + in_tile;
         const int n = p.nt * kTileM + half * 64;
 #pragma unroll
         for (int i = 0; i < 64; ++i) v[i] = quick_silu(v[i] * alpha) * (v[64 + i] * alpha);
@@ -341,6 +369,57 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             uint8_t* ys = a.y_scale + m * a.ldys + (n + c) / fp4_block(a.format);
             if (a.format == B2C_MXFP4) ys[0] = (uint8_t)s[0].code;
             else *reinterpret_cast<uint16_t*>(ys) = (uint16_t)(s[0].code | (s[1].code << 8));  // (ldys is a multiple of 16)
+          }
+        }
+      } else if constexpr (TURNED) {
+        // A lane has a column.  Runs of 32 columns (a warp's) of 16 or 32 rows go to shared memory, and from there, as below, by one copy or by the lanes.
+        // (Stored from the registers, 128 bytes of a row an instruction, the second product of 8192 tokens, 4 of 64 experts, 2048 x 1024, took 123 us.)
+        constexpr int kBoxRows = kBoxBytes / (32 * (int)sizeof(YT));
+        const int n = p.nt * TN + (int)rank * kTileM + quad * 32, rows = min(mine, p.row_end - p.row0 - c0), m0 = p.row0 + c0;
+        const uint32_t box = box_base + (uint32_t)((warp - kEpiWarp0) * kBoxBytes), here = box + (uint32_t)(lane * (int)sizeof(YT));
+#pragma unroll
+        for (int i = 0; i < S::kWarpCols; i += kBoxRows) {
+          if (i < rows && n < a.N) {
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < kBoxRows; j += 2) {
+              const float x0 = v[i + j] * alpha, x1 = v[i + j + 1] * alpha;
+              if constexpr (sizeof(YT) == 4) {
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(here + (uint32_t)(j * 128)), "f"(x0) : "memory");
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(here + (uint32_t)(j * 128 + 128)), "f"(x1) : "memory");
+              } else {
+                const uint32_t w = pack2<YT>(x0, x1);
+                asm volatile("st.shared.b16 [%0], %1;" ::"r"(here + (uint32_t)(j * 64)), "h"((unsigned short)w) : "memory");
+                asm volatile("st.shared.b16 [%0], %1;" ::"r"(here + (uint32_t)(j * 64 + 64)), "h"((unsigned short)(w >> 16)) : "memory");
+              }
+            }
+            if (y_boxes && i + kBoxRows <= rows && (n + 32 <= a.N || a.N * (int)sizeof(YT) % 16 == 0)) {
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              __syncwarp();
+              if (lane == 0 && ok) {
+                asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(&tmap_y), "r"(n * (int)sizeof(YT)), "r"(m0 + i), "r"(box)
+                             : "memory");
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+              }
+            } else {
+              __syncwarp();
+              YT* y = (YT*)a.y + (long long)(m0 + i) * a.ldy + n + lane;
+              if (ok && n + lane < a.N)
+#pragma unroll 4
+                for (int j = 0; j < min(kBoxRows, rows - i); ++j, y += a.ldy) {
+                  if constexpr (sizeof(YT) == 4) {
+                    float x;
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(here + (uint32_t)(j * 128)) : "memory");
+                    *y = x;
+                  } else {
+                    unsigned short x;
+                    asm volatile("ld.shared.b16 %0, [%1];" : "=h"(x) : "r"(here + (uint32_t)(j * 64)) : "memory");
+                    *reinterpret_cast<unsigned short*>(y) = x;
+                  }
+                }
+              __syncwarp();
+            }
           }
         }
       } else {
@@ -415,12 +494,13 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 
 // Whether the copy engine can take a product's results out (see results_by_copy).
 bool boxes_of(const Matmul4Args& a, int bytes) {
-  return !a.gated && (reinterpret_cast<uintptr_t>(a.y) & 15) == 0 && a.ldy * bytes % 16 == 0 && (long long)a.N * bytes <= 0x7FFFFFFFLL;
+  return (reinterpret_cast<uintptr_t>(a.y) & 15) == 0 && a.ldy * bytes % 16 == 0 && (long long)a.N * bytes <= 0x7FFFFFFFLL;
 }
 
-template <int CTAS, int TN, bool GATED, typename YT>
+template <int CTAS, int TN, int FORM, typename YT>
 int launch_pair(const Matmul4Args& a, cudaStream_t st) {
   using S = TileShape4<CTAS, TN>;
+  constexpr bool TURNED = FORM == kWeightsFirst, GATED = FORM == kGated;
   const long long cols = GATED ? kTileM : TN;
   const long long n_tiles = (a.N + cols - 1) / cols;
   const long long row_tiles = a.offsets ? a.rows / S::kRows + std::min(a.groups, a.rows) : (a.rows + S::kRows - 1) / S::kRows;
@@ -428,17 +508,20 @@ int launch_pair(const Matmul4Args& a, cudaStream_t st) {
   const uint64_t bytes = a.K / 2, scales = fp4_scales(a.K, a.format), planes = (uint64_t)a.groups * (GATED ? 2 : 1);
   const int width = group_row(a.format);
   CUtensorMap ta, tas, tb, tbs, ty;
-  int rc = encode_tiled_2d(&ta, a.a, bytes, a.rows, a.rows > 1 ? a.lda : bytes, kStageRow, kTileM, 128);
+  int rc = encode_tiled_2d(&ta, a.a, bytes, a.rows, a.rows > 1 ? a.lda : bytes, kStageRow, TURNED ? kTokenBox : kTileM, 128);
   if (rc == B2C_OK) rc = encode_tiled_2d(&tas, a.a_scale, scales, a.rows, a.rows > 1 ? a.lds : fp4_scale_pitch(a.K, a.format), width, kTileM, width);
-  if (rc == B2C_OK) rc = encode_tiled_3d(&tb, a.b, bytes, a.N, planes, bytes, (uint64_t)a.N * bytes, kStageRow, S::kBoxRows, 128);
+  if (rc == B2C_OK) rc = encode_tiled_3d(&tb, a.b, bytes, a.N, planes, bytes, (uint64_t)a.N * bytes, kStageRow, TURNED ? kTileM : S::kBoxRows, 128);
   if (rc == B2C_OK) rc = encode_tiled_3d(&tbs, a.b_scale, scales, a.N, planes, a.ldbs, (uint64_t)a.N * a.ldbs, width, kTileM, width);
   if (rc != B2C_OK) return rc;
-  const bool y_boxes = boxes_of(a, (int)sizeof(YT));  // (of 64 bytes x 32 rows)
+  const bool y_boxes = !GATED && boxes_of(a, (int)sizeof(YT));  // 64 bytes x 32 rows, weights first 32 columns
+  const int box_row = TURNED ? 32 * (int)sizeof(YT) : kBoxRow;
   ty = ta;
-  if (y_boxes) rc = encode_tiled_2d(&ty, a.y, (uint64_t)a.N * sizeof(YT), a.rows, a.rows > 1 ? (uint64_t)a.ldy * sizeof(YT) : ((uint64_t)a.N * sizeof(YT) + 15) / 16 * 16, kBoxRow, 32, kBoxRow);
+  if (y_boxes)
+    rc = encode_tiled_2d(&ty, a.y, (uint64_t)a.N * sizeof(YT), a.rows, a.rows > 1 ? (uint64_t)a.ldy * sizeof(YT) : ((uint64_t)a.N * sizeof(YT) + 15) / 16 * 16, box_row,
+                         kBoxBytes / box_row, TURNED ? 0 : kBoxRow);
   if (rc != B2C_OK) return rc;
   static std::atomic<unsigned long long> configured{0};
-  cudaError_t e = set_max_dynamic_smem_once(configured, (const void*)matmul4_pair_kernel<CTAS, TN, GATED, YT>, S::kSmem);
+  cudaError_t e = set_max_dynamic_smem_once(configured, (const void*)matmul4_pair_kernel<CTAS, TN, FORM, YT>, S::kSmem);
   if (e == cudaSuccess) {
     const int pairs = (int)std::min<long long>(row_tiles * n_tiles, kNumSMs / CTAS);
     cudaLaunchConfig_t cfg = {};
@@ -455,7 +538,7 @@ int launch_pair(const Matmul4Args& a, cudaStream_t st) {
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = CTAS == 2 ? 2 : 1;
-    e = cudaLaunchKernelEx(&cfg, matmul4_pair_kernel<CTAS, TN, GATED, YT>, ta, tas, tb, tbs, ty, a, y_boxes);
+    e = cudaLaunchKernelEx(&cfg, matmul4_pair_kernel<CTAS, TN, FORM, YT>, ta, tas, tb, tbs, ty, a, y_boxes);
   }
   if (e != cudaSuccess) {
     set_last_cuda_error((int)e);
@@ -464,11 +547,11 @@ int launch_pair(const Matmul4Args& a, cudaStream_t st) {
   return B2C_OK;
 }
 
-template <int CTAS, int TN>
+template <int CTAS, int TN, int FORM>
 int launch_type(const Matmul4Args& a, cudaStream_t st) {
-  if (a.y_type == B2C_F32) return launch_pair<CTAS, TN, false, float>(a, st);
-  if (a.y_type == B2C_F16) return launch_pair<CTAS, TN, false, __half>(a, st);
-  return launch_pair<CTAS, TN, false, __nv_bfloat16>(a, st);
+  if (a.y_type == B2C_F32) return launch_pair<CTAS, TN, FORM, float>(a, st);
+  if (a.y_type == B2C_F16) return launch_pair<CTAS, TN, FORM, __half>(a, st);
+  return launch_pair<CTAS, TN, FORM, __nv_bfloat16>(a, st);
 }
 
 // Nanoseconds by tiles of 128 x 128 on one SM, and by those of 256 x 256 on a pair: the small ones where the large ones are fewer than the pairs.
@@ -490,10 +573,17 @@ long long fp4_pair_ns(const Matmul4Args& a) { return std::min(small_ns(a), large
 
 int launch_fp4_matmul_pair(const Matmul4Args& a, cudaStream_t st) {
   const int rows = a.offsets ? (int)(((long long)a.rows + a.groups - 1) / a.groups) : a.rows;
-  // Half a tile of every group is empty: 64 rows of a tile of its own, 128 of a pair's.  At 240 rows of a group within 5 % either way.
-  if (a.gated) return rows <= 768 ? launch_pair<1, 256, true, uint8_t>(a, st) : launch_pair<2, 256, true, uint8_t>(a, st);
-  if (a.offsets) return rows <= 768 ? launch_type<1, 256>(a, st) : launch_type<2, 256>(a, st);
-  return small_ns(a) < large_ns(a) ? launch_type<1, 128>(a, st) : launch_type<2, 256>(a, st);
+  if (a.gated) return launch_pair<1, 256, kGated, uint8_t>(a, st);
+  if (a.offsets) {
+    // Half a tile of every group is empty: 64 rows of a tile of its own, 128 of a pair's, 16 of a pair's with the weights first.  That one's results take
+    // longer, which shows unless the reduction is long, and its tiles are fewer.  One SM / weights first, us, N 2048: 32 groups of 128, 256, 512 rows and
+    // K 4096: 38.9 / 37.6, 49.8 / 46.0, 76.7 / 69.8, K 8192: 68.4 / 62.9, 90.8 / 83.3, 143 / 128;  8 groups of 256, K 4096: 19.1 / 20.7;  32 of 64: 33.1 /
+    // 36.0;  16 of 512, K 2048: 26.0 / 26.5.  At 240 rows of a group and more the pair with the rows first is within 5 % of one SM either way.
+    const long long large = (a.rows / 256 + a.groups / 2) * (long long)((a.N + 255) / 256);  // tiles, about
+    if (a.K >= 4096 && rows >= 100 && large >= 3 * (kNumSMs / 2)) return launch_type<2, 256, kWeightsFirst>(a, st);
+    return rows <= 768 ? launch_type<1, 256, kRowsFirst>(a, st) : launch_type<2, 256, kRowsFirst>(a, st);
+  }
+  return small_ns(a) < large_ns(a) ? launch_type<1, 128, kRowsFirst>(a, st) : launch_type<2, 256, kRowsFirst>(a, st);
 }
 
 cudaError_t fp4_pair_wait_selftest(cudaStream_t st) { return launch_wait_selftest(st); }

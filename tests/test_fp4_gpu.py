@@ -231,6 +231,10 @@ def check_matmul(y, qa, sa, qb, sb, fmt, alpha=None):
     err = ref.sum_error(K) * size
     bound = err + half * (want.abs() + err) + torch.finfo(y.dtype).smallest_normal * 2.0 ** -10
     off = (y.double() - want).abs()
+    # from half a step beyond the largest number on (65504 + 16 in fp16) a result rounds to infinity
+    most = torch.finfo(y.dtype).max
+    top = most + 2.0 ** math.floor(math.log2(most)) * half
+    off[y.isinf() & (want.abs() + err >= top) & (y.sign() == want.sign())] = 0.0
     assert bool((off <= bound).all()), (float((off / bound).max()), float(off.max()), float(want.abs().max()))
 
 
@@ -301,6 +305,38 @@ def test_matmul_groups(lib, mean, fmt):
         for e in range(G):
             if at[e + 1] > at[e]:
                 check_matmul(y[at[e]:at[e + 1]], qa[at[e]:at[e + 1]], sa[at[e]:at[e + 1]], qb[e], sb[e], fmt)
+
+
+@FMT
+@pytest.mark.parametrize("yt,N,first,ld", [(torch.bfloat16, 1504, 0, 1504), (torch.float16, 1501, 3, 1511), (torch.bfloat16, 1530, 8, 1552), (torch.float32, 1476, 4, 1488),
+                                           (torch.float32, 1501, 1, 1505)], ids=str)
+def test_matmul_many_long_groups(lib, yt, N, first, ld, fmt):
+    """Many groups and a long reduction: the weights take the accumulator's rows, a group's last tile has as many columns as there are rows left."""
+    K, count = 4128, [0, 1, 31, 32, 33, 63, 64, 65, 127, 128, 129, 159, 160, 161, 192, 224, 225, 0, 255, 256, 257, 288, 400, 513, 300, 100, 7, 140, 260, 90, 350, 16, 48,
+                      200, 330, 30, 170, 0]
+    G, g, before = len(count), gen(N), 5
+    offsets = torch.tensor([0] + count, device="cuda").cumsum(0).int() + before
+    rows = int(offsets[-1]) + 6
+    qa, sa = operands(lib, rows, K, fmt, N)
+    qb, sb = operands(lib, N, K, fmt, N + 1, (G,))
+    alpha = torch.rand(G, generator=g, device="cuda") + 0.5
+    whole = torch.full((rows, ld + 16), 5.0, device="cuda", dtype=yt)
+    y = whole[:, first:first + N]
+    lib.fp4_matmul(qa, sa, qb, sb, y, alpha=alpha, offsets=offsets)
+    assert lib.fp4_status() == lib.OK
+    at = offsets.tolist()
+    for e in range(G):
+        if count[e]:
+            check_matmul(y[at[e]:at[e + 1]], qa[at[e]:at[e + 1]], sa[at[e]:at[e + 1]], qb[e], sb[e], fmt, alpha[e])
+    assert bool((whole[:before] == 5.0).all()) and bool((whole[at[-1]:] == 5.0).all())
+    assert bool((whole[:, :first] == 5.0).all()) and bool((whole[:, first + N:] == 5.0).all())
+    bad = at[20] + 100  # a row with a NaN is NaN, and no other, also where its neighbours are another group's
+    sa.view(torch.uint8)[bad, 3] = 255 if fmt == MX else 127
+    again = whole.clone()
+    lib.fp4_matmul(qa, sa, qb, sb, again[:, first:first + N], alpha=alpha, offsets=offsets)
+    assert bool(again[bad, first:first + N].isnan().all())
+    again[bad] = whole[bad]
+    assert torch.equal(again, whole)
 
 
 @FMT
