@@ -271,10 +271,11 @@ int64_t round16(int64_t n) { return (n + 15) / 16 * 16; }
 bool is_one_float(const at::Tensor* t) { return t == nullptr || (t->numel() == 1 && is_f32(*t)); }
 const float* floats(const at::Tensor* t) { return t ? (const float*)t->data_ptr() : nullptr; }
 // Distance between the rows of one matrix, or of matrices that follow each other without a gap, in bytes; -1 if there is none such.  A single
-// row has the distance that its length rounds up to.
+// row, or none, has the distance that its length rounds up to.
 int64_t ld_of_stack(const at::Tensor& t) {
   const int d = (int)t.dim();
   const int64_t cols = t.size(d - 1);
+  if (t.numel() == 0) return round16(cols);  // (`rows` below would become 0, and a remainder by it ends the process)
   if (cols > 1 && t.stride(d - 1) != 1) return -1;
   int64_t step = -1, rows = 1;  // of the rows counted so far
   for (int i = d - 2; i >= 0; --i) {

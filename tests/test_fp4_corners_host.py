@@ -1,0 +1,41 @@
+"""What of the 4-bit float operators can be checked without a device: refusals of unusual tensors, decisions of the host."""
+import pytest
+import torch
+
+import paper_2104_04731_b200 as b2c
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2104_04731_b200 import build
+
+    build.build()
+    return b2c.load()
+
+
+def code_of(call, *args, **kw):
+    with pytest.raises(b2c.B2CError) as e:
+        call(*args, **kw)
+    return e.value.code
+
+
+def layer(hidden, inter, experts=2, tokens=4, topk=2, fmt=b2c.NVFP4):
+    """Arguments of an expert layer, on the CPU."""
+    (w1, s1), (w2, s2) = (b2c.fp4_empty(shape, cols, fmt, device="cpu") for shape, cols in (((experts, 2, inter), hidden), ((experts, hidden), inter)))
+    return dict(x=torch.zeros(tokens, hidden), ids=torch.zeros(tokens, topk, dtype=torch.int32), weights=torch.zeros(tokens, topk), w1=w1, w1_scale=s1, w2=w2,
+                w2_scale=s2, y=torch.zeros(tokens, hidden), workspace=torch.zeros(1 << 20, dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("fmt", [b2c.MXFP4, b2c.NVFP4], ids=["mx", "nv"])
+@pytest.mark.parametrize("groups,N,K", [(4, 0, 64), (1, 0, 64), (0, 8, 64), (4, 8, 0), (4, 0, 0)])
+def test_product_refuses_empty_stacks(lib, groups, N, K, fmt):
+    """Matrices without rows or columns, or none at all: the distance between rows was sought by a remainder by 0, which ended the process."""
+    q, s = b2c.fp4_empty(3, K, fmt, device="cpu")
+    b, bs = b2c.fp4_empty((groups, N), K, fmt, device="cpu")
+    assert code_of(b2c.fp4_matmul, q, s, b, bs, torch.zeros(3, N), offsets=torch.zeros(groups + 1, dtype=torch.int32)) == b2c.E_INVALID_ARG
+
+
+@pytest.mark.parametrize("fmt", [b2c.MXFP4, b2c.NVFP4], ids=["mx", "nv"])
+@pytest.mark.parametrize("kw", [dict(hidden=256, inter=0), dict(hidden=0, inter=64), dict(hidden=0, inter=0), dict(hidden=256, inter=64, experts=0)], ids=str)
+def test_experts_refuse_empty_matrices(lib, kw, fmt):
+    assert code_of(b2c.fp4_experts, **layer(fmt=fmt, **kw)) == b2c.E_INVALID_ARG
