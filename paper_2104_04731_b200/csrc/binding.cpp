@@ -87,8 +87,9 @@ bool shaped(const at::Tensor& t, int64_t a, int64_t b, int64_t c, int64_t d) {
   return t.dim() == 4 && t.size(0) == a && t.size(1) == b && t.size(2) == c && t.size(3) == d;
 }
 int64_t blocks(int64_t n) { return (n + 127) / 128; }
-// Distance between the rows of a matrix with contiguous rows; -1 if it has none or they overlap.
+// Distance between the rows of a matrix with contiguous rows; -1 if it has none or they overlap, or if it is no matrix.
 int64_t ld(const at::Tensor& t) {
+  if (t.dim() != 2) return -1;
   const int64_t rows = t.size(0), cols = t.size(1);
   if (cols > 1 && t.stride(1) != 1) return -1;
   if (rows <= 1) return cols;

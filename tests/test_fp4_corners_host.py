@@ -39,3 +39,13 @@ def test_product_refuses_empty_stacks(lib, groups, N, K, fmt):
 @pytest.mark.parametrize("kw", [dict(hidden=256, inter=0), dict(hidden=0, inter=64), dict(hidden=0, inter=0), dict(hidden=256, inter=64, experts=0)], ids=str)
 def test_experts_refuse_empty_matrices(lib, kw, fmt):
     assert code_of(b2c.fp4_experts, **layer(fmt=fmt, **kw)) == b2c.E_INVALID_ARG
+
+
+@pytest.mark.parametrize("shape", [(), (4,), (1024,), (4, 256, 1), (1, 4, 256)], ids=str)
+def test_experts_refuse_results_that_are_no_matrix(lib, shape):
+    """As every refusal by an error of the library, in 8 bits and in 4 (torch's own came out for a y of fewer dimensions)."""
+    args = layer(256, 64)
+    assert code_of(b2c.fp4_experts, **{**args, "y": torch.zeros(shape)}) == b2c.E_INVALID_ARG
+    w1, w2 = torch.zeros(2, 2, 64, 256).to(torch.float8_e4m3fn), torch.zeros(2, 256, 64).to(torch.float8_e4m3fn)
+    eight = dict(args, w1=w1, w1_scale=torch.zeros(2, 2, 1, 2), w2=w2, w2_scale=torch.zeros(2, 2, 1), y=torch.zeros(shape))
+    assert code_of(b2c.fp8_experts, **eight) == b2c.E_INVALID_ARG
