@@ -511,8 +511,8 @@ int b2c_fp4_matmul(const b2c_fp4_matmul_desc* desc, int64_t rows, const void* a_
  * [experts][hidden][inter / 2], scales [experts][hidden] rows ld_w2_scale_bytes apart; matrices dense, all 16-byte aligned, distances multiples of
  * 16.  hidden and inter are multiples of 32.  The factors are fp32 on the device, one for x and h, [experts] for the weights; each may be
  * NULL (1), and is for B2C_MXFP4.  h is not rounded before it is quantised (in fp32: a border
- * between two results may be off by 3 * 2^-24 of itself, as h is by its sums' errors); the rows of the slots and their weighted sum are formed in
- * fp32, in the order of the slots, and rounded once.  ids outside 0..experts-1 add nothing.  workspace_dev: as there, of
+ * between two results may be off by 3 * 2^-24 of itself, as h is by its sums' errors; gates below -153 give 0, those above it keep their h however large up
+ * is); the rows of the slots and their weighted sum are formed in fp32, in the order of the slots, and rounded once.  ids outside 0..experts-1 add nothing.  workspace_dev: as there, of
  * b2c_fp4_experts_workspace_bytes bytes. */
 typedef struct {
   int32_t hidden, inter, experts, topk;

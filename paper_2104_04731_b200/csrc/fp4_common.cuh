@@ -204,13 +204,27 @@ __device__ __forceinline__ float max_abs3(float a, float b, float c) {
   asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// silu as in the 8-bit layer, with e^-|v| as a power of two from one rounded product: it is off by |v| 2^-24 of itself more, and silu with it where v
-// is negative; v^2 e^-|v| 2^-24 is 0.6 units of 2^-24 at most.  Eight operations, two of them on the unit of 16 results a cycle.
-__device__ __forceinline__ float quick_silu(float v) {
+// silu(gate) * up, silu as in the 8-bit layer with e^-|v| as a power of two whose exponent is one rounded product: the power is off by 1.25 |v| 2^-24 of
+// itself more, and silu with it where v is negative; where it is positive by 1.25 v e^-v 2^-24, half a unit at most.
+//   Below v = kFarGate (e^v is above 2^-122 there, and no longer counts beside 1) the power is formed 2^96 times too large and h is scaled back behind
+// the product with up, which may be large: scales go down to 2^-127, and e^v alone leaves the range of fp32 at -87.  The range of the larger power
+// ends at v = -153, below which h is 0.  The exponent is a sum rounded once, by less than without the shift.
+//   Eight operations, two of them on the unit of 16 results a cycle, and four more with FAR, for gates that may be below kFarGate.
+constexpr float kFarGate = -84.0f;
+template <bool FAR>
+__device__ __forceinline__ float quick_gated(float gate, float up) {
+  const bool far = FAR && gate < kFarGate;
   float e, r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(v) * -1.44269504f));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fmaf(fabsf(gate), -1.44269504f, far ? 96.0f : 0.0f)));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
-  return (v < 0.0f ? v * e : v) * r;
+  const float h = (gate < 0.0f ? gate * e : gate) * r * up;
+  return far ? h * 0x1p-96f : h;
+}
+// The least of three (a NaN is left out).
+__device__ __forceinline__ float min3(float a, float b, float c) {
+  float r;
+  asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 
 }  // namespace

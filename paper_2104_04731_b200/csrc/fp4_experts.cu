@@ -454,7 +454,7 @@ __global__ void __launch_bounds__(kUpThreads, 1) experts4_up_kernel(const __grid
       for (int r = 2 * quad + (lane >> 4); r - (lane >> 4) < t.rows; r += 8) {
         float h[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = r < t.rows ? quick_silu(sums[r][4 * l + i]) * sums[r][64 + 4 * l + i] : 0.0f;
+        for (int i = 0; i < 4; ++i) h[i] = r < t.rows ? quick_gated<true>(sums[r][4 * l + i], sums[r][64 + 4 * l + i]) : 0.0f;
         uint32_t mx = max(max(abs_bits(h[0]), abs_bits(h[1])), max(abs_bits(h[2]), abs_bits(h[3])));
         mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 2));

@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, RowsShape<NT, WT>
         }
       } else {
         // a block of 16 (32) columns is four (eight) neighbouring lanes
-        const float h[4] = {quick_silu(v[0].x) * v[1].x, quick_silu(v[0].y) * v[1].y, quick_silu(v[0].z) * v[1].z, quick_silu(v[0].w) * v[1].w};
+        const float h[4] = {quick_gated<true>(v[0].x, v[1].x), quick_gated<true>(v[0].y, v[1].y), quick_gated<true>(v[0].z, v[1].z), quick_gated<true>(v[0].w, v[1].w)};
         uint32_t mx = max(max(abs_bits(h[0]), abs_bits(h[1])), max(abs_bits(h[2]), abs_bits(h[3])));
         mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 2));

@@ -346,8 +346,47 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       if constexpr (GATED) {
         const long long m = (long long)p.row0 + in_tile;
         const int n = p.nt * kTileM + half * 64;
+        float low = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 64; ++i) v[i] = quick_silu(v[i] * alpha) * (v[64 + i] * alpha);
+        for (int i = 0; i < 64; ++i) v[i] *= alpha;
+#pragma unroll
+        for (int i = 0; i < 64; i += 2) low = min3(low, v[i], v[i + 1]);
+        if (__any_sync(0xffffffffu, low < kFarGate)) {
+          // Rare, so by short code: eight columns at a time go through shared memory (the box for results has no other use here), where a loop can index
+          // them.  (Four more operations for every value made 8192 tokens 250 us instead of 240; a second copy of the 64 beside the first made
+          // 2048 tokens, 4 of 32, 1024 x 512, 49.7 instead of 47.4, of which it takes no step.)
+          const uint32_t at = box_base + (uint32_t)((warp - kEpiWarp0) * kBoxBytes + lane * 16);
+#pragma unroll
+          for (int i = 0; i < 64; i += 8) {
+            auto put = [&](int p, const float* u) {
+              asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at + 512 * p), "f"(u[0]), "f"(u[1]), "f"(u[2]), "f"(u[3]) : "memory");
+            };
+            put(0, v + i);
+            put(1, v + i + 4);
+            put(2, v + 64 + i);
+            put(3, v + 64 + i + 4);
+#pragma unroll 1
+            for (int j = 0; j < 8; ++j) {
+              const uint32_t here = at + (uint32_t)(512 * (j >> 2) + 4 * (j & 3));
+              float g, u;
+              asm volatile("ld.shared.f32 %0, [%1];" : "=f"(g) : "r"(here) : "memory");
+              asm volatile("ld.shared.f32 %0, [%1];" : "=f"(u) : "r"(here + 1024) : "memory");
+              g = quick_gated<true>(g, u * alpha);
+              asm volatile("st.shared.f32 [%0], %1;" ::"r"(here), "f"(g) : "memory");
+            }
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+              const float4 h = ld_shared_f4(at + 512 * p);
+              v[i + 4 * p] = h.x;
+              v[i + 4 * p + 1] = h.y;
+              v[i + 4 * p + 2] = h.z;
+              v[i + 4 * p + 3] = h.w;
+            }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 64; ++i) v[i] = quick_gated<false>(v[i], v[64 + i] * alpha);
+        }
         uint8_t* y = (uint8_t*)a.y + m * a.ldy + n / 2;
         const bool on = ok && m < p.row_end;
 #pragma unroll

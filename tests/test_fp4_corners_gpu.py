@@ -2,6 +2,12 @@
 import pytest
 import torch
 
+import fp4_ref as ref
+from fp4_ref import MX, NV
+
+FMT = pytest.mark.parametrize("fmt", [MX, NV], ids=["mx", "nv"])
+U = 2.0 ** -24  # half a step of fp32 at most, relative
+
 pytestmark = pytest.mark.gpu
 
 
@@ -22,3 +28,71 @@ def test_empty_matrices_are_refused(lib):
         (w1, s1), (w2, s2) = lib.fp4_empty((2, 2, inter), hidden, lib.NVFP4), lib.fp4_empty((2, hidden), inter, lib.NVFP4)
         x, y = (torch.zeros(3, hidden, device="cuda") for _ in range(2))
         assert code_of(lib, lib.fp4_experts, x, ids, weights, w1, s1, w2, s2, y, ws) == lib.E_INVALID_ARG
+
+
+# ---- hidden rows of an expert layer, seen through a second matrix that is the identity ---------------------------------------------------
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def identity(lib, experts, n, fmt):
+    """[experts, n, n] in 4 bits: the layer's result for a token of one expert with weight 1 is its hidden row as quantised (times the factor)."""
+    code = 2 * torch.eye(n, dtype=torch.uint8, device="cuda")  # (code 2 is 1.0)
+    q, s = lib.fp4_empty((experts, n), n, fmt)
+    q.copy_(ref.pack(code).expand(experts, n, n // 2))
+    s.view(torch.uint8).fill_(127 if fmt == MX else 56)
+    return q, s
+
+
+def run_layer(lib, x, ids, w1, s1, w2, s2, fmt, **factors):
+    T, H = x.shape
+    n = lib.fp4_experts_workspace_bytes(H, w1.shape[2], w1.shape[0], ids.shape[1], T, fmt, lib.F32)
+    y = torch.full_like(x, 9.0)
+    lib.fp4_experts(x, ids, torch.ones(ids.shape, device="cuda"), w1, s1, w2, s2, y, torch.empty(n, dtype=torch.uint8, device="cuda"), **factors)
+    assert lib.fp4_status() == lib.OK
+    return y
+
+
+def block_max(v):
+    return v.reshape(v.shape[0], -1, 32).amax(-1)
+
+
+# (one expert: up to 4 tokens go to the two kernels for few, tiles of 16 rows, tiles of 128)
+@pytest.mark.parametrize("T", [2, 4, 10, 100])
+def test_gates_far_below_zero(lib, T):
+    """Gates from -6 to -153 (a few below it) beside up values of up to 2^115: e^gate leaves the range of fp32, the gated product and its scale do not.  Sums of the first
+    product are whole multiples of a power of two below 2^24 of it, so they are exact."""
+    n, g = 512, gen(T)
+    codes = lambda lo, hi, *shape: torch.randint(lo, hi, shape, generator=g, device="cuda")  # noqa: E731
+    x = torch.zeros(T, n, device="cuda")
+    x[:, :32] = torch.tensor(ref.VALUES, device="cuda")[codes(1, 8, T, 32)]
+    x[:, 31] = 6.0  # (the scale is 1)
+    w, sw = lib.fp4_empty((1, 2, n), n, MX)
+    full = torch.zeros(2, n, n, dtype=torch.long, device="cuda")
+    # a block's 32 columns have the same weights but for the first: their gates are near each other, so that many of a block are not rounded to zero
+    full[:, :, :32] = codes(1, 5, 2, n // 32, 32).repeat_interleave(32, 1)
+    full[:, :, 0] = codes(1, 6, 2, n)
+    full[0, :, :32] += 8  # (gates are negative)
+    w[0] = ref.pack(full)
+    shift = torch.zeros(2, n // 32, dtype=torch.long, device="cuda")
+    shift[0] = torch.tensor([0, 0, 0, 0, 0, -1, 0, 0, -4, 0, 0, 0, 0, -2, 0, 0], device="cuda")
+    shift[1] = torch.tensor([108, 104, 100, 96, 92, 40, 84, 106, 3, 100, 90, 95, 105, 20, 70, 108], device="cuda")
+    sw.view(torch.uint8)[0] = (127 + shift).repeat_interleave(32, 1)[:, :, None].to(torch.uint8)
+    y = run_layer(lib, x, torch.zeros(T, 1, dtype=torch.int32, device="cuda"), w, sw, *identity(lib, 1, n, MX), MX).double()
+
+    gate, up = (x.double() @ ref.values(w[0, j], sw[0, j], MX).t() for j in (0, 1))
+    assert float(gate.max()) > -20 and float((gate < -88).double().mean()) > 0.5
+    h = gate / (1 + torch.exp(-gate)) * up
+    # in units of U: the power of two 4 (2^-22), its exponent's rounding and constant 1.25 |gate|, the sum 1, its reciprocal 2, three products
+    dh = (10 + 1.25 * gate.abs()) * U * h.abs()
+    amax = ref.block_amax(h, MX)
+    scale = ref.scales_of(amax, MX)
+    damax = ref.block_amax(dh, MX)
+    low, high = (ref.rounded(h.abs() + d * dh, scale, MX) * ref.spread(scale, n, MX) for d in (-1, 1))
+    sure = (ref.scales_of(amax - damax, MX) == scale) & (ref.scales_of(amax + damax, MX) == scale) & (amax > 2.0 ** -118)  # (results below are not normal)
+    sure = ref.spread(sure & (block_max(gate) > -153), n, MX) & (gate > -153) & (low == high)  # (h is 0 below)
+    assert float(sure.double().mean()) > 0.5 and float((sure & (low > 0) & (gate < -88)).double().mean()) > 0.1
+    assert bool((y == -low)[sure].all())
