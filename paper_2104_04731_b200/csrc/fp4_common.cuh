@@ -169,18 +169,24 @@ __device__ __forceinline__ Scale4 scale_of(uint32_t amax, const Factor4& f, int 
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
 // The hidden rows of an expert layer are quantised from values that are off by the errors of their sums, so the residuals that decide
-// borders exactly have nothing to decide: scale and quotients are formed in fp32 (a border moves by 3 units of the last place).
-__device__ __forceinline__ float quick_inv_6g(const float* p, int format) {
-  if (p == nullptr || format != B2C_NVFP4) return 1.0f / 6.0f;
-  return __frcp_rn(6.0f * fminf(fmaxf(*p, 0x1p-100f), 0x1p100f));
+// borders exactly have nothing to decide: scale and quotients are formed in fp32.  A border moves by 3 units of 2^-24 at most: that of a scale by the
+// roundings of 6 g, its reciprocal and the product, that of a value by those of the step, its reciprocal and the product.  (The step's reciprocal
+// as 6 / (6 g) by a quick quotient was off by up to 8: values 3.7 units from a border went to the wrong side of it.)
+struct QuickFactor4 {
+  float g, inv_6;
+};
+__device__ __forceinline__ QuickFactor4 quick_factor4(const float* p, int format) {
+  if (p == nullptr || format != B2C_NVFP4) return {1.0f, 1.0f / 6.0f};
+  const float g = fminf(fmaxf(*p, 0x1p-100f), 0x1p100f);
+  return {g, __frcp_rn(6.0f * g)};
 }
-__device__ __forceinline__ Scale4 quick_scale(uint32_t amax, float inv_6g, int format) {
+__device__ __forceinline__ Scale4 quick_scale(uint32_t amax, const QuickFactor4& f, int format) {
   if (format == B2C_MXFP4) return scale_mx(amax);
   Scale4 s;
   const bool fine = amax < kInfBits;
-  s.code = fine ? (uint32_t)__nv_cvt_float_to_fp8(__uint_as_float(amax) * inv_6g, __NV_SATFINITE, __NV_E4M3) : 0x7Fu;
+  s.code = fine ? (uint32_t)__nv_cvt_float_to_fp8(__uint_as_float(amax) * f.inv_6, __NV_SATFINITE, __NV_E4M3) : 0x7Fu;
   const float t = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)s.code, __NV_E4M3)));
-  s.r = fine && s.code != 0 ? __fdividef(6.0f * inv_6g, t) : 0.0f;  // (inv_6g is 2^-103 to 2^98, t 2^-9 to 448)
+  s.r = fine && s.code != 0 ? __frcp_rn(t * f.g) : 0.0f;  // (the step is 2^-109 to 2^109)
   s.step = s.lo = 0.0f;
   return s;
 }

@@ -306,9 +306,9 @@ __global__ void __launch_bounds__(kUpThreads, 1) experts4_up_kernel(const __grid
   pdl_wait();
   pdl_launch_dependents();
   Factor4 f = {};  // of what this warp quantises
-  float inv_6g = 0.0f;
+  QuickFactor4 hf = {};
   if (warp >= kQuantWarp0) f = load_factor4(a.x_global, a.format);
-  else if (warp >= 4) inv_6g = quick_inv_6g(a.h_global, a.format);
+  else if (warp >= 4) hf = quick_factor4(a.h_global, a.format);
   plan_few(plan, reinterpret_cast<uint32_t*>(smem_raw + (smem - smem_u32(smem_raw))), a.ids, a.pairs, a.experts);
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = __shfl_sync(0xffffffffu, c.ctl.tmem_base, 0);
@@ -459,7 +459,7 @@ __global__ void __launch_bounds__(kUpThreads, 1) experts4_up_kernel(const __grid
         mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
         if (a.format == B2C_MXFP4) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-        const Scale4 s = quick_scale(mx, inv_6g, a.format);
+        const Scale4 s = quick_scale(mx, hf, a.format);
         uint32_t q;
         quick_quantise4<4>(s, h, &q);
         if (ok && r < t.rows && n < a.inter) {  // (inter is a multiple of 32)

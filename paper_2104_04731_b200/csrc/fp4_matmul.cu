@@ -253,8 +253,8 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, RowsShape<NT, WT>
     const int rows = min(NT, tile.row_end - row0);
     const int n = n0 + 4 * lane;
     const float alpha = alpha_of(a, group);
-    float inv_6g = 0.0f;
-    if constexpr (WT == 2) inv_6g = quick_inv_6g(a.y_global, a.format);
+    QuickFactor4 hf = {};
+    if constexpr (WT == 2) hf = quick_factor4(a.y_global, a.format);
     // (code that runs once or twice is paid for when it is fetched, not when it runs)
 #pragma unroll 1
     for (int j = rank + split * warp; j < rows; j += split * (S::kThreads / 32)) {
@@ -296,7 +296,7 @@ __global__ void __launch_bounds__(RowsShape<NT, WT>::kThreads, RowsShape<NT, WT>
         mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
         if (a.format == B2C_MXFP4) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-        const Scale4 s = quick_scale(mx, inv_6g, a.format);
+        const Scale4 s = quick_scale(mx, hf, a.format);
         uint32_t q;
         quick_quantise4<4>(s, h, &q);
         if (n < a.N) {  // (N is a multiple of 32)

@@ -316,8 +316,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     const uint32_t leader_empty = CTAS == 2 ? map_to_rank(smem_u32(&ctl.tmem_empty[0]), 0u) : smem_u32(&ctl.tmem_empty[0]);
     const uint32_t taddr0 = tmem_acc + ((uint32_t)(quad * 32) << 16);
     const int in_tile = quad * 32 + lane;
-    float inv_6g = 0.0f;
-    if constexpr (GATED) inv_6g = quick_inv_6g(a.y_global, a.format);
+    QuickFactor4 hf = {};
+    if constexpr (GATED) hf = quick_factor4(a.y_global, a.format);
     int buf = 0;
     uint32_t bph = 0;
     bool ok = true;
@@ -400,7 +400,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           Scale4 s[2];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            s[i] = quick_scale(mx[i], inv_6g, a.format);
+            s[i] = quick_scale(mx[i], hf, a.format);
             quick_quantise4<16>(s[i], v + c + 16 * i, q + 2 * i);
           }
           if (on && n + c < a.N) {  // (N is a multiple of 32, ldy of 16)

@@ -96,3 +96,41 @@ def test_gates_far_below_zero(lib, T):
     sure = ref.spread(sure & (block_max(gate) > -153), n, MX) & (gate > -153) & (low == high)  # (h is 0 below)
     assert float(sure.double().mean()) > 0.5 and float((sure & (low > 0) & (gate < -88)).double().mean()) > 0.1
     assert bool((y == -low)[sure].all())
+
+
+# (a row an expert goes to the two kernels for few tokens, 8 and 30 to tiles of 16 and 64 rows, 64 to those of 128)
+@pytest.mark.parametrize("rows", [1, 8, 30, 64])
+def test_hidden_rows_next_to_borders(lib, rows):
+    """Hidden rows within some units of 2^-24 of the borders between two 4-bit values: who is further than 3 units from one is on its right side.
+    A token's only value is 6, gates are so large that silu is the gate itself, and 36 times the square of an expert's factor is next to h's, so the
+    columns of a block are 6 and the seven borders times the scale that the gate's weights have, nearly; everything before h is exact but for its
+    three roundings, which are made here too."""
+    E, n, g = 32, 64, gen(rows)
+    up = torch.tensor([6.0] + 2 * [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0] + [5.0], dtype=torch.float64, device="cuda").repeat(n // 16)
+    x = torch.zeros(E, n, device="cuda")
+    x[:, 0] = 6.0
+    moved = torch.linspace(-6, 6, E, dtype=torch.float64, device="cuda") * U
+    # factors whose reciprocal by way of six times them and back, each step rounded, is furthest off (up to three units)
+    some = (torch.rand(1 << 20, generator=g, device="cuda") + 1) * 4096
+    worst = (6.0 * (1.0 / (6.0 * some)).double() * some.double() - 1).abs().topk(24).indices
+    for gh in some[worst][:, None]:
+        f1 = (gh.double() / 36 * (1 + moved)).sqrt().float()
+        code = torch.randint(56, 120, (E, n // 16), generator=g, device="cuda", dtype=torch.uint8).repeat_interleave(16, 1)  # scales from 1 to 240
+        w, sw = lib.fp4_empty((E, 2, n), n, NV)
+        w.zero_()
+        w[..., 0] = 2  # 1.0 in the first column, times the block's scale
+        sw.view(torch.uint8)[:, 0, :, 0] = code
+        sw[:, 1, :, 0] = up.float().to(torch.float8_e4m3fn)
+        ids = torch.arange(E, dtype=torch.int32, device="cuda").repeat(rows)[:, None]
+        y = run_layer(lib, x.repeat(rows, 1), ids, w, sw, *identity(lib, E, n, NV), NV, w1_global=f1, h_global=gh)
+
+        scale = ref.scale_numbers(code, NV)
+        gate = (6 * scale).float() * f1[:, None]
+        h = (gate * ((6 * up).float() * f1[:, None])).double()  # (two products rounded, and theirs)
+        assert float(gate.min()) >= 40  # (e^-40 does not count beside 1)
+        off = h / (up * scale * gh.double()) - 1
+        assert bool((off.abs() < 12 * U).all()) and float((off.abs() > 3 * U).double().mean()) > 0.2
+        ends = [(ref.round4(h * (1 + d * 3 * U) / (scale * gh.double())) * scale).float() * gh for d in (-1, 1)]
+        y = y.reshape(rows, E, n)
+        wrong = (y != ends[0]) & (y != ends[1])
+        assert not bool(wrong.any()), (int(wrong.sum()), float(off[wrong.any(0)].abs().max() / U))
