@@ -378,10 +378,7 @@ int launch_rows_of(const Matmul4Args& a, cudaStream_t st) {
 int launch_fp4_matmul(const Matmul4Args& a, cudaStream_t st) {
   int rows = a.rows;
   if (a.offsets) {
-    // half as many rows again as a group has on average: a second tile of a group reads its weights again (256 tokens, 4 of 64 experts, 16 rows
-    // a group: 89 us by tiles of 16, 74 of 32; 64 rows a group: 113 us by tiles of 64 here, 81 by those of 128 there)
-    rows = (int)(((long long)a.rows + a.groups - 1) / a.groups);
-    rows += rows / 2;
+    rows = rows_of_a_group_tile(a);
     if (rows > 64) return launch_fp4_matmul_pair(a, st);
   } else if (rows > 64) {
     // 5.4 us and 0.3 for every stage that a block fetches: with few tiles and a long reduction the cut is worth more than larger tiles (us here and

@@ -611,7 +611,7 @@ long long large_ns(const Matmul4Args& a) {
 long long fp4_pair_ns(const Matmul4Args& a) { return std::min(small_ns(a), large_ns(a)); }
 
 int launch_fp4_matmul_pair(const Matmul4Args& a, cudaStream_t st) {
-  const int rows = a.offsets ? (int)(((long long)a.rows + a.groups - 1) / a.groups) : a.rows;
+  const int rows = rows_of_a_group(a);
   if (a.gated) return launch_pair<1, 256, kGated, uint8_t>(a, st);
   if (a.offsets) {
     // Half a tile of every group is empty: 64 rows of a tile of its own, 128 of a pair's, 16 of a pair's with the weights first.  That one's results take

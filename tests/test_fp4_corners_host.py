@@ -1,8 +1,24 @@
 """What of the 4-bit float operators can be checked without a device: refusals of unusual tensors, decisions of the host."""
+import os
+import subprocess
+
 import pytest
 import torch
 
 import paper_2104_04731_b200 as b2c
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2104_04731_b200", "csrc")
+
+
+def test_decisions_about_large_groups(tmp_path):
+    """Sizes that no test can run (a group of more than 1.4e9 rows), as a small program."""
+    exe = str(tmp_path / "fp4_decisions")
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-I", os.path.join(cuda, "include"), "-I", os.path.join(ROOT, "include"), "-I", CSRC,
+                           os.path.join(ROOT, "tests", "fp4_decisions.cpp"), "-o", exe])
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout + r.stderr
 
 
 @pytest.fixture(scope="module")
