@@ -28,9 +28,11 @@ __device__ __forceinline__ Factor4 load_factor4(const float* p, int format) {
 }
 
 // A number on the same side as the quotient x / (hi + lo) of every border with few bits: t, which is the quotient q (good to some units) rounded to
-// BITS bits, as all borders are such numbers, moved by 2^-10 of itself (less than to the next one) to where x - t * (hi + lo) says.
-// x - t * hi is exact where it is small, and the rounding of the last sum keeps its sign.  `large` makes every d but 0 more than 1/2: d is 2^-33
-// of the divisor at least.  All of it on the unit of the multiplications, which has twice the rate of that of comparisons.
+// as many bits as a border has, moved by 2^-10 of itself (less than to the next such number) to where d = x - t * (hi + lo) says.
+// x - t * hi is exact where it is small, and the rounding of the last sum keeps its sign.  Where d is not 0 it is 2^-36 of the divisor at least (the
+// lowest border between scales is 2^-10, and 6 g has 26 bits), and `large` makes it more than 1/2.  Below divisors of 2^-87 `large` is at its limit:
+// d is a multiple of 2^-134 (of the last places of g, 2^-123, of a scale, 2^-9, and of a border, 2^-2), so 2^-7 are left and t moves by 2^-16 of
+// itself, still to the right side.  All of it on the unit of the multiplications, which has twice the rate of that of comparisons.
 __device__ __forceinline__ float side_of(float t, float d, float large) {
   return fmaf(fabsf(t), fmaf(__saturatef(fmaf(d, large, 0.5f)), 0x1p-9f, -0x1p-10f), t);
 }

@@ -30,6 +30,35 @@ def test_empty_matrices_are_refused(lib):
         assert code_of(lib, lib.fp4_experts, x, ids, weights, w1, s1, w2, s2, y, ws) == lib.E_INVALID_ARG
 
 
+# ---- quantisation ----------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("g", [1.1 * 2.0 ** -100, 1.9999999 * 2.0 ** -100, 2.0 ** -100, 1.3333334 * 2.0 ** -97, 1.7 * 2.0 ** -88, 0.77, 1.1 * 2.0 ** 99, 2.0 ** 100])
+def test_quantize_next_to_borders_of_any_factor(lib, g):
+    """fp32 numbers within a few units of the borders between values, and blocks whose largest is within a few of those between scales, for the smallest
+    and the largest factors and scales: equal to the quotients in 64 bits in every value."""
+    f = torch.tensor([g], dtype=torch.float32, device="cuda")
+    g = float(f)
+    v = torch.tensor(ref.VALUES, dtype=torch.float64)
+    mid = (v[:-1] + v[1:]) / 2
+    scales = ref.scale_numbers(torch.arange(127, dtype=torch.uint8).view(torch.float8_e4m3fn), NV)
+    near = lambda a, d: (a.float().view(torch.int32) + d).view(torch.float32)  # noqa: E731
+    rows = []
+    for s in scales[1:].tolist():
+        for d in range(-3, 4):
+            x = near(mid * s * g, d)
+            rows.append(torch.cat([x, -x, torch.tensor([6 * s * g, 0.0]).float()]))
+    borders = (scales[:-1] + scales[1:]) / 2
+    for d in range(-3, 4):
+        x = torch.zeros(126, 16)
+        x[torch.arange(126), torch.arange(126) % 16] = near(borders * 6 * g, d) * (-1) ** d
+        rows += list(x)
+    x = torch.stack(rows).cuda()
+    q, s = torch.empty(x.shape[0], 8, dtype=torch.uint8, device="cuda"), torch.empty(x.shape[0], 1, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    lib.fp4_quantize(x, q, s, global_scale=f)
+    want, scale = ref.quantize(x, NV, f)
+    assert bool((ref.scale_numbers(s, NV) == scale).all()) and bool((ref.unpack(q, 16) == want).all())
+
+
 # ---- hidden rows of an expert layer, seen through a second matrix that is the identity ---------------------------------------------------
 
 def gen(seed):
