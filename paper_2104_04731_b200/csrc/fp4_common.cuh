@@ -115,7 +115,7 @@ __device__ __forceinline__ void cvt_f16x8(uint32_t q, uint32_t* h) {
       : "r"(q));
 }
 
-// N (4, 8 or 16) values of one block to 4 bits each, as if x / (scale * g) had been rounded as a real number.
+// N (8 or 16) values of one block to 4 bits each, as if x / (scale * g) had been rounded as a real number.
 //   MX: multiplication by a power of two.
 //   NV, few_bits: the correctly rounded quotient by Markstein's residual step (as in quantize2 of the 8-bit operators).  Every product of the step with a border t has 24
 // bits at most, so x is either that product, and the quotient t itself, or differs from it by a unit of x's last place, more than half a
@@ -158,10 +158,9 @@ __device__ __forceinline__ void quantise4(const Scale4& s, const Factor4& f, int
   }
 #pragma unroll
   for (int i = 0; i < N / 8; ++i) q[i] = cvt_e2m1x8(v + 8 * i);
-  if constexpr (N == 4) q[0] = cvt_e2m1x4(v);
   if (s.r == 0.0f) {
 #pragma unroll
-    for (int i = 0; i < (N + 7) / 8; ++i) q[i] = 0;
+    for (int i = 0; i < N / 8; ++i) q[i] = 0;
   }
 }
 __device__ __forceinline__ Scale4 scale_of(uint32_t amax, const Factor4& f, int format) {
