@@ -4,6 +4,7 @@ import torch
 
 import fp4_ref as ref
 from fp4_ref import MX, NV
+from test_fp4_gpu import check_experts, layer, routes, run_experts
 
 FMT = pytest.mark.parametrize("fmt", [MX, NV], ids=["mx", "nv"])
 U = 2.0 ** -24  # half a step of fp32 at most, relative
@@ -163,3 +164,48 @@ def test_hidden_rows_next_to_borders(lib, rows):
         y = y.reshape(rows, E, n)
         wrong = (y != ends[0]) & (y != ends[1])
         assert not bool(wrong.any()), (int(wrong.sum()), float(off[wrong.any(0)].abs().max() / U))
+
+
+# ---- expert layers of real sizes -------------------------------------------------------------------------------------------------------
+
+# Reductions of more than one group of scales (1024) and of more stages (256 each) than any ring holds, last stages that are not full, in both products.
+# One and 16 tokens and 100 of many experts go to the two kernels for few, the others to tiles of 32, 64 and 128 rows.
+@FMT
+@pytest.mark.parametrize("T,experts,topk,hidden,inter", [(1, 16, 8, 2336, 1312), (16, 16, 4, 1312, 2336), (3, 4, 4, 2336, 2336), (100, 32, 1, 1056, 2080), (100, 16, 3, 2336, 1312),
+                                                         (100, 8, 3, 1312, 2336), (150, 3, 2, 2336, 1312), (400, 6, 3, 1312, 2336)])
+def test_experts_long_reductions(lib, T, experts, topk, hidden, inter, fmt):
+    w = layer(lib, hidden, inter, experts, fmt, T)
+    x = torch.randn(T, hidden, generator=gen(T + 1), device="cuda").bfloat16()
+    ids, weights = routes(T, experts, topk, T + 2)
+    gx, gh = (torch.tensor([v / 2688], device="cuda") for v in (6, 9)) if fmt == NV else (None, None)
+    y = run_experts(lib, x, ids, weights, w, fmt, gx, gh, extra=64)
+    check_experts(y, x, ids, weights, w, fmt, gx, gh)
+
+
+# Routes on which the average says little: one expert has 15 to 33 of a few tokens (more than one tile of the kernels for few), or most of many.
+@FMT
+@pytest.mark.parametrize("T,experts,topk,most", [(64, 64, 4, 15), (64, 64, 4, 16), (64, 64, 4, 17), (64, 64, 4, 32), (64, 64, 4, 33), (64, 64, 4, 64), (40, 128, 8, 40),
+                                                 (600, 64, 2, 600), (700, 40, 4, 650)])
+def test_experts_skewed_routes(lib, T, experts, topk, most, fmt):
+    hidden, inter, hot = 288, 160, 5
+    w = layer(lib, hidden, inter, experts, fmt, most)
+    x = torch.randn(T, hidden, generator=gen(most + 1), device="cuda").half()
+    ids, weights = routes(T, experts - 1, topk, most + 2)
+    ids += ids >= hot  # (all but the hot one)
+    chosen = torch.randperm(T, generator=gen(most + 3), device="cuda")[:most]
+    ids[chosen, chosen % topk] = hot
+    assert int((ids == hot).sum()) == most
+    y = run_experts(lib, x, ids, weights, w, fmt, extra=64)
+    check_experts(y, x, ids, weights, w, fmt)
+
+
+@FMT
+@pytest.mark.parametrize("T,experts", [(2, 16), (30, 64), (200, 16)])
+def test_experts_many_slots(lib, T, experts, fmt):
+    """Eight slots a token, of which every third token has two."""
+    w = layer(lib, 512, 256, experts, fmt, T)
+    x = torch.randn(T, 512, generator=gen(T + 1), device="cuda").bfloat16()
+    ids, weights = routes(T, experts, 8, T + 2)
+    ids[1::3, 2:] = -1
+    y = run_experts(lib, x, ids, weights, w, fmt)
+    check_experts(y, x, ids, weights, w, fmt)
