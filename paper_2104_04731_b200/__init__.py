@@ -496,7 +496,7 @@ def fp4_scale_pitch(cols: int, fmt: int) -> int:
 
 def fp4_empty(rows, cols: int, fmt: int, device="cuda"):
     """(q, scale) for a matrix of rows x cols values, or a stack of them (rows: a tuple), laid out as the products read them: q of
-    ceil(cols / 2) bytes a row, scale a view into rows of fp4_scale_pitch bytes."""
+    ceil(cols / 2) bytes a row, scale a view into rows of fp4_scale_pitch bytes.  Any cols can be stored; a product takes multiples of 32 (pad with zeros)."""
     import torch
 
     lead = tuple(rows) if isinstance(rows, (tuple, list)) else (rows,)

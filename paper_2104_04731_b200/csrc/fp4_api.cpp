@@ -161,7 +161,8 @@ int b2c_fp4_experts(const b2c_fp4_experts_desc* d, int64_t tokens, const void* x
   char* ws = (char*)workspace;
   const long long pairs = tokens * d->topk;
   // Two kernels where an expert has few rows (its tiles are 16 rows wide, and are quantised again for every tile of columns): us by them and by
-  // the five launches below, of 2048 x 1024, 4 of 64 experts: 1 token 13 and 18, 16 37 and 43, 64 57 and 58, 100 70 and 63.
+  // the five launches below, NV: 2048 x 1024, 4 of 64 experts: 1 token 14 and 20, 16 37 and 45, 64 58 and 58, 100 76 and 64 (MX 14 and 18, 36 and 42, 53
+  // and 54, 67 and 60);  1024 x 512: 16 tokens 22 and 25, 64 32 and 31, 100 40 and 32;  4096 x 1024, 4 of 32: 16 51 and 56, 64 84 and 64.
   if (pairs <= kFewPairs && pairs <= 4ll * d->experts) {
     Few4Args f = {};
     f.x = x;

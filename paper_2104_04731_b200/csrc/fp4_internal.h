@@ -73,8 +73,8 @@ struct Matmul4Args {
 inline int rows_of_a_group(const Matmul4Args& a) { return a.offsets ? (int)(((long long)a.rows + a.groups - 1) / a.groups) : a.rows; }
 
 // Rows of a tile of a product by groups: 16, 32 or 64 by the kernel for few rows, 128 by that for many.  A tile holds half as many rows again as a
-// group has on average: a second tile of a group reads its weights again (256 tokens, 4 of 64 experts, 16 rows a group: 89 us by tiles of 16, 74 of
-// 32; 64 rows a group: 113 us by tiles of 64, 81 of 128).  (In 64 bits: one group may have all rows.)
+// group has on average: a second tile of a group reads its weights again (256 tokens, 4 of 64 experts, 16 rows a group: 87 us by tiles of 16, 74 of
+// 32; 64 rows a group: 109 us by tiles of 64, 80 of 128).  (In 64 bits: one group may have all rows.)
 inline int rows_of_a_group_tile(const Matmul4Args& a) {
   const long long average = rows_of_a_group(a), rows = average + average / 2;
   return rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 64 ? 64 : 128));

@@ -3,7 +3,7 @@
 // With few rows the weights are the bytes, and the tensor core's 128 accumulator rows are given to them (the axes are swapped): a
 // thread block owns 128 weight rows and 16, 32 or 64 activation rows.  What bounds it is the way from the launch to the first sums and how many bytes
 // are in flight: the reduction is cut over the blocks of a cluster until all SMs have a share, and the partial sums meet in distributed shared
-// memory, in a fixed order.  1 x 8192 x 8192 NV: 10.8 us, 3.5 TB/s (37.8 MB; 5.9 at the rate of a copy);  37 x 5136 x 4128: 7.9.
+// memory, in a fixed order.  1 x 8192 x 8192 NV: 9.8 us, 3.9 TB/s (37.8 MB; 5.9 at the rate of a copy);  37 x 5136 x 4128 MX: 7.0.
 //
 // Roles: warp 0 copies (TMA), warp 1 carries the scales to tensor memory and issues the MMAs, the others copy the scales and turn them round (a
 // warp an operand, see fp4_mma.cuh) and take the sums out of tensor memory when all stages have been added there.
@@ -319,9 +319,10 @@ int fail(cudaError_t e) {
 
 // How many thread blocks share a tile's reduction: what counts is the stages that a block fetches, one after another.  Blocks that share an SM are
 // a fifth slower each; a cut costs the exchange of the partial sums, about as long as two stages and one more for every block of the cluster.
-// Measured, us with 1, 2, 3, 4, 6 blocks a tile:
-//   1 x 8192 x 8192 (64 tiles of 32 stages) 17.3, 13.1, 11.8, 11.3, 16.7;   37 x 5136 x 4128 (41 of 17) 10.1, 8.9, 8.3, 9.0, 8.9;
-//   16 x 4096 x 4096 (32 of 16) 10.3, 8.5, 7.5, 6.9, 7.2;   128 x 4096 x 4096 (64 of 16) 11.2, 9.7, 9.8, 9.3, 16.2.
+// Measured, us with 1, 2, 3, 4, 6 blocks a tile (four sets of operands in turn, more than L2 holds):
+//   1 x 8192 x 8192 (64 tiles of 32 stages) 13.9, 12.1, 11.1, 10.7, 15.4;   37 x 5136 x 4128 (41 of 17) 9.2, 8.3, 7.8, 9.0, 8.7;
+//   16 x 4096 x 4096 (32 of 16) 8.0, 7.5, 6.7, 6.3, 6.8;   128 x 4096 x 4096 (64 of 16) 9.3, 8.6, 9.0, 8.8, 15.3;
+//   300 x 1024 x 8192 (40 of 32) 13.9, 10.7, 9.4, 9.7, 9.7.
 int choose_split(long long tiles, int kb_all, int per_sm, bool counted, double* stages = nullptr) {
   if (!counted && tiles >= kNumSMs) return 1;  // (a guess of the tiles says nothing about the last wave)
   int best = 1;
@@ -329,7 +330,7 @@ int choose_split(long long tiles, int kb_all, int per_sm, bool counted, double* 
   for (int s = 1; s <= kMaxSplit && 2 * s <= std::max(2, kb_all); ++s) {
     const int per = (kb_all + s - 1) / s;
     if ((kb_all + per - 1) / per != s) continue;  // (no thread block without work)
-    if (s > 4 && tiles * s > kNumSMs) break;  // (300 x 1024 x 8192, 40 tiles: 15.2 us by seven)
+    if (s > 4 && tiles * s > kNumSMs) break;  // (300 x 1024 x 8192, 40 tiles: 15.0 us by seven)
     const long long blocks = tiles * s, waves = (blocks + kNumSMs * per_sm - 1) / (kNumSMs * per_sm);
     const double cost = (double)waves * per * (per_sm > 1 && blocks > kNumSMs ? 1.2 : 1.0) + (s > 1 ? 1.5 + s : 0.0);
     if (s == 1 || cost < least) {
@@ -382,7 +383,7 @@ int launch_fp4_matmul(const Matmul4Args& a, cudaStream_t st) {
     if (rows > 64) return launch_fp4_matmul_pair(a, st);
   } else if (rows > 64) {
     // 5.4 us and 0.3 for every stage that a block fetches: with few tiles and a long reduction the cut is worth more than larger tiles (us here and
-    // there: 128 x 2048 x 8192 8.8 and 12.3, 100 x 4096 x 4096 8.8 and 8.4)
+    // there: 128 x 2048 x 8192 8.6 and 12.4, 100 x 4096 x 4096 8.8 and 8.3)
     const long long tiles = (long long)((a.N + kTileM - 1) / kTileM) * ((rows + 63) / 64);
     double stages = 0;
     choose_split(tiles, (a.K + kFp4Stage - 1) / kFp4Stage, RowsShape<64, 1>::kPerSm, true, &stages);

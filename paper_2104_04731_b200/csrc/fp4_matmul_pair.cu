@@ -2,8 +2,8 @@
 // cta_group::2), or x 128 rows of one block.
 //
 // The tensor core applies the scales and keeps the sums of the whole reduction, so a tile's accumulators are read once, at its end: eight warps
-// take them into registers, hand the columns back and turn them into results while the next tile's MMAs run.  8192^3: NV 204 us, 5.4 PFLOP/s, MX 180
-// and 6.1 in a short run; one after another for seconds the power limit makes it 247.  What else there is: the copies of scales to tensor
+// take them into registers, hand the columns back and turn them into results while the next tile's MMAs run.  8192^3: NV 203 us, 5.4 PFLOP/s, MX 181
+// and 6.1 in a short run; one after another for seconds the power limit makes it 244.  What else there is: the copies of scales to tensor
 // memory, twelve a stage (NV) beside MMAs of 512 cycles (without them, a wrong result, 190 us), and the drain at a tile's end.
 // Tried and slower: copies of a stage's scales issued before the MMAs of the stage before it (240 us), a ring of scales for every stage (256).
 //
@@ -594,8 +594,8 @@ int launch_type(const Matmul4Args& a, cudaStream_t st) {
 }
 
 // Nanoseconds by tiles of 128 x 128 on one SM, and by those of 256 x 256 on a pair: the small ones where the large ones are fewer than the pairs.
-// Measured, us small / large: 384 x 4096 x 4096 9.3 / 11.6, 300 x 1024 x 8192 12.3 / 16.2, 1000 x 1024 x 1024 5.3 / 7.4,
-// 4096 x 512 x 4096 9.3 / 11.7;   768 x 4096 x 4096 14.1 / 12.6, 512 x 8192 x 8192 24.1 / 19.8, 2048 x 2048 x 2048 9.4 / 9.4.
+// Measured, us small / large: 384 x 4096 x 4096 9.2 / 11.6, 300 x 1024 x 8192 12.3 / 16.2, 1000 x 1024 x 1024 5.2 / 7.5,
+// 4096 x 512 x 4096 9.3 / 11.5;   768 x 4096 x 4096 13.8 / 12.4, 512 x 8192 x 8192 24.2 / 19.5, 2048 x 2048 x 2048 9.2 / 9.3.
 long long small_ns(const Matmul4Args& a) {
   const long long tiles = (long long)((a.N + 127) / 128) * ((a.rows + 127) / 128), kb = (a.K + kFp4Stage - 1) / kFp4Stage;
   const long long waves = (tiles + kNumSMs - 1) / kNumSMs;
@@ -615,9 +615,14 @@ int launch_fp4_matmul_pair(const Matmul4Args& a, cudaStream_t st) {
   if (a.gated) return launch_pair<1, 256, kGated, uint8_t>(a, st);
   if (a.offsets) {
     // Half a tile of every group is empty: 64 rows of a tile of its own, 128 of a pair's, 16 of a pair's with the weights first.  That one's results take
-    // longer, which shows unless the reduction is long, and its tiles are fewer.  One SM / weights first, us, N 2048: 32 groups of 128, 256, 512 rows and
-    // K 4096: 38.9 / 37.6, 49.8 / 46.0, 76.7 / 69.8, K 8192: 68.4 / 62.9, 90.8 / 83.3, 143 / 128;  8 groups of 256, K 4096: 19.1 / 20.7;  32 of 64: 33.1 /
-    // 36.0;  16 of 512, K 2048: 26.0 / 26.5.  At 240 rows of a group and more the pair with the rows first is within 5 % of one SM either way.
+    // longer, which shows unless the reduction is long, and its tiles are fewer.  One SM / weights first, us, NV, 32 groups of 128, 256, 512 rows:
+    //   K 8192, N 2048: 68.6 / 62.9, 90.4 / 83.5, 142 / 128;
+    //   K 4096, N 1024: 26.7 / 23.9, 34.3 / 30.6, 42.5 / 43.1;  N 2048: 38.8 / 38.0, 49.0 / 44.8, 76.4 / 69.1;  N 4096: 66.6 / 65.9, 92.7 / 83.4, 144 / 131;
+    //   K 3584, N 1024: 24.9 / 22.0, 26.0 / 28.9, 41.0 / 42.1;  N 2048: 35.4 / 35.8, 43.4 / 43.6, 72.7 / 66.4;  N 4096: 59.2 / 60.9, 83.6 / 78.3, 136 / 124;
+    //   K 2560, N 1024: 20.2 / 18.9, 23.3 / 24.5, 33.1 / 33.2;  N 2048: 28.6 / 29.5, 37.0 / 36.0, 56.4 / 52.6;  N 4096: 45.1 / 48.8, 66.2 / 61.4, 104 / 97;
+    // and 8 of 256, K 4096, N 2048: 19.6 / 21.4;  32 of 64: 33.9 / 35.7;  16 of 512, K 2048: 25.7 / 26.2.  MX is like it (K 4096, N 2048: 36.7 / 36.2, 47.2 /
+    // 42.5, 73.0 / 63.6).  What the rule gives to the weights first loses 2 % at most.  Of the rest, N 1024 would gain 11 % with short groups, and
+    // below K 4096 long groups gain up to 9 % and short ones lose as much, by how either form's tiles divide the SMs: one SM stays.  At 240 rows of a group and more the pair with the rows first is within 5 % of one SM either way.
     const long long large = (a.rows / 256 + a.groups / 2) * (long long)((a.N + 255) / 256);  // tiles, about
     if (a.K >= 4096 && rows >= 100 && large >= 3 * (kNumSMs / 2)) return launch_type<2, 256, kWeightsFirst>(a, st);
     return rows <= 768 ? launch_type<1, 256, kRowsFirst>(a, st) : launch_type<2, 256, kRowsFirst>(a, st);
