@@ -28,6 +28,7 @@ constexpr int kRegsSums = 208, kRegsRest = 88;
 constexpr int kABytes = kTileM * kStageRow;
 constexpr int kBoxRow = 64;
 constexpr int kBoxBytes = 32 * kBoxRow;  // results of a warp on their way out: 32 rows
+constexpr int kGateBytes = 32 * 32 * 4;  // 32 values of every lane of a warp: gated, in the place of the boxes
 constexpr int kGroups = 2;               // groups of scales in shared memory
 // Which operand has the accumulator's rows.  The rows of a, and a tile's columns are rows of b; gated, 128 gate rows and the 128 up rows of the same
 // columns.  Or the weights (groups): the rows of a group are the tile's columns then, as many of them, in steps of 32, as there are.
@@ -352,30 +353,29 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 #pragma unroll
         for (int i = 0; i < 64; i += 2) low = min3(low, v[i], v[i + 1]);
         if (__any_sync(0xffffffffu, low < kFarGate)) {
-          // Rare, so by short code: eight columns at a time go through shared memory (the box for results has no other use here), where a loop can index
-          // them.  (Four more operations for every value made 8192 tokens 250 us instead of 240; a second copy of the 64 beside the first made
-          // 2048 tokens, 4 of 32, 1024 x 512, 49.7 instead of 47.4, of which it takes no step.)
-          const uint32_t at = box_base + (uint32_t)((warp - kEpiWarp0) * kBoxBytes + lane * 16);
+          // Rare, so by short code: 16 columns at a time go through shared memory, where a loop can index them.  (us of 8192 tokens, 4 of 64 experts,
+          // 2048 x 1024, and of 2048 tokens, 4 of 32, 1024 x 512: 240 and 47.9; 257 and 54 with such gates in every tile.  The longer form for every
+          // value made them 250 and 48.9, a second copy of the 64 beside the first 240 and 49.7, the longer form of one value at a time here 307
+          // and 62 with such gates.)
+          const uint32_t at = box_base + (uint32_t)((warp - kEpiWarp0) * kGateBytes + lane * 16);
+          auto put = [&](int p, const float* u) {
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at + 512 * p), "f"(u[0]), "f"(u[1]), "f"(u[2]), "f"(u[3]) : "memory");
+          };
 #pragma unroll
-          for (int i = 0; i < 64; i += 8) {
-            auto put = [&](int p, const float* u) {
-              asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at + 512 * p), "f"(u[0]), "f"(u[1]), "f"(u[2]), "f"(u[3]) : "memory");
-            };
-            put(0, v + i);
-            put(1, v + i + 4);
-            put(2, v + 64 + i);
-            put(3, v + 64 + i + 4);
+          for (int i = 0; i < 64; i += 16) {
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+              put(p, v + i + 4 * p);
+              put(4 + p, v + 64 + i + 4 * p);
+            }
 #pragma unroll 1
-            for (int j = 0; j < 8; ++j) {
-              const uint32_t here = at + (uint32_t)(512 * (j >> 2) + 4 * (j & 3));
-              float g, u;
-              asm volatile("ld.shared.f32 %0, [%1];" : "=f"(g) : "r"(here) : "memory");
-              asm volatile("ld.shared.f32 %0, [%1];" : "=f"(u) : "r"(here + 1024) : "memory");
-              g = quick_gated<true>(g, u * alpha);
-              asm volatile("st.shared.f32 [%0], %1;" ::"r"(here), "f"(g) : "memory");
+            for (int p = 0; p < 4; ++p) {
+              const float4 g = ld_shared_f4(at + 512 * p), u = ld_shared_f4(at + 512 * (4 + p));
+              const float h[4] = {quick_gated<true>(g.x, u.x * alpha), quick_gated<true>(g.y, u.y * alpha), quick_gated<true>(g.z, u.z * alpha), quick_gated<true>(g.w, u.w * alpha)};
+              put(p, h);
             }
 #pragma unroll
-            for (int p = 0; p < 2; ++p) {
+            for (int p = 0; p < 4; ++p) {
               const float4 h = ld_shared_f4(at + 512 * p);
               v[i + 4 * p] = h.x;
               v[i + 4 * p + 1] = h.y;
@@ -540,6 +540,8 @@ template <int CTAS, int TN, int FORM, typename YT>
 int launch_pair(const Matmul4Args& a, cudaStream_t st) {
   using S = TileShape4<CTAS, TN>;
   constexpr bool TURNED = FORM == kWeightsFirst, GATED = FORM == kGated;
+  constexpr int kSmem = S::kSmem + (GATED ? kEpiWarps * (kGateBytes - kBoxBytes) : 0);
+  static_assert(kSmem <= 226 * 1024, "shared memory, some static beside it");
   const long long cols = GATED ? kTileM : TN;
   const long long n_tiles = (a.N + cols - 1) / cols;
   const long long row_tiles = a.offsets ? a.rows / S::kRows + std::min(a.groups, a.rows) : (a.rows + S::kRows - 1) / S::kRows;
@@ -560,13 +562,13 @@ int launch_pair(const Matmul4Args& a, cudaStream_t st) {
                          kBoxBytes / box_row, TURNED ? 0 : kBoxRow);
   if (rc != B2C_OK) return rc;
   static std::atomic<unsigned long long> configured{0};
-  cudaError_t e = set_max_dynamic_smem_once(configured, (const void*)matmul4_pair_kernel<CTAS, TN, FORM, YT>, S::kSmem);
+  cudaError_t e = set_max_dynamic_smem_once(configured, (const void*)matmul4_pair_kernel<CTAS, TN, FORM, YT>, kSmem);
   if (e == cudaSuccess) {
     const int pairs = (int)std::min<long long>(row_tiles * n_tiles, kNumSMs / CTAS);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(CTAS * pairs));
     cfg.blockDim = dim3(kPairThreads);
-    cfg.dynamicSmemBytes = S::kSmem;
+    cfg.dynamicSmemBytes = kSmem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
